@@ -12,10 +12,13 @@ SOURCES = [os.path.join(PKG, "csrc", "ftattn.hip"), os.path.join(PKG, "csrc", "f
            os.path.join(PKG, "csrc", "ftattn_elementwide.hip"), os.path.join(PKG, "csrc", "ftattn_lazy.hip"),
            os.path.join(PKG, "csrc", "ftattn_split.hip"), os.path.join(PKG, "csrc", "ftattn_self.hip"),
            os.path.join(PKG, "csrc", "ftgemm.hip"), os.path.join(PKG, "csrc", "ftgemm_f16.hip"),
-           os.path.join(PKG, "csrc", "ftgemm_bf16.hip"), os.path.join(PKG, "csrc", "ftdecoupled.hip")]
+           os.path.join(PKG, "csrc", "ftgemm_bf16.hip"), os.path.join(PKG, "csrc", "ftdecoupled.hip"),
+           os.path.join(PKG, "csrc", "ftprompt.hip"), os.path.join(PKG, "csrc", "ftcache.hip")]
 HEADERS = [os.path.join(PKG, "csrc", "ftattn_device.h"), os.path.join(PKG, "csrc", "ftattn_main.h"),
            os.path.join(PKG, "csrc", "ftgemm_main.h"), os.path.join(ROOT, "include", "ftattn.h"),
-           os.path.join(ROOT, "include", "ftgemm.h"), os.path.join(ROOT, "include", "ftdecoupled.h")]
+           os.path.join(PKG, "csrc", "ftserve_device.h"),
+           os.path.join(ROOT, "include", "ftgemm.h"), os.path.join(ROOT, "include", "ftdecoupled.h"),
+           os.path.join(ROOT, "include", "ftprompt.h"), os.path.join(ROOT, "include", "ftcache.h")]
 OBJDIR = os.path.join(PKG, "_build")
 
 

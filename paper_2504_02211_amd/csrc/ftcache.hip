@@ -1,0 +1,882 @@
+// Paged key / value cache in 4 bits: the kernels and the C ABI of include/ftcache.h.
+//
+//   ftcache_put     rotates the new tokens' queries and keys, writes both, and puts keys and values into their pages
+//   ftcache_get     the reverse of the second half: cached tokens as 16-bit rows
+//   ftcache_one     attention of one token per sequence over the cache
+//
+// Bound of all three: memory.  A token of a key / value head is head_dim + 8 bytes of cache, 136 at head_dim 128 where 16 bits
+// would be 512.
+#include "ftcache.h"
+#include "ftserve_device.h"
+
+#include <cmath>
+#include <new>
+#include <string>
+
+namespace ftcache {
+using namespace ftserve;
+
+struct Rows { char* data; int64_t token, head; };       // strides in bytes
+
+struct Places {
+  const int32_t *cu, *starts, *table;
+  int64_t table_stride;
+  int32_t batch, tokens, width;
+};
+
+struct Pool {
+  char* data;
+  int32_t pages, kv_heads, page_shift;
+  int32_t head_bytes;                // of one head of a page
+  __device__ __forceinline__ char* head(int page, int hk) const { return data + ((int64_t)page * kv_heads + hk) * head_bytes; }
+};
+
+struct Args {
+  Pool pool;
+  Places at;
+  Rows q, k, v, q_out, k_out;
+  const float* rotation;
+  int32_t positions, heads, rotary;
+  unsigned long long* refused;       // [0] tokens, [1] sequences
+};
+
+// Tokens of 8 consecutive places of a sequence (a block of the page layout), one of them per lane group of 8.
+struct Block {
+  int b, first;            // sequence, its first place in the block
+  int place, row;          // of this lane's token; packed row
+  bool real;               // the block holds a new token for this lane
+  bool whole;              // all 8 places are new tokens (uniform)
+  char* page;              // the page, or nullptr where the table names none
+};
+
+// Sequence b owns the blocks from cu[b] / 8 + 2b on, at least as many as n new tokens can touch: (n + 6) / 8 + 1.
+__device__ __forceinline__ bool block_of(const Places& p, const Pool& pool, int id, Block& x) {
+  auto before = [&](int b) { return (int64_t)(clamped(p.cu[b], p.tokens) / 8 + 2 * b); };
+  x.b = sequence_of(p.batch, id, before);
+  const int r0 = clamped(p.cu[x.b], p.tokens), r1 = clamped(p.cu[x.b + 1], p.tokens), start = p.starts[x.b];
+  const int64_t from = start < 0 ? 0 : start, first = (from / 8 + (id - before(x.b))) * 8;
+  if (r1 <= r0 || id < before(x.b) || first >= from + (r1 - r0) || first > 0x7FFFFFF0) return false;
+  const int lane = threadIdx.x & 63, place = (int)first + (lane >> 3);
+  x.first = (int)first;
+  x.place = place;
+  x.real = place >= from && place < from + (r1 - r0);
+  x.row = r0 + (int)(place - from);
+  x.whole = first >= from && first + 8 <= from + (r1 - r0);
+  x.page = nullptr;
+  const int entry = (int)first >> pool.page_shift;
+  if (start >= 0 && entry < p.width) {
+    const int page = p.table[x.b * p.table_stride + entry];
+    if (page >= 0 && page < pool.pages) x.page = pool.head(page, 0);
+  }
+  return true;
+}
+
+
+// over the 8 lanes of a token
+__device__ __forceinline__ float lanes8(float x, bool largest) {
+  auto step = [&](auto moved) { x = largest ? __builtin_fmaxf(x, moved) : __builtin_fminf(x, moved); };
+  step(as_f((uint32_t)__builtin_amdgcn_update_dpp((int)as_u(x), (int)as_u(x), 0xB1, 0xF, 0xF, false)));        // lane ^ 1
+  step(as_f((uint32_t)__builtin_amdgcn_update_dpp((int)as_u(x), (int)as_u(x), 0x4E, 0xF, 0xF, false)));        // lane ^ 2
+  step(as_f((uint32_t)__builtin_amdgcn_update_dpp((int)as_u(x), (int)as_u(x), 0x141, 0xF, 0xF, false)));       // 7 - lane
+  return x;
+}
+__device__ __forceinline__ uint32_t lanes8_max(uint32_t x) {
+  auto step = [&](uint32_t moved) { x = moved > x ? moved : x; };
+  step((uint32_t)__builtin_amdgcn_update_dpp((int)x, (int)x, 0xB1, 0xF, 0xF, false));
+  step((uint32_t)__builtin_amdgcn_update_dpp((int)x, (int)x, 0x4E, 0xF, 0xF, false));
+  step((uint32_t)__builtin_amdgcn_update_dpp((int)x, (int)x, 0x141, 0xF, 0xF, false));
+  return x;
+}
+
+// N elements of a lane, 16-bit, as they lie in memory
+template <int N> struct Elements { uint32_t w[N / 2]; };
+
+template <int N> __device__ __forceinline__ Elements<N> load(const char* p) {
+  Elements<N> x;
+#pragma unroll
+  for (int i = 0; i < N / 8; ++i) {
+    const uint4v y = *reinterpret_cast<const uint4v*>(p + 16 * i);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x.w[4 * i + j] = y[j];
+  }
+  return x;
+}
+template <int N> __device__ __forceinline__ void store(char* p, const Elements<N>& x) {
+#pragma unroll
+  for (int i = 0; i < N / 8; ++i) *reinterpret_cast<uint4v*>(p + 16 * i) = uint4v{x.w[4 * i], x.w[4 * i + 1], x.w[4 * i + 2], x.w[4 * i + 3]};
+}
+
+// The rotation of a lane's elements e0 .. e0 + N of a token, in chunks of 8: cosines and sines, which are the same for every head.
+template <int N> struct Turn {
+  float c[N], s[N];      // (interleaved: the first half of each chunk only)
+  int part[N / 8];       // 0: the chunk is not rotated, 1: its elements come first in their pairs, 2: second, 3: pairs side by side
+};
+template <int N> __device__ __forceinline__ void turn_of(Turn<N>& t, const float* row, int e0, int rotary, bool interleaved) {
+  const int half = rotary / 2;
+#pragma unroll
+  for (int i = 0; i < N / 8; ++i) {
+    const int e = e0 + 8 * i;
+    t.part[i] = e >= rotary ? 0 : interleaved ? 3 : e < half ? 1 : 2;
+    const int at = e >= rotary ? 0 : interleaved ? e / 2 : e < half ? e : e - half;
+#pragma unroll
+    for (int j = 0; j < 8; j += 4) {
+      const bool used = !interleaved || j == 0;
+      const float4v c = used ? *reinterpret_cast<const float4v*>(row + at + j) : (float4v)0.f, s = used ? *reinterpret_cast<const float4v*>(row + half + at + j) : (float4v)0.f;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) { t.c[8 * i + j + x] = c[x]; t.s[8 * i + j + x] = s[x]; }
+    }
+  }
+}
+
+// x rotated and rounded; p: the row's address at element 0, for the partners (every lane of a token has read them before any stores)
+template <int N, bool BF> __device__ __forceinline__ Elements<N> rotated(const Elements<N>& x, const Turn<N>& t, const char* row, int e0, int rotary) {
+#pragma clang fp contract(off)
+  Elements<N> y;
+  const int half = rotary / 2;
+#pragma unroll
+  for (int i = 0; i < N / 8; ++i) {
+    const int part = t.part[i], other = part == 1 ? half : part == 2 ? -half : 0;
+    const uint4v z = *reinterpret_cast<const uint4v*>(row + 2 * (e0 + 8 * i + other));
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t w = x.w[4 * i + j];
+      const float a = low_of<BF>(w), b = high_of<BF>(w);
+      float u, v;
+      if (part == 3) {
+        const float c = t.c[8 * i + j], s = t.s[8 * i + j];
+        u = a * c - b * s;
+        v = b * c + a * s;
+      } else {
+        const float pa = low_of<BF>(z[j]), pb = high_of<BF>(z[j]), c0 = t.c[8 * i + 2 * j], c1 = t.c[8 * i + 2 * j + 1];
+        const float s0 = t.s[8 * i + 2 * j], s1 = t.s[8 * i + 2 * j + 1];
+        const float m0 = pa * s0, m1 = pb * s1, n0 = a * c0, n1 = b * c1;
+        u = part == 1 ? n0 - m0 : n0 + m0;
+        v = part == 1 ? n1 - m1 : n1 + m1;
+      }
+      y.w[4 * i + j] = part == 0 ? w : pack2<BF>(u, v);
+    }
+  }
+  return y;
+}
+
+template <int N> struct Codes { uint32_t w[N / 8]; uint32_t params; };      // 8 codes a word, lowest bits first; scale and minimum (in_dtype)
+
+template <int N, bool BF> __device__ __forceinline__ Codes<N> coded(const Elements<N>& x) {
+#pragma clang fp contract(off)
+  Codes<N> r;
+  float lo = low_of<BF>(x.w[0]), hi = lo;
+  ushort2v most = {0, 0};
+#pragma unroll
+  for (int i = 0; i < N / 2; ++i) {
+    const float a = low_of<BF>(x.w[i]), b = high_of<BF>(x.w[i]);
+    lo = __builtin_fminf(lo, __builtin_fminf(a, b));
+    hi = __builtin_fmaxf(hi, __builtin_fmaxf(a, b));
+    most = __builtin_elementwise_max(most, __builtin_bit_cast(ushort2v, x.w[i] & 0x7FFF7FFFu));
+  }
+  lo = lanes8(lo, false);
+  hi = lanes8(hi, true);
+  const uint32_t top = lanes8_max(most[0] > most[1] ? most[0] : most[1]);
+  const bool fine = top < largest_finite_plus_one<BF>();
+  const uint32_t params = pack2<BF>(hi / 15.f - lo / 15.f, lo);
+  const float step = low_of<BF>(params) * 0.5f, base = lo * 0.5f;
+  r.params = fine ? params : 0x7FFF7FFFu;
+#pragma unroll
+  for (int i = 0; i < N / 8; ++i) {
+    uint32_t w = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float e = j & 1 ? high_of<BF>(x.w[4 * i + j / 2]) : low_of<BF>(x.w[4 * i + j / 2]);
+      const float c = __builtin_rintf((e * 0.5f - base) / step);
+      w |= (uint32_t)__builtin_fminf(__builtin_fmaxf(c, 0.f), 15.f) << (4 * j);
+    }
+    r.w[i] = fine && step != 0.f ? w : 0u;
+  }
+  return r;
+}
+
+// A wave takes 8 places of a sequence and one head at a time: lane 8t + c has elements c * D/8 .. of token t.
+template <int D, bool BF>
+__global__ __launch_bounds__(256) void ftcache_put(const Args a, const bool interleaved) {
+  constexpr int N = D / 8;
+  __shared__ uint16_t turned[4][D / 4][8];            // value codes of 8 tokens, to be written 16 bytes at a time
+  Block x;
+  if (!block_of(a.at, a.pool, blockIdx.x, x)) return;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, t = lane >> 3, c = lane & 7, e0 = c * N;
+  const bool known = x.place < a.positions, kept = x.real && known && x.page;
+  if (blockIdx.y == 0 && wave == 0) {
+    const uint64_t refused = __ballot(x.real && !kept && c == 0);
+    if (refused && lane == 0) atomicAdd(a.refused, (unsigned long long)__popcll(refused));
+  }
+  const bool whole = x.whole && __all(kept);
+  Turn<N> turn;
+  turn_of<N>(turn, a.rotation + (int64_t)(known ? x.place : 0) * a.rotary, e0, a.rotary, interleaved);
+  const int first = a.q.data ? 0 : a.heads, kv = a.pool.kv_heads, items = a.heads + 2 * kv;
+  const int in_page = x.place & ((1 << a.pool.page_shift) - 1);
+  for (int item = first + blockIdx.y * 4 + wave; item < items; item += gridDim.y * 4) {
+    const bool is_q = item < a.heads, is_v = item >= a.heads + kv;
+    const int head = is_q ? item : is_v ? item - a.heads - kv : item - a.heads;
+    const Rows& in = is_q ? a.q : is_v ? a.v : a.k;
+    Elements<N> y;
+    if (x.real) {
+      const char* row = in.data + (int64_t)x.row * in.token + (int64_t)head * in.head;
+      y = load<N>(row + 2 * e0);
+      if (!is_v) {
+        y = rotated<N, BF>(y, turn, row, e0, a.rotary);
+        if (!known)
+#pragma unroll
+          for (int i = 0; i < N / 2; ++i) y.w[i] = 0x7FFF7FFFu;
+        const Rows& out = is_q ? a.q_out : a.k_out;
+        if (out.data) store<N>(out.data + (int64_t)x.row * out.token + (int64_t)head * out.head + 2 * e0, y);
+      }
+    }
+    if (is_q) continue;
+    if (!x.real)
+#pragma unroll
+      for (int i = 0; i < N / 2; ++i) y.w[i] = 0;
+    const Codes<N> z = coded<N, BF>(y);
+    char* const page = x.page + (int64_t)head * a.pool.head_bytes;      // (used where kept only)
+    const int ps = 1 << a.pool.page_shift;
+    if (kept && c == 0) {
+      uint16_t* par = reinterpret_cast<uint16_t*>(page + ps * D) + (in_page >> 3) * 32 + (is_v ? 16 : 0) + t;
+      par[0] = (uint16_t)z.params;
+      par[8] = (uint16_t)(z.params >> 16);
+    }
+    if (!is_v) {
+      if (kept) {
+        if constexpr (N == 16) *reinterpret_cast<uint2v*>(page + in_page * (D / 2) + e0 / 2) = uint2v{z.w[0], z.w[1]};
+        else *reinterpret_cast<uint32_t*>(page + in_page * (D / 2) + e0 / 2) = z.w[0];
+      }
+    } else {
+      char* const block = page + ps * (D / 2) + (in_page >> 3) * (4 * D);
+      if (whole) {
+#pragma unroll
+        for (int i = 0; i < N / 4; ++i) turned[wave][c * (N / 4) + i][t] = (uint16_t)(z.w[i / 2] >> (16 * (i & 1)));
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        if (lane < D / 4) *reinterpret_cast<uint4v*>(block + lane * 16) = *reinterpret_cast<const uint4v*>(turned[wave][lane]);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+      } else if (kept) {
+#pragma unroll
+        for (int i = 0; i < N / 4; ++i)
+          *reinterpret_cast<uint16_t*>(block + (c * (N / 4) + i) * 16 + t * 2) = (uint16_t)(z.w[i / 2] >> (16 * (i & 1)));
+      }
+    }
+  }
+}
+
+template <int D, bool BF>
+__global__ __launch_bounds__(256) void ftcache_get(const Args a) {
+#pragma clang fp contract(off)
+  constexpr int N = D / 8;
+  Block x;
+  if (!block_of(a.at, a.pool, blockIdx.x, x)) return;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, t = lane >> 3, c = lane & 7, e0 = c * N;
+  if (blockIdx.y == 0 && wave == 0 && !x.page) {
+    const uint64_t refused = __ballot(x.real && c == 0);
+    if (refused && lane == 0) atomicAdd(a.refused, (unsigned long long)__popcll(refused));
+  }
+  if (!x.real) return;
+  const int kv = a.pool.kv_heads, in_page = x.place & ((1 << a.pool.page_shift) - 1), ps = 1 << a.pool.page_shift;
+  for (int item = blockIdx.y * 4 + wave; item < 2 * kv; item += gridDim.y * 4) {
+    const bool is_v = item >= kv;
+    const int head = is_v ? item - kv : item;
+    Elements<N> y;
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) y.w[i] = 0x7FFF7FFFu;
+    if (x.page) {
+      const char* const page = x.page + (int64_t)head * a.pool.head_bytes;
+      uint32_t w[N / 8];
+      if (is_v) {
+        const char* const block = page + ps * (D / 2) + (in_page >> 3) * (4 * D) + t * 2;
+#pragma unroll
+        for (int i = 0; i < N / 8; ++i)
+          w[i] = (uint32_t)*reinterpret_cast<const uint16_t*>(block + (c * (N / 4) + 2 * i) * 16) |
+                 (uint32_t)*reinterpret_cast<const uint16_t*>(block + (c * (N / 4) + 2 * i + 1) * 16) << 16;
+      } else {
+#pragma unroll
+        for (int i = 0; i < N / 8; ++i) w[i] = *reinterpret_cast<const uint32_t*>(page + in_page * (D / 2) + e0 / 2 + 4 * i);
+      }
+      const uint16_t* par = reinterpret_cast<const uint16_t*>(page + ps * D) + (in_page >> 3) * 32 + (is_v ? 16 : 0) + t;
+      const float scale = low_of<BF>(par[0]), low = low_of<BF>(par[8]);
+#pragma unroll
+      for (int i = 0; i < N / 2; ++i) {
+        const uint32_t v = w[i / 4] >> (8 * (i & 3));
+        y.w[i] = pack2<BF>((float)(v & 15) * scale + low, (float)(v >> 4 & 15) * scale + low);
+      }
+    }
+    const Rows& out = is_v ? a.v : a.k;
+    store<N>(out.data + (int64_t)x.row * out.token + (int64_t)head * out.head + 2 * e0, y);
+  }
+}
+
+// ------------------------------------------------------------------ attention of single tokens
+//
+// The query heads of a group are rows of the matrix instructions (16 a pass): scores transposed, S^T = K q^T with 16x16x32, keys down and
+// heads across, so that lane l owns row l % 16 and, of a step of 32 tokens, the 8 tokens 8g .. 8g + 7 (g = l / 16) whose weights are its
+// operand of O^T = V^T P^T as they lie.  Neither codes nor weights pass through LDS.
+//
+// Codes enter the products as they are.  A key code's bits alone are the number c * 2^-24 in fp16, c * 2^-133 in bf16 (and 16 c of them four
+// bits higher): subnormal or next to it, which the matrix instructions take like any other, and one AND gives two of them.  The query's row is scaled up by a
+// power of two, which the score loses again.  Value codes lie under the bits of 128 in bf16, 128 + c; the offset leaves through the sum of the weights.
+// Scale and minimum of a token are applied to its scores and to its weights, in 32 bits:
+//     score = ks (q . c) + kz (sum q),   O = sum (p vs) c' + sum p vz.
+struct OneArgs {
+  Pool pool;
+  Rows q, o;
+  const int32_t *lengths, *table;
+  int64_t table_stride;
+  int32_t batch, width, group, row_tiles;       // row_tiles: passes of 16 heads for a group
+  int32_t chunks;                               // wanted, over all sequences
+  float scale_log2;
+  float* ws;                                    // states of divided sequences
+  uint32_t* done;                               // [batch][kv_heads * row_tiles], 0 between calls
+  unsigned long long* refused;
+};
+
+constexpr int ONE_WAVES = 4, ONE_STEP = 32, ONE_UNIT = ONE_WAVES * ONE_STEP;      // tokens of a step of a wave, of a workgroup
+
+template <bool BF> __device__ __forceinline__ float4v mfma16(uint4v a, uint4v b, float4v c) {
+  if constexpr (BF) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf8v, a), __builtin_bit_cast(bf8v, b), c, 0, 0, 0);
+  else return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8v, a), __builtin_bit_cast(half8v, b), c, 0, 0, 0);
+}
+
+// 8 codes of a word as an operand: words (c0, c4), (16 c1, 16 c5), (c2, c6), (16 c3, 16 c7)
+__device__ __forceinline__ uint4v key_operand(uint32_t w) {
+  const uint32_t u = w >> 8;
+  return uint4v{w & 0x000F000Fu, w & 0x00F000F0u, u & 0x000F000Fu, u & 0x00F000F0u};
+}
+__device__ __forceinline__ uint32_t value_codes(uint32_t w, int nibble) { return (w >> (4 * nibble) & 0x000F000Fu) | 0x43004300u; }
+
+__device__ __forceinline__ int64_t sum64(int64_t x) {
+#pragma unroll
+  for (int d = 32; d; d >>= 1) x += __shfl_xor(x, d);
+  return x;
+}
+
+struct Piece { int b, first, count, part, parts, slot; };      // tokens first .. first + count of sequence b, part of parts; place of part 0's state
+
+// Sequences are divided into pieces of one length, the same for all, chosen so that there are about `chunks` pieces in all: the last of a sequence is shorter.
+__device__ __forceinline__ bool piece_of(const OneArgs& a, int id, Piece& p, bool& known) {
+  const int lane = threadIdx.x & 63, per = (a.batch + 63) / 64, most = (int)((int64_t)a.width << a.pool.page_shift > 0x7FFFFF00 ? 0x7FFFFF00 : (int64_t)a.width << a.pool.page_shift);
+  auto length = [&](int b) { const int n = b < a.batch ? a.lengths[b] : 0; return n < 0 || n > most ? 0 : n; };
+  int64_t total = 0;
+  for (int i = 0; i < per; ++i) total += length(lane * per + i);
+  total = sum64(total);
+  int64_t units = ((total + a.chunks - 1) / a.chunks + ONE_UNIT - 1) / ONE_UNIT;
+  units = units < 1 ? 1 : units > 0x7FFFFF00 / ONE_UNIT ? 0x7FFFFF00 / ONE_UNIT : units;
+  const int size = (int)units * ONE_UNIT;
+  auto parts_of = [&](int n) { return n > size ? (int)(((int64_t)n + size - 1) / size) : 1; };
+  int mine = 0, slots = 0;          // pieces; those of divided sequences, which leave a state
+  for (int i = 0; i < per; ++i) {
+    const int b = lane * per + i, n = parts_of(length(b));
+    mine += b < a.batch ? n : 0;
+    slots += n > 1 ? n : 0;
+  }
+  int upto = mine, slots_upto = slots;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int x = __shfl_up(upto, d), y = __shfl_up(slots_upto, d);
+    upto += lane >= d ? x : 0;
+    slots_upto += lane >= d ? y : 0;
+  }
+  const uint64_t beyond = __ballot(upto > id);
+  if (!beyond) return false;
+  const int owner = __ffsll((unsigned long long)beyond) - 1;
+  int left = id - __shfl(upto - mine, owner), slot = __shfl(slots_upto - slots, owner);
+  for (int i = 0; i < per; ++i) {
+    const int b = owner * per + i;
+    if (b >= a.batch) return false;
+    const int n = length(b), parts = parts_of(n);
+    if (left < parts) {
+      const int raw = a.lengths[b];
+      known = raw >= 0 && raw <= most;
+      p = Piece{b, left * size, n - left * size < size ? n - left * size : size, left, parts, slot};
+      return true;
+    }
+    left -= parts;
+    slot += parts > 1 ? parts : 0;
+  }
+  return false;
+}
+
+template <int D> struct State {       // what a piece leaves of 16 rows: reference, sum of weights, then the output before its division
+  static constexpr int ROW = D + 2;
+};
+
+template <int D, bool BF, bool F32OUT>
+__global__ __launch_bounds__(ONE_WAVES * 64) void ftcache_one(const OneArgs a) {
+  constexpr int KW = D / 32;              // words of key codes per lane and token = matrix instructions over the head
+  constexpr int VQ = D / 64;              // value words of 4 elements per lane
+  constexpr int NO = D / 16;              // accumulators of the output
+  __shared__ float merged[ONE_WAVES][16][D + 1];
+  __shared__ float refs[ONE_WAVES][16], sums[ONE_WAVES][16];
+  __shared__ int last;
+  const int heads = a.pool.kv_heads * a.row_tiles, hr = blockIdx.x % heads, hk = hr / a.row_tiles, tile = hr % a.row_tiles;
+  Piece p;
+  bool known;
+  if (!piece_of(a, blockIdx.x / heads, p, known)) return;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, n = lane & 15;
+  const int rows = a.group - 16 * tile < 16 ? a.group - 16 * tile : 16, head0 = hk * a.group + 16 * tile;
+
+  // the row's query as an operand, scaled by a power of two so that its largest element lies in [2^10, 2^11) (fp16), at 2^126 or as far up as one
+  // factor brings it (bf16): the products with codes are then far from both ends of 32 bits, and sixteenths of small elements keep their bits
+  uint4v qf[KW];
+  float alpha, gamma;
+  {
+    const char* qp = a.q.data + (int64_t)p.b * a.q.token + (int64_t)(head0 + (n < rows ? n : 0)) * a.q.head + 2 * (8 * KW * g);
+    uint32_t w[4 * KW];
+    uint32_t most = 0;
+#pragma unroll
+    for (int i = 0; i < KW; ++i) {
+      const uint4v y = *reinterpret_cast<const uint4v*>(qp + 16 * i);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        w[4 * i + j] = y[j];
+        const uint32_t lo = as_u(low_of<BF>(y[j])) & 0x7FFFFFFFu, hi = as_u(high_of<BF>(y[j])) & 0x7FFFFFFFu;
+        most = lo > most ? lo : most;
+        most = hi > most ? hi : most;
+      }
+    }
+#pragma unroll
+    for (int d = 16; d < 64; d <<= 1) { const uint32_t x = __shfl_xor(most, d); most = x > most ? x : most; }
+    const int e = (int)(most >> 23) - 127;
+    int up_by = (BF ? 126 : 10) - e;
+    up_by = up_by > 126 ? 126 : up_by < -126 ? -126 : up_by;
+    const float up = as_f((uint32_t)(127 + up_by) << 23);
+    float plain = 0.f;
+#pragma unroll
+    for (int i = 0; i < KW; ++i) {
+      float f[8];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        plain += low_of<BF>(w[4 * i + j]);
+        plain += high_of<BF>(w[4 * i + j]);
+        f[2 * j] = low_of<BF>(w[4 * i + j]) * up;
+        f[2 * j + 1] = high_of<BF>(w[4 * i + j]) * up;
+      }
+      const float odd = 0.0625f;
+      qf[i] = uint4v{pack2<BF>(f[0], f[4]), pack2<BF>(f[1] * odd, f[5] * odd), pack2<BF>(f[2], f[6]), pack2<BF>(f[3] * odd, f[7] * odd)};
+    }
+#pragma unroll
+    for (int d = 16; d < 64; d <<= 1) plain += __shfl_xor(plain, d);
+    alpha = __builtin_ldexpf(a.scale_log2, (BF ? 133 : 24) - up_by);
+    gamma = a.scale_log2 * plain;
+  }
+
+  float4v o[NO], ones = (float4v)0.f;
+#pragma unroll
+  for (int i = 0; i < NO; ++i) o[i] = (float4v)0.f;
+  float ref = -3.4028234e38f, l = 0.f, z = 0.f;
+  bool bad = !known;
+  const int ps = 1 << a.pool.page_shift, end = p.first + p.count;
+  const int32_t* const table = a.table + p.b * a.table_stride;
+  auto page_of = [&](int token) {       // the page of a block of 8 tokens, the last one's for blocks behind the end
+    const int t = token < end ? token : end - 1, page = table[t >> a.pool.page_shift];
+    const bool fine = page >= 0 && page < a.pool.pages;
+    bad |= !fine;
+    return fine ? page : 0;
+  };
+  for (int t0 = p.first + wave * ONE_STEP; t0 < end; t0 += ONE_UNIT) {
+    const int kb = t0 + 8 * (n >> 2), vb = t0 + 8 * g, kc = kb < end ? kb : (end - 1) & ~7, vc = vb < end ? vb : (end - 1) & ~7;
+    const char* const kp = a.pool.head(page_of(kb), hk);
+    const char* const vp = a.pool.head(page_of(vb), hk);
+    const int kin = (kc & (ps - 1)) + (n & 3), vin = (vc & (ps - 1)) >> 3;
+    uint32_t kw[2][KW];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const char* at = kp + (kin + 4 * t) * (D / 2) + g * (4 * KW);
+      if constexpr (KW == 4) { const uint4v y = *reinterpret_cast<const uint4v*>(at); kw[t][0] = y[0]; kw[t][1] = y[1]; kw[t][2] = y[2]; kw[t][3] = y[3]; }
+      else { const uint2v y = *reinterpret_cast<const uint2v*>(at); kw[t][0] = y[0]; kw[t][1] = y[1]; }
+    }
+    uint4v vw[VQ], par[4];
+#pragma unroll
+    for (int i = 0; i < VQ; ++i) vw[i] = *reinterpret_cast<const uint4v*>(vp + ps * (D / 2) + vin * (4 * D) + (n * VQ + i) * 16);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) par[i] = *reinterpret_cast<const uint4v*>(vp + ps * D + vin * 64 + 16 * i);
+
+    float4v s[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      s[t] = (float4v)0.f;
+#pragma unroll
+      for (int i = 0; i < KW; ++i) s[t] = mfma16<BF>(key_operand(kw[t][i]), qf[i], s[t]);
+    }
+    float x[8], vs[8], vz[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float ks = j & 1 ? high_of<BF>(par[0][j / 2]) : low_of<BF>(par[0][j / 2]), kz = j & 1 ? high_of<BF>(par[1][j / 2]) : low_of<BF>(par[1][j / 2]);
+      vs[j] = j & 1 ? high_of<BF>(par[2][j / 2]) : low_of<BF>(par[2][j / 2]);
+      vz[j] = j & 1 ? high_of<BF>(par[3][j / 2]) : low_of<BF>(par[3][j / 2]);
+      x[j] = __builtin_fmaf(ks, alpha * s[j >> 2][j & 3], kz * gamma);
+    }
+    if (t0 + ONE_STEP > end) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (t0 + 8 * g + j >= end) { x[j] = -__builtin_inff(); vs[j] = 0.f; vz[j] = 0.f; }
+    }
+    float m = x[0];
+#pragma unroll
+    for (int j = 1; j < 8; ++j) m = __builtin_fmaxf(m, x[j]);
+    if (__any(m > ref + 8.f)) {
+      m = __builtin_fmaxf(m, __shfl_xor(m, 16));
+      m = __builtin_fmaxf(m, __shfl_xor(m, 32));
+      const float next = __builtin_fmaxf(m, ref), f = ex2(ref - next);
+      ref = next;
+      l *= f;
+      z *= f;
+      ones *= f;
+#pragma unroll
+      for (int i = 0; i < NO; ++i) o[i] *= f;
+    }
+    float w[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float e = ex2(x[j] - ref);
+      l += e;
+      z = __builtin_fmaf(e, vz[j], z);
+      w[j] = e * vs[j];
+    }
+    // weights in bf16; for fp16 tokens in two words, the second what the first leaves, so that they are no coarser than the tokens
+    uint4v ph, pl;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      ph[j] = pack2<true>(w[2 * j], w[2 * j + 1]);
+      if constexpr (!BF) pl[j] = pack2<true>(w[2 * j] - low_of<true>(ph[j]), w[2 * j + 1] - high_of<true>(ph[j]));
+    }
+    const uint4v one = {0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
+    ones = mfma16<true>(one, ph, ones);
+    if constexpr (!BF) ones = mfma16<true>(one, pl, ones);
+#pragma unroll
+    for (int i = 0; i < NO; ++i) {
+      const uint4v v = vw[i / 4];
+      const uint4v c = {value_codes(v[0], i & 3), value_codes(v[1], i & 3), value_codes(v[2], i & 3), value_codes(v[3], i & 3)};
+      o[i] = mfma16<true>(c, ph, o[i]);
+      if constexpr (!BF) o[i] = mfma16<true>(c, pl, o[i]);
+    }
+  }
+  bad = __any(bad);
+#pragma unroll
+  for (int d = 16; d < 64; d <<= 1) { l += __shfl_xor(l, d); z += __shfl_xor(z, d); }
+  const float shift = z - 128.f * ones[0];
+  if (bad) l = __builtin_nanf("");
+  if (g == 0) { refs[wave][n] = ref; sums[wave][n] = l; }
+#pragma unroll
+  for (int i = 0; i < NO; ++i)
+#pragma unroll
+    for (int v = 0; v < 4; ++v) merged[wave][n][(4 * g + v) * NO + i] = o[i][v] + shift;
+  __syncthreads();
+
+  const int tid = threadIdx.x;
+  float* const ws = a.ws + ((int64_t)(p.slot + p.part) * heads + hr) * 16 * State<D>::ROW;      // (of a divided sequence)
+  auto finish = [&](int row, int e, float value, float sum) {
+    const float y = sum == 0.f ? 0.f : value / sum;
+    char* op = a.o.data + (int64_t)p.b * a.o.token + (int64_t)(head0 + row) * a.o.head;
+    if constexpr (F32OUT) reinterpret_cast<float*>(op)[e] = y;
+    else reinterpret_cast<uint16_t*>(op)[e] = (uint16_t)pack2<BF>(y, y);
+  };
+  for (int x = tid; x < rows * D; x += ONE_WAVES * 64) {
+    const int row = x / D, e = x % D;
+    float most = refs[0][row];
+#pragma unroll
+    for (int w = 1; w < ONE_WAVES; ++w) most = __builtin_fmaxf(most, refs[w][row]);
+    float value = 0.f, sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < ONE_WAVES; ++w) {
+      const float f = ex2(refs[w][row] - most);
+      value += f * merged[w][row][e];
+      sum += f * sums[w][row];
+    }
+    if (p.parts == 1) finish(row, e, value, sum);
+    else {
+      float* const r = ws + row * State<D>::ROW;
+      r[2 + e] = value;
+      if (e == 0) { r[0] = most; r[1] = sum; }
+    }
+  }
+  if (tid == 0 && bad && p.part == 0 && hr == 0) atomicAdd(a.refused + 1, 1ull);
+  if (p.parts == 1) return;
+  __threadfence();
+  __syncthreads();
+  if (tid == 0) {
+    uint32_t* const done = a.done + (int64_t)p.b * heads + hr;
+    const uint32_t before = atomicAdd(done, 1u);
+    last = before + 1 == (uint32_t)p.parts;
+    if (last) *done = 0;
+  }
+  __syncthreads();
+  if (!last) return;
+  __threadfence();
+  // this workgroup came last: the states of all parts, in their order
+  const float* const first = a.ws + ((int64_t)p.slot * heads + hr) * 16 * State<D>::ROW;
+  const int64_t next = (int64_t)heads * 16 * State<D>::ROW;
+  for (int x = tid; x < rows * D; x += ONE_WAVES * 64) {
+    const int row = x / D, e = x % D;
+    const float* const r = first + row * State<D>::ROW;
+    float most = r[0];
+    for (int i = 1; i < p.parts; ++i) most = __builtin_fmaxf(most, r[i * next]);
+    float value = 0.f, sum = 0.f;
+    for (int i = 0; i < p.parts; ++i) {
+      const float f = ex2(r[i * next] - most);
+      value += f * r[i * next + 2 + e];
+      sum += f * r[i * next + 1];
+    }
+    finish(row, e, value, sum);
+  }
+}
+
+typedef void (*put_fn)(const Args, const bool);
+typedef void (*get_fn)(const Args);
+typedef void (*one_fn)(const OneArgs);
+template <int D, bool BF> static one_fn one_of(bool f32) { return f32 ? ftcache_one<D, BF, true> : ftcache_one<D, BF, false>; }
+
+}  // namespace ftcache
+
+using namespace ftcache;
+
+struct ftcache_ctx {
+  ftcache_config cfg;
+  put_fn put = nullptr;
+  get_fn get = nullptr;
+  one_fn one = nullptr;
+  int shift = 0, row_tiles = 1, chunks = 1;
+  void* scratch = nullptr;
+  float* ws = nullptr;
+  uint32_t* done = nullptr;
+  unsigned long long* refused = nullptr;
+  std::string err;
+};
+
+static thread_local std::string g_cache_create_err;
+
+static int cfail(ftcache_ctx* c, int code, const char* msg) {
+  try {
+    (c ? c->err : g_cache_create_err) = msg;
+  } catch (...) {
+  }
+  return code;
+}
+static int cfail_hip(ftcache_ctx* c, const char* what, hipError_t e) {
+  try {
+    (c ? c->err : g_cache_create_err) = std::string(what) + ": " + hipGetErrorString(e);
+  } catch (...) {
+  }
+  return e == hipErrorOutOfMemory ? FTCACHE_ENOMEM : FTCACHE_EHIP;
+}
+
+namespace {
+// the context's device for the time of a call
+struct OnDevice {
+  int before = 0, device;
+  hipError_t status;
+  explicit OnDevice(int d) : device(d) {
+    status = hipGetDevice(&before);
+    if (status == hipSuccess && before != device) status = hipSetDevice(device);
+  }
+  ~OnDevice() { if (before != device) (void)hipSetDevice(before); }
+};
+
+// nullptr, or what is wrong with a tensor of rows
+const char* rows_of(const ftcache_rows* r, int size, bool none, Rows& out) {
+  if (!r) return "null argument";
+  if ((!r->data && !none) || ((uintptr_t)r->data & 15)) return "tensors must be 16-byte aligned device pointers";
+  if (((uintptr_t)r->token_stride | (uintptr_t)r->head_stride) % (16 / size)) return "strides must be whole 16-byte words";
+  if (r->token_stride < 0 || r->head_stride < 0 || r->token_stride > (1ll << 40) || r->head_stride > (1ll << 40)) return "strides must lie in 0 to 2^40 elements";
+  out = Rows{static_cast<char*>(r->data), r->token_stride * size, r->head_stride * size};
+  return nullptr;
+}
+const char* places_of(const ftcache_places* p, Places& out) {
+  if (!p || !p->cu_seqlens || !p->starts || !p->page_table) return "null argument";
+  if (p->batch < 1 || p->tokens < 0) return "batch must be >= 1 and tokens >= 0";
+  if (p->table_width < 1 || p->table_stride < p->table_width) return "table_width must be >= 1 and at most table_stride";
+  if ((int64_t)p->tokens / 8 + 2ll * p->batch > 0x7FFFFFFFll) return "too many tokens";
+  out = Places{p->cu_seqlens, p->starts, p->page_table, p->table_stride, p->batch, p->tokens, p->table_width};
+  return nullptr;
+}
+constexpr int CUS = 256;
+}  // namespace
+
+extern "C" int ftcache_create(const ftcache_config* cfg, ftcache_ctx** out) {
+  if (!cfg || !out) return cfail(nullptr, FTCACHE_EINVAL, "null argument");
+  *out = nullptr;
+  if (cfg->struct_size != sizeof(ftcache_config)) return cfail(nullptr, FTCACHE_EINVAL, "struct_size mismatch");
+  if (cfg->heads < 1 || cfg->kv_heads < 1 || cfg->heads % cfg->kv_heads) return cfail(nullptr, FTCACHE_EINVAL, "heads must be a positive multiple of kv_heads");
+  if (cfg->heads > 4096) return cfail(nullptr, FTCACHE_EUNSUPPORTED, "more than 4096 heads");
+  if (cfg->head_dim != 64 && cfg->head_dim != 128) return cfail(nullptr, FTCACHE_EUNSUPPORTED, "head_dim must be 64 or 128");
+  if (cfg->pages < 1) return cfail(nullptr, FTCACHE_EINVAL, "pages must be >= 1");
+  if (cfg->page_size < 16 || cfg->page_size > 1024 || (cfg->page_size & (cfg->page_size - 1))) return cfail(nullptr, FTCACHE_EUNSUPPORTED, "page_size must be a power of two, 16 to 1024");
+  if (cfg->in_dtype != FTCACHE_F16 && cfg->in_dtype != FTCACHE_BF16) return cfail(nullptr, FTCACHE_EINVAL, "in_dtype must be F16 or BF16");
+  if (cfg->out_dtype != FTCACHE_F32 && cfg->out_dtype != cfg->in_dtype) return cfail(nullptr, FTCACHE_EINVAL, "out_dtype must be F32 or the input type");
+  if (cfg->rotary_dim < 0 || cfg->rotary_dim > cfg->head_dim || cfg->rotary_dim % 16) return cfail(nullptr, FTCACHE_EUNSUPPORTED, "rotary_dim must be a multiple of 16 up to head_dim");
+  if (cfg->interleaved != 0 && cfg->interleaved != 1) return cfail(nullptr, FTCACHE_EINVAL, "interleaved must be 0 or 1");
+  if (!(std::fabs(cfg->softmax_scale) <= 3.0e38f)) return cfail(nullptr, FTCACHE_EINVAL, "softmax_scale is not finite");
+  if (cfg->max_batch < 1 || cfg->max_batch > 65536) return cfail(nullptr, FTCACHE_EINVAL, "max_batch must be 1 to 65536");
+  ftcache_ctx* c = new (std::nothrow) ftcache_ctx();
+  if (!c) return cfail(nullptr, FTCACHE_ENOMEM, "out of host memory");
+  c->cfg = *cfg;
+  ftcache_config& e = c->cfg;
+  if (!(e.softmax_scale > 0.f)) e.softmax_scale = 1.0f / std::sqrt((float)e.head_dim);
+  if (e.rotary_dim == 0) e.rotary_dim = e.head_dim;
+  while ((1 << c->shift) < e.page_size) ++c->shift;
+  c->row_tiles = (e.heads / e.kv_heads + 15) / 16;
+  const bool bf = e.in_dtype == FTCACHE_BF16, f32 = e.out_dtype == FTCACHE_F32;
+  if (e.head_dim == 128) {
+    c->put = bf ? ftcache_put<128, true> : ftcache_put<128, false>;
+    c->get = bf ? ftcache_get<128, true> : ftcache_get<128, false>;
+    c->one = bf ? one_of<128, true>(f32) : one_of<128, false>(f32);
+  } else {
+    c->put = bf ? ftcache_put<64, true> : ftcache_put<64, false>;
+    c->get = bf ? ftcache_get<64, true> : ftcache_get<64, false>;
+    c->one = bf ? one_of<64, true>(f32) : one_of<64, false>(f32);
+  }
+  const int64_t heads = (int64_t)e.kv_heads * c->row_tiles;
+  c->chunks = (int)(4 * CUS / heads < 1 ? 1 : 4 * CUS / heads);
+  // divided sequences are longer than a piece: together they have fewer than twice `chunks` pieces
+  const size_t ws = (size_t)2 * c->chunks * heads * 16 * (e.head_dim + 2) * sizeof(float), done = (size_t)e.max_batch * heads * sizeof(uint32_t);
+  OnDevice here(e.device);
+  hipError_t he = here.status;
+  if (he == hipSuccess) he = hipMalloc(&c->scratch, 256 + ((done + 255) & ~(size_t)255) + ws);
+  if (he == hipSuccess) he = hipMemset(c->scratch, 0, 256 + done);
+  if (he == hipSuccess) he = hipDeviceSynchronize();
+  if (he != hipSuccess) {
+    const int rc = cfail_hip(nullptr, "device memory", he);
+    if (c->scratch) (void)hipFree(c->scratch);
+    delete c;
+    return rc;
+  }
+  c->refused = static_cast<unsigned long long*>(c->scratch);
+  c->done = reinterpret_cast<uint32_t*>(static_cast<char*>(c->scratch) + 256);
+  c->ws = reinterpret_cast<float*>(static_cast<char*>(c->scratch) + 256 + ((done + 255) & ~(size_t)255));
+  *out = c;
+  return FTCACHE_OK;
+}
+
+extern "C" int ftcache_get_config(const ftcache_ctx* ctx, ftcache_config* effective) {
+  if (!ctx || !effective) return FTCACHE_EINVAL;
+  *effective = ctx->cfg;
+  return FTCACHE_OK;
+}
+
+extern "C" int64_t ftcache_page_bytes(const ftcache_ctx* c) {
+  return c ? (int64_t)c->cfg.kv_heads * c->cfg.page_size * (c->cfg.head_dim + 8) : FTCACHE_EINVAL;
+}
+
+static Pool pool_of(const ftcache_ctx* c, const void* pool) {
+  return Pool{static_cast<char*>(const_cast<void*>(pool)), c->cfg.pages, c->cfg.kv_heads, c->shift, c->cfg.page_size * (c->cfg.head_dim + 8)};
+}
+
+extern "C" int ftcache_append(ftcache_ctx* c, void* pool, const ftcache_places* places, const float* rotation, int32_t positions,
+                              const ftcache_rows* q, const ftcache_rows* k, const ftcache_rows* v, const ftcache_rows* q_out,
+                              const ftcache_rows* k_out, void* hip_stream) {
+  if (!c) return FTCACHE_EINVAL;
+  if (!pool || ((uintptr_t)pool & 15)) return cfail(c, FTCACHE_EINVAL, "pool must be a 16-byte aligned device pointer");
+  if (!rotation || ((uintptr_t)rotation & 15) || positions < 1) return cfail(c, FTCACHE_EINVAL, "rotation must be a 16-byte aligned device pointer to at least one position");
+  const ftcache_config& e = c->cfg;
+  Args a;
+  const char* wrong = places_of(places, a.at);
+  if (wrong) return cfail(c, FTCACHE_EINVAL, wrong);
+  const bool none = a.at.tokens == 0;
+  if ((wrong = rows_of(q, 2, true, a.q)) || (wrong = rows_of(k, 2, none, a.k)) || (wrong = rows_of(v, 2, none, a.v)) ||
+      (wrong = rows_of(q_out, 2, true, a.q_out)) || (wrong = rows_of(k_out, 2, true, a.k_out)))
+    return cfail(c, FTCACHE_EINVAL, wrong);
+  if (!a.q.data != !a.q_out.data) return cfail(c, FTCACHE_EINVAL, "q and q_out go together");
+  if (none) return FTCACHE_OK;
+  a.pool = pool_of(c, pool);
+  a.rotation = rotation;
+  a.positions = positions;
+  a.heads = e.heads;
+  a.rotary = e.rotary_dim;
+  a.refused = c->refused;
+  const int blocks = a.at.tokens / 8 + 2 * a.at.batch, items = (a.q.data ? e.heads : 0) + 2 * e.kv_heads;
+  // few blocks: their heads are dealt to more workgroups
+  int split = (4 * CUS + blocks - 1) / blocks;
+  split = split < 1 ? 1 : split > (items + 3) / 4 ? (items + 3) / 4 : split;
+  OnDevice here(e.device);
+  if (here.status != hipSuccess) return cfail_hip(c, "device", here.status);
+  hipLaunchKernelGGL(c->put, dim3(blocks, split), dim3(256), 0, (hipStream_t)hip_stream, a, e.interleaved != 0);
+  const hipError_t he = hipGetLastError();
+  return he == hipSuccess ? FTCACHE_OK : cfail_hip(c, "launch", he);
+}
+
+extern "C" int ftcache_read(ftcache_ctx* c, const void* pool, const ftcache_places* places, const ftcache_rows* k, const ftcache_rows* v,
+                            void* hip_stream) {
+  if (!c) return FTCACHE_EINVAL;
+  if (!pool || ((uintptr_t)pool & 15)) return cfail(c, FTCACHE_EINVAL, "pool must be a 16-byte aligned device pointer");
+  const ftcache_config& e = c->cfg;
+  Args a{};
+  const char* wrong = places_of(places, a.at);
+  if (wrong) return cfail(c, FTCACHE_EINVAL, wrong);
+  const bool none = a.at.tokens == 0;
+  if ((wrong = rows_of(k, 2, none, a.k)) || (wrong = rows_of(v, 2, none, a.v))) return cfail(c, FTCACHE_EINVAL, wrong);
+  if (none) return FTCACHE_OK;
+  a.pool = pool_of(c, pool);
+  a.refused = c->refused;
+  const int blocks = a.at.tokens / 8 + 2 * a.at.batch, items = 2 * e.kv_heads;
+  int split = (4 * CUS + blocks - 1) / blocks;
+  split = split < 1 ? 1 : split > (items + 3) / 4 ? (items + 3) / 4 : split;
+  OnDevice here(e.device);
+  if (here.status != hipSuccess) return cfail_hip(c, "device", here.status);
+  hipLaunchKernelGGL(c->get, dim3(blocks, split), dim3(256), 0, (hipStream_t)hip_stream, a);
+  const hipError_t he = hipGetLastError();
+  return he == hipSuccess ? FTCACHE_OK : cfail_hip(c, "launch", he);
+}
+
+extern "C" int ftcache_attend(ftcache_ctx* c, const void* pool, int32_t batch, const int32_t* lengths, const int32_t* page_table,
+                              int32_t table_width, int64_t table_stride, const ftcache_rows* q, const ftcache_rows* o, void* hip_stream) {
+  if (!c) return FTCACHE_EINVAL;
+  if (!pool || ((uintptr_t)pool & 15)) return cfail(c, FTCACHE_EINVAL, "pool must be a 16-byte aligned device pointer");
+  const ftcache_config& e = c->cfg;
+  if (batch < 1 || batch > e.max_batch) return cfail(c, FTCACHE_EINVAL, "batch must be 1 to max_batch");
+  if (!lengths || !page_table) return cfail(c, FTCACHE_EINVAL, "null argument");
+  if (table_width < 1 || table_stride < table_width) return cfail(c, FTCACHE_EINVAL, "table_width must be >= 1 and at most table_stride");
+  OneArgs a;
+  const char* wrong = rows_of(q, 2, false, a.q);
+  if (!wrong) wrong = rows_of(o, e.out_dtype == FTCACHE_F32 ? 4 : 2, false, a.o);
+  if (wrong) return cfail(c, FTCACHE_EINVAL, wrong);
+  a.pool = pool_of(c, pool);
+  a.lengths = lengths;
+  a.table = page_table;
+  a.table_stride = table_stride;
+  a.batch = batch;
+  a.width = table_width;
+  a.group = e.heads / e.kv_heads;
+  a.row_tiles = c->row_tiles;
+  a.chunks = c->chunks;
+  a.scale_log2 = e.softmax_scale * LOG2E;
+  a.ws = c->ws;
+  a.done = c->done;
+  a.refused = c->refused;
+  OnDevice here(e.device);
+  if (here.status != hipSuccess) return cfail_hip(c, "device", here.status);
+  hipLaunchKernelGGL(c->one, dim3((uint32_t)((c->chunks + batch) * e.kv_heads * c->row_tiles)), dim3(ONE_WAVES * 64), 0, (hipStream_t)hip_stream, a);
+  const hipError_t he = hipGetLastError();
+  return he == hipSuccess ? FTCACHE_OK : cfail_hip(c, "launch", he);
+}
+
+extern "C" int ftcache_report(ftcache_ctx* c, ftcache_report_view* out) {
+  if (!c) return FTCACHE_EINVAL;
+  if (!out) return cfail(c, FTCACHE_EINVAL, "null argument");
+  OnDevice here(c->cfg.device);
+  hipError_t he = here.status;
+  unsigned long long n[2] = {0, 0};
+  if (he == hipSuccess) he = hipDeviceSynchronize();
+  if (he == hipSuccess) he = hipMemcpy(n, c->refused, sizeof n, hipMemcpyDeviceToHost);
+  if (he == hipSuccess) he = hipMemset(c->refused, 0, sizeof n);
+  if (he == hipSuccess) he = hipDeviceSynchronize();
+  if (he != hipSuccess) return cfail_hip(c, "report", he);
+  out->refused_tokens = (int64_t)n[0];
+  out->refused_sequences = (int64_t)n[1];
+  return FTCACHE_OK;
+}
+
+extern "C" int ftcache_destroy(ftcache_ctx* c) {
+  if (!c) return FTCACHE_OK;
+  {
+    OnDevice here(c->cfg.device);
+    (void)hipFree(c->scratch);
+  }
+  delete c;
+  return FTCACHE_OK;
+}
+
+extern "C" const char* ftcache_last_error(const ftcache_ctx* c) { return c ? c->err.c_str() : g_cache_create_err.c_str(); }
