@@ -90,7 +90,7 @@ int64_t ftcache_page_bytes(const ftcache_ctx* ctx);
 int ftcache_append(ftcache_ctx* ctx, void* pool, const ftcache_places* places, const float* rotation, int32_t positions,
                    const ftcache_rows* q, const ftcache_rows* k, const ftcache_rows* v, const ftcache_rows* q_out,
                    const ftcache_rows* k_out, void* hip_stream);
-/* The cached keys and values of the given places, scale * c + minimum rounded to in_dtype.  A place that nothing was appended
+/* The cached keys and values of the given places, scale * c + minimum (in 32 bits) rounded to in_dtype and held to its finite numbers.  A place that nothing was appended
  * to gives what the pool holds there. */
 int ftcache_read(ftcache_ctx* ctx, const void* pool, const ftcache_places* places, const ftcache_rows* k, const ftcache_rows* v,
                  void* hip_stream);

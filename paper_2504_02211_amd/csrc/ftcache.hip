@@ -265,6 +265,12 @@ __global__ __launch_bounds__(256) void ftcache_put(const Args a, const bool inte
   }
 }
 
+// the type's finite numbers: a scale that was rounded up can take the largest code of the largest element beyond them (NaN stays)
+template <bool BF> __device__ __forceinline__ float held(float x) {
+  constexpr float top = BF ? 3.38953139e38f : 65504.f;
+  return x > top ? top : x < -top ? -top : x;
+}
+
 template <int D, bool BF>
 __global__ __launch_bounds__(256) void ftcache_get(const Args a) {
 #pragma clang fp contract(off)
@@ -302,7 +308,7 @@ __global__ __launch_bounds__(256) void ftcache_get(const Args a) {
 #pragma unroll
       for (int i = 0; i < N / 2; ++i) {
         const uint32_t v = w[i / 4] >> (8 * (i & 3));
-        y.w[i] = pack2<BF>((float)(v & 15) * scale + low, (float)(v >> 4 & 15) * scale + low);
+        y.w[i] = pack2<BF>(held<BF>((float)(v & 15) * scale + low), held<BF>((float)(v >> 4 & 15) * scale + low));
       }
     }
     const Rows& out = is_v ? a.v : a.k;
