@@ -340,7 +340,9 @@ struct OneArgs {
   unsigned long long* refused;
 };
 
-constexpr int ONE_WAVES = 4, ONE_STEP = 32, ONE_UNIT = ONE_WAVES * ONE_STEP;      // tokens of a step of a wave, of a workgroup
+constexpr int ONE_WAVES = 8, ONE_STEP = 32, ONE_UNIT = ONE_WAVES * ONE_STEP;      // tokens of a step of a wave, of a workgroup
+constexpr int CUS = 256, ONE_GROUPS = 2 * CUS;       // workgroups that a call is divided among, or more where sequences are many
+constexpr int MOST_PARTS = ONE_GROUPS;               // of one sequence (a sequence alone is divided into at most ONE_GROUPS pieces)
 
 template <bool BF> __device__ __forceinline__ float4v mfma16(uint4v a, uint4v b, float4v c) {
   if constexpr (BF) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf8v, a), __builtin_bit_cast(bf8v, b), c, 0, 0, 0);
@@ -406,16 +408,33 @@ __device__ __forceinline__ bool piece_of(const OneArgs& a, int id, Piece& p, boo
   return false;
 }
 
-template <int D> struct State {       // what a piece leaves of 16 rows: reference, sum of weights, then the output before its division
-  static constexpr int ROW = D + 2;
+// What a piece leaves of its 16 rows: reference and sum of weights of each, then the output before its division.
+template <int D> constexpr int STATE = 16 * 2 + 16 * D;
+
+// States go from workgroup to workgroup, whose XCDs may differ, past the L2 caches: written through and read from memory.  (A fence for the whole
+// device writes back and invalidates an L2 at a time: with one in every workgroup 35,000 tokens of 32 sequences took 94 us.)
+__device__ __forceinline__ void put_state(float* p, float a, float b) {
+  __hip_atomic_store(reinterpret_cast<uint64_t*>(p), (uint64_t)as_u(a) | (uint64_t)as_u(b) << 32, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2v get_state(const float* p) {
+  const uint64_t x = __hip_atomic_load(reinterpret_cast<const uint64_t*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return float2v{as_f((uint32_t)x), as_f((uint32_t)(x >> 32))};
+}
+
+// What a wave has loaded of a step: two tokens' key codes a lane, the value codes and parameters of its 8 tokens.
+template <int D> struct Loaded {
+  uint32_t k[2][D / 32];
+  uint4v v[D / 64], par[4];
 };
 
 template <int D, bool BF, bool F32OUT>
 __global__ __launch_bounds__(ONE_WAVES * 64) void ftcache_one(const OneArgs a) {
   constexpr int KW = D / 32;              // words of key codes per lane and token = matrix instructions over the head
-  constexpr int VQ = D / 64;              // value words of 4 elements per lane
   constexpr int NO = D / 16;              // accumulators of the output
-  __shared__ float merged[ONE_WAVES][16][D + 1];
+  constexpr int THREADS = ONE_WAVES * 64;
+  // the waves' outputs, [wave][row][D + 4]; then, where a divided sequence is put together, weights of the parts and sums of the columns
+  constexpr int PITCH = D + 4, WAVES_USE = ONE_WAVES * 16 * PITCH, JOIN_USES = 16 * MOST_PARTS + THREADS * 4;
+  __shared__ __attribute__((aligned(16))) float merged[WAVES_USE > JOIN_USES ? WAVES_USE : JOIN_USES];
   __shared__ float refs[ONE_WAVES][16], sums[ONE_WAVES][16];
   __shared__ int last;
   const int heads = a.pool.kv_heads * a.row_tiles, hr = blockIdx.x % heads, hk = hr / a.row_tiles, tile = hr % a.row_tiles;
@@ -477,43 +496,49 @@ __global__ __launch_bounds__(ONE_WAVES * 64) void ftcache_one(const OneArgs a) {
   bool bad = !known;
   const int ps = 1 << a.pool.page_shift, end = p.first + p.count;
   const int32_t* const table = a.table + p.b * a.table_stride;
-  auto page_of = [&](int token) {       // the page of a block of 8 tokens, the last one's for blocks behind the end
-    const int t = token < end ? token : end - 1, page = table[t >> a.pool.page_shift];
-    const bool fine = page >= 0 && page < a.pool.pages;
-    bad |= !fine;
-    return fine ? page : 0;
+  // entries of the table for the blocks of 8 tokens that a lane reads in a step, keys' and values' (the last block's behind the end)
+  struct Entries { int k, v; };
+  const int my_k = 8 * (n >> 2), my_v = 8 * g, last_block = (end - 1) & ~7;
+  auto entries_of = [&](int t0) {
+    const int kb = t0 + my_k < end ? t0 + my_k : last_block, vb = t0 + my_v < end ? t0 + my_v : last_block;
+    return Entries{table[kb >> a.pool.page_shift], table[vb >> a.pool.page_shift]};
   };
-  for (int t0 = p.first + wave * ONE_STEP; t0 < end; t0 += ONE_UNIT) {
-    const int kb = t0 + 8 * (n >> 2), vb = t0 + 8 * g, kc = kb < end ? kb : (end - 1) & ~7, vc = vb < end ? vb : (end - 1) & ~7;
-    const char* const kp = a.pool.head(page_of(kb), hk);
-    const char* const vp = a.pool.head(page_of(vb), hk);
-    const int kin = (kc & (ps - 1)) + (n & 3), vin = (vc & (ps - 1)) >> 3;
-    uint32_t kw[2][KW];
+  auto page_of = [&](int page) {
+    const bool fine = (uint32_t)page < (uint32_t)a.pool.pages;
+    bad |= !fine;
+    return a.pool.head(fine ? page : 0, hk);
+  };
+  auto load = [&](int t0, Entries at) {
+    Loaded<D> x;
+    const int kb = t0 + my_k < end ? t0 + my_k : last_block, vb = t0 + my_v < end ? t0 + my_v : last_block;
+    const char* const kp = page_of(at.k) + ((kb & (ps - 1)) + (n & 3)) * (D / 2) + g * (4 * KW);
+    const int vin = (vb & (ps - 1)) >> 3;
+    const char* const vp = page_of(at.v) + ps * (D / 2);
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      const char* at = kp + (kin + 4 * t) * (D / 2) + g * (4 * KW);
-      if constexpr (KW == 4) { const uint4v y = *reinterpret_cast<const uint4v*>(at); kw[t][0] = y[0]; kw[t][1] = y[1]; kw[t][2] = y[2]; kw[t][3] = y[3]; }
-      else { const uint2v y = *reinterpret_cast<const uint2v*>(at); kw[t][0] = y[0]; kw[t][1] = y[1]; }
+      if constexpr (KW == 4) { const uint4v y = *reinterpret_cast<const uint4v*>(kp + t * (2 * D)); x.k[t][0] = y[0]; x.k[t][1] = y[1]; x.k[t][2] = y[2]; x.k[t][3] = y[3]; }
+      else { const uint2v y = *reinterpret_cast<const uint2v*>(kp + t * (2 * D)); x.k[t][0] = y[0]; x.k[t][1] = y[1]; }
     }
-    uint4v vw[VQ], par[4];
 #pragma unroll
-    for (int i = 0; i < VQ; ++i) vw[i] = *reinterpret_cast<const uint4v*>(vp + ps * (D / 2) + vin * (4 * D) + (n * VQ + i) * 16);
+    for (int i = 0; i < D / 64; ++i) x.v[i] = *reinterpret_cast<const uint4v*>(vp + vin * (4 * D) + (n * (D / 64) + i) * 16);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) par[i] = *reinterpret_cast<const uint4v*>(vp + ps * D + vin * 64 + 16 * i);
-
+    for (int i = 0; i < 4; ++i) x.par[i] = *reinterpret_cast<const uint4v*>(vp + ps * (D / 2) + vin * 64 + 16 * i);
+    return x;
+  };
+  auto step = [&](int t0, const Loaded<D>& y) __attribute__((always_inline)) {
     float4v s[2];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       s[t] = (float4v)0.f;
 #pragma unroll
-      for (int i = 0; i < KW; ++i) s[t] = mfma16<BF>(key_operand(kw[t][i]), qf[i], s[t]);
+      for (int i = 0; i < KW; ++i) s[t] = mfma16<BF>(key_operand(y.k[t][i]), qf[i], s[t]);
     }
     float x[8], vs[8], vz[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const float ks = j & 1 ? high_of<BF>(par[0][j / 2]) : low_of<BF>(par[0][j / 2]), kz = j & 1 ? high_of<BF>(par[1][j / 2]) : low_of<BF>(par[1][j / 2]);
-      vs[j] = j & 1 ? high_of<BF>(par[2][j / 2]) : low_of<BF>(par[2][j / 2]);
-      vz[j] = j & 1 ? high_of<BF>(par[3][j / 2]) : low_of<BF>(par[3][j / 2]);
+      const float ks = j & 1 ? high_of<BF>(y.par[0][j / 2]) : low_of<BF>(y.par[0][j / 2]), kz = j & 1 ? high_of<BF>(y.par[1][j / 2]) : low_of<BF>(y.par[1][j / 2]);
+      vs[j] = j & 1 ? high_of<BF>(y.par[2][j / 2]) : low_of<BF>(y.par[2][j / 2]);
+      vz[j] = j & 1 ? high_of<BF>(y.par[3][j / 2]) : low_of<BF>(y.par[3][j / 2]);
       x[j] = __builtin_fmaf(ks, alpha * s[j >> 2][j & 3], kz * gamma);
     }
     if (t0 + ONE_STEP > end) {
@@ -542,6 +567,7 @@ __global__ __launch_bounds__(ONE_WAVES * 64) void ftcache_one(const OneArgs a) {
       l += e;
       z = __builtin_fmaf(e, vz[j], z);
       w[j] = e * vs[j];
+      z = __builtin_fmaf(w[j], 8.f, z);
     }
     // weights in bf16; for fp16 tokens in two words, the second what the first leaves, so that they are no coarser than the tokens
     uint4v ph, pl;
@@ -555,54 +581,77 @@ __global__ __launch_bounds__(ONE_WAVES * 64) void ftcache_one(const OneArgs a) {
     if constexpr (!BF) ones = mfma16<true>(one, pl, ones);
 #pragma unroll
     for (int i = 0; i < NO; ++i) {
-      const uint4v v = vw[i / 4];
+      const uint4v v = y.v[i / 4];
       const uint4v c = {value_codes(v[0], i & 3), value_codes(v[1], i & 3), value_codes(v[2], i & 3), value_codes(v[3], i & 3)};
       o[i] = mfma16<true>(c, ph, o[i]);
       if constexpr (!BF) o[i] = mfma16<true>(c, pl, o[i]);
+    }
+  };
+  // the next step's loads are under way while a step is computed, and the entries of the one after
+  int t0 = p.first + wave * ONE_STEP;
+  if (t0 < end) {
+    Loaded<D> now = load(t0, entries_of(t0));
+    Entries next = entries_of(t0 + ONE_UNIT);
+    for (;;) {
+      const int t1 = t0 + ONE_UNIT, t2 = t1 + ONE_UNIT;
+      Loaded<D> then;
+      if (t1 < end) then = load(t1, next);
+      next = entries_of(t2);
+      __builtin_amdgcn_sched_barrier(0);
+      step(t0, now);
+      if (t1 >= end) break;
+      if (t2 < end) now = load(t2, next);
+      next = entries_of(t2 + ONE_UNIT);
+      __builtin_amdgcn_sched_barrier(0);
+      step(t1, then);
+      if (t2 >= end) break;
+      t0 = t2;
     }
   }
   bad = __any(bad);
 #pragma unroll
   for (int d = 16; d < 64; d <<= 1) { l += __shfl_xor(l, d); z += __shfl_xor(z, d); }
-  const float shift = z - 128.f * ones[0];
+  const float shift = z - 136.f * ones[0];
   if (bad) l = __builtin_nanf("");
   if (g == 0) { refs[wave][n] = ref; sums[wave][n] = l; }
 #pragma unroll
   for (int i = 0; i < NO; ++i)
 #pragma unroll
-    for (int v = 0; v < 4; ++v) merged[wave][n][(4 * g + v) * NO + i] = o[i][v] + shift;
+    for (int v = 0; v < 4; ++v) merged[(wave * 16 + n) * PITCH + (4 * g + v) * NO + i] = o[i][v] + shift;
   __syncthreads();
 
   const int tid = threadIdx.x;
-  float* const ws = a.ws + ((int64_t)(p.slot + p.part) * heads + hr) * 16 * State<D>::ROW;      // (of a divided sequence)
-  auto finish = [&](int row, int e, float value, float sum) {
-    const float y = sum == 0.f ? 0.f : value / sum;
+  float* const ws = a.ws + ((int64_t)(p.slot + p.part) * heads + hr) * STATE<D>;      // (of a divided sequence)
+  auto finish = [&](int row, int e, float4v value, float sum) {
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
     char* op = a.o.data + (int64_t)p.b * a.o.token + (int64_t)(head0 + row) * a.o.head;
-    if constexpr (F32OUT) reinterpret_cast<float*>(op)[e] = y;
-    else reinterpret_cast<uint16_t*>(op)[e] = (uint16_t)pack2<BF>(y, y);
+    if constexpr (F32OUT) *reinterpret_cast<float4v*>(op + 4 * e) = value * inv;
+    else *reinterpret_cast<uint2v*>(op + 2 * e) = uint2v{pack2<BF>(value[0] * inv, value[1] * inv), pack2<BF>(value[2] * inv, value[3] * inv)};
   };
-  for (int x = tid; x < rows * D; x += ONE_WAVES * 64) {
-    const int row = x / D, e = x % D;
+  constexpr int CD = D / 4;               // columns of four elements of a row
+  for (int x = tid; x < rows * CD; x += THREADS) {
+    const int row = x / CD, e = x % CD * 4;
     float most = refs[0][row];
 #pragma unroll
     for (int w = 1; w < ONE_WAVES; ++w) most = __builtin_fmaxf(most, refs[w][row]);
-    float value = 0.f, sum = 0.f;
+    float4v value = (float4v)0.f;
+    float sum = 0.f;
 #pragma unroll
     for (int w = 0; w < ONE_WAVES; ++w) {
       const float f = ex2(refs[w][row] - most);
-      value += f * merged[w][row][e];
+      value += f * *reinterpret_cast<const float4v*>(&merged[(w * 16 + row) * PITCH + e]);
       sum += f * sums[w][row];
     }
     if (p.parts == 1) finish(row, e, value, sum);
     else {
-      float* const r = ws + row * State<D>::ROW;
-      r[2 + e] = value;
-      if (e == 0) { r[0] = most; r[1] = sum; }
+      put_state(ws + 32 + row * D + e, value[0], value[1]);
+      put_state(ws + 32 + row * D + e + 2, value[2], value[3]);
+      if (e == 0) put_state(ws + 2 * row, most, sum);
     }
   }
   if (tid == 0 && bad && p.part == 0 && hr == 0) atomicAdd(a.refused + 1, 1ull);
   if (p.parts == 1) return;
-  __threadfence();
+  __builtin_amdgcn_s_waitcnt(0x0F70);          // (vmcnt(0): the state is where every XCD sees it)
   __syncthreads();
   if (tid == 0) {
     uint32_t* const done = a.done + (int64_t)p.b * heads + hr;
@@ -612,22 +661,61 @@ __global__ __launch_bounds__(ONE_WAVES * 64) void ftcache_one(const OneArgs a) {
   }
   __syncthreads();
   if (!last) return;
-  __threadfence();
-  // this workgroup came last: the states of all parts, in their order
-  const float* const first = a.ws + ((int64_t)p.slot * heads + hr) * 16 * State<D>::ROW;
-  const int64_t next = (int64_t)heads * 16 * State<D>::ROW;
-  for (int x = tid; x < rows * D; x += ONE_WAVES * 64) {
-    const int row = x / D, e = x % D;
-    const float* const r = first + row * State<D>::ROW;
-    float most = r[0];
-    for (int i = 1; i < p.parts; ++i) most = __builtin_fmaxf(most, r[i * next]);
-    float value = 0.f, sum = 0.f;
-    for (int i = 0; i < p.parts; ++i) {
-      const float f = ex2(r[i * next] - most);
-      value += f * r[i * next + 2 + e];
-      sum += f * r[i * next + 1];
+  // this workgroup came last: it puts the states of all parts together, in their order.  Weights of the parts first (row tid % 16)
+  const float* const first = a.ws + ((int64_t)p.slot * heads + hr) * STATE<D>;
+  const int64_t next = (int64_t)heads * STATE<D>;
+  float* const weight = merged;                           // [part][16]
+  constexpr int SIDE = THREADS / 16;                      // parts taken side by side
+  const int row = tid & 15;
+  float most = -3.4028234e38f;
+  for (int i = tid >> 4; i < p.parts; i += SIDE) {
+    const float2v r = get_state(first + i * next + 2 * row);
+    weight[i * 16 + row] = r[0];
+    most = __builtin_fmaxf(most, r[0]);
+  }
+  most = __builtin_fmaxf(most, __shfl_xor(most, 16));
+  most = __builtin_fmaxf(most, __shfl_xor(most, 32));
+  if (lane < 16) refs[wave][row] = most;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < ONE_WAVES; ++w) most = __builtin_fmaxf(most, refs[w][row]);
+  float sum = 0.f;
+  for (int i = tid >> 4; i < p.parts; i += SIDE) {
+    const float f = ex2(weight[i * 16 + row] - most);
+    weight[i * 16 + row] = f;
+    sum += f * get_state(first + i * next + 2 * row)[1];
+  }
+  sum += __shfl_xor(sum, 16);
+  sum += __shfl_xor(sum, 32);
+  if (lane < 16) sums[wave][row] = sum;
+  __syncthreads();
+  // then the columns: as many groups of parts side by side as there are threads for
+  const int columns = rows * CD, groups = columns < THREADS ? THREADS / columns : 1, group = tid / columns;
+  float4v* const partial = reinterpret_cast<float4v*>(weight + 16 * MOST_PARTS);
+  for (int c0 = 0; c0 < columns; c0 += THREADS) {
+    const int c = c0 + (groups > 1 ? tid % columns : tid), r = c / CD, e = c % CD * 4;
+    float4v value = (float4v)0.f;
+    if (c < columns && group < groups) {
+      const int from = p.parts * group / groups, to = groups > 1 ? p.parts * (group + 1) / groups : p.parts;
+#pragma unroll 8
+      for (int i = from; i < to; ++i) {
+        const float* const at = first + i * next + 32 + r * D + e;
+        const float2v x = get_state(at), y = get_state(at + 2);
+        value += weight[i * 16 + r] * float4v{x[0], x[1], y[0], y[1]};
+      }
     }
-    finish(row, e, value, sum);
+    if (groups > 1) {
+      if (group < groups) partial[tid] = value;
+      __syncthreads();
+      if (group == 0)
+        for (int i = 1; i < groups; ++i) value += partial[i * columns + c];
+    }
+    if (c < columns && (groups == 1 || group == 0)) {
+      float total = 0.f;
+#pragma unroll
+      for (int w = 0; w < ONE_WAVES; ++w) total += sums[w][r];
+      finish(r, e, value, total);
+    }
   }
 }
 
@@ -699,7 +787,6 @@ const char* places_of(const ftcache_places* p, Places& out) {
   out = Places{p->cu_seqlens, p->starts, p->page_table, p->table_stride, p->batch, p->tokens, p->table_width};
   return nullptr;
 }
-constexpr int CUS = 256;
 }  // namespace
 
 extern "C" int ftcache_create(const ftcache_config* cfg, ftcache_ctx** out) {
@@ -736,9 +823,9 @@ extern "C" int ftcache_create(const ftcache_config* cfg, ftcache_ctx** out) {
     c->one = bf ? one_of<64, true>(f32) : one_of<64, false>(f32);
   }
   const int64_t heads = (int64_t)e.kv_heads * c->row_tiles;
-  c->chunks = (int)(4 * CUS / heads < 1 ? 1 : 4 * CUS / heads);
+  c->chunks = (int)(ONE_GROUPS / heads < 1 ? 1 : ONE_GROUPS / heads);
   // divided sequences are longer than a piece: together they have fewer than twice `chunks` pieces
-  const size_t ws = (size_t)2 * c->chunks * heads * 16 * (e.head_dim + 2) * sizeof(float), done = (size_t)e.max_batch * heads * sizeof(uint32_t);
+  const size_t ws = (size_t)2 * c->chunks * heads * (32 + 16 * e.head_dim) * sizeof(float), done = (size_t)e.max_batch * heads * sizeof(uint32_t);
   OnDevice here(e.device);
   hipError_t he = here.status;
   if (he == hipSuccess) he = hipMalloc(&c->scratch, 256 + ((done + 255) & ~(size_t)255) + ws);
