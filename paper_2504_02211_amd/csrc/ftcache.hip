@@ -332,7 +332,7 @@ struct OneArgs {
   Rows q, o;
   const int32_t *lengths, *table;
   int64_t table_stride;
-  int32_t batch, width, group, row_tiles;       // row_tiles: passes of 16 heads for a group
+  int32_t batch, most, group, row_tiles;        // most: tokens that a row of the table holds; row_tiles: passes of 16 heads for a group
   int32_t chunks;                               // wanted, over all sequences
   float scale_log2;
   float* ws;                                    // states of divided sequences
@@ -356,50 +356,54 @@ __device__ __forceinline__ uint4v key_operand(uint32_t w) {
 }
 __device__ __forceinline__ uint32_t value_codes(uint32_t w, int nibble) { return (w >> (4 * nibble) & 0x000F000Fu) | 0x43004300u; }
 
-__device__ __forceinline__ int64_t sum64(int64_t x) {
-#pragma unroll
-  for (int d = 32; d; d >>= 1) x += __shfl_xor(x, d);
+// sum over the lanes up to this one: register moves within rows of 16 lanes, then from row to row
+__device__ __forceinline__ int sum_upto(int x) {
+  auto step = [&](int moved) { x += moved; };
+  step(__builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false));      // row_shr 1, 2, 4, 8
+  step(__builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false));
+  step(__builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false));
+  step(__builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false));
+  step(__builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false));      // row_bcast 15, 31
+  step(__builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false));
   return x;
 }
 
 struct Piece { int b, first, count, part, parts, slot; };      // tokens first .. first + count of sequence b, part of parts; place of part 0's state
 
-// Sequences are divided into pieces of one length, the same for all, chosen so that there are about `chunks` pieces in all: the last of a sequence is shorter.
+// Sequences are divided into pieces of one length, the same for all, chosen so that there are about `chunks` pieces in all: the last of a sequence is
+// shorter.  Lengths count in units of ONE_UNIT tokens (all of them together below 2^31, see ftcache_attend).  Lane l looks after sequences l * per ..;
+// with up to 64 of them each length is loaded once.
 __device__ __forceinline__ bool piece_of(const OneArgs& a, int id, Piece& p, bool& known) {
-  const int lane = threadIdx.x & 63, per = (a.batch + 63) / 64, most = (int)((int64_t)a.width << a.pool.page_shift > 0x7FFFFF00 ? 0x7FFFFF00 : (int64_t)a.width << a.pool.page_shift);
-  auto length = [&](int b) { const int n = b < a.batch ? a.lengths[b] : 0; return n < 0 || n > most ? 0 : n; };
-  int64_t total = 0;
-  for (int i = 0; i < per; ++i) total += length(lane * per + i);
-  total = sum64(total);
-  int64_t units = ((total + a.chunks - 1) / a.chunks + ONE_UNIT - 1) / ONE_UNIT;
-  units = units < 1 ? 1 : units > 0x7FFFFF00 / ONE_UNIT ? 0x7FFFFF00 / ONE_UNIT : units;
-  const int size = (int)units * ONE_UNIT;
-  auto parts_of = [&](int n) { return n > size ? (int)(((int64_t)n + size - 1) / size) : 1; };
-  int mine = 0, slots = 0;          // pieces; those of divided sequences, which leave a state
+  const int lane = threadIdx.x & 63, per = (a.batch + 63) / 64, most = a.most;
+  auto length = [&](int b) { return b < a.batch ? a.lengths[b] : 0; };
+  auto sound = [&](int n) { return n < 0 || n > most ? 0 : n; };
+  auto units = [&](int n) { return (int)(((uint32_t)sound(n) + ONE_UNIT - 1) / ONE_UNIT); };
+  const int mine = length(lane * per);
+  int total = units(mine);
+  for (int i = 1; i < per; ++i) total += units(length(lane * per + i));
+  total = __builtin_amdgcn_readlane(sum_upto(total), 63);
+  const int size = total <= a.chunks ? 1 : (total + a.chunks - 1) / a.chunks;
+  auto parts_of = [&](int n) { const int u = units(n); return u > size ? (u + size - 1) / size : 1; };
+  int pieces = 0, slots = 0;          // and those of divided sequences, which leave a state
   for (int i = 0; i < per; ++i) {
-    const int b = lane * per + i, n = parts_of(length(b));
-    mine += b < a.batch ? n : 0;
+    const int b = lane * per + i, n = parts_of(i == 0 ? mine : length(b));
+    pieces += b < a.batch ? n : 0;
     slots += n > 1 ? n : 0;
   }
-  int upto = mine, slots_upto = slots;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int x = __shfl_up(upto, d), y = __shfl_up(slots_upto, d);
-    upto += lane >= d ? x : 0;
-    slots_upto += lane >= d ? y : 0;
-  }
+  const int upto = sum_upto(pieces), slots_upto = sum_upto(slots);
   const uint64_t beyond = __ballot(upto > id);
   if (!beyond) return false;
   const int owner = __ffsll((unsigned long long)beyond) - 1;
-  int left = id - __shfl(upto - mine, owner), slot = __shfl(slots_upto - slots, owner);
-  for (int i = 0; i < per; ++i) {
-    const int b = owner * per + i;
+  int left = id - __builtin_amdgcn_readlane(upto - pieces, owner), slot = __builtin_amdgcn_readlane(slots_upto - slots, owner);
+  int n = __builtin_amdgcn_readlane(mine, owner), b = owner * per;
+  for (int i = 0; i < per; ++i, ++b) {
     if (b >= a.batch) return false;
-    const int n = length(b), parts = parts_of(n);
+    if (i) n = __builtin_amdgcn_readfirstlane(length(b));
+    const int parts = parts_of(n);
     if (left < parts) {
-      const int raw = a.lengths[b];
-      known = raw >= 0 && raw <= most;
-      p = Piece{b, left * size, n - left * size < size ? n - left * size : size, left, parts, slot};
+      known = n == sound(n);
+      const int first = left * size * ONE_UNIT, rest = sound(n) - first;
+      p = Piece{b, first, rest < size * ONE_UNIT ? rest : size * ONE_UNIT, left, parts, slot};
       return true;
     }
     left -= parts;
@@ -411,14 +415,11 @@ __device__ __forceinline__ bool piece_of(const OneArgs& a, int id, Piece& p, boo
 // What a piece leaves of its 16 rows: reference and sum of weights of each, then the output before its division.
 template <int D> constexpr int STATE = 16 * 2 + 16 * D;
 
-// States go from workgroup to workgroup, whose XCDs may differ, past the L2 caches: written through and read from memory.  (A fence for the whole
-// device writes back and invalidates an L2 at a time: with one in every workgroup 35,000 tokens of 32 sequences took 94 us.)
+// States go from workgroup to workgroup, whose XCDs may differ, past the L2 caches: written through to memory, and read behind an
+// invalidation by the one workgroup that reads them.  (A fence for the whole device writes back an L2 at a time: with one in every workgroup 35,000 tokens of
+// 32 sequences took 94 us.)
 __device__ __forceinline__ void put_state(float* p, float a, float b) {
   __hip_atomic_store(reinterpret_cast<uint64_t*>(p), (uint64_t)as_u(a) | (uint64_t)as_u(b) << 32, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-__device__ __forceinline__ float2v get_state(const float* p) {
-  const uint64_t x = __hip_atomic_load(reinterpret_cast<const uint64_t*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  return float2v{as_f((uint32_t)x), as_f((uint32_t)(x >> 32))};
 }
 
 // What a wave has loaded of a step: two tokens' key codes a lane, the value codes and parameters of its 8 tokens.
@@ -661,6 +662,7 @@ __global__ __launch_bounds__(ONE_WAVES * 64) void ftcache_one(const OneArgs a) {
   }
   __syncthreads();
   if (!last) return;
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
   // this workgroup came last: it puts the states of all parts together, in their order.  Weights of the parts first (row tid % 16)
   const float* const first = a.ws + ((int64_t)p.slot * heads + hr) * STATE<D>;
   const int64_t next = (int64_t)heads * STATE<D>;
@@ -669,7 +671,7 @@ __global__ __launch_bounds__(ONE_WAVES * 64) void ftcache_one(const OneArgs a) {
   const int row = tid & 15;
   float most = -3.4028234e38f;
   for (int i = tid >> 4; i < p.parts; i += SIDE) {
-    const float2v r = get_state(first + i * next + 2 * row);
+    const float2v r = *reinterpret_cast<const float2v*>(first + i * next + 2 * row);
     weight[i * 16 + row] = r[0];
     most = __builtin_fmaxf(most, r[0]);
   }
@@ -683,7 +685,7 @@ __global__ __launch_bounds__(ONE_WAVES * 64) void ftcache_one(const OneArgs a) {
   for (int i = tid >> 4; i < p.parts; i += SIDE) {
     const float f = ex2(weight[i * 16 + row] - most);
     weight[i * 16 + row] = f;
-    sum += f * get_state(first + i * next + 2 * row)[1];
+    sum += f * first[i * next + 2 * row + 1];
   }
   sum += __shfl_xor(sum, 16);
   sum += __shfl_xor(sum, 32);
@@ -698,11 +700,7 @@ __global__ __launch_bounds__(ONE_WAVES * 64) void ftcache_one(const OneArgs a) {
     if (c < columns && group < groups) {
       const int from = p.parts * group / groups, to = groups > 1 ? p.parts * (group + 1) / groups : p.parts;
 #pragma unroll 8
-      for (int i = from; i < to; ++i) {
-        const float* const at = first + i * next + 32 + r * D + e;
-        const float2v x = get_state(at), y = get_state(at + 2);
-        value += weight[i * 16 + r] * float4v{x[0], x[1], y[0], y[1]};
-      }
+      for (int i = from; i < to; ++i) value += weight[i * 16 + r] * *reinterpret_cast<const float4v*>(first + i * next + 32 + r * D + e);
     }
     if (groups > 1) {
       if (group < groups) partial[tid] = value;
@@ -931,7 +929,9 @@ extern "C" int ftcache_attend(ftcache_ctx* c, const void* pool, int32_t batch, c
   a.table = page_table;
   a.table_stride = table_stride;
   a.batch = batch;
-  a.width = table_width;
+  const int64_t most = (int64_t)table_width << c->shift;
+  a.most = (int32_t)(most > 0x7FFFFF00 ? 0x7FFFFF00 : most);
+  if (((int64_t)a.most + ONE_UNIT - 1) / ONE_UNIT * batch > 0x7FFFFFFFll) return cfail(c, FTCACHE_EUNSUPPORTED, "the page table has room for too many tokens");
   a.group = e.heads / e.kv_heads;
   a.row_tiles = c->row_tiles;
   a.chunks = c->chunks;
