@@ -12,6 +12,7 @@
 #include <cmath>
 #include <new>
 #include <string>
+#include <type_traits>
 
 namespace ftcache {
 using namespace ftserve;
@@ -333,7 +334,7 @@ struct OneArgs {
   const int32_t *lengths, *table;
   int64_t table_stride;
   int32_t batch, most, group, row_tiles;        // most: tokens that a row of the table holds; row_tiles: passes of 16 heads for a group
-  int32_t chunks;                               // wanted, over all sequences
+  int32_t chunks, most_parts;                   // pieces wanted over all sequences, allowed of one
   float scale_log2;
   float* ws;                                    // states of divided sequences
   uint32_t* done;                               // [batch][kv_heads * row_tiles], 0 between calls
@@ -342,7 +343,7 @@ struct OneArgs {
 
 constexpr int ONE_WAVES = 8, ONE_STEP = 32, ONE_UNIT = ONE_WAVES * ONE_STEP;      // tokens of a step of a wave, of a workgroup
 constexpr int CUS = 256, ONE_GROUPS = 2 * CUS;       // workgroups that a call is divided among, or more where sequences are many
-constexpr int MOST_PARTS = ONE_GROUPS;               // of one sequence (a sequence alone is divided into at most ONE_GROUPS pieces)
+constexpr int MOST_PARTS = CUS;                // of one sequence, where there is one head
 
 template <bool BF> __device__ __forceinline__ float4v mfma16(uint4v a, uint4v b, float4v c) {
   if constexpr (BF) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf8v, a), __builtin_bit_cast(bf8v, b), c, 0, 0, 0);
@@ -354,7 +355,12 @@ __device__ __forceinline__ uint4v key_operand(uint32_t w) {
   const uint32_t u = w >> 8;
   return uint4v{w & 0x000F000Fu, w & 0x00F000F0u, u & 0x000F000Fu, u & 0x00F000F0u};
 }
-__device__ __forceinline__ uint32_t value_codes(uint32_t w, int nibble) { return (w >> (4 * nibble) & 0x000F000Fu) | 0x43004300u; }
+// (as an instruction: of two constants one has to lie in a vector register, else it is an AND and an OR)
+__device__ __forceinline__ uint32_t value_codes(uint32_t w, uint32_t bits128) {
+  uint32_t x;
+  asm("v_and_or_b32 %0, %1, %2, %3" : "=v"(x) : "v"(w), "s"(0x000F000Fu), "v"(bits128));
+  return x;
+}
 
 // sum over the lanes up to this one: register moves within rows of 16 lanes, then from row to row
 __device__ __forceinline__ int sum_upto(int x) {
@@ -364,6 +370,17 @@ __device__ __forceinline__ int sum_upto(int x) {
   step(__builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false));
   step(__builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false));
   step(__builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false));      // row_bcast 15, 31
+  step(__builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false));
+  return x;
+}
+
+__device__ __forceinline__ int max_upto(int x) {      // of values >= 0
+  auto step = [&](int moved) { x = moved > x ? moved : x; };
+  step(__builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false));
+  step(__builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false));
+  step(__builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false));
+  step(__builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false));
+  step(__builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false));
   step(__builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false));
   return x;
 }
@@ -379,10 +396,16 @@ __device__ __forceinline__ bool piece_of(const OneArgs& a, int id, Piece& p, boo
   auto sound = [&](int n) { return n < 0 || n > most ? 0 : n; };
   auto units = [&](int n) { return (int)(((uint32_t)sound(n) + ONE_UNIT - 1) / ONE_UNIT); };
   const int mine = length(lane * per);
-  int total = units(mine);
-  for (int i = 1; i < per; ++i) total += units(length(lane * per + i));
+  int total = units(mine), longest = total;
+  for (int i = 1; i < per; ++i) {
+    const int u = units(length(lane * per + i));
+    total += u;
+    longest = u > longest ? u : longest;
+  }
   total = __builtin_amdgcn_readlane(sum_upto(total), 63);
-  const int size = total <= a.chunks ? 1 : (total + a.chunks - 1) / a.chunks;
+  longest = __builtin_amdgcn_readlane(max_upto(longest), 63);
+  const int fair = (total + a.chunks - 1) / a.chunks, few = (longest + a.most_parts - 1) / a.most_parts;
+  const int size = fair < 1 ? 1 : fair > few ? fair : few;
   auto parts_of = [&](int n) { const int u = units(n); return u > size ? (u + size - 1) / size : 1; };
   int pieces = 0, slots = 0;          // and those of divided sequences, which leave a state
   for (int i = 0; i < per; ++i) {
@@ -422,11 +445,14 @@ __device__ __forceinline__ void put_state(float* p, float a, float b) {
   __hip_atomic_store(reinterpret_cast<uint64_t*>(p), (uint64_t)as_u(a) | (uint64_t)as_u(b) << 32, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
-// What a wave has loaded of a step: two tokens' key codes a lane, the value codes and parameters of its 8 tokens.
+// What a wave has loaded of a step: two tokens' key codes a lane, the value codes of its 8 tokens, and one of the 16 words of their parameters.
 template <int D> struct Loaded {
   uint32_t k[2][D / 32];
-  uint4v v[D / 64], par[4];
+  uint4v v[D / 64];
+  uint32_t par;
 };
+// what lane I of each 16 holds: part of the instruction that uses it
+template <int I> __device__ __forceinline__ float of_lane(float x) { return as_f((uint32_t)__builtin_amdgcn_mov_dpp((int)as_u(x), 0x150 + I, 0xF, 0xF, true)); }
 
 template <int D, bool BF, bool F32OUT>
 __global__ __launch_bounds__(ONE_WAVES * 64) void ftcache_one(const OneArgs a) {
@@ -448,7 +474,7 @@ __global__ __launch_bounds__(ONE_WAVES * 64) void ftcache_one(const OneArgs a) {
   // the row's query as an operand, scaled by a power of two so that its largest element lies in [2^10, 2^11) (fp16), at 2^126 or as far up as one
   // factor brings it (bf16): the products with codes are then far from both ends of 32 bits, and sixteenths of small elements keep their bits
   uint4v qf[KW];
-  float alpha, gamma;
+  float alpha, qsum;       // what a score of products with codes still lacks; the sum of the query's elements, in the same measure
   {
     const char* qp = a.q.data + (int64_t)p.b * a.q.token + (int64_t)(head0 + (n < rows ? n : 0)) * a.q.head + 2 * (8 * KW * g);
     uint32_t w[4 * KW];
@@ -487,7 +513,7 @@ __global__ __launch_bounds__(ONE_WAVES * 64) void ftcache_one(const OneArgs a) {
 #pragma unroll
     for (int d = 16; d < 64; d <<= 1) plain += __shfl_xor(plain, d);
     alpha = __builtin_ldexpf(a.scale_log2, (BF ? 133 : 24) - up_by);
-    gamma = a.scale_log2 * plain;
+    qsum = __builtin_ldexpf(plain, up_by - (BF ? 133 : 24));
   }
 
   float4v o[NO], ones = (float4v)0.f;
@@ -495,35 +521,40 @@ __global__ __launch_bounds__(ONE_WAVES * 64) void ftcache_one(const OneArgs a) {
   for (int i = 0; i < NO; ++i) o[i] = (float4v)0.f;
   float ref = -3.4028234e38f, l = 0.f, z = 0.f;
   bool bad = !known;
+  uint32_t bits128 = 0x43004300u;
+  asm("" : "+v"(bits128));
   const int ps = 1 << a.pool.page_shift, end = p.first + p.count;
   const int32_t* const table = a.table + p.b * a.table_stride;
   // entries of the table for the blocks of 8 tokens that a lane reads in a step, keys' and values' (the last block's behind the end)
-  struct Entries { int k, v; };
-  const int my_k = 8 * (n >> 2), my_v = 8 * g, last_block = (end - 1) & ~7;
+  struct Entries { uint32_t k, v; };
+  const int last_block = (end - 1) & ~7, my_k = 8 * (n >> 2), my_v = 8 * g;
+  const char* const kpool = a.pool.head(0, hk) + (n & 3) * (D / 2) + g * (4 * KW);
+  const char* const vpool = a.pool.head(0, hk) + ps * (D / 2) + n * (D / 4);
+  const char* const ppool = a.pool.head(0, hk) + ps * D + 4 * n;
+  const uint32_t page_bytes = (uint32_t)a.pool.kv_heads * (uint32_t)a.pool.head_bytes, in_page = (uint32_t)ps - 1, pages = (uint32_t)a.pool.pages;
+  uint32_t highest = 0;                   // entry met
+  auto block = [&](int t) { return t < last_block ? t : last_block; };
   auto entries_of = [&](int t0) {
-    const int kb = t0 + my_k < end ? t0 + my_k : last_block, vb = t0 + my_v < end ? t0 + my_v : last_block;
-    return Entries{table[kb >> a.pool.page_shift], table[vb >> a.pool.page_shift]};
+    return Entries{(uint32_t)table[block(t0 + my_k) >> a.pool.page_shift], (uint32_t)table[block(t0 + my_v) >> a.pool.page_shift]};
   };
-  auto page_of = [&](int page) {
-    const bool fine = (uint32_t)page < (uint32_t)a.pool.pages;
-    bad |= !fine;
-    return a.pool.head(fine ? page : 0, hk);
+  auto page_at = [&](uint32_t entry) {
+    highest = entry > highest ? entry : highest;
+    return (uint64_t)(entry < pages ? entry : pages - 1) * page_bytes;
   };
   auto load = [&](int t0, Entries at) {
     Loaded<D> x;
-    const int kb = t0 + my_k < end ? t0 + my_k : last_block, vb = t0 + my_v < end ? t0 + my_v : last_block;
-    const char* const kp = page_of(at.k) + ((kb & (ps - 1)) + (n & 3)) * (D / 2) + g * (4 * KW);
-    const int vin = (vb & (ps - 1)) >> 3;
-    const char* const vp = page_of(at.v) + ps * (D / 2);
+    const uint64_t kpage = page_at(at.k), vpage = page_at(at.v);
+    const uint32_t kin = (uint32_t)block(t0 + my_k) & in_page, vin = (uint32_t)block(t0 + my_v) & in_page;
+    const char* const kp = kpool + (kpage + kin * (D / 2));
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       if constexpr (KW == 4) { const uint4v y = *reinterpret_cast<const uint4v*>(kp + t * (2 * D)); x.k[t][0] = y[0]; x.k[t][1] = y[1]; x.k[t][2] = y[2]; x.k[t][3] = y[3]; }
       else { const uint2v y = *reinterpret_cast<const uint2v*>(kp + t * (2 * D)); x.k[t][0] = y[0]; x.k[t][1] = y[1]; }
     }
+    const char* const vp = vpool + (vpage + vin * (D / 2));
 #pragma unroll
-    for (int i = 0; i < D / 64; ++i) x.v[i] = *reinterpret_cast<const uint4v*>(vp + vin * (4 * D) + (n * (D / 64) + i) * 16);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x.par[i] = *reinterpret_cast<const uint4v*>(vp + ps * (D / 2) + vin * 64 + 16 * i);
+    for (int i = 0; i < D / 64; ++i) x.v[i] = *reinterpret_cast<const uint4v*>(vp + 16 * i);
+    x.par = *reinterpret_cast<const uint32_t*>(ppool + (vpage + vin * 8));
     return x;
   };
   auto step = [&](int t0, const Loaded<D>& y) __attribute__((always_inline)) {
@@ -534,22 +565,32 @@ __global__ __launch_bounds__(ONE_WAVES * 64) void ftcache_one(const OneArgs a) {
 #pragma unroll
       for (int i = 0; i < KW; ++i) s[t] = mfma16<BF>(key_operand(y.k[t][i]), qf[i], s[t]);
     }
-    float x[8], vs[8], vz[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float ks = j & 1 ? high_of<BF>(y.par[0][j / 2]) : low_of<BF>(y.par[0][j / 2]), kz = j & 1 ? high_of<BF>(y.par[1][j / 2]) : low_of<BF>(y.par[1][j / 2]);
-      vs[j] = j & 1 ? high_of<BF>(y.par[2][j / 2]) : low_of<BF>(y.par[2][j / 2]);
-      vz[j] = j & 1 ? high_of<BF>(y.par[3][j / 2]) : low_of<BF>(y.par[3][j / 2]);
-      x[j] = __builtin_fmaf(ks, alpha * s[j >> 2][j & 3], kz * gamma);
-    }
+    // scores before softmax_scale * log2(e), from the words that the 16 lanes of a block hold together
+    float x[8];
+    const float plo = low_of<BF>(y.par), phi = high_of<BF>(y.par);
+    auto scores = [&](auto i) __attribute__((always_inline)) {            // tokens 2i and 2i + 1
+      constexpr int I = decltype(i)::value;
+      x[2 * I] = __builtin_fmaf(of_lane<I>(plo), s[I >> 1][2 * (I & 1)], of_lane<4 + I>(plo) * qsum);
+      x[2 * I + 1] = __builtin_fmaf(of_lane<I>(phi), s[I >> 1][2 * (I & 1) + 1], of_lane<4 + I>(phi) * qsum);
+    };
+    scores(std::integral_constant<int, 0>{});
+    scores(std::integral_constant<int, 1>{});
+    scores(std::integral_constant<int, 2>{});
+    scores(std::integral_constant<int, 3>{});
+    float vlo = plo, vhi = phi;
     if (t0 + ONE_STEP > end) {
+      asm volatile("; the last step of a sequence");         // (a branch, not selections in every step)
 #pragma unroll
       for (int j = 0; j < 8; ++j)
-        if (t0 + 8 * g + j >= end) { x[j] = -__builtin_inff(); vs[j] = 0.f; vz[j] = 0.f; }
+        if (t0 + 8 * g + j >= end) x[j] = -__builtin_inff();
+      // scales and minima of values behind the end
+      if (t0 + 8 * g + 2 * (n & 3) >= end) vlo = 0.f;
+      if (t0 + 8 * g + 2 * (n & 3) + 1 >= end) vhi = 0.f;
     }
-    float m = x[0];
+    float m = __builtin_fmaxf(x[0], x[1]);
 #pragma unroll
-    for (int j = 1; j < 8; ++j) m = __builtin_fmaxf(m, x[j]);
+    for (int j = 2; j < 8; ++j) m = __builtin_fmaxf(m, x[j]);
+    m *= alpha;
     if (__any(m > ref + 8.f)) {
       m = __builtin_fmaxf(m, __shfl_xor(m, 16));
       m = __builtin_fmaxf(m, __shfl_xor(m, 32));
@@ -562,14 +603,22 @@ __global__ __launch_bounds__(ONE_WAVES * 64) void ftcache_one(const OneArgs a) {
       for (int i = 0; i < NO; ++i) o[i] *= f;
     }
     float w[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float e = ex2(x[j] - ref);
-      l += e;
-      z = __builtin_fmaf(e, vz[j], z);
-      w[j] = e * vs[j];
-      z = __builtin_fmaf(w[j], 8.f, z);
-    }
+    auto weights = [&](auto i) __attribute__((always_inline)) {
+      constexpr int I = decltype(i)::value;
+      const float e0 = ex2(__builtin_fmaf(x[2 * I], alpha, -ref)), e1 = ex2(__builtin_fmaf(x[2 * I + 1], alpha, -ref));
+      l += e0;
+      l += e1;
+      z = __builtin_fmaf(of_lane<12 + I>(vlo), e0, z);
+      z = __builtin_fmaf(of_lane<12 + I>(vhi), e1, z);
+      w[2 * I] = of_lane<8 + I>(vlo) * e0;
+      w[2 * I + 1] = of_lane<8 + I>(vhi) * e1;
+      z = __builtin_fmaf(w[2 * I], 8.f, z);
+      z = __builtin_fmaf(w[2 * I + 1], 8.f, z);
+    };
+    weights(std::integral_constant<int, 0>{});
+    weights(std::integral_constant<int, 1>{});
+    weights(std::integral_constant<int, 2>{});
+    weights(std::integral_constant<int, 3>{});
     // weights in bf16; for fp16 tokens in two words, the second what the first leaves, so that they are no coarser than the tokens
     uint4v ph, pl;
 #pragma unroll
@@ -583,33 +632,36 @@ __global__ __launch_bounds__(ONE_WAVES * 64) void ftcache_one(const OneArgs a) {
 #pragma unroll
     for (int i = 0; i < NO; ++i) {
       const uint4v v = y.v[i / 4];
-      const uint4v c = {value_codes(v[0], i & 3), value_codes(v[1], i & 3), value_codes(v[2], i & 3), value_codes(v[3], i & 3)};
+      const int by = 4 * (i & 3);
+      const uint4v c = {value_codes(v[0] >> by, bits128), value_codes(v[1] >> by, bits128), value_codes(v[2] >> by, bits128), value_codes(v[3] >> by, bits128)};
       o[i] = mfma16<true>(c, ph, o[i]);
       if constexpr (!BF) o[i] = mfma16<true>(c, pl, o[i]);
     }
   };
-  // the next step's loads are under way while a step is computed, and the entries of the one after
-  int t0 = p.first + wave * ONE_STEP;
+  // the loads of the next AHEAD steps are under way while a step is computed, and the entries of the one after those
+  constexpr int AHEAD = 1;
+  const int t0 = p.first + wave * ONE_STEP;
   if (t0 < end) {
-    Loaded<D> now = load(t0, entries_of(t0));
-    Entries next = entries_of(t0 + ONE_UNIT);
-    for (;;) {
-      const int t1 = t0 + ONE_UNIT, t2 = t1 + ONE_UNIT;
-      Loaded<D> then;
-      if (t1 < end) then = load(t1, next);
-      next = entries_of(t2);
-      __builtin_amdgcn_sched_barrier(0);
-      step(t0, now);
-      if (t1 >= end) break;
-      if (t2 < end) now = load(t2, next);
-      next = entries_of(t2 + ONE_UNIT);
-      __builtin_amdgcn_sched_barrier(0);
-      step(t1, then);
-      if (t2 >= end) break;
-      t0 = t2;
+    Loaded<D> ring[AHEAD + 1];
+    Entries next = entries_of(t0);
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      if (t0 + i * ONE_UNIT < end) ring[i] = load(t0 + i * ONE_UNIT, next);
+      next = entries_of(t0 + (i + 1) * ONE_UNIT);
+    }
+    for (int t = t0; t < end;) {
+#pragma unroll
+      for (int i = 0; i <= AHEAD; ++i) {
+        if (t + AHEAD * ONE_UNIT < end) ring[(i + AHEAD) % (AHEAD + 1)] = load(t + AHEAD * ONE_UNIT, next);
+        next = entries_of(t + (AHEAD + 1) * ONE_UNIT);
+        __builtin_amdgcn_sched_barrier(0);
+        step(t, ring[i]);
+        t += ONE_UNIT;
+        if (t >= end) break;
+      }
     }
   }
-  bad = __any(bad);
+  bad = __any(bad || highest >= pages);
 #pragma unroll
   for (int d = 16; d < 64; d <<= 1) { l += __shfl_xor(l, d); z += __shfl_xor(z, d); }
   const float shift = z - 136.f * ones[0];
@@ -731,7 +783,7 @@ struct ftcache_ctx {
   put_fn put = nullptr;
   get_fn get = nullptr;
   one_fn one = nullptr;
-  int shift = 0, row_tiles = 1, chunks = 1;
+  int shift = 0, row_tiles = 1, chunks = 1, most_parts = 1;
   void* scratch = nullptr;
   float* ws = nullptr;
   uint32_t* done = nullptr;
@@ -822,6 +874,7 @@ extern "C" int ftcache_create(const ftcache_config* cfg, ftcache_ctx** out) {
   }
   const int64_t heads = (int64_t)e.kv_heads * c->row_tiles;
   c->chunks = (int)(ONE_GROUPS / heads < 1 ? 1 : ONE_GROUPS / heads);
+  c->most_parts = (int)(MOST_PARTS / heads < 1 ? 1 : MOST_PARTS / heads);
   // divided sequences are longer than a piece: together they have fewer than twice `chunks` pieces
   const size_t ws = (size_t)2 * c->chunks * heads * (32 + 16 * e.head_dim) * sizeof(float), done = (size_t)e.max_batch * heads * sizeof(uint32_t);
   OnDevice here(e.device);
@@ -935,6 +988,7 @@ extern "C" int ftcache_attend(ftcache_ctx* c, const void* pool, int32_t batch, c
   a.group = e.heads / e.kv_heads;
   a.row_tiles = c->row_tiles;
   a.chunks = c->chunks;
+  a.most_parts = c->most_parts;
   a.scale_log2 = e.softmax_scale * LOG2E;
   a.ws = c->ws;
   a.done = c->done;
