@@ -334,16 +334,20 @@ struct OneArgs {
   const int32_t *lengths, *table;
   int64_t table_stride;
   int32_t batch, most, group, row_tiles;        // most: tokens that a row of the table holds; row_tiles: passes of 16 heads for a group
-  int32_t chunks, most_parts;                   // pieces wanted over all sequences, allowed of one
+  int32_t chunks, one_round, most_parts;        // pieces over all sequences: at most about, at a time; at most of one
   float scale_log2;
   float* ws;                                    // states of divided sequences
-  uint32_t* done;                               // [batch][kv_heads * row_tiles], 0 between calls
+  uint32_t* done;                               // [level][state]: parts that are there, 0 between calls
+  int64_t done_level;
   unsigned long long* refused;
 };
 
-constexpr int ONE_WAVES = 8, ONE_STEP = 32, ONE_UNIT = ONE_WAVES * ONE_STEP;      // tokens of a step of a wave, of a workgroup
-constexpr int CUS = 256, ONE_GROUPS = 2 * CUS;       // workgroups that a call is divided among, or more where sequences are many
-constexpr int MOST_PARTS = CUS;                // of one sequence, where there is one head
+constexpr int ONE_WAVES = 4, ONE_STEP = 32, ONE_UNIT = ONE_WAVES * ONE_STEP;      // tokens of a step of a wave, of a workgroup
+constexpr int CUS = 256, ONE_GROUPS = 8 * CUS, ROUND = 3 * CUS;      // workgroups that a call is divided among (more where sequences are many), and that fit side by side
+constexpr int MOST_PARTS = 2 * CUS, JOIN = 16, LEVELS = 3;      // of one sequence, where there is one head; put together at a time
+static_assert(JOIN * JOIN * JOIN >= MOST_PARTS, "levels");
+constexpr int LONG = 8, SOME = 6;                    // units of a piece, see piece_of
+constexpr int SHORT = 8;                             // units of a sequence that is not divided: joining two parts takes about 3 us, the time of some steps
 
 template <bool BF> __device__ __forceinline__ float4v mfma16(uint4v a, uint4v b, float4v c) {
   if constexpr (BF) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf8v, a), __builtin_bit_cast(bf8v, b), c, 0, 0, 0);
@@ -404,9 +408,14 @@ __device__ __forceinline__ bool piece_of(const OneArgs& a, int id, Piece& p, boo
   }
   total = __builtin_amdgcn_readlane(sum_upto(total), 63);
   longest = __builtin_amdgcn_readlane(max_upto(longest), 63);
-  const int fair = (total + a.chunks - 1) / a.chunks, few = (longest + a.most_parts - 1) / a.most_parts;
-  const int size = fair < 1 ? 1 : fair > few ? fair : few;
-  auto parts_of = [&](int n) { const int u = units(n); return u > size ? (u + size - 1) / size : 1; };
+  // Pieces that leave every CU several are best where there is enough to read (1.25 M tokens of 96 sequences and 8 heads: 297 us in 3 workgroups a CU,
+  // 265 in 8), one round of what fits side by side where there is not (35,000 tokens of 32: 15.9 us in 3, 17.4 in 8), and few enough parts to be put together
+  // at once where that makes them no longer than some steps
+  auto of = [&](int n, int chunks) { return (n + chunks - 1) / chunks; };
+  auto larger = [](int x, int y) { return x > y ? x : y; };
+  auto smaller = [](int x, int y) { return x < y ? x : y; };
+  const int size = larger(larger(larger(of(total, a.chunks), of(longest, a.most_parts)), 1), larger(smaller(of(total, a.one_round), LONG), smaller(of(longest, JOIN), SOME)));
+  auto parts_of = [&](int n) { const int u = units(n); return u > size && u > SHORT ? (u + size - 1) / size : 1; };
   int pieces = 0, slots = 0;          // and those of divided sequences, which leave a state
   for (int i = 0; i < per; ++i) {
     const int b = lane * per + i, n = parts_of(i == 0 ? mine : length(b));
@@ -426,7 +435,7 @@ __device__ __forceinline__ bool piece_of(const OneArgs& a, int id, Piece& p, boo
     if (left < parts) {
       known = n == sound(n);
       const int first = left * size * ONE_UNIT, rest = sound(n) - first;
-      p = Piece{b, first, rest < size * ONE_UNIT ? rest : size * ONE_UNIT, left, parts, slot};
+      p = Piece{b, first, parts == 1 || rest < size * ONE_UNIT ? rest : size * ONE_UNIT, left, parts, slot};
       return true;
     }
     left -= parts;
@@ -455,13 +464,12 @@ template <int D> struct Loaded {
 template <int I> __device__ __forceinline__ float of_lane(float x) { return as_f((uint32_t)__builtin_amdgcn_mov_dpp((int)as_u(x), 0x150 + I, 0xF, 0xF, true)); }
 
 template <int D, bool BF, bool F32OUT>
-__global__ __launch_bounds__(ONE_WAVES * 64) void ftcache_one(const OneArgs a) {
+__global__ __launch_bounds__(ONE_WAVES * 64, 3) void ftcache_one(const OneArgs a) {
   constexpr int KW = D / 32;              // words of key codes per lane and token = matrix instructions over the head
   constexpr int NO = D / 16;              // accumulators of the output
   constexpr int THREADS = ONE_WAVES * 64;
-  // the waves' outputs, [wave][row][D + 4]; then, where a divided sequence is put together, weights of the parts and sums of the columns
-  constexpr int PITCH = D + 4, WAVES_USE = ONE_WAVES * 16 * PITCH, JOIN_USES = 16 * MOST_PARTS + THREADS * 4;
-  __shared__ __attribute__((aligned(16))) float merged[WAVES_USE > JOIN_USES ? WAVES_USE : JOIN_USES];
+  constexpr int PITCH = D + 4;
+  __shared__ __attribute__((aligned(16))) float merged[ONE_WAVES * 16 * PITCH];      // the waves' outputs
   __shared__ float refs[ONE_WAVES][16], sums[ONE_WAVES][16];
   __shared__ int last;
   const int heads = a.pool.kv_heads * a.row_tiles, hr = blockIdx.x % heads, hk = hr / a.row_tiles, tile = hr % a.row_tiles;
@@ -674,7 +682,6 @@ __global__ __launch_bounds__(ONE_WAVES * 64) void ftcache_one(const OneArgs a) {
   __syncthreads();
 
   const int tid = threadIdx.x;
-  float* const ws = a.ws + ((int64_t)(p.slot + p.part) * heads + hr) * STATE<D>;      // (of a divided sequence)
   auto finish = [&](int row, int e, float4v value, float sum) {
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
     char* op = a.o.data + (int64_t)p.b * a.o.token + (int64_t)(head0 + row) * a.o.head;
@@ -697,75 +704,69 @@ __global__ __launch_bounds__(ONE_WAVES * 64) void ftcache_one(const OneArgs a) {
     }
     if (p.parts == 1) finish(row, e, value, sum);
     else {
+      float* const ws = a.ws + ((int64_t)(p.slot + p.part) * heads + hr) * STATE<D>;
       put_state(ws + 32 + row * D + e, value[0], value[1]);
       put_state(ws + 32 + row * D + e + 2, value[2], value[3]);
       if (e == 0) put_state(ws + 2 * row, most, sum);
     }
   }
   if (tid == 0 && bad && p.part == 0 && hr == 0) atomicAdd(a.refused + 1, 1ull);
-  if (p.parts == 1) return;
-  __builtin_amdgcn_s_waitcnt(0x0F70);          // (vmcnt(0): the state is where every XCD sees it)
-  __syncthreads();
-  if (tid == 0) {
-    uint32_t* const done = a.done + (int64_t)p.b * heads + hr;
-    const uint32_t before = atomicAdd(done, 1u);
-    last = before + 1 == (uint32_t)p.parts;
-    if (last) *done = 0;
-  }
-  __syncthreads();
-  if (!last) return;
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
-  // this workgroup came last: it puts the states of all parts together, in their order.  Weights of the parts first (row tid % 16)
-  const float* const first = a.ws + ((int64_t)p.slot * heads + hr) * STATE<D>;
-  const int64_t next = (int64_t)heads * STATE<D>;
-  float* const weight = merged;                           // [part][16]
-  constexpr int SIDE = THREADS / 16;                      // parts taken side by side
-  const int row = tid & 15;
-  float most = -3.4028234e38f;
-  for (int i = tid >> 4; i < p.parts; i += SIDE) {
-    const float2v r = *reinterpret_cast<const float2v*>(first + i * next + 2 * row);
-    weight[i * 16 + row] = r[0];
-    most = __builtin_fmaxf(most, r[0]);
-  }
-  most = __builtin_fmaxf(most, __shfl_xor(most, 16));
-  most = __builtin_fmaxf(most, __shfl_xor(most, 32));
-  if (lane < 16) refs[wave][row] = most;
-  __syncthreads();
+  // Parts are put together by sixteens: the workgroup that comes last of sixteen leaves their sum where the first of them had its state and goes on as one part of
+  // the next sixteen.  (One workgroup for 128 parts took 11 us for them.)
+  int parts = p.parts, part = p.part, apart = 1;                   // of this level; a part's states lie `apart` pieces from the next one's
+  for (uint32_t* level = a.done; parts > 1; level += a.done_level) {
+    const int first = part / JOIN * JOIN, members = parts - first < JOIN ? parts - first : JOIN;
+    __builtin_amdgcn_s_waitcnt(0x0F70);          // (vmcnt(0): the state is where every XCD sees it)
+    __syncthreads();
+    if (tid == 0) {
+      uint32_t* const done = level + (int64_t)(p.slot + first * apart) * heads + hr;
+      last = atomicAdd(done, 1u) + 1 == (uint32_t)members;
+      if (last) *done = 0;
+    }
+    __syncthreads();
+    if (!last) return;
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+    float* const at = a.ws + ((int64_t)(p.slot + first * apart) * heads + hr) * STATE<D>;
+    // (byte offsets in 32 bits: all states together are less, see ftcache_create)
+    const uint32_t next = (uint32_t)apart * (uint32_t)heads * (STATE<D> * 4);
+    const bool whole = parts <= JOIN;
+    for (int x = tid; x < rows * CD; x += THREADS) {
+      const int row = x / CD, e = x % CD * 4;
+      float2v head[JOIN];
+      float4v part_of[JOIN];
+      uint32_t from = 0;
 #pragma unroll
-  for (int w = 0; w < ONE_WAVES; ++w) most = __builtin_fmaxf(most, refs[w][row]);
-  float sum = 0.f;
-  for (int i = tid >> 4; i < p.parts; i += SIDE) {
-    const float f = ex2(weight[i * 16 + row] - most);
-    weight[i * 16 + row] = f;
-    sum += f * first[i * next + 2 * row + 1];
-  }
-  sum += __shfl_xor(sum, 16);
-  sum += __shfl_xor(sum, 32);
-  if (lane < 16) sums[wave][row] = sum;
-  __syncthreads();
-  // then the columns: as many groups of parts side by side as there are threads for
-  const int columns = rows * CD, groups = columns < THREADS ? THREADS / columns : 1, group = tid / columns;
-  float4v* const partial = reinterpret_cast<float4v*>(weight + 16 * MOST_PARTS);
-  for (int c0 = 0; c0 < columns; c0 += THREADS) {
-    const int c = c0 + (groups > 1 ? tid % columns : tid), r = c / CD, e = c % CD * 4;
-    float4v value = (float4v)0.f;
-    if (c < columns && group < groups) {
-      const int from = p.parts * group / groups, to = groups > 1 ? p.parts * (group + 1) / groups : p.parts;
-#pragma unroll 8
-      for (int i = from; i < to; ++i) value += weight[i * 16 + r] * *reinterpret_cast<const float4v*>(first + i * next + 32 + r * D + e);
-    }
-    if (groups > 1) {
-      if (group < groups) partial[tid] = value;
-      __syncthreads();
-      if (group == 0)
-        for (int i = 1; i < groups; ++i) value += partial[i * columns + c];
-    }
-    if (c < columns && (groups == 1 || group == 0)) {
-      float total = 0.f;
+      for (int i = 0; i < JOIN; ++i) {
+        head[i] = *reinterpret_cast<const float2v*>(reinterpret_cast<const char*>(at) + (from + 8 * row));
+        part_of[i] = *reinterpret_cast<const float4v*>(reinterpret_cast<const char*>(at) + (from + 4 * (32 + row * D + e)));
+        from += i + 1 < members ? next : 0;        // (the last one again behind it)
+      }
+      float most = head[0][0];
 #pragma unroll
-      for (int w = 0; w < ONE_WAVES; ++w) total += sums[w][r];
-      finish(r, e, value, total);
+      for (int i = 1; i < JOIN; ++i) most = __builtin_fmaxf(most, head[i][0]);
+      float4v value = (float4v)0.f;
+      float sum = 0.f;
+      int left = members;
+      asm volatile("" : "+v"(left));               // (compared where it is used: sixteen conditions do not lie in scalar registers for the whole loop)
+#pragma unroll
+      for (int i = 0; i < JOIN; ++i) {
+        const float f = ex2(head[i][0] - most);
+        const bool there = i < left;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) value[j] = there ? __builtin_fmaf(f, part_of[i][j], value[j]) : value[j];
+        sum = there ? __builtin_fmaf(f, head[i][1], sum) : sum;
+      }
+      if (whole) finish(row, e, value, sum);
+      else {
+        // (a row's reference and sum are read by all of its lanes, which lie in one wave or, at head_dim 128, half of one: they have all read them)
+        put_state(at + 32 + row * D + e, value[0], value[1]);
+        put_state(at + 32 + row * D + e + 2, value[2], value[3]);
+        if (e == 0) put_state(at + 2 * row, most, sum);
+      }
     }
+    part /= JOIN;
+    parts = (parts + JOIN - 1) / JOIN;
+    apart *= JOIN;
   }
 }
 
@@ -783,10 +784,11 @@ struct ftcache_ctx {
   put_fn put = nullptr;
   get_fn get = nullptr;
   one_fn one = nullptr;
-  int shift = 0, row_tiles = 1, chunks = 1, most_parts = 1;
+  int shift = 0, row_tiles = 1, chunks = 1, one_round = 1, most_parts = 1;
   void* scratch = nullptr;
   float* ws = nullptr;
   uint32_t* done = nullptr;
+  int64_t done_level = 0;
   unsigned long long* refused = nullptr;
   std::string err;
 };
@@ -874,9 +876,11 @@ extern "C" int ftcache_create(const ftcache_config* cfg, ftcache_ctx** out) {
   }
   const int64_t heads = (int64_t)e.kv_heads * c->row_tiles;
   c->chunks = (int)(ONE_GROUPS / heads < 1 ? 1 : ONE_GROUPS / heads);
+  c->one_round = (int)(ROUND / heads < 1 ? 1 : ROUND / heads);
   c->most_parts = (int)(MOST_PARTS / heads < 1 ? 1 : MOST_PARTS / heads);
   // divided sequences are longer than a piece: together they have fewer than twice `chunks` pieces
-  const size_t ws = (size_t)2 * c->chunks * heads * (32 + 16 * e.head_dim) * sizeof(float), done = (size_t)e.max_batch * heads * sizeof(uint32_t);
+  const size_t states = (size_t)2 * c->chunks * heads, ws = states * (32 + 16 * e.head_dim) * sizeof(float), done = LEVELS * states * sizeof(uint32_t);
+  c->done_level = (int64_t)states;
   OnDevice here(e.device);
   hipError_t he = here.status;
   if (he == hipSuccess) he = hipMalloc(&c->scratch, 256 + ((done + 255) & ~(size_t)255) + ws);
@@ -988,10 +992,12 @@ extern "C" int ftcache_attend(ftcache_ctx* c, const void* pool, int32_t batch, c
   a.group = e.heads / e.kv_heads;
   a.row_tiles = c->row_tiles;
   a.chunks = c->chunks;
+  a.one_round = c->one_round;
   a.most_parts = c->most_parts;
   a.scale_log2 = e.softmax_scale * LOG2E;
   a.ws = c->ws;
   a.done = c->done;
+  a.done_level = c->done_level;
   a.refused = c->refused;
   OnDevice here(e.device);
   if (here.status != hipSuccess) return cfail_hip(c, "device", here.status);
