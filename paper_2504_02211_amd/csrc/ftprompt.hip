@@ -15,13 +15,16 @@
 #include <cmath>
 #include <new>
 #include <string>
+#include <type_traits>
 
 namespace ftprompt {
 using namespace ftserve;
 
-constexpr int BM = 128, BN = 64, NW = 4;
+constexpr int BN = 64, SUB = 64, NW = 4, STAGES = 2;      // keys of a tile, of a step; waves; tiles in LDS
+constexpr int64_t WIDE_FROM = 2 * 256 * 256;
+constexpr int bm_of(int rb) { return NW * 32 * rb; }      // rows of a workgroup whose waves have rb blocks of 32
 
-struct Rows { char* data; int64_t token, head; };       // strides in bytes
+struct Rows { char* data; int64_t token, head; };         // strides in bytes
 
 struct Args {
   Rows q, k, v, o;
@@ -31,19 +34,23 @@ struct Args {
 };
 
 template <int D> constexpr int tile_bytes() { return BN * D * 2; }
-template <int D> constexpr int lds_bytes() { return 2 * tile_bytes<D>(); }
+template <int D> constexpr int lds_bytes() { return STAGES * 2 * tile_bytes<D>(); }
 
-// Place of 16-byte chunk c of row r in a tile.  Key tiles are read 16 bytes a lane from 32 rows, value tiles 4 rows of 32 bytes for every 16 lanes: ...
-template <int D> __device__ __forceinline__ int k_place(int r, int c) {
-  return D == 128 ? r * 16 + (c ^ (r & 15)) : r * 8 + (c ^ ((r >> 1) & 7));
-}
-template <int D> __device__ __forceinline__ int v_place(int r, int c) {
-  return D == 128 ? r * 16 + (c ^ ((r & 3) << 2)) : r * 8 + (c ^ ((r >> 1 & 1) << 2));
+// 16 bytes per lane from (uniform base + per-lane byte offset) straight into LDS at (uniform LDS address + 16 * lane).
+// (Opaque to the compiler, which would wait for the tile in flight before it reads another; ordering against barriers and counted waits is kept
+// because all of them are side-effecting instructions.)
+__device__ __forceinline__ void load_lds16(const void* base, uint32_t byte_off, uint32_t lds_addr) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(byte_off), "s"(base), "s"(lds_addr) : "memory");
 }
 
 template <bool BF> __device__ __forceinline__ float16v mfma32(uint4v a, uint4v b, float16v c) {
   if constexpr (BF) return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf8v, a), __builtin_bit_cast(bf8v, b), c, 0, 0, 0);
   else return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8v, a), __builtin_bit_cast(half8v, b), c, 0, 0, 0);
+}
+// c plus the lane's own four values (sixteen products of 4x4 with ones side by side): a sum on the matrix pipe
+template <bool BF> __device__ __forceinline__ float4v add4(uint2v x, float4v c) {
+  if constexpr (BF) return __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(short4v{0x3F80, 0x3F80, 0x3F80, 0x3F80}, __builtin_bit_cast(short4v, x), c, 0, 0, 0);
+  else return __builtin_amdgcn_mfma_f32_4x4x4f16(half4v{1, 1, 1, 1}, __builtin_bit_cast(half4v, x), c, 0, 0, 0);
 }
 
 __device__ __forceinline__ float max32(float x) {
@@ -55,11 +62,13 @@ __device__ __forceinline__ float sum32(float x) {
   return as_f(r[0]) + as_f(r[1]);
 }
 
-template <int D, bool BF, bool F32OUT>
+typedef __attribute__((address_space(3))) char lds_char;
+
+template <int D, bool BF, bool F32OUT, int RB>
 __global__ __launch_bounds__(NW * 64, 2) void ftprompt_main(const Args a) {
   extern __shared__ uint4v lds[];
-  uint4v* const kt = lds;
-  uint4v* const vt = lds + tile_bytes<D>() / 16;
+  constexpr int BM = bm_of(RB), NF = D / 32, TILE = tile_bytes<D>();
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_char*)lds;
   const int hk = blockIdx.x % a.kv_heads, slot = a.slots - 1 - blockIdx.x / a.kv_heads;
   const int G = a.group;
   // sequence b owns the row tiles from cu_q[b] * G / BM + b on: at least as many as it has rows for
@@ -70,149 +79,233 @@ __global__ __launch_bounds__(NW * 64, 2) void ftprompt_main(const Args a) {
   const int k0 = clamped(a.cu_k[b], a.total_k), k1 = clamped(a.cu_k[b + 1], a.total_k);
   const int nq = q1 - q0, nk = k1 - k0;
   if (tile < 0 || nq <= 0 || (int64_t)tile * BM >= (int64_t)nq * G) return;
-  const int rows = nq * G, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, h = lane >> 5, n = lane & 31;
+  const int rows = nq * G, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5, n = lane & 31;
 
-  const int row = tile * BM + wave * 32 + n, rowc = row < rows ? row : rows - 1;
-  const int qi = rowc / G, head = hk * G + rowc % G;
-  const int seen = nk - nq + qi + 1;                       // keys that the row sees: may be <= 0
-  const int last_of = [&](int r) { return nk - nq + (r < rows ? r : rows - 1) / G + 1; }(tile * BM + BM - 1);
-  const int keys = last_of < 0 ? 0 : last_of;              // of the longest row of the workgroup
-  const int wave_row = tile * BM + wave * 32;
-  const int all_seen = nk - nq + (wave_row < rows ? wave_row : rows - 1) / G + 1;      // keys that every row of the wave sees
-  const int any_seen = nk - nq + (wave_row + 31 < rows ? wave_row + 31 : rows - 1) / G + 1;
+  // keys that row r of the sequence sees (may be <= 0); rows behind the last count as it
+  auto seen_by = [&](int r) { return nk - nq + (r < rows ? r : rows - 1) / G + 1; };
+  const int row0 = tile * BM + wave * (32 * RB);
+  const int all_seen = seen_by(row0), any_seen = seen_by(row0 + 32 * RB - 1), keys = seen_by(tile * BM + BM - 1);
+  const int tiles = keys > 0 ? (keys + BN - 1) / BN : 0;
+  const int steps = any_seen > 0 ? (any_seen + SUB - 1) / SUB : 0, full = all_seen > 0 ? all_seen / SUB : 0;      // steps of this wave; that every row sees whole
 
-  uint4v qf[D / 16];
-  const char* qp = a.q.data + (int64_t)(q0 + qi) * a.q.token + (int64_t)head * a.q.head + 16 * h;
+  int seen[RB];
+  uint4v qf[RB][D / 16];
+  auto row_of = [&](int rb, int& query, int& head) {
+    const int r = row0 + 32 * rb + n, rc = r < rows ? r : rows - 1;
+    query = rc / G;
+    head = hk * G + rc - query * G;
+    return r < rows;
+  };
 #pragma unroll
-  for (int i = 0; i < D / 16; ++i) qf[i] = *reinterpret_cast<const uint4v*>(qp + 32 * i);
-
-  float16v o[D / 32];
+  for (int rb = 0; rb < RB; ++rb) {
+    int query, head;
+    row_of(rb, query, head);
+    seen[rb] = nk - nq + query + 1;
+    const char* qp = a.q.data + (int64_t)(q0 + query) * a.q.token + (int64_t)head * a.q.head + 16 * h;
 #pragma unroll
-  for (int f = 0; f < D / 32; ++f) o[f] = (float16v)0.f;
-  float ref = -3.4028234e38f, l = 0.f;
+    for (int i = 0; i < D / 16; ++i) qf[rb][i] = *reinterpret_cast<const uint4v*>(qp + 32 * i);
+  }
+
+  // Tiles: row r of keys has its 16-byte chunk c at place c ^ (r & 15) (head_dim 64: c ^ (r / 2 & 7)), a row of values its 64 bytes f at f ^ (r & 3) (f ^ (r / 2 & 1)).
+  // Sixteen lanes that read 16 bytes of as many rows of keys then meet all banks once, and so do 32 that read 32 bytes of four rows of values, twice.
+  constexpr int CH = D / 8, LOADS = TILE / 1024 / NW, RPL = 64 / CH;      // chunks of a row; loads of a wave for a tile; rows of a load
+  uint32_t koff[LOADS], voff[LOADS];
   const char* kbase = a.k.data + (int64_t)k0 * a.k.token + (int64_t)hk * a.k.head;
   const char* vbase = a.v.data + (int64_t)k0 * a.v.token + (int64_t)hk * a.v.head;
-  constexpr int CH = D / 8, PER = BN * CH / (NW * 64);      // chunks per row, per thread
-
-  for (int j0 = 0; j0 < keys; j0 += BN) {
-    uint4v ks[PER], vs[PER];
+  auto chunk_k = [&](int r) { return (uint32_t)((lane % CH) ^ (D == 128 ? r & 15 : r >> 1 & 7)) * 16; };
+  auto chunk_v = [&](int r) { return (uint32_t)((lane % CH) ^ (D == 128 ? (r & 3) << 2 : (r >> 1 & 1) << 2)) * 16; };
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int x = tid + i * NW * 64, r = x / CH, c = x % CH;
-      const int64_t t = j0 + r < nk ? j0 + r : nk - 1;
-      ks[i] = *reinterpret_cast<const uint4v*>(kbase + t * a.k.token + 16 * c);
-      vs[i] = *reinterpret_cast<const uint4v*>(vbase + t * a.v.token + 16 * c);
-    }
-    __syncthreads();
+  for (int i = 0; i < LOADS; ++i) {
+    const int r = (wave * LOADS + i) * RPL + lane / CH;
+    koff[i] = (uint32_t)r * (uint32_t)a.k.token + chunk_k(r);
+    voff[i] = (uint32_t)r * (uint32_t)a.v.token + chunk_v(r);
+  }
+  auto issue = [&](int t, uint32_t stage) {
+    const uint32_t to = lds0 + stage * (2 * TILE) + (uint32_t)wave * (LOADS * 1024);
+    const char* const kp = kbase + (int64_t)t * BN * a.k.token;
+    const char* const vp = vbase + (int64_t)t * BN * a.v.token;
+    if ((t + 1) * BN <= nk) {
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int x = tid + i * NW * 64, r = x / CH, c = x % CH;
-      kt[k_place<D>(r, c)] = ks[i];
-      vt[v_place<D>(r, c)] = vs[i];
+      for (int i = 0; i < LOADS; ++i) load_lds16(kp, koff[i], to + i * 1024);
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) load_lds16(vp, voff[i], to + TILE + i * 1024);
+    } else {           // rows behind the last key: the last one again (no row sees them)
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) {
+        const int r = (wave * LOADS + i) * RPL + lane / CH, rc = r < nk - 1 - t * BN ? r : nk - 1 - t * BN;
+        load_lds16(kp, (uint32_t)rc * (uint32_t)a.k.token + chunk_k(r), to + i * 1024);
+        load_lds16(vp, (uint32_t)rc * (uint32_t)a.v.token + chunk_v(r), to + TILE + i * 1024);
+      }
     }
-    __syncthreads();
-    if (j0 >= any_seen) continue;
+  };
 
-    float16v s[2];
+  // operands from LDS.  k_at / v_at: address of a step's first row
+  const uint32_t klane = (uint32_t)n * (2 * D) + (uint32_t)(h ^ (D == 128 ? n & 15 : n >> 1 & 7)) * 16;
+  const int rr = (lane & 15) >> 2;
+  const uint32_t vlane = (uint32_t)(4 * h + rr) * (2 * D) + (uint32_t)((lane >> 4 & 1) * 32 + (lane & 3) * 8) + (uint32_t)(D == 128 ? rr : rr >> 1) * 64;
+  auto key = [&](uint32_t k_at, int i) { return *(__attribute__((address_space(3))) uint4v*)(uintptr_t)(k_at + (klane ^ (32u * i))); };
+  auto value = [&](uint32_t v_at, int i, int f) {      // V^T: elements 32f + lane % 32, keys 16i + 4h + 0..3 and 8 on
+    const uint32_t at = v_at + (vlane ^ (64u * f)) + (uint32_t)i * (32 * D);
+    const uint2v x = __builtin_bit_cast(uint2v, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)(uintptr_t)at));
+    const uint2v y = __builtin_bit_cast(uint2v, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)(uintptr_t)(at + 16 * D)));
+    return uint4v{x[0], x[1], y[0], y[1]};
+  };
+
+  float16v o[RB][NF];
+  float4v sums[RB];
+  float ref[RB];
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    ref[rb] = -3.4028234e38f;
+    sums[rb] = (float4v)0.f;
+#pragma unroll
+    for (int f = 0; f < NF; ++f) o[rb][f] = (float16v)0.f;
+  }
+
+  // scores of a tile, transposed
+  auto scores = [&](uint32_t k_at, float16v (&to)[2]) __attribute__((always_inline)) {
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      s[t] = (float16v)0.f;
+      to[t] = (float16v)0.f;
 #pragma unroll
-      for (int i = 0; i < D / 16; ++i) s[t] = mfma32<BF>(kt[k_place<D>(32 * t + n, 2 * i + h)], qf[i], s[t]);
+      for (int i = 0; i < D / 16; ++i) to[t] = mfma32<BF>(key(k_at + t * (64 * D), i), qf[0][i], to[t]);
     }
-    const bool masked = j0 + BN > all_seen;
-    if (masked) {
+  };
+  auto mask = [&](int t, float16v (&x)[2]) __attribute__((always_inline)) {
+    const int limit = seen[0] - t * BN - 4 * h;
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
+    for (int v = 0; v < 32; ++v)
+      if (limit <= 8 * (v >> 2) + (v & 3)) x[v >> 4][v & 15] = -__builtin_inff();
+  };
+  // fp16 weights reach 2^14 rather than 2^8, so that those far below the largest keep their bits
+  constexpr float ROOM = 8.f, UP = BF ? 0.f : 6.f;
+  auto largest = [&](const float16v (&x)[2]) __attribute__((always_inline)) {
+    float m = __builtin_fmaxf(x[0][0], x[1][0]);
 #pragma unroll
-        for (int v = 0; v < 16; ++v)
-          if (j0 + 32 * t + 8 * (v >> 2) + 4 * h + (v & 3) >= seen) s[t][v] = -__builtin_inff();
-    }
-    float m = s[0][0];
+    for (int v = 1; v < 16; ++v) m = __builtin_fmaxf(__builtin_fmaxf(m, x[0][v]), x[1][v]);
+    return max32(m) * a.scale_log2;
+  };
+  // a row's reference moves when a score exceeds it by more than there is room for: rarely after the first step
+  auto renew = [&](const float (&m)[RB]) __attribute__((always_inline)) {
+    bool any = false;
 #pragma unroll
-    for (int v = 0; v < 16; ++v) m = __builtin_fmaxf(m, __builtin_fmaxf(s[0][v], s[1][v]));
-    m = max32(m) * a.scale_log2;
-    if (__any(m > ref + 8.f)) {
-      const float next = __builtin_fmaxf(m, ref), f = ex2(ref - next);
-      ref = next;
-      l *= f;
+    for (int rb = 0; rb < RB; ++rb) any |= m[rb] > ref[rb] + (ROOM + UP);
+    if (__any(any)) {
 #pragma unroll
-      for (int x = 0; x < D / 32; ++x) o[x] *= f;
-    }
-    uint4v p[4];
+      for (int rb = 0; rb < RB; ++rb) {
+        const float next = __builtin_fmaxf(m[rb] - UP, ref[rb]), f = ex2(ref[rb] - next);
+        ref[rb] = next;
+        sums[rb] *= f;
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int v = 0; v < 16; v += 2) {
-        const float x = ex2(__builtin_fmaf(s[t][v], a.scale_log2, -ref)), y = ex2(__builtin_fmaf(s[t][v + 1], a.scale_log2, -ref));
-        l += x;
-        l += y;
-        p[2 * t + (v >> 3)][(v & 7) >> 1] = pack2<BF>(x, y);
+        for (int x = 0; x < NF; ++x) o[rb][x] *= f;
       }
-    // a value that a row does not see must not reach it, and 0 times infinity would: in tiles that some row does not see whole,
-    // such values are taken out of the product and given to the rows that see them
-    auto value = [&](int i, int f, int s4) {      // V^T: elements 32f + lane % 32, keys 16i + 8 s4 + 4h + 0..3
-      const int r = 16 * i + 8 * s4 + 4 * h + ((lane & 15) >> 2), e = 32 * f + (lane & 16) + 4 * (lane & 3);
-      const uint32_t at = (uint32_t)(tile_bytes<D>() + v_place<D>(r, e >> 3) * 16 + (e & 4) * 2);
-      return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)((__attribute__((address_space(3))) char*)lds + at));
-    };
+    }
+  };
+  auto weights = [&](const float16v (&x)[2], uint4v (&p)[4]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int v = 0; v < 32; v += 2)
+      p[v >> 3][(v & 7) >> 1] = pack2<BF>(ex2(__builtin_fmaf(x[v >> 4][v & 15], a.scale_log2, -ref[0])), ex2(__builtin_fmaf(x[v >> 4][(v & 15) + 1], a.scale_log2, -ref[0])));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      sums[0] = add4<BF>(uint2v{p[i][0], p[i][1]}, sums[0]);
+      sums[0] = add4<BF>(uint2v{p[i][2], p[i][3]}, sums[0]);
+    }
+  };
+  // clean: values that are not finite count as 0, and are found
+  short2v finite = {-1, -1};
+  auto products = [&](uint32_t v_at, const uint4v (&p)[4], auto clean) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int f = 0; f < D / 32; ++f) {
-        const uint2v x = __builtin_bit_cast(uint2v, value(i, f, 0)), y = __builtin_bit_cast(uint2v, value(i, f, 1));
-        uint4v av = {x[0], x[1], y[0], y[1]};
-        if (masked) {
-          uint32_t bad = 0;
+      for (int f = 0; f < NF; ++f) {
+        uint4v av = value(v_at, i, f);
+        if constexpr (decltype(clean)::value) {
+          constexpr short E = BF ? 0x7F80 : 0x7C00;
 #pragma unroll
           for (int w = 0; w < 4; ++w) {
-            const uint32_t e = largest_finite_plus_one<BF>();
-            const bool lo = (av[w] & e) == e, hi = (av[w] & (e << 16)) == (e << 16);
-            bad |= (lo ? 1u : 0u) << (2 * w) | (hi ? 1u : 0u) << (2 * w + 1);
-          }
-          if (__any(bad != 0)) {
-            // keys (h', slot) with such a value in any element of this block, one after the other
-            for (int key = 0; key < 16; ++key) {
-              const int hh = key >> 3, sl = key & 7;
-              const uint64_t who = __ballot(h == hh && (bad >> sl & 1));
-              if (!who) continue;
-              const int j = j0 + 16 * i + 8 * (sl >> 2) + 4 * hh + (sl & 3);
-              const uint32_t pw = p[i][sl >> 1];
-              const float own = sl & 1 ? high_of<BF>(pw) : low_of<BF>(pw), w = __shfl(own, 32 * hh + n);
-              const uint32_t vw = av[sl >> 1];
-              const float val = sl & 1 ? high_of<BF>(vw) : low_of<BF>(vw);
-#pragma unroll
-              for (int r = 0; r < 16; ++r) {
-                const int e = 8 * (r >> 2) + 4 * h + (r & 3);
-                const float ve = __shfl(val, 32 * hh + e);
-                const bool is_bad = who >> (32 * hh + e) & 1;
-                if (is_bad && j < seen) o[f][r] += w * ve;
-              }
-            }
-#pragma unroll
-            for (int w = 0; w < 4; ++w) av[w] &= (bad >> (2 * w) & 1 ? 0u : 0xFFFFu) | (bad >> (2 * w + 1) & 1 ? 0u : 0xFFFF0000u);
+            const short2v is = (__builtin_bit_cast(short2v, av[w] & 0x7FFF7FFFu) - short2v{E, E}) >> 15;      // -1 where the exponent is not all ones
+            finite &= is;
+            av[w] &= __builtin_bit_cast(uint32_t, is);
           }
         }
-        o[f] = mfma32<BF>(av, p[i], o[f]);
+        o[0][f] = mfma32<BF>(av, p[i], o[0][f]);
+      }
+  };
+
+  if (tiles > 0) issue(0, 0);
+  // A value that a row does not see must not reach it, and 0 times infinity would: in steps that some row does not see whole, values that are not finite are
+  // left out of the products, and added behind the loop to the rows that see them.
+  auto arrive = [&](int t) __attribute__((always_inline)) {
+    // tile t is there and nobody reads tile t - 1 any more: tile t + 1 may take its place
+    __builtin_amdgcn_s_waitcnt(0x0F70);
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    if (t + 1 < tiles) issue(t + 1, (t + 1) & 1);
+    return lds0 + (t & 1) * (2 * TILE);
+  };
+  int t = 0;
+  for (; t < full; ++t) {              // tiles that every row of the wave sees whole
+    const uint32_t k_at = arrive(t);
+    float16v s[2];
+    scores(k_at, s);
+    const float m[RB] = {largest(s)};
+    renew(m);
+    uint4v p[4];
+    weights(s, p);
+    products(k_at + TILE, p, std::false_type{});
+  }
+#pragma unroll 1
+  for (; t < tiles; ++t) {
+    const uint32_t k_at = arrive(t);
+    if (t >= steps) continue;
+    float16v s[2];
+    scores(k_at, s);
+    mask(t, s);
+    const float m[RB] = {largest(s)};
+    renew(m);
+    uint4v p[4];
+    weights(s, p);
+    products(k_at + TILE, p, std::true_type{});
+  }
+  if (__any(__builtin_bit_cast(uint32_t, finite) != 0xFFFFFFFFu)) {
+    for (int j = full * SUB; j < any_seen; ++j)
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+        for (int f = 0; f < NF; ++f)
+#pragma unroll
+          for (int r = 0; r < 16; r += 2) {
+            const uint32_t w = *reinterpret_cast<const uint32_t*>(vbase + (int64_t)j * a.v.token + 2 * (32 * f + 8 * (r >> 2) + 4 * h + (r & 3)));
+            const float lo = low_of<BF>(w), hi = high_of<BF>(w);
+            if (j < seen[rb] && !(__builtin_fabsf(lo) <= 3.4e38f)) o[rb][f][r] += lo;
+            if (j < seen[rb] && !(__builtin_fabsf(hi) <= 3.4e38f)) o[rb][f][r + 1] += hi;
+          }
+  }
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    int query, head;
+    const bool real = row_of(rb, query, head);
+    const float l = sum32(sums[rb][0]), inv = l == 0.f ? 0.f : 1.f / l;
+    if (!real) continue;
+    char* op = a.o.data + (int64_t)(q0 + query) * a.o.token + (int64_t)head * a.o.head;
+#pragma unroll
+    for (int f = 0; f < NF; ++f)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const float x0 = o[rb][f][4 * g] * inv, x1 = o[rb][f][4 * g + 1] * inv, x2 = o[rb][f][4 * g + 2] * inv, x3 = o[rb][f][4 * g + 3] * inv;
+        const int e = 32 * f + 8 * g + 4 * h;
+        if constexpr (F32OUT) *reinterpret_cast<float4v*>(op + 4 * e) = float4v{x0, x1, x2, x3};
+        else *reinterpret_cast<uint2v*>(op + 2 * e) = uint2v{pack2<BF>(x0, x1), pack2<BF>(x2, x3)};
       }
   }
-  l = sum32(l);
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  if (row >= rows) return;
-  char* op = a.o.data + (int64_t)(q0 + qi) * a.o.token + (int64_t)head * a.o.head;
-#pragma unroll
-  for (int f = 0; f < D / 32; ++f)
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      const float x0 = o[f][4 * g] * inv, x1 = o[f][4 * g + 1] * inv, x2 = o[f][4 * g + 2] * inv, x3 = o[f][4 * g + 3] * inv;
-      const int e = 32 * f + 8 * g + 4 * h;
-      if constexpr (F32OUT) *reinterpret_cast<float4v*>(op + 4 * e) = float4v{x0, x1, x2, x3};
-      else *reinterpret_cast<uint2v*>(op + 2 * e) = uint2v{pack2<BF>(x0, x1), pack2<BF>(x2, x3)};
-    }
 }
 
 typedef void (*kernel_fn)(const Args);
-template <int D, bool BF> static kernel_fn kernel_of(bool f32) { return f32 ? ftprompt_main<D, BF, true> : ftprompt_main<D, BF, false>; }
+template <int D, bool BF, int RB> static kernel_fn kernel_of(bool f32) { return f32 ? ftprompt_main<D, BF, true, RB> : ftprompt_main<D, BF, false, RB>; }
+template <int RB> static kernel_fn kernel_for(const ftprompt_config& e) {
+  const bool bf = e.in_dtype == FTPROMPT_BF16, f32 = e.out_dtype == FTPROMPT_F32;
+  return e.head_dim == 128 ? (bf ? kernel_of<128, true, RB>(f32) : kernel_of<128, false, RB>(f32)) : (bf ? kernel_of<64, true, RB>(f32) : kernel_of<64, false, RB>(f32));
+}
 
 }  // namespace ftprompt
 
@@ -220,10 +313,13 @@ using namespace ftprompt;
 
 struct ftprompt_ctx {
   ftprompt_config cfg;
-  kernel_fn fn = nullptr;
+  kernel_fn fn[2] = {nullptr, nullptr};       // one block of rows to a wave, two
   int lds = 0;
   std::string err;
 };
+
+// Whether waves take two blocks of 32 rows.
+static int ftprompt_wide(int64_t total_q, int heads) { return total_q * heads >= WIDE_FROM; }
 
 static thread_local std::string g_prompt_create_err;
 
@@ -256,14 +352,14 @@ extern "C" int ftprompt_create(const ftprompt_config* cfg, ftprompt_ctx** out) {
   if (!c) return pfail(nullptr, FTPROMPT_ENOMEM, "out of host memory");
   c->cfg = *cfg;
   if (!(c->cfg.softmax_scale > 0.f)) c->cfg.softmax_scale = 1.0f / std::sqrt((float)cfg->head_dim);
-  const bool bf = cfg->in_dtype == FTPROMPT_BF16, f32 = cfg->out_dtype == FTPROMPT_F32;
-  c->fn = cfg->head_dim == 128 ? (bf ? kernel_of<128, true>(f32) : kernel_of<128, false>(f32)) : (bf ? kernel_of<64, true>(f32) : kernel_of<64, false>(f32));
+  c->fn[0] = kernel_for<1>(*cfg);
+  c->fn[1] = kernel_for<1>(*cfg);
   c->lds = cfg->head_dim == 128 ? lds_bytes<128>() : lds_bytes<64>();
   int before = 0;
   hipError_t he = hipGetDevice(&before);
   if (he == hipSuccess) he = hipSetDevice(cfg->device);
   if (he == hipSuccess) {
-    he = hipFuncSetAttribute((const void*)c->fn, hipFuncAttributeMaxDynamicSharedMemorySize, c->lds);
+    for (int i = 0; i < 2 && he == hipSuccess; ++i) he = hipFuncSetAttribute((const void*)c->fn[i], hipFuncAttributeMaxDynamicSharedMemorySize, c->lds);
     (void)hipSetDevice(before);
   }
   if (he != hipSuccess) {
@@ -300,14 +396,15 @@ extern "C" int ftprompt_forward(ftprompt_ctx* c, const ftprompt_rows* q, const f
   }
   if (total_q == 0) return FTPROMPT_OK;
   const int group = e.heads / e.kv_heads;
-  const int64_t slots = (int64_t)total_q * group / BM + batch;
+  const int wide = 0;
+  const int64_t slots = (int64_t)total_q * group / bm_of(wide + 1) + batch;
   if ((int64_t)total_q * group > 0x7FFFFF00ll || slots * e.kv_heads > 0x7FFFFFFFll) return pfail(c, FTPROMPT_EUNSUPPORTED, "too many rows");
   Args a{r[0], r[1], r[2], r[3], cu_q, cu_k, batch, total_q, total_k, e.kv_heads, group, (int32_t)slots, e.softmax_scale * LOG2E};
   int before = 0;
   hipError_t he = hipGetDevice(&before);
   if (he == hipSuccess && before != e.device) he = hipSetDevice(e.device);
   if (he != hipSuccess) return pfail_hip(c, "device", he);
-  hipLaunchKernelGGL(c->fn, dim3((uint32_t)(slots * e.kv_heads)), dim3(NW * 64), c->lds, (hipStream_t)hip_stream, a);
+  hipLaunchKernelGGL(c->fn[wide], dim3((uint32_t)(slots * e.kv_heads)), dim3(NW * 64), c->lds, (hipStream_t)hip_stream, a);
   he = hipGetLastError();
   if (before != e.device) (void)hipSetDevice(before);
   return he == hipSuccess ? FTPROMPT_OK : pfail_hip(c, "launch", he);
