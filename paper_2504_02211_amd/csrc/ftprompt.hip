@@ -120,24 +120,22 @@ __global__ __launch_bounds__(NW * 64, 2) void ftprompt_main(const Args a) {
     koff[i] = (uint32_t)r * (uint32_t)a.k.token + chunk_k(r);
     voff[i] = (uint32_t)r * (uint32_t)a.v.token + chunk_v(r);
   }
-  auto issue = [&](int t, uint32_t stage) {
-    const uint32_t to = lds0 + stage * (2 * TILE) + (uint32_t)wave * (LOADS * 1024);
-    const char* const kp = kbase + (int64_t)t * BN * a.k.token;
-    const char* const vp = vbase + (int64_t)t * BN * a.v.token;
+  auto issue_one = [&](const char* base, int64_t stride, const uint32_t (&off)[LOADS], auto chunk, int t, uint32_t to) __attribute__((always_inline)) {
+    const char* const p = base + (int64_t)t * BN * stride;
+    to += (uint32_t)wave * (LOADS * 1024);
     if ((t + 1) * BN <= nk) {
 #pragma unroll
-      for (int i = 0; i < LOADS; ++i) load_lds16(kp, koff[i], to + i * 1024);
-#pragma unroll
-      for (int i = 0; i < LOADS; ++i) load_lds16(vp, voff[i], to + TILE + i * 1024);
+      for (int i = 0; i < LOADS; ++i) load_lds16(p, off[i], to + i * 1024);
     } else {           // rows behind the last key: the last one again (no row sees them)
 #pragma unroll
       for (int i = 0; i < LOADS; ++i) {
         const int r = (wave * LOADS + i) * RPL + lane / CH, rc = r < nk - 1 - t * BN ? r : nk - 1 - t * BN;
-        load_lds16(kp, (uint32_t)rc * (uint32_t)a.k.token + chunk_k(r), to + i * 1024);
-        load_lds16(vp, (uint32_t)rc * (uint32_t)a.v.token + chunk_v(r), to + TILE + i * 1024);
+        load_lds16(p, (uint32_t)rc * (uint32_t)stride + chunk(r), to + i * 1024);
       }
     }
   };
+  auto issue_k = [&](int t, uint32_t to) __attribute__((always_inline)) { issue_one(kbase, a.k.token, koff, chunk_k, t, to); };
+  auto issue_v = [&](int t, uint32_t to) __attribute__((always_inline)) { issue_one(vbase, a.v.token, voff, chunk_v, t, to); };
 
   // operands from LDS.  k_at / v_at: address of a step's first row
   const uint32_t klane = (uint32_t)n * (2 * D) + (uint32_t)(h ^ (D == 128 ? n & 15 : n >> 1 & 7)) * 16;
@@ -232,43 +230,76 @@ __global__ __launch_bounds__(NW * 64, 2) void ftprompt_main(const Args a) {
       }
   };
 
-  if (tiles > 0) issue(0, 0);
   // A value that a row does not see must not reach it, and 0 times infinity would: in steps that some row does not see whole, values that are not finite are
   // left out of the products, and added behind the loop to the rows that see them.
+  // Stage t & 1 holds what iteration t reads: the values of tile t and the keys of tile t + 1.  An iteration computes the scores of the next tile beside the
+  // exponentials of its own (vector instructions in the shadow of the wave's own matrix instructions are nearly free), then its products beside the maxima of the next.
   auto arrive = [&](int t) __attribute__((always_inline)) {
-    // tile t is there and nobody reads tile t - 1 any more: tile t + 1 may take its place
+    // what iteration t reads is there, and nobody reads what t - 1 did any more: it makes room for t + 1
     __builtin_amdgcn_s_waitcnt(0x0F70);
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    if (t + 1 < tiles) issue(t + 1, (t + 1) & 1);
+    const uint32_t next = lds0 + ((t + 1) & 1) * (2 * TILE);
+    if (t + 1 < tiles) issue_v(t + 1, next + TILE);
+    if (t + 2 < tiles) issue_k(t + 2, next);
     return lds0 + (t & 1) * (2 * TILE);
   };
-  int t = 0;
-  for (; t < full; ++t) {              // tiles that every row of the wave sees whole
-    const uint32_t k_at = arrive(t);
-    float16v s[2];
-    scores(k_at, s);
+  float16v s[2];
+  if (tiles > 0) {
+    issue_k(0, lds0 + 2 * TILE);
+    issue_v(0, lds0 + TILE);
+    if (tiles > 1) issue_k(1, lds0);
+    __builtin_amdgcn_s_waitcnt(0x0F70);
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    scores(lds0 + 2 * TILE, s);
+    if (full < 1) mask(0, s);
     const float m[RB] = {largest(s)};
     renew(m);
+  }
+  int t = 0;
+  for (; t + 1 < full; ++t) {              // this tile and the next one are seen whole by every row of the wave
+    const uint32_t at = arrive(t);
+    float16v then[2];
     uint4v p[4];
+    scores(at, then);
     weights(s, p);
-    products(k_at + TILE, p, std::false_type{});
+    products(at + TILE, p, std::false_type{});
+    const float m[RB] = {largest(then)};
+    s[0] = then[0];
+    s[1] = then[1];
+#ifdef SGB
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x2, SGB, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < 24; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+      __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x2, 2, 0);
+    }
+#endif
+    renew(m);
   }
 #pragma unroll 1
   for (; t < tiles; ++t) {
-    const uint32_t k_at = arrive(t);
+    const uint32_t at = arrive(t);
     if (t >= steps) continue;
-    float16v s[2];
-    scores(k_at, s);
-    mask(t, s);
-    const float m[RB] = {largest(s)};
-    renew(m);
     uint4v p[4];
     weights(s, p);
-    products(k_at + TILE, p, std::true_type{});
+    products(at + TILE, p, std::true_type{});
+    if (t + 1 < steps) {
+      scores(at, s);
+      mask(t + 1, s);
+      const float m[RB] = {largest(s)};
+      renew(m);
+    }
   }
   if (__any(__builtin_bit_cast(uint32_t, finite) != 0xFFFFFFFFu)) {
-    for (int j = full * SUB; j < any_seen; ++j)
+    for (int j = full > 1 ? (full - 1) * BN : 0; j < any_seen; ++j)
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
