@@ -141,9 +141,14 @@ __global__ __launch_bounds__(NW * 64, 2) void ftprompt_main(const Args a) {
   const uint32_t klane = (uint32_t)n * (2 * D) + (uint32_t)(h ^ (D == 128 ? n & 15 : n >> 1 & 7)) * 16;
   const int rr = (lane & 15) >> 2;
   const uint32_t vlane = (uint32_t)(4 * h + rr) * (2 * D) + (uint32_t)((lane >> 4 & 1) * 32 + (lane & 3) * 8) + (uint32_t)(D == 128 ? rr : rr >> 1) * 64;
-  auto key = [&](uint32_t k_at, int i) { return *(__attribute__((address_space(3))) uint4v*)(uintptr_t)(k_at + (klane ^ (32u * i))); };
+  uint32_t kplace[D / 16], vplace[NF];
+#pragma unroll
+  for (int i = 0; i < D / 16; ++i) kplace[i] = lds0 + (klane ^ (32u * i));
+#pragma unroll
+  for (int f = 0; f < NF; ++f) vplace[f] = lds0 + (vlane ^ (64u * f));
+  auto key = [&](uint32_t k_at, int i) { return *(__attribute__((address_space(3))) uint4v*)(uintptr_t)(kplace[i] + k_at); };
   auto value = [&](uint32_t v_at, int i, int f) {      // V^T: elements 32f + lane % 32, keys 16i + 4h + 0..3 and 8 on
-    const uint32_t at = v_at + (vlane ^ (64u * f)) + (uint32_t)i * (32 * D);
+    const uint32_t at = vplace[f] + v_at + (uint32_t)i * (32 * D);
     const uint2v x = __builtin_bit_cast(uint2v, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)(uintptr_t)at));
     const uint2v y = __builtin_bit_cast(uint2v, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)(uintptr_t)(at + 16 * D)));
     return uint4v{x[0], x[1], y[0], y[1]};
@@ -242,7 +247,7 @@ __global__ __launch_bounds__(NW * 64, 2) void ftprompt_main(const Args a) {
     const uint32_t next = lds0 + ((t + 1) & 1) * (2 * TILE);
     if (t + 1 < tiles) issue_v(t + 1, next + TILE);
     if (t + 2 < tiles) issue_k(t + 2, next);
-    return lds0 + (t & 1) * (2 * TILE);
+    return (uint32_t)(t & 1) * (2 * TILE);      // (from the beginning of LDS)
   };
   float16v s[2];
   if (tiles > 0) {
@@ -252,7 +257,7 @@ __global__ __launch_bounds__(NW * 64, 2) void ftprompt_main(const Args a) {
     __builtin_amdgcn_s_waitcnt(0x0F70);
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    scores(lds0 + 2 * TILE, s);
+    scores(2 * TILE, s);
     if (full < 1) mask(0, s);
     const float m[RB] = {largest(s)};
     renew(m);
@@ -269,17 +274,18 @@ __global__ __launch_bounds__(NW * 64, 2) void ftprompt_main(const Args a) {
     s[0] = then[0];
     s[1] = then[1];
 #ifdef SGB
+    __builtin_amdgcn_sched_group_barrier(0x100, PRE, 0);
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
       __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
       __builtin_amdgcn_sched_group_barrier(0x2, SGB, 0);
     }
 #pragma unroll
     for (int i = 0; i < 24; ++i) {
-      __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
       __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(0x2, 2, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+      __builtin_amdgcn_sched_group_barrier(0x2, 1, 0);
     }
 #endif
     renew(m);
