@@ -204,15 +204,17 @@ __global__ __launch_bounds__(NW * 64, 2) void ftprompt_main(const Args a) {
       }
     }
   };
+  auto weight_pair = [&](const float16v (&x)[2], int v, uint4v (&p)[4]) __attribute__((always_inline)) {
+    p[v >> 3][(v & 7) >> 1] = pack2<BF>(ex2(__builtin_fmaf(x[v >> 4][v & 15], a.scale_log2, -ref[0])), ex2(__builtin_fmaf(x[v >> 4][(v & 15) + 1], a.scale_log2, -ref[0])));
+  };
+  auto add_up = [&](const uint4v (&p)[4], int i) __attribute__((always_inline)) {        // the i-th four weights
+    sums[0] = add4<BF>(i & 1 ? uint2v{p[i >> 1][2], p[i >> 1][3]} : uint2v{p[i >> 1][0], p[i >> 1][1]}, sums[0]);
+  };
   auto weights = [&](const float16v (&x)[2], uint4v (&p)[4]) __attribute__((always_inline)) {
 #pragma unroll
-    for (int v = 0; v < 32; v += 2)
-      p[v >> 3][(v & 7) >> 1] = pack2<BF>(ex2(__builtin_fmaf(x[v >> 4][v & 15], a.scale_log2, -ref[0])), ex2(__builtin_fmaf(x[v >> 4][(v & 15) + 1], a.scale_log2, -ref[0])));
+    for (int v = 0; v < 32; v += 2) weight_pair(x, v, p);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      sums[0] = add4<BF>(uint2v{p[i][0], p[i][1]}, sums[0]);
-      sums[0] = add4<BF>(uint2v{p[i][2], p[i][3]}, sums[0]);
-    }
+    for (int i = 0; i < 8; ++i) add_up(p, i);
   };
   // clean: values that are not finite count as 0, and are found
   short2v finite = {-1, -1};
@@ -265,29 +267,38 @@ __global__ __launch_bounds__(NW * 64, 2) void ftprompt_main(const Args a) {
   int t = 0;
   for (; t + 1 < full; ++t) {              // this tile and the next one are seen whole by every row of the wave
     const uint32_t at = arrive(t);
+    // Written out in the order that it runs in: every matrix instruction with the operand that was requested AHEAD instructions before, the request of
+    // another, and the vector instructions that fit beside it.
+    constexpr int NK = D / 8, NV = 4 * NF, N = NK + NV, AHEAD = 4, PER = 32 / NK, MAXIMA = 16 / NV;
+    auto operand = [&](int x) __attribute__((always_inline)) { return x < NK ? key(at + (x & 1) * (64 * D), x >> 1) : value(at + TILE, (x - NK) / NF, (x - NK) % NF); };
+    uint4v ring[AHEAD], p[4];
     float16v then[2];
-    uint4v p[4];
-    scores(at, then);
-    weights(s, p);
-    products(at + TILE, p, std::false_type{});
-    const float m[RB] = {largest(then)};
+    float m[RB];
+#pragma unroll
+    for (int x = 0; x < AHEAD; ++x) ring[x] = operand(x);
+#pragma unroll
+    for (int x = 0; x < N; ++x) {
+      const uint4v mine = ring[x % AHEAD];
+      if (x < NK) then[x & 1] = mfma32<BF>(mine, qf[0][x >> 1], x < 2 ? (float16v)0.f : then[x & 1]);
+      else o[0][(x - NK) % NF] = mfma32<BF>(mine, p[(x - NK) / NF], o[0][(x - NK) % NF]);
+      if (x + AHEAD < N) ring[x % AHEAD] = operand(x + AHEAD);
+      if (x < NK) {
+#pragma unroll
+        for (int v = x * PER; v < (x + 1) * PER; v += 2) weight_pair(s, v, p);
+      } else {
+        constexpr int SUMS = 8 * 2 / NV;
+        const int y = x - NK;
+        if ((y & 1) == 0)
+#pragma unroll
+          for (int i = y / 2 * SUMS; i < (y / 2 + 1) * SUMS; ++i) add_up(p, i);
+#pragma unroll
+        for (int v = y * MAXIMA; v < (y + 1) * MAXIMA; ++v) m[0] = v == 0 ? __builtin_fmaxf(then[0][0], then[1][0]) : __builtin_fmaxf(__builtin_fmaxf(m[0], then[0][v]), then[1][v]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    m[0] = max32(m[0]) * a.scale_log2;
     s[0] = then[0];
     s[1] = then[1];
-#ifdef SGB
-    __builtin_amdgcn_sched_group_barrier(0x100, PRE, 0);
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(0x2, SGB, 0);
-    }
-#pragma unroll
-    for (int i = 0; i < 24; ++i) {
-      __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-      __builtin_amdgcn_sched_group_barrier(0x2, 1, 0);
-    }
-#endif
     renew(m);
   }
 #pragma unroll 1
