@@ -5,12 +5,13 @@ It raises if the library has not been built -- there is no fallback.
 from __future__ import annotations
 
 import ctypes as C
+import struct
 from typing import Optional
 
 import numpy as np
 
 from . import ftattn as _base
-from .ftprompt import ints, rows
+from .ftprompt import ints, load_library as _load_prompt, rows
 
 F16, BF16, F32 = 0, 1, 2
 OK, EINVAL, EUNSUPPORTED, EHIP, ENOMEM = 0, -1, -2, -3, -4
@@ -26,16 +27,12 @@ class Config(C.Structure):
                 ("device", C.c_int32)]
 
 
-class Places(C.Structure):
-    _fields_ = [("batch", C.c_int32), ("tokens", C.c_int32), ("cu_seqlens", C.c_void_p), ("starts", C.c_void_p),
-                ("page_table", C.c_void_p), ("table_width", C.c_int32), ("table_stride", C.c_int64)]
-
-
 class ReportView(C.Structure):
     _fields_ = [("refused_tokens", C.c_int64), ("refused_sequences", C.c_int64)]
 
 
 _typed = False
+_types = {}
 
 
 class FtCacheError(RuntimeError):
@@ -47,14 +44,16 @@ class FtCacheError(RuntimeError):
 def load_library() -> C.CDLL:
     """The shared library with the ftcache_* prototypes set; raises if it is not built."""
     global _typed
-    lib = _base.load_library()
+    lib = _load_prompt()          # (which knows torch's types)
     if not _typed:
+        import torch
+        _types.update(uint8=torch.uint8, int32=torch.int32, float32=torch.float32)
         p = C.c_void_p
         lib.ftcache_create.argtypes = [C.POINTER(Config), C.POINTER(p)]
         lib.ftcache_get_config.argtypes = [p, C.POINTER(Config)]
         lib.ftcache_page_bytes.argtypes = [p]
-        lib.ftcache_append.argtypes = [p, p, C.POINTER(Places), p, C.c_int32, p, p, p, p, p, p]
-        lib.ftcache_read.argtypes = [p, p, C.POINTER(Places), p, p, p]
+        lib.ftcache_append.argtypes = [p, p, p, p, C.c_int32, p, p, p, p, p, p]
+        lib.ftcache_read.argtypes = [p, p, p, p, p, p]
         lib.ftcache_attend.argtypes = [p, p, C.c_int32, p, p, C.c_int32, C.c_int64, p, p, p]
         lib.ftcache_report.argtypes = [p, C.POINTER(ReportView)]
         lib.ftcache_destroy.argtypes = [p]
@@ -75,8 +74,8 @@ def rotation_table(positions: int, rotary_dim: int, base: float = 10000.0) -> np
     return np.concatenate([np.cos(angle), np.sin(angle)], axis=1).astype(np.float32)
 
 
-_Rows2, _Rows5 = C.c_int64 * 6, C.c_int64 * 15
-_NONE = (0, 0, 0)
+_PLACES = struct.Struct("@iiPPPiq")          # ftcache_places
+_NONE = bytes(24)                            # ftcache_rows without a tensor
 
 
 class FtCache:
@@ -102,7 +101,8 @@ class FtCache:
         self.page_bytes = self.lib.ftcache_page_bytes(self.handle)
         self._q = (e.heads, e.head_dim, e.in_dtype, e.device)
         self._kv = (e.kv_heads, e.head_dim, e.in_dtype, e.device)
-        self._device = e.device
+        self._device, self._bytes, self._rotary = e.device, e.pages * self.page_bytes, e.rotary_dim
+        self._o = (e.heads, e.head_dim, e.out_dtype, e.device, True)
 
     def _check(self, rc: int) -> None:
         if rc != OK:
@@ -111,31 +111,31 @@ class FtCache:
     def _pool(self, pool) -> int:
         if not hasattr(pool, "data_ptr"):
             raise TypeError(f"pool: expected a device tensor, got {type(pool).__name__}")
-        if str(pool.dtype) != "torch.uint8" or not pool.is_contiguous() or pool.numel() != self.config.pages * self.page_bytes:
-            raise ValueError(f"pool: expected {self.config.pages * self.page_bytes} contiguous elements of torch.uint8, got {pool.numel()} of {pool.dtype}")
-        if not pool.is_cuda or pool.get_device() != self._device:
+        if pool.dtype is not _types["uint8"] or not pool.is_contiguous() or pool.numel() != self._bytes:
+            raise ValueError(f"pool: expected {self._bytes} contiguous elements of torch.uint8, got {pool.numel()} of {pool.dtype}")
+        if pool.get_device() != self._device:
             raise ValueError(f"pool: tensor is not on device {self._device}")
         return pool.data_ptr()
 
     def _table(self, table, batch: int):
         if not hasattr(table, "data_ptr"):
             raise TypeError(f"page_table: expected a device tensor, got {type(table).__name__}")
-        if str(table.dtype) != "torch.int32" or table.dim() != 2 or table.shape[0] != batch or table.shape[1] < 1:
+        if table.dtype is not _types["int32"] or table.dim() != 2 or table.shape[0] != batch or table.shape[1] < 1:
             raise ValueError(f"page_table: tensor is {tuple(table.shape)} of {table.dtype}, expected [{batch}, width] of torch.int32")
-        if not table.is_cuda or table.get_device() != self._device:
+        if table.get_device() != self._device:
             raise ValueError(f"page_table: tensor is not on device {self._device}")
         width, stride = table.shape[1], table.stride()
         if (width > 1 and stride[1] != 1) or (batch > 1 and stride[0] < width):
             raise ValueError("page_table: the entries of a sequence do not lie side by side")
         return table.data_ptr(), width, stride[0] if batch > 1 else width
 
-    def _places(self, cu_seqlens, starts, page_table, tokens: int) -> Places:
+    def _places(self, cu_seqlens, starts, page_table, tokens: int) -> bytes:
         batch = cu_seqlens.numel() - 1
         if batch < 1:
             raise ValueError("cu_seqlens: expected at least two bounds")
         at, width, stride = self._table(page_table, batch)
-        return Places(batch, tokens, ints(cu_seqlens, "cu_seqlens", batch + 1, self._device), ints(starts, "starts", batch, self._device),
-                      at, width, stride)
+        return _PLACES.pack(batch, tokens, ints(cu_seqlens, "cu_seqlens", batch + 1, self._device), ints(starts, "starts", batch, self._device),
+                            at, width, stride)
 
     def append(self, pool, q, k, v, rotation, cu_seqlens, starts, page_table, q_out, k_out, stream: int = 0) -> None:
         """Rotates the packed tokens' q and k into q_out and k_out, and puts keys and values into their pages.
@@ -144,35 +144,32 @@ class FtCache:
         tokens = k.shape[0]
         if (q is None) != (q_out is None):
             raise ValueError("q and q_out go together")
-        e = self.config
         if not hasattr(rotation, "data_ptr"):
             raise TypeError(f"rotation: expected a device tensor, got {type(rotation).__name__}")
-        if str(rotation.dtype) != "torch.float32" or rotation.dim() != 2 or rotation.shape[1] != e.rotary_dim or not rotation.is_contiguous():
-            raise ValueError(f"rotation: tensor is {tuple(rotation.shape)} of {rotation.dtype}, expected contiguous [positions, {e.rotary_dim}] of torch.float32")
-        if not rotation.is_cuda or rotation.get_device() != self._device:
+        if rotation.dtype is not _types["float32"] or rotation.dim() != 2 or rotation.shape[1] != self._rotary or not rotation.is_contiguous():
+            raise ValueError(f"rotation: tensor is {tuple(rotation.shape)} of {rotation.dtype}, expected contiguous [positions, {self._rotary}] of torch.float32")
+        if rotation.get_device() != self._device:
             raise ValueError(f"rotation: tensor is not on device {self._device}")
         places = self._places(cu_seqlens, starts, page_table, tokens)
-        r = _Rows5(*(_NONE if q is None else rows(q, "q", tokens, *self._q)), *rows(k, "k", tokens, *self._kv), *rows(v, "v", tokens, *self._kv),
-                   *(_NONE if q_out is None else rows(q_out, "q_out", tokens, *self._q, True)),
-                   *(_NONE if k_out is None else rows(k_out, "k_out", tokens, *self._kv, True)))
-        self._check(self.lib.ftcache_append(self.handle, self._pool(pool), C.byref(places), rotation.data_ptr(), rotation.shape[0], C.byref(r),
-                                            C.byref(r, 24), C.byref(r, 48), C.byref(r, 72), C.byref(r, 96), stream))
+        self._check(self.lib.ftcache_append(
+            self.handle, self._pool(pool), places, rotation.data_ptr(), rotation.shape[0],
+            _NONE if q is None else rows(q, "q", tokens, *self._q), rows(k, "k", tokens, *self._kv), rows(v, "v", tokens, *self._kv),
+            _NONE if q_out is None else rows(q_out, "q_out", tokens, *self._q, True),
+            _NONE if k_out is None else rows(k_out, "k_out", tokens, *self._kv, True), stream))
 
     def read(self, pool, k, v, cu_seqlens, starts, page_table, stream: int = 0) -> None:
         """The cached keys and values of the given places into k and v, [tokens, kv_heads, head_dim]."""
         tokens = k.shape[0]
         places = self._places(cu_seqlens, starts, page_table, tokens)
-        r = _Rows2(*rows(k, "k", tokens, *self._kv, True), *rows(v, "v", tokens, *self._kv, True))
-        self._check(self.lib.ftcache_read(self.handle, self._pool(pool), C.byref(places), C.byref(r), C.byref(r, 24), stream))
+        self._check(self.lib.ftcache_read(self.handle, self._pool(pool), places, rows(k, "k", tokens, *self._kv, True),
+                                          rows(v, "v", tokens, *self._kv, True), stream))
 
     def attend(self, pool, q, o, lengths, page_table, stream: int = 0) -> None:
         """Attention of one token per sequence, q and o [batch, heads, head_dim], over the first lengths[b] cached tokens."""
         batch = q.shape[0]
         at, width, stride = self._table(page_table, batch)
-        e = self.config
-        r = _Rows2(*rows(q, "q", batch, *self._q), *rows(o, "o", batch, e.heads, e.head_dim, e.out_dtype, e.device, True))
         self._check(self.lib.ftcache_attend(self.handle, self._pool(pool), batch, ints(lengths, "lengths", batch, self._device), at, width,
-                                            stride, C.byref(r), C.byref(r, 24), stream))
+                                            stride, rows(q, "q", batch, *self._q), rows(o, "o", batch, *self._o), stream))
 
     def report(self):
         """(refused tokens, refused sequences) since the last report; waits for the device."""
