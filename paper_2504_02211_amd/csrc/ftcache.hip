@@ -107,55 +107,68 @@ template <int N> __device__ __forceinline__ void store(char* p, const Elements<N
   for (int i = 0; i < N / 8; ++i) *reinterpret_cast<uint4v*>(p + 16 * i) = uint4v{x.w[4 * i], x.w[4 * i + 1], x.w[4 * i + 2], x.w[4 * i + 3]};
 }
 
-// The rotation of a lane's elements e0 .. e0 + N of a token, in chunks of 8: cosines and sines, which are the same for every head.
-template <int N> struct Turn {
-  float c[N], s[N];      // (interleaved: the first half of each chunk only)
-  int part[N / 8];       // 0: the chunk is not rotated, 1: its elements come first in their pairs, 2: second, 3: pairs side by side
+// The rotation of a lane's elements e0 .. e0 + N of a token, in chunks of 8: cosines and sines, which are the same for every head.  Halves: an element
+// and its partner rotary/2 away, sines with the sign that the element's product with its partner has.  Pairs: elements side by side, four of each in a chunk.
+template <int N, bool PAIRS> struct Turn {
+  static constexpr int PER = PAIRS ? 4 : 8;
+  float c[N / 8 * PER], s[N / 8 * PER];
+  int partner[N / 8];      // bytes from the chunk to its partners
+  bool turned[N / 8];
 };
-template <int N> __device__ __forceinline__ void turn_of(Turn<N>& t, const float* row, int e0, int rotary, bool interleaved) {
+template <int N, bool PAIRS> __device__ __forceinline__ void turn_of(Turn<N, PAIRS>& t, const float* row, int e0, int rotary) {
   const int half = rotary / 2;
+  constexpr int PER = Turn<N, PAIRS>::PER;
 #pragma unroll
   for (int i = 0; i < N / 8; ++i) {
     const int e = e0 + 8 * i;
-    t.part[i] = e >= rotary ? 0 : interleaved ? 3 : e < half ? 1 : 2;
-    const int at = e >= rotary ? 0 : interleaved ? e / 2 : e < half ? e : e - half;
+    const bool first = e < half;
+    t.turned[i] = e < rotary;
+    t.partner[i] = PAIRS || !t.turned[i] ? 0 : first ? 2 * half : -2 * half;
+    const int at = !t.turned[i] ? 0 : PAIRS ? e / 2 : first ? e : e - half;
 #pragma unroll
-    for (int j = 0; j < 8; j += 4) {
-      const bool used = !interleaved || j == 0;
-      const float4v c = used ? *reinterpret_cast<const float4v*>(row + at + j) : (float4v)0.f, s = used ? *reinterpret_cast<const float4v*>(row + half + at + j) : (float4v)0.f;
+    for (int j = 0; j < PER; j += 4) {
+      const float4v c = *reinterpret_cast<const float4v*>(row + at + j), s = *reinterpret_cast<const float4v*>(row + half + at + j);
 #pragma unroll
-      for (int x = 0; x < 4; ++x) { t.c[8 * i + j + x] = c[x]; t.s[8 * i + j + x] = s[x]; }
+      for (int x = 0; x < 4; ++x) { t.c[PER * i + j + x] = c[x]; t.s[PER * i + j + x] = !PAIRS && first ? -s[x] : s[x]; }
     }
   }
 }
 
-// x rotated and rounded; p: the row's address at element 0, for the partners (every lane of a token has read them before any stores)
-template <int N, bool BF> __device__ __forceinline__ Elements<N> rotated(const Elements<N>& x, const Turn<N>& t, const char* row, int e0, int rotary) {
+// What a rotation reads: the lane's elements, and their partners (every lane of a token has read them before any stores).
+template <int N, bool PAIRS> struct Loaded2 {
+  Elements<N> x, partners;
+};
+template <int N, bool PAIRS> __device__ __forceinline__ Loaded2<N, PAIRS> load(const char* p, const Turn<N, PAIRS>& t) {
+  Loaded2<N, PAIRS> y;
+  y.x = load<N>(p);
+  if constexpr (!PAIRS) {
+#pragma unroll
+    for (int i = 0; i < N / 8; ++i) {
+      const uint4v z = *reinterpret_cast<const uint4v*>(p + 16 * i + t.partner[i]);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) y.partners.w[4 * i + j] = z[j];
+    }
+  }
+  return y;
+}
+template <int N, bool BF, bool PAIRS> __device__ __forceinline__ Elements<N> rotated(const Loaded2<N, PAIRS>& in, const Turn<N, PAIRS>& t) {
 #pragma clang fp contract(off)
   Elements<N> y;
-  const int half = rotary / 2;
 #pragma unroll
-  for (int i = 0; i < N / 8; ++i) {
-    const int part = t.part[i], other = part == 1 ? half : part == 2 ? -half : 0;
-    const uint4v z = *reinterpret_cast<const uint4v*>(row + 2 * (e0 + 8 * i + other));
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const uint32_t w = x.w[4 * i + j];
-      const float a = low_of<BF>(w), b = high_of<BF>(w);
-      float u, v;
-      if (part == 3) {
-        const float c = t.c[8 * i + j], s = t.s[8 * i + j];
-        u = a * c - b * s;
-        v = b * c + a * s;
-      } else {
-        const float pa = low_of<BF>(z[j]), pb = high_of<BF>(z[j]), c0 = t.c[8 * i + 2 * j], c1 = t.c[8 * i + 2 * j + 1];
-        const float s0 = t.s[8 * i + 2 * j], s1 = t.s[8 * i + 2 * j + 1];
-        const float m0 = pa * s0, m1 = pb * s1, n0 = a * c0, n1 = b * c1;
-        u = part == 1 ? n0 - m0 : n0 + m0;
-        v = part == 1 ? n1 - m1 : n1 + m1;
-      }
-      y.w[4 * i + j] = part == 0 ? w : pack2<BF>(u, v);
+  for (int i = 0; i < N / 2; ++i) {
+    const uint32_t w = in.x.w[i];
+    const float a = low_of<BF>(w), b = high_of<BF>(w);
+    float u, v;
+    if constexpr (PAIRS) {
+      const float c = t.c[i], s = t.s[i];
+      u = a * c - b * s;
+      v = b * c + a * s;
+    } else {
+      const uint32_t z = in.partners.w[i];
+      u = a * t.c[2 * i] + low_of<BF>(z) * t.s[2 * i];
+      v = b * t.c[2 * i + 1] + high_of<BF>(z) * t.s[2 * i + 1];
     }
+    y.w[i] = t.turned[i / 4] ? pack2<BF>(u, v) : w;
   }
   return y;
 }
@@ -195,74 +208,80 @@ template <int N, bool BF> __device__ __forceinline__ Codes<N> coded(const Elemen
   return r;
 }
 
-// A wave takes 8 places of a sequence and one head at a time: lane 8t + c has elements c * D/8 .. of token t.
-template <int D, bool BF>
-__global__ __launch_bounds__(256) void ftcache_put(const Args a, const bool interleaved) {
+// A wave takes 8 places of a sequence, two query heads, or the key and value of a head, at a time: lane 8t + c has elements c * D/8 .. of token t.
+// Bound by memory: 20,278 tokens of 32 + 8 heads of 128 in 101 us, 484 MB at 4.8 TB/s; with one head at a time and its partners' sign by
+// branches it took 147.
+template <int D, bool BF, bool PAIRS>
+__global__ __launch_bounds__(256) void ftcache_put(const Args a) {
   constexpr int N = D / 8;
   __shared__ uint16_t turned[4][D / 4][8];            // value codes of 8 tokens, to be written 16 bytes at a time
   Block x;
   if (!block_of(a.at, a.pool, blockIdx.x, x)) return;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, t = lane >> 3, c = lane & 7, e0 = c * N;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), t = lane >> 3, c = lane & 7, e0 = c * N;
   const bool known = x.place < a.positions, kept = x.real && known && x.page;
   if (blockIdx.y == 0 && wave == 0) {
     const uint64_t refused = __ballot(x.real && !kept && c == 0);
     if (refused && lane == 0) atomicAdd(a.refused, (unsigned long long)__popcll(refused));
   }
   const bool whole = x.whole && __all(kept);
-  Turn<N> turn;
-  turn_of<N>(turn, a.rotation + (int64_t)(known ? x.place : 0) * a.rotary, e0, a.rotary, interleaved);
-  const int first = a.q.data ? 0 : a.heads, kv = a.pool.kv_heads, items = a.heads + 2 * kv;
-  const int in_page = x.place & ((1 << a.pool.page_shift) - 1);
-  for (int item = first + blockIdx.y * 4 + wave; item < items; item += gridDim.y * 4) {
-    const bool is_q = item < a.heads, is_v = item >= a.heads + kv;
-    const int head = is_q ? item : is_v ? item - a.heads - kv : item - a.heads;
-    const Rows& in = is_q ? a.q : is_v ? a.v : a.k;
-    Elements<N> y;
-    if (x.real) {
-      const char* row = in.data + (int64_t)x.row * in.token + (int64_t)head * in.head;
-      y = load<N>(row + 2 * e0);
-      if (!is_v) {
-        y = rotated<N, BF>(y, turn, row, e0, a.rotary);
-        if (!known)
+  Turn<N, PAIRS> turn;
+  turn_of<N, PAIRS>(turn, a.rotation + (int64_t)(known ? x.place : 0) * a.rotary, e0, a.rotary);
+  const int kv = a.pool.kv_heads, step = gridDim.y * 4;
+  // heads of keys and values first: they take longer
+  const int64_t row = x.real ? x.row : 0;
+  auto finish = [&](Elements<N> y, char* out, bool store_it) __attribute__((always_inline)) {
+    if (!known)
 #pragma unroll
-          for (int i = 0; i < N / 2; ++i) y.w[i] = 0x7FFF7FFFu;
-        const Rows& out = is_q ? a.q_out : a.k_out;
-        if (out.data) store<N>(out.data + (int64_t)x.row * out.token + (int64_t)head * out.head + 2 * e0, y);
+      for (int i = 0; i < N / 2; ++i) y.w[i] = 0x7FFF7FFFu;
+    if (store_it && x.real) store<N>(out, y);
+    return y;
+  };
+  const int ps = 1 << a.pool.page_shift, in_page = x.place & (ps - 1);
+  const char* const krow = a.k.data + row * a.k.token + 2 * e0;
+  const char* const vrow = a.v.data + row * a.v.token + 2 * e0;
+  char* const kout = a.k_out.data + row * a.k_out.token + 2 * e0;
+  int item = blockIdx.y * 4 + wave;
+  for (; item < kv; item += step) {
+    // (a lane without a token reads the first row: a call has one)
+    const Loaded2<N, PAIRS> in = load<N, PAIRS>(krow + item * a.k.head, turn);
+    const Elements<N> v = load<N>(vrow + item * a.v.head);
+    const Elements<N> k = finish(rotated<N, BF, PAIRS>(in, turn), kout + item * a.k_out.head, a.k_out.data != nullptr);
+    const Codes<N> zk = coded<N, BF>(k), zv = coded<N, BF>(v);
+    char* const page = x.page + (int64_t)item * a.pool.head_bytes;      // (used where kept only)
+    if (kept) {
+      if (c == 0) {
+        uint16_t* par = reinterpret_cast<uint16_t*>(page + ps * D) + (in_page >> 3) * 32 + t;
+        par[0] = (uint16_t)zk.params;
+        par[8] = (uint16_t)(zk.params >> 16);
+        par[16] = (uint16_t)zv.params;
+        par[24] = (uint16_t)(zv.params >> 16);
       }
+      if constexpr (N == 16) *reinterpret_cast<uint2v*>(page + in_page * (D / 2) + e0 / 2) = uint2v{zk.w[0], zk.w[1]};
+      else *reinterpret_cast<uint32_t*>(page + in_page * (D / 2) + e0 / 2) = zk.w[0];
     }
-    if (is_q) continue;
-    if (!x.real)
+    char* const block = page + ps * (D / 2) + (in_page >> 3) * (4 * D);
+    if (whole) {
 #pragma unroll
-      for (int i = 0; i < N / 2; ++i) y.w[i] = 0;
-    const Codes<N> z = coded<N, BF>(y);
-    char* const page = x.page + (int64_t)head * a.pool.head_bytes;      // (used where kept only)
-    const int ps = 1 << a.pool.page_shift;
-    if (kept && c == 0) {
-      uint16_t* par = reinterpret_cast<uint16_t*>(page + ps * D) + (in_page >> 3) * 32 + (is_v ? 16 : 0) + t;
-      par[0] = (uint16_t)z.params;
-      par[8] = (uint16_t)(z.params >> 16);
+      for (int i = 0; i < N / 4; ++i) turned[wave][c * (N / 4) + i][t] = (uint16_t)(zv.w[i / 2] >> (16 * (i & 1)));
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      if (lane < D / 4) *reinterpret_cast<uint4v*>(block + lane * 16) = *reinterpret_cast<const uint4v*>(turned[wave][lane]);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+    } else if (kept) {
+#pragma unroll
+      for (int i = 0; i < N / 4; ++i)
+        *reinterpret_cast<uint16_t*>(block + (c * (N / 4) + i) * 16 + t * 2) = (uint16_t)(zv.w[i / 2] >> (16 * (i & 1)));
     }
-    if (!is_v) {
-      if (kept) {
-        if constexpr (N == 16) *reinterpret_cast<uint2v*>(page + in_page * (D / 2) + e0 / 2) = uint2v{z.w[0], z.w[1]};
-        else *reinterpret_cast<uint32_t*>(page + in_page * (D / 2) + e0 / 2) = z.w[0];
-      }
-    } else {
-      char* const block = page + ps * (D / 2) + (in_page >> 3) * (4 * D);
-      if (whole) {
-#pragma unroll
-        for (int i = 0; i < N / 4; ++i) turned[wave][c * (N / 4) + i][t] = (uint16_t)(z.w[i / 2] >> (16 * (i & 1)));
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        if (lane < D / 4) *reinterpret_cast<uint4v*>(block + lane * 16) = *reinterpret_cast<const uint4v*>(turned[wave][lane]);
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-      } else if (kept) {
-#pragma unroll
-        for (int i = 0; i < N / 4; ++i)
-          *reinterpret_cast<uint16_t*>(block + (c * (N / 4) + i) * 16 + t * 2) = (uint16_t)(z.w[i / 2] >> (16 * (i & 1)));
-      }
-    }
+  }
+  if (!a.q.data) return;
+  const char* const qrow = a.q.data + row * a.q.token + 2 * e0;
+  char* const qout = a.q_out.data + row * a.q_out.token + 2 * e0;
+  for (item -= kv; item < a.heads; item += 2 * step) {
+    const int64_t other = item + step < a.heads ? item + step : item;
+    const Loaded2<N, PAIRS> in = load<N, PAIRS>(qrow + item * a.q.head, turn), in2 = load<N, PAIRS>(qrow + other * a.q.head, turn);
+    finish(rotated<N, BF, PAIRS>(in, turn), qout + item * a.q_out.head, true);
+    if (other != item) finish(rotated<N, BF, PAIRS>(in2, turn), qout + other * a.q_out.head, true);
   }
 }
 
@@ -770,9 +789,12 @@ __global__ __launch_bounds__(ONE_WAVES * 64, 3) void ftcache_one(const OneArgs a
   }
 }
 
-typedef void (*put_fn)(const Args, const bool);
+typedef void (*put_fn)(const Args);
 typedef void (*get_fn)(const Args);
 typedef void (*one_fn)(const OneArgs);
+template <int D> static put_fn put_of(bool bf, bool pairs) {
+  return bf ? (pairs ? ftcache_put<D, true, true> : ftcache_put<D, true, false>) : (pairs ? ftcache_put<D, false, true> : ftcache_put<D, false, false>);
+}
 template <int D, bool BF> static one_fn one_of(bool f32) { return f32 ? ftcache_one<D, BF, true> : ftcache_one<D, BF, false>; }
 
 }  // namespace ftcache
@@ -866,11 +888,11 @@ extern "C" int ftcache_create(const ftcache_config* cfg, ftcache_ctx** out) {
   c->row_tiles = (e.heads / e.kv_heads + 15) / 16;
   const bool bf = e.in_dtype == FTCACHE_BF16, f32 = e.out_dtype == FTCACHE_F32;
   if (e.head_dim == 128) {
-    c->put = bf ? ftcache_put<128, true> : ftcache_put<128, false>;
+    c->put = put_of<128>(bf, e.interleaved != 0);
     c->get = bf ? ftcache_get<128, true> : ftcache_get<128, false>;
     c->one = bf ? one_of<128, true>(f32) : one_of<128, false>(f32);
   } else {
-    c->put = bf ? ftcache_put<64, true> : ftcache_put<64, false>;
+    c->put = put_of<64>(bf, e.interleaved != 0);
     c->get = bf ? ftcache_get<64, true> : ftcache_get<64, false>;
     c->one = bf ? one_of<64, true>(f32) : one_of<64, false>(f32);
   }
@@ -935,13 +957,13 @@ extern "C" int ftcache_append(ftcache_ctx* c, void* pool, const ftcache_places* 
   a.heads = e.heads;
   a.rotary = e.rotary_dim;
   a.refused = c->refused;
-  const int blocks = a.at.tokens / 8 + 2 * a.at.batch, items = (a.q.data ? e.heads : 0) + 2 * e.kv_heads;
+  const int blocks = a.at.tokens / 8 + 2 * a.at.batch, items = (a.q.data ? e.heads : 0) + e.kv_heads;
   // few blocks: their heads are dealt to more workgroups
   int split = (4 * CUS + blocks - 1) / blocks;
   split = split < 1 ? 1 : split > (items + 3) / 4 ? (items + 3) / 4 : split;
   OnDevice here(e.device);
   if (here.status != hipSuccess) return cfail_hip(c, "device", here.status);
-  hipLaunchKernelGGL(c->put, dim3(blocks, split), dim3(256), 0, (hipStream_t)hip_stream, a, e.interleaved != 0);
+  hipLaunchKernelGGL(c->put, dim3(blocks, split), dim3(256), 0, (hipStream_t)hip_stream, a);
   const hipError_t he = hipGetLastError();
   return he == hipSuccess ? FTCACHE_OK : cfail_hip(c, "launch", he);
 }
