@@ -20,17 +20,23 @@
 namespace ftprompt {
 using namespace ftserve;
 
-constexpr int BN = 64, SUB = 64, NW = 4, STAGES = 2;      // keys of a tile, of a step; waves; tiles in LDS
-constexpr int64_t WIDE_FROM = 2 * 256 * 256;
-constexpr int bm_of(int rb) { return NW * 32 * rb; }      // rows of a workgroup whose waves have rb blocks of 32
+constexpr int BM = 128, BN = 64, NW = 4, STAGES = 2;      // rows of a workgroup, keys of a tile; waves; stages in LDS
+// Long row tiles are divided by their keys where there are too few of them to keep the chip busy to the end: into shares of equal length, about `piece` key tiles
+// long, so that a call has about SHARES workgroups of as much to do.  A share costs its state through memory beside its keys, together about the time of ten
+// tiles: pieces have LEAST tiles, or FEW where row tiles leave half of the CUs idle, and a row tile a third longer than a piece stays whole.  Measured (us; whole,
+// divided): 3 x 20 queries over 8000 keys, 32 heads on 8: 135, 38; 6 chunks of up to 509 over 3000, 16 on 4: 70, 55; 1 x 4000, 8 on 2: 79, 58;
+// 2 x 9090, 5 on 1, of 64: 120, 99.  With pieces of 10: 1 x 2000, 32 on 8: 53, 60; 24 of up to 1531, 12, of 64: 29, 36.
+constexpr int SHARES = 512, LEAST = 24, FEW = 12, STATES = 2 * SHARES;
 
 struct Rows { char* data; int64_t token, head; };         // strides in bytes
 
 struct Args {
   Rows q, k, v, o;
   const int32_t *cu_q, *cu_k;
-  int32_t batch, total_q, total_k, kv_heads, group, slots;
+  int32_t batch, total_q, total_k, kv_heads, group;
   float scale_log2;
+  float* ws;               // states of shares, STATES of them
+  uint32_t* done;          // shares of a row tile that are there, by its first state; 0 between calls
 };
 
 template <int D> constexpr int tile_bytes() { return BN * D * 2; }
@@ -62,49 +68,140 @@ __device__ __forceinline__ float sum32(float x) {
   return as_f(r[0]) + as_f(r[1]);
 }
 
+// Sums over the lanes up to this one.
+__device__ __forceinline__ int sum_upto(int x) {
+  auto step = [&](int moved) { x += moved; };
+  step(__builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false));      // row_shr 1, 2, 4, 8
+  step(__builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false));
+  step(__builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false));
+  step(__builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false));
+  step(__builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false));      // row_bcast 15, 31
+  step(__builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false));
+  return x;
+}
+
+// A sequence: its first rows, its queries and keys, its rows and row tiles; row r sees nk - nq + r / G + 1 keys.
+struct Sequence {
+  int q0, k0, nq, nk, rows, tiles;
+  __device__ __forceinline__ int seen_by(int r, int G) const { return nk - nq + (r < rows ? r : rows - 1) / G + 1; }
+  __device__ __forceinline__ int key_tiles(int tile, int G) const {
+    const int keys = seen_by(tile * BM + BM - 1, G);
+    return keys > 0 ? (keys + BN - 1) / BN : 0;
+  }
+  // the first row tile of more than `part` shares (part >= 1), `tiles` if there is none: one that sees more than part * piece key tiles, for a second share a third more
+  __device__ __forceinline__ int first_with(int part, int piece, int G) const {
+    const int64_t more = part == 1 ? piece + piece / 3 : (int64_t)part * piece;
+    const int64_t at = (more * BN - (nk - nq)) * G;      // the first row that sees more
+    return at <= 0 ? 0 : at > rows - 1 ? tiles : (int)(at / BM);
+  }
+};
+__device__ __forceinline__ Sequence sequence(const Args& a, int b) {
+  Sequence s{0, 0, 0, 0, 0, 0};
+  if (b >= a.batch) return s;
+  s.q0 = clamped(a.cu_q[b], a.total_q);
+  s.k0 = clamped(a.cu_k[b], a.total_k);
+  const int q1 = clamped(a.cu_q[b + 1], a.total_q), k1 = clamped(a.cu_k[b + 1], a.total_k);
+  s.nq = q1 > s.q0 ? q1 - s.q0 : 0;
+  s.nk = k1 > s.k0 ? k1 - s.k0 : 0;
+  s.rows = s.nq * a.group;
+  s.tiles = (s.rows + BM - 1) / BM;
+  return s;
+}
+
+// Share `id` of a key / value head: first all row tiles' first shares, longest tiles of a sequence first, then the second shares of those that have one, and
+// so on.  Lane l looks after sequences l * per ..; all waves come to the same result.
+struct Share {
+  Sequence s;
+  int tile, part, parts, slot;      // slot: number of the row tile's first state
+};
+__device__ __forceinline__ bool share_of(const Args& a, int id, Share& x) {
+  const int lane = threadIdx.x & 63, per = (a.batch + 63) / 64, G = a.group;
+  const Sequence mine = sequence(a, lane * per);
+  auto of_lane = [&](int i) { return i == 0 ? mine : sequence(a, lane * per + i); };
+  // key tiles of all row tiles, not too few: they rise by at most one tile's worth of rows from one to the next
+  float work = 0.f;
+  int row_tiles = 0;
+  for (int i = 0; i < per; ++i) {
+    const Sequence s = of_lane(i);
+    row_tiles += s.tiles;
+    if (s.tiles) work += (0.5f * (float)(s.key_tiles(0, G) + s.key_tiles(s.tiles - 1, G)) + 1.f) * (float)s.tiles;
+  }
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) work += __shfl_xor(work, d);
+  const float fair = work * (float)a.kv_heads * (1.001f / SHARES);
+  const int row_tiles_upto = sum_upto(row_tiles), all_tiles = __builtin_amdgcn_readlane(row_tiles_upto, 63);
+  const int least = all_tiles < 128 / a.kv_heads ? FEW : LEAST;
+  const int piece = __builtin_amdgcn_readfirstlane(fair < (float)least ? least : fair > 1e8f ? 100000000 : (int)fair + 1);
+  auto count = [&](const Sequence& s, int part) { return part == 0 ? s.tiles : s.tiles - s.first_with(part, piece, G); };
+  for (int part = 0;; ++part) {
+    int n = row_tiles;
+    if (part) {
+      n = 0;
+      for (int i = 0; i < per; ++i) n += count(of_lane(i), part);
+    }
+    const int upto = part ? sum_upto(n) : row_tiles_upto, all = __builtin_amdgcn_readlane(upto, 63);
+    if (all == 0) return false;
+    if (id >= all) {
+      id -= all;
+      continue;
+    }
+    const int owner = __ffsll((unsigned long long)__ballot(upto > id)) - 1;
+    int left = id - __builtin_amdgcn_readlane(upto - n, owner), b = __builtin_amdgcn_readfirstlane(owner * per);
+    for (;; ++b) {
+      x.s = sequence(a, b);
+      const int c = count(x.s, part);
+      if (left < c || b + 1 >= a.batch) break;
+      left -= c;
+    }
+    x.tile = x.s.tiles - 1 - left;
+    x.part = part;
+    const int length = x.s.key_tiles(x.tile, G);
+    x.parts = length > piece + piece / 3 ? (length + piece - 1) / piece : 1;
+    x.slot = 0;
+    if (x.parts > 1)      // states of the divided row tiles before this one: of each q, the tiles of more than q shares; those of more than 0 are those of more than 1
+      for (int q = 1;; ++q) {
+        int m = 0, before = 0;
+        for (int i = 0; i < per; ++i) {
+          const int c = count(of_lane(i), q);
+          m += c;
+          before += lane * per + i < b ? c : 0;
+        }
+        if (__builtin_amdgcn_readlane(sum_upto(m), 63) == 0) break;
+        const int first = x.s.first_with(q, piece, G), here = x.tile > first ? x.tile - first : 0;
+        x.slot += (q == 1 ? 2 : 1) * (__builtin_amdgcn_readlane(sum_upto(before), 63) + here);
+      }
+    return true;
+  }
+}
+
 typedef __attribute__((address_space(3))) char lds_char;
 
-template <int D, bool BF, bool F32OUT, int RB>
+template <int D, bool BF, bool F32OUT>
 __global__ __launch_bounds__(NW * 64, 2) void ftprompt_main(const Args a) {
   extern __shared__ uint4v lds[];
-  constexpr int BM = bm_of(RB), NF = D / 32, TILE = tile_bytes<D>();
+  constexpr int NF = D / 32, TILE = tile_bytes<D>();
   const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_char*)lds;
-  const int hk = blockIdx.x % a.kv_heads, slot = a.slots - 1 - blockIdx.x / a.kv_heads;
-  const int G = a.group;
-  // sequence b owns the row tiles from cu_q[b] * G / BM + b on: at least as many as it has rows for
-  auto tiles_before = [&](int b) { return (int64_t)clamped(a.cu_q[b], a.total_q) * G / BM + b; };
-  const int b = sequence_of(a.batch, slot, tiles_before);
-  const int tile = slot - (int)tiles_before(b);
-  const int q0 = clamped(a.cu_q[b], a.total_q), q1 = clamped(a.cu_q[b + 1], a.total_q);
-  const int k0 = clamped(a.cu_k[b], a.total_k), k1 = clamped(a.cu_k[b + 1], a.total_k);
-  const int nq = q1 - q0, nk = k1 - k0;
-  if (tile < 0 || nq <= 0 || (int64_t)tile * BM >= (int64_t)nq * G) return;
-  const int rows = nq * G, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5, n = lane & 31;
+  const int hk = blockIdx.x % a.kv_heads, G = a.group;
+  Share x;
+  if (!share_of(a, blockIdx.x / a.kv_heads, x)) return;
+  const int tile = x.tile, q0 = x.s.q0, k0 = x.s.k0, nq = x.s.nq, nk = x.s.nk, rows = x.s.rows;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5, n = lane & 31;
 
   // keys that row r of the sequence sees (may be <= 0); rows behind the last count as it
-  auto seen_by = [&](int r) { return nk - nq + (r < rows ? r : rows - 1) / G + 1; };
-  const int row0 = tile * BM + wave * (32 * RB);
-  const int all_seen = seen_by(row0), any_seen = seen_by(row0 + 32 * RB - 1), keys = seen_by(tile * BM + BM - 1);
-  const int tiles = keys > 0 ? (keys + BN - 1) / BN : 0;
-  const int steps = any_seen > 0 ? (any_seen + SUB - 1) / SUB : 0, full = all_seen > 0 ? all_seen / SUB : 0;      // steps of this wave; that every row sees whole
+  auto seen_by = [&](int r) { return x.s.seen_by(r, G); };
+  const int row0 = tile * BM + wave * 32, length = x.s.key_tiles(tile, G);
+  const int all_seen = seen_by(row0), any_seen = seen_by(row0 + 31);
+  // key tiles of this share; of this wave; that every row of it sees whole (counted from the beginning of the sequence)
+  const int begin = (int)((int64_t)length * x.part / x.parts), tiles = (int)((int64_t)length * (x.part + 1) / x.parts);
+  auto at_most = [&](int n) { return n < tiles ? n : tiles; };
+  const int steps = at_most(any_seen > 0 ? (any_seen + BN - 1) / BN : 0), full = at_most(all_seen > 0 ? all_seen / BN : 0);
 
-  int seen[RB];
-  uint4v qf[RB][D / 16];
-  auto row_of = [&](int rb, int& query, int& head) {
-    const int r = row0 + 32 * rb + n, rc = r < rows ? r : rows - 1;
-    query = rc / G;
-    head = hk * G + rc - query * G;
-    return r < rows;
-  };
+  const int row = row0 + n, rowc = row < rows ? row : rows - 1;
+  const int query = rowc / G, head = hk * G + rowc - query * G, seen = nk - nq + query + 1;
+  uint4v qf[D / 16];
+  const char* const qp = a.q.data + (int64_t)(q0 + query) * a.q.token + (int64_t)head * a.q.head + 16 * h;
 #pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-    int query, head;
-    row_of(rb, query, head);
-    seen[rb] = nk - nq + query + 1;
-    const char* qp = a.q.data + (int64_t)(q0 + query) * a.q.token + (int64_t)head * a.q.head + 16 * h;
-#pragma unroll
-    for (int i = 0; i < D / 16; ++i) qf[rb][i] = *reinterpret_cast<const uint4v*>(qp + 32 * i);
-  }
+  for (int i = 0; i < D / 16; ++i) qf[i] = *reinterpret_cast<const uint4v*>(qp + 32 * i);
 
   // Tiles: row r of keys has its 16-byte chunk c at place c ^ (r & 15) (head_dim 64: c ^ (r / 2 & 7)), a row of values its 64 bytes f at f ^ (r & 3) (f ^ (r / 2 & 1)).
   // Sixteen lanes that read 16 bytes of as many rows of keys then meet all banks once, and so do 32 that read 32 bytes of four rows of values, twice.
@@ -154,16 +251,11 @@ __global__ __launch_bounds__(NW * 64, 2) void ftprompt_main(const Args a) {
     return uint4v{x[0], x[1], y[0], y[1]};
   };
 
-  float16v o[RB][NF];
-  float4v sums[RB];
-  float ref[RB];
+  float16v o[NF];
+  float4v sums = (float4v)0.f;
+  float ref = -3.4028234e38f;
 #pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-    ref[rb] = -3.4028234e38f;
-    sums[rb] = (float4v)0.f;
-#pragma unroll
-    for (int f = 0; f < NF; ++f) o[rb][f] = (float16v)0.f;
-  }
+  for (int f = 0; f < NF; ++f) o[f] = (float16v)0.f;
 
   // scores of a tile, transposed
   auto scores = [&](uint32_t k_at, float16v (&to)[2]) __attribute__((always_inline)) {
@@ -171,11 +263,11 @@ __global__ __launch_bounds__(NW * 64, 2) void ftprompt_main(const Args a) {
     for (int t = 0; t < 2; ++t) {
       to[t] = (float16v)0.f;
 #pragma unroll
-      for (int i = 0; i < D / 16; ++i) to[t] = mfma32<BF>(key(k_at + t * (64 * D), i), qf[0][i], to[t]);
+      for (int i = 0; i < D / 16; ++i) to[t] = mfma32<BF>(key(k_at + t * (64 * D), i), qf[i], to[t]);
     }
   };
   auto mask = [&](int t, float16v (&x)[2]) __attribute__((always_inline)) {
-    const int limit = seen[0] - t * BN - 4 * h;
+    const int limit = seen - t * BN - 4 * h;
 #pragma unroll
     for (int v = 0; v < 32; ++v)
       if (limit <= 8 * (v >> 2) + (v & 3)) x[v >> 4][v & 15] = -__builtin_inff();
@@ -189,26 +281,20 @@ __global__ __launch_bounds__(NW * 64, 2) void ftprompt_main(const Args a) {
     return max32(m) * a.scale_log2;
   };
   // a row's reference moves when a score exceeds it by more than there is room for: rarely after the first step
-  auto renew = [&](const float (&m)[RB]) __attribute__((always_inline)) {
-    bool any = false;
+  auto renew = [&](float m) __attribute__((always_inline)) {
+    if (__any(m > ref + (ROOM + UP))) {
+      const float next = __builtin_fmaxf(m - UP, ref), f = ex2(ref - next);
+      ref = next;
+      sums *= f;
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb) any |= m[rb] > ref[rb] + (ROOM + UP);
-    if (__any(any)) {
-#pragma unroll
-      for (int rb = 0; rb < RB; ++rb) {
-        const float next = __builtin_fmaxf(m[rb] - UP, ref[rb]), f = ex2(ref[rb] - next);
-        ref[rb] = next;
-        sums[rb] *= f;
-#pragma unroll
-        for (int x = 0; x < NF; ++x) o[rb][x] *= f;
-      }
+      for (int x = 0; x < NF; ++x) o[x] *= f;
     }
   };
   auto weight_pair = [&](const float16v (&x)[2], int v, uint4v (&p)[4]) __attribute__((always_inline)) {
-    p[v >> 3][(v & 7) >> 1] = pack2<BF>(ex2(__builtin_fmaf(x[v >> 4][v & 15], a.scale_log2, -ref[0])), ex2(__builtin_fmaf(x[v >> 4][(v & 15) + 1], a.scale_log2, -ref[0])));
+    p[v >> 3][(v & 7) >> 1] = pack2<BF>(ex2(__builtin_fmaf(x[v >> 4][v & 15], a.scale_log2, -ref)), ex2(__builtin_fmaf(x[v >> 4][(v & 15) + 1], a.scale_log2, -ref)));
   };
   auto add_up = [&](const uint4v (&p)[4], int i) __attribute__((always_inline)) {        // the i-th four weights
-    sums[0] = add4<BF>(i & 1 ? uint2v{p[i >> 1][2], p[i >> 1][3]} : uint2v{p[i >> 1][0], p[i >> 1][1]}, sums[0]);
+    sums = add4<BF>(i & 1 ? uint2v{p[i >> 1][2], p[i >> 1][3]} : uint2v{p[i >> 1][0], p[i >> 1][1]}, sums);
   };
   auto weights = [&](const float16v (&x)[2], uint4v (&p)[4]) __attribute__((always_inline)) {
 #pragma unroll
@@ -233,7 +319,7 @@ __global__ __launch_bounds__(NW * 64, 2) void ftprompt_main(const Args a) {
             av[w] &= __builtin_bit_cast(uint32_t, is);
           }
         }
-        o[0][f] = mfma32<BF>(av, p[i], o[0][f]);
+        o[f] = mfma32<BF>(av, p[i], o[f]);
       }
   };
 
@@ -252,19 +338,21 @@ __global__ __launch_bounds__(NW * 64, 2) void ftprompt_main(const Args a) {
     return (uint32_t)(t & 1) * (2 * TILE);      // (from the beginning of LDS)
   };
   float16v s[2];
-  if (tiles > 0) {
-    issue_k(0, lds0 + 2 * TILE);
-    issue_v(0, lds0 + TILE);
-    if (tiles > 1) issue_k(1, lds0);
+  if (tiles > begin) {
+    const uint32_t first = (uint32_t)(begin & 1) * (2 * TILE), other = 2 * TILE - first;
+    issue_k(begin, lds0 + other);
+    issue_v(begin, lds0 + first + TILE);
+    if (tiles > begin + 1) issue_k(begin + 1, lds0 + first);
     __builtin_amdgcn_s_waitcnt(0x0F70);
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    scores(2 * TILE, s);
-    if (full < 1) mask(0, s);
-    const float m[RB] = {largest(s)};
-    renew(m);
+    if (steps > begin) {
+      scores(other, s);
+      if (full <= begin) mask(begin, s);
+      renew(largest(s));
+    }
   }
-  int t = 0;
+  int t = begin;
   for (; t + 1 < full; ++t) {              // this tile and the next one are seen whole by every row of the wave
     const uint32_t at = arrive(t);
     // Written out in the order that it runs in: every matrix instruction with the operand that was requested AHEAD instructions before, the request of
@@ -273,14 +361,14 @@ __global__ __launch_bounds__(NW * 64, 2) void ftprompt_main(const Args a) {
     auto operand = [&](int x) __attribute__((always_inline)) { return x < NK ? key(at + (x & 1) * (64 * D), x >> 1) : value(at + TILE, (x - NK) / NF, (x - NK) % NF); };
     uint4v ring[AHEAD], p[4];
     float16v then[2];
-    float m[RB];
+    float m = 0.f;
 #pragma unroll
     for (int x = 0; x < AHEAD; ++x) ring[x] = operand(x);
 #pragma unroll
     for (int x = 0; x < N; ++x) {
       const uint4v mine = ring[x % AHEAD];
-      if (x < NK) then[x & 1] = mfma32<BF>(mine, qf[0][x >> 1], x < 2 ? (float16v)0.f : then[x & 1]);
-      else o[0][(x - NK) % NF] = mfma32<BF>(mine, p[(x - NK) / NF], o[0][(x - NK) % NF]);
+      if (x < NK) then[x & 1] = mfma32<BF>(mine, qf[x >> 1], x < 2 ? (float16v)0.f : then[x & 1]);
+      else o[(x - NK) % NF] = mfma32<BF>(mine, p[(x - NK) / NF], o[(x - NK) % NF]);
       if (x + AHEAD < N) ring[x % AHEAD] = operand(x + AHEAD);
       if (x < NK) {
 #pragma unroll
@@ -292,11 +380,11 @@ __global__ __launch_bounds__(NW * 64, 2) void ftprompt_main(const Args a) {
 #pragma unroll
           for (int i = y / 2 * SUMS; i < (y / 2 + 1) * SUMS; ++i) add_up(p, i);
 #pragma unroll
-        for (int v = y * MAXIMA; v < (y + 1) * MAXIMA; ++v) m[0] = v == 0 ? __builtin_fmaxf(then[0][0], then[1][0]) : __builtin_fmaxf(__builtin_fmaxf(m[0], then[0][v]), then[1][v]);
+        for (int v = y * MAXIMA; v < (y + 1) * MAXIMA; ++v) m = v == 0 ? __builtin_fmaxf(then[0][0], then[1][0]) : __builtin_fmaxf(__builtin_fmaxf(m, then[0][v]), then[1][v]);
       }
       __builtin_amdgcn_sched_barrier(0);
     }
-    m[0] = max32(m[0]) * a.scale_log2;
+    m = max32(m) * a.scale_log2;
     s[0] = then[0];
     s[1] = then[1];
     renew(m);
@@ -311,49 +399,89 @@ __global__ __launch_bounds__(NW * 64, 2) void ftprompt_main(const Args a) {
     if (t + 1 < steps) {
       scores(at, s);
       mask(t + 1, s);
-      const float m[RB] = {largest(s)};
-      renew(m);
+      renew(largest(s));
     }
   }
   if (__any(__builtin_bit_cast(uint32_t, finite) != 0xFFFFFFFFu)) {
-    for (int j = full > 1 ? (full - 1) * BN : 0; j < any_seen; ++j)
+    const int from = full - 1 > begin ? full - 1 : begin;
+    for (int j = from * BN; j < any_seen && j < tiles * BN; ++j)
 #pragma unroll
-      for (int rb = 0; rb < RB; ++rb)
+      for (int f = 0; f < NF; ++f)
 #pragma unroll
-        for (int f = 0; f < NF; ++f)
-#pragma unroll
-          for (int r = 0; r < 16; r += 2) {
-            const uint32_t w = *reinterpret_cast<const uint32_t*>(vbase + (int64_t)j * a.v.token + 2 * (32 * f + 8 * (r >> 2) + 4 * h + (r & 3)));
-            const float lo = low_of<BF>(w), hi = high_of<BF>(w);
-            if (j < seen[rb] && !(__builtin_fabsf(lo) <= 3.4e38f)) o[rb][f][r] += lo;
-            if (j < seen[rb] && !(__builtin_fabsf(hi) <= 3.4e38f)) o[rb][f][r + 1] += hi;
-          }
+        for (int r = 0; r < 16; r += 2) {
+          const uint32_t w = *reinterpret_cast<const uint32_t*>(vbase + (int64_t)j * a.v.token + 2 * (32 * f + 8 * (r >> 2) + 4 * h + (r & 3)));
+          const float lo = low_of<BF>(w), hi = high_of<BF>(w);
+          if (j < seen && !(__builtin_fabsf(lo) <= 3.4e38f)) o[f][r] += lo;
+          if (j < seen && !(__builtin_fabsf(hi) <= 3.4e38f)) o[f][r + 1] += hi;
+        }
   }
+  float l = sum32(sums[0]);
+  if (x.parts > 1) {
+    // The state of a share: its rows' references and sums, then the output before its division, as the lanes hold it.  Written through to memory, since the
+    // workgroup that reads it may lie on another XCD; the one that comes last puts all shares together, in their order.
+    constexpr int ROWS = NW * 64 * 2, STATE = ROWS + NW * NF * 16 * 64;
+    const int64_t next = (int64_t)a.kv_heads * STATE;
+    float* const first = a.ws + ((int64_t)x.slot * a.kv_heads + hk) * STATE;
+    float* const mine = first + x.part * next;
+    const bool used = row0 < rows;               // (waves without rows have no state)
+    if (used) {
+      __hip_atomic_store(reinterpret_cast<uint64_t*>(mine + (wave * 64 + lane) * 2), (uint64_t)as_u(ref) | (uint64_t)as_u(l) << 32, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 #pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-    int query, head;
-    const bool real = row_of(rb, query, head);
-    const float l = sum32(sums[rb][0]), inv = l == 0.f ? 0.f : 1.f / l;
-    if (!real) continue;
-    char* op = a.o.data + (int64_t)(q0 + query) * a.o.token + (int64_t)head * a.o.head;
+      for (int f = 0; f < NF; ++f)
 #pragma unroll
-    for (int f = 0; f < NF; ++f)
+        for (int g = 0; g < 4; ++g) {
+          const float4v y = {o[f][4 * g], o[f][4 * g + 1], o[f][4 * g + 2], o[f][4 * g + 3]};
+          asm volatile("global_store_dwordx4 %0, %1, off sc0 sc1" ::"v"(mine + ROWS + ((wave * NF + f) * 4 + g) * 256 + lane * 4), "v"(y) : "memory");
+        }
+    }
+    __builtin_amdgcn_s_waitcnt(0x0F70);
+    __syncthreads();
+    uint32_t* const last = reinterpret_cast<uint32_t*>(lds);
+    if (threadIdx.x == 0) {
+      uint32_t* const done = a.done + (int64_t)x.slot * a.kv_heads + hk;
+      *last = atomicAdd(done, 1u) + 1 == (uint32_t)x.parts;
+      if (*last) *done = 0;
+    }
+    __syncthreads();
+    if (!*last) return;
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+    if (!used) return;
+    ref = -3.4028234e38f;
+    for (int i = 0; i < x.parts; ++i) ref = __builtin_fmaxf(ref, first[i * next + (wave * 64 + lane) * 2]);
+    l = 0.f;
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const float x0 = o[rb][f][4 * g] * inv, x1 = o[rb][f][4 * g + 1] * inv, x2 = o[rb][f][4 * g + 2] * inv, x3 = o[rb][f][4 * g + 3] * inv;
-        const int e = 32 * f + 8 * g + 4 * h;
-        if constexpr (F32OUT) *reinterpret_cast<float4v*>(op + 4 * e) = float4v{x0, x1, x2, x3};
-        else *reinterpret_cast<uint2v*>(op + 2 * e) = uint2v{pack2<BF>(x0, x1), pack2<BF>(x2, x3)};
-      }
+    for (int f = 0; f < NF; ++f) o[f] = (float16v)0.f;
+    for (int i = 0; i < x.parts; ++i) {
+      const float* const from = first + i * next;
+      const float2v head = *reinterpret_cast<const float2v*>(from + (wave * 64 + lane) * 2);
+      float4v y[NF * 4];
+#pragma unroll
+      for (int g = 0; g < NF * 4; ++g) y[g] = *reinterpret_cast<const float4v*>(from + ROWS + (wave * NF * 4 + g) * 256 + lane * 4);
+      const float scale = ex2(head[0] - ref);
+      l += scale * head[1];
+#pragma unroll
+      for (int g = 0; g < NF * 4; ++g)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) o[g >> 2][4 * (g & 3) + r] += scale * y[g][r];
+    }
   }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  if (row >= rows) return;
+  char* op = a.o.data + (int64_t)(q0 + query) * a.o.token + (int64_t)head * a.o.head;
+#pragma unroll
+  for (int f = 0; f < NF; ++f)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const float x0 = o[f][4 * g] * inv, x1 = o[f][4 * g + 1] * inv, x2 = o[f][4 * g + 2] * inv, x3 = o[f][4 * g + 3] * inv;
+      const int e = 32 * f + 8 * g + 4 * h;
+      if constexpr (F32OUT) *reinterpret_cast<float4v*>(op + 4 * e) = float4v{x0, x1, x2, x3};
+      else *reinterpret_cast<uint2v*>(op + 2 * e) = uint2v{pack2<BF>(x0, x1), pack2<BF>(x2, x3)};
+    }
 }
 
 typedef void (*kernel_fn)(const Args);
-template <int D, bool BF, int RB> static kernel_fn kernel_of(bool f32) { return f32 ? ftprompt_main<D, BF, true, RB> : ftprompt_main<D, BF, false, RB>; }
-template <int RB> static kernel_fn kernel_for(const ftprompt_config& e) {
-  const bool bf = e.in_dtype == FTPROMPT_BF16, f32 = e.out_dtype == FTPROMPT_F32;
-  return e.head_dim == 128 ? (bf ? kernel_of<128, true, RB>(f32) : kernel_of<128, false, RB>(f32)) : (bf ? kernel_of<64, true, RB>(f32) : kernel_of<64, false, RB>(f32));
-}
+template <int D, bool BF> static kernel_fn kernel_of(bool f32) { return f32 ? ftprompt_main<D, BF, true> : ftprompt_main<D, BF, false>; }
+constexpr int64_t state_floats(int d) { return NW * 64 * 2 + NW * 32 * d; }
 
 }  // namespace ftprompt
 
@@ -361,13 +489,11 @@ using namespace ftprompt;
 
 struct ftprompt_ctx {
   ftprompt_config cfg;
-  kernel_fn fn[2] = {nullptr, nullptr};       // one block of rows to a wave, two
+  kernel_fn fn = nullptr;
   int lds = 0;
+  void* scratch = nullptr;       // STATES counters, then as many states
   std::string err;
 };
-
-// Whether waves take two blocks of 32 rows.
-static int ftprompt_wide(int64_t total_q, int heads) { return total_q * heads >= WIDE_FROM; }
 
 static thread_local std::string g_prompt_create_err;
 
@@ -400,14 +526,18 @@ extern "C" int ftprompt_create(const ftprompt_config* cfg, ftprompt_ctx** out) {
   if (!c) return pfail(nullptr, FTPROMPT_ENOMEM, "out of host memory");
   c->cfg = *cfg;
   if (!(c->cfg.softmax_scale > 0.f)) c->cfg.softmax_scale = 1.0f / std::sqrt((float)cfg->head_dim);
-  c->fn[0] = kernel_for<1>(*cfg);
-  c->fn[1] = kernel_for<1>(*cfg);
+  const bool bf = cfg->in_dtype == FTPROMPT_BF16, f32 = cfg->out_dtype == FTPROMPT_F32;
+  c->fn = cfg->head_dim == 128 ? (bf ? kernel_of<128, true>(f32) : kernel_of<128, false>(f32)) : (bf ? kernel_of<64, true>(f32) : kernel_of<64, false>(f32));
   c->lds = cfg->head_dim == 128 ? lds_bytes<128>() : lds_bytes<64>();
   int before = 0;
   hipError_t he = hipGetDevice(&before);
   if (he == hipSuccess) he = hipSetDevice(cfg->device);
   if (he == hipSuccess) {
-    for (int i = 0; i < 2 && he == hipSuccess; ++i) he = hipFuncSetAttribute((const void*)c->fn[i], hipFuncAttributeMaxDynamicSharedMemorySize, c->lds);
+    he = hipFuncSetAttribute((const void*)c->fn, hipFuncAttributeMaxDynamicSharedMemorySize, c->lds);
+    if (he == hipSuccess) he = hipMalloc(&c->scratch, STATES * (sizeof(uint32_t) + state_floats(cfg->head_dim) * sizeof(float)));
+    if (he == hipSuccess) he = hipMemset(c->scratch, 0, STATES * sizeof(uint32_t));
+    if (he == hipSuccess) he = hipDeviceSynchronize();
+    if (he != hipSuccess && c->scratch) (void)hipFree(c->scratch);
     (void)hipSetDevice(before);
   }
   if (he != hipSuccess) {
@@ -444,21 +574,27 @@ extern "C" int ftprompt_forward(ftprompt_ctx* c, const ftprompt_rows* q, const f
   }
   if (total_q == 0) return FTPROMPT_OK;
   const int group = e.heads / e.kv_heads;
-  const int wide = 0;
-  const int64_t slots = (int64_t)total_q * group / bm_of(wide + 1) + batch;
-  if ((int64_t)total_q * group > 0x7FFFFF00ll || slots * e.kv_heads > 0x7FFFFFFFll) return pfail(c, FTPROMPT_EUNSUPPORTED, "too many rows");
-  Args a{r[0], r[1], r[2], r[3], cu_q, cu_k, batch, total_q, total_k, e.kv_heads, group, (int32_t)slots, e.softmax_scale * LOG2E};
+  // row tiles at most, and as many shares again as they are divided into at most
+  const int64_t shares = (int64_t)total_q * group / BM + batch + (SHARES + e.kv_heads - 1) / e.kv_heads;
+  if ((int64_t)total_q * group > 0x7FFFFF00ll || shares * e.kv_heads > 0x7FFFFFFFll) return pfail(c, FTPROMPT_EUNSUPPORTED, "too many rows");
+  Args a{r[0], r[1], r[2], r[3], cu_q, cu_k, batch, total_q, total_k, e.kv_heads, group, e.softmax_scale * LOG2E,
+         reinterpret_cast<float*>(static_cast<char*>(c->scratch) + STATES * sizeof(uint32_t)), static_cast<uint32_t*>(c->scratch)};
   int before = 0;
   hipError_t he = hipGetDevice(&before);
   if (he == hipSuccess && before != e.device) he = hipSetDevice(e.device);
   if (he != hipSuccess) return pfail_hip(c, "device", he);
-  hipLaunchKernelGGL(c->fn[wide], dim3((uint32_t)(slots * e.kv_heads)), dim3(NW * 64), c->lds, (hipStream_t)hip_stream, a);
+  hipLaunchKernelGGL(c->fn, dim3((uint32_t)(shares * e.kv_heads)), dim3(NW * 64), c->lds, (hipStream_t)hip_stream, a);
   he = hipGetLastError();
   if (before != e.device) (void)hipSetDevice(before);
   return he == hipSuccess ? FTPROMPT_OK : pfail_hip(c, "launch", he);
 }
 
 extern "C" int ftprompt_destroy(ftprompt_ctx* c) {
+  if (!c) return FTPROMPT_OK;
+  int before = 0;
+  const bool moved = hipGetDevice(&before) == hipSuccess && before != c->cfg.device && hipSetDevice(c->cfg.device) == hipSuccess;
+  (void)hipFree(c->scratch);
+  if (moved) (void)hipSetDevice(before);
   delete c;
   return FTPROMPT_OK;
 }
