@@ -34,6 +34,7 @@ struct Args {
   Rows q, k, v, o;
   const int32_t *cu_q, *cu_k;
   int32_t batch, total_q, total_k, kv_heads, group;
+  int32_t divide;          // 0: no row tile can be long enough to be divided
   float scale_log2;
   float* ws;               // states of shares, STATES of them
   uint32_t* done;          // shares of a row tile that are there, by its first state; 0 between calls
@@ -69,16 +70,17 @@ __device__ __forceinline__ float sum32(float x) {
 }
 
 // Sums over the lanes up to this one.
-__device__ __forceinline__ int sum_upto(int x) {
-  auto step = [&](int moved) { x += moved; };
-  step(__builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false));      // row_shr 1, 2, 4, 8
-  step(__builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false));
-  step(__builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false));
-  step(__builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false));
-  step(__builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false));      // row_bcast 15, 31
-  step(__builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false));
-  return x;
+__device__ __forceinline__ int plus(int a, int b) { return a + b; }
+__device__ __forceinline__ int plus_float(int a, int b) { return (int)as_u(as_f((uint32_t)a) + as_f((uint32_t)b)); }
+template <int (*ADD)(int, int)> __device__ __forceinline__ int scan(int x) {
+  x = ADD(x, __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false));      // row_shr 1, 2, 4, 8
+  x = ADD(x, __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false));
+  x = ADD(x, __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false));
+  x = ADD(x, __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false));
+  x = ADD(x, __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false));      // row_bcast 15, 31
+  return ADD(x, __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false));
 }
+__device__ __forceinline__ int sum_upto(int x) { return scan<plus>(x); }
 
 // A sequence: its first rows, its queries and keys, its rows and row tiles; row r sees nk - nq + r / G + 1 keys.
 struct Sequence {
@@ -124,14 +126,16 @@ __device__ __forceinline__ bool share_of(const Args& a, int id, Share& x) {
   for (int i = 0; i < per; ++i) {
     const Sequence s = of_lane(i);
     row_tiles += s.tiles;
-    if (s.tiles) work += (0.5f * (float)(s.key_tiles(0, G) + s.key_tiles(s.tiles - 1, G)) + 1.f) * (float)s.tiles;
+    if (a.divide && s.tiles) work += (0.5f * (float)(s.key_tiles(0, G) + s.key_tiles(s.tiles - 1, G)) + 1.f) * (float)s.tiles;
   }
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) work += __shfl_xor(work, d);
-  const float fair = work * (float)a.kv_heads * (1.001f / SHARES);
   const int row_tiles_upto = sum_upto(row_tiles), all_tiles = __builtin_amdgcn_readlane(row_tiles_upto, 63);
-  const int least = all_tiles < 128 / a.kv_heads ? FEW : LEAST;
-  const int piece = __builtin_amdgcn_readfirstlane(fair < (float)least ? least : fair > 1e8f ? 100000000 : (int)fair + 1);
+  int piece = 100000000;
+  if (a.divide) {
+    work = as_f((uint32_t)__builtin_amdgcn_readlane(scan<plus_float>((int)as_u(work)), 63));
+    const float fair = work * (float)a.kv_heads * (1.001f / SHARES);
+    const int least = all_tiles < 128 / a.kv_heads ? FEW : LEAST;
+    piece = __builtin_amdgcn_readfirstlane(fair < (float)least ? least : fair > 1e8f ? 100000000 : (int)fair + 1);
+  }
   auto count = [&](const Sequence& s, int part) { return part == 0 ? s.tiles : s.tiles - s.first_with(part, piece, G); };
   for (int part = 0;; ++part) {
     int n = row_tiles;
@@ -147,11 +151,13 @@ __device__ __forceinline__ bool share_of(const Args& a, int id, Share& x) {
     }
     const int owner = __ffsll((unsigned long long)__ballot(upto > id)) - 1;
     int left = id - __builtin_amdgcn_readlane(upto - n, owner), b = __builtin_amdgcn_readfirstlane(owner * per);
-    for (;; ++b) {
-      x.s = sequence(a, b);
+    auto from_owner = [&](int v) { return __builtin_amdgcn_readlane(v, owner); };
+    x.s = Sequence{from_owner(mine.q0), from_owner(mine.k0), from_owner(mine.nq), from_owner(mine.nk), from_owner(mine.rows), from_owner(mine.tiles)};
+    for (;;) {
       const int c = count(x.s, part);
       if (left < c || b + 1 >= a.batch) break;
       left -= c;
+      x.s = sequence(a, ++b);
     }
     x.tile = x.s.tiles - 1 - left;
     x.part = part;
@@ -577,7 +583,7 @@ extern "C" int ftprompt_forward(ftprompt_ctx* c, const ftprompt_rows* q, const f
   // row tiles at most, and as many shares again as they are divided into at most
   const int64_t shares = (int64_t)total_q * group / BM + batch + (SHARES + e.kv_heads - 1) / e.kv_heads;
   if ((int64_t)total_q * group > 0x7FFFFF00ll || shares * e.kv_heads > 0x7FFFFFFFll) return pfail(c, FTPROMPT_EUNSUPPORTED, "too many rows");
-  Args a{r[0], r[1], r[2], r[3], cu_q, cu_k, batch, total_q, total_k, e.kv_heads, group, e.softmax_scale * LOG2E,
+  Args a{r[0], r[1], r[2], r[3], cu_q, cu_k, batch, total_q, total_k, e.kv_heads, group, total_k > (FEW + FEW / 3) * BN, e.softmax_scale * LOG2E,
          reinterpret_cast<float*>(static_cast<char*>(c->scratch) + STATES * sizeof(uint32_t)), static_cast<uint32_t*>(c->scratch)};
   int before = 0;
   hipError_t he = hipGetDevice(&before);
