@@ -32,7 +32,7 @@ class ReportView(C.Structure):
 
 
 _typed = False
-_types = {}
+_uint8 = _int32 = _float32 = None          # torch's, once load_library has run
 
 
 class FtCacheError(RuntimeError):
@@ -43,11 +43,11 @@ class FtCacheError(RuntimeError):
 
 def load_library() -> C.CDLL:
     """The shared library with the ftcache_* prototypes set; raises if it is not built."""
-    global _typed
+    global _typed, _uint8, _int32, _float32
     lib = _load_prompt()          # (which knows torch's types)
     if not _typed:
         import torch
-        _types.update(uint8=torch.uint8, int32=torch.int32, float32=torch.float32)
+        _uint8, _int32, _float32 = torch.uint8, torch.int32, torch.float32
         p = C.c_void_p
         lib.ftcache_create.argtypes = [C.POINTER(Config), C.POINTER(p)]
         lib.ftcache_get_config.argtypes = [p, C.POINTER(Config)]
@@ -76,6 +76,13 @@ def rotation_table(positions: int, rotary_dim: int, base: float = 10000.0) -> np
 
 _PLACES = struct.Struct("@iiPPPiq")          # ftcache_places
 _NONE = bytes(24)                            # ftcache_rows without a tensor
+
+
+def _count(t, name: str) -> int:
+    try:
+        return t.shape[0]
+    except (AttributeError, IndexError):
+        raise TypeError(f"{name}: expected a device tensor, got {type(t).__name__}") from None
 
 
 class FtCache:
@@ -109,28 +116,31 @@ class FtCache:
             raise FtCacheError(rc, self.lib.ftcache_last_error(self.handle).decode())
 
     def _pool(self, pool) -> int:
+        if isinstance(pool, _base._torch_tensor) and pool.dtype is _uint8 and pool.get_device() == self._device and pool.is_contiguous() and pool.numel() == self._bytes:
+            return pool.data_ptr()
         if not hasattr(pool, "data_ptr"):
             raise TypeError(f"pool: expected a device tensor, got {type(pool).__name__}")
-        if pool.dtype is not _types["uint8"] or not pool.is_contiguous() or pool.numel() != self._bytes:
-            raise ValueError(f"pool: expected {self._bytes} contiguous elements of torch.uint8, got {pool.numel()} of {pool.dtype}")
         if pool.get_device() != self._device:
             raise ValueError(f"pool: tensor is not on device {self._device}")
-        return pool.data_ptr()
+        raise ValueError(f"pool: expected {self._bytes} contiguous elements of torch.uint8, got {pool.numel()} of {pool.dtype}")
 
     def _table(self, table, batch: int):
         if not hasattr(table, "data_ptr"):
             raise TypeError(f"page_table: expected a device tensor, got {type(table).__name__}")
-        if table.dtype is not _types["int32"] or table.dim() != 2 or table.shape[0] != batch or table.shape[1] < 1:
-            raise ValueError(f"page_table: tensor is {tuple(table.shape)} of {table.dtype}, expected [{batch}, width] of torch.int32")
+        shape = table.shape
+        if table.dtype is not _int32 or len(shape) != 2 or shape[0] != batch or shape[1] < 1:
+            raise ValueError(f"page_table: tensor is {tuple(shape)} of {table.dtype}, expected [{batch}, width] of torch.int32")
         if table.get_device() != self._device:
             raise ValueError(f"page_table: tensor is not on device {self._device}")
-        width, stride = table.shape[1], table.stride()
-        if (width > 1 and stride[1] != 1) or (batch > 1 and stride[0] < width):
+        width, (apart, element) = shape[1], table.stride()
+        if batch < 2:
+            apart = width
+        if (width > 1 and element != 1) or apart < width:
             raise ValueError("page_table: the entries of a sequence do not lie side by side")
-        return table.data_ptr(), width, stride[0] if batch > 1 else width
+        return table.data_ptr(), width, apart
 
     def _places(self, cu_seqlens, starts, page_table, tokens: int) -> bytes:
-        batch = cu_seqlens.numel() - 1
+        batch = _count(cu_seqlens, "cu_seqlens") - 1
         if batch < 1:
             raise ValueError("cu_seqlens: expected at least two bounds")
         at, width, stride = self._table(page_table, batch)
@@ -141,12 +151,12 @@ class FtCache:
         """Rotates the packed tokens' q and k into q_out and k_out, and puts keys and values into their pages.
         q, q_out: [tokens, heads, head_dim], both or neither; k, v: [tokens, kv_heads, head_dim]; k_out like k, or None;
         rotation: float32 device tensor [positions, rotary_dim], see rotation_table()."""
-        tokens = k.shape[0]
+        tokens = _count(k, "k")
         if (q is None) != (q_out is None):
             raise ValueError("q and q_out go together")
         if not hasattr(rotation, "data_ptr"):
             raise TypeError(f"rotation: expected a device tensor, got {type(rotation).__name__}")
-        if rotation.dtype is not _types["float32"] or rotation.dim() != 2 or rotation.shape[1] != self._rotary or not rotation.is_contiguous():
+        if rotation.dtype is not _float32 or rotation.dim() != 2 or rotation.shape[1] != self._rotary or not rotation.is_contiguous():
             raise ValueError(f"rotation: tensor is {tuple(rotation.shape)} of {rotation.dtype}, expected contiguous [positions, {self._rotary}] of torch.float32")
         if rotation.get_device() != self._device:
             raise ValueError(f"rotation: tensor is not on device {self._device}")
@@ -159,14 +169,14 @@ class FtCache:
 
     def read(self, pool, k, v, cu_seqlens, starts, page_table, stream: int = 0) -> None:
         """The cached keys and values of the given places into k and v, [tokens, kv_heads, head_dim]."""
-        tokens = k.shape[0]
+        tokens = _count(k, "k")
         places = self._places(cu_seqlens, starts, page_table, tokens)
         self._check(self.lib.ftcache_read(self.handle, self._pool(pool), places, rows(k, "k", tokens, *self._kv, True),
                                           rows(v, "v", tokens, *self._kv, True), stream))
 
     def attend(self, pool, q, o, lengths, page_table, stream: int = 0) -> None:
         """Attention of one token per sequence, q and o [batch, heads, head_dim], over the first lengths[b] cached tokens."""
-        batch = q.shape[0]
+        batch = _count(q, "q")
         at, width, stride = self._table(page_table, batch)
         self._check(self.lib.ftcache_attend(self.handle, self._pool(pool), batch, ints(lengths, "lengths", batch, self._device), at, width,
                                             stride, rows(q, "q", batch, *self._q), rows(o, "o", batch, *self._o), stream))

@@ -58,9 +58,11 @@ def rows(t, name: str, tokens: int, heads: int, head_dim: int, dtype: int, devic
     """The C structure of a tensor [tokens, heads, head_dim].  Elements of a head lie side by side; the strides of tokens and heads are
     free, those of a result not 0.  A tensor of another size, type or device would be an access out of bounds on the GPU, which the library
     cannot see, so it is refused here.  The ordinary tensor passes all checks in the cheapest way: 0.5 us where the general form takes 0.7."""
-    if (tokens > 1 and heads > 1 and isinstance(t, _base._torch_tensor) and t.dtype is _base._torch_dtype[dtype] and t.get_device() == device
+    if (heads > 1 and isinstance(t, _base._torch_tensor) and t.dtype is _base._torch_dtype[dtype] and t.get_device() == device
             and t.shape == (tokens, heads, head_dim)):
         token, head, element = t.stride()
+        if tokens < 2:
+            token = heads * head_dim
         if element == 1 and (not out or (token and head)):
             return _ROWS.pack(t.data_ptr(), token, head)
     if not hasattr(t, "data_ptr"):
@@ -125,8 +127,10 @@ class FtPrompt:
     def forward(self, q, k, v, o, cu_q, cu_k=None, stream: int = 0) -> None:
         """q, o: [total_q, heads, head_dim], k, v: [total_k, kv_heads, head_dim] device tensors, views of a fused projection among them;
         cu_q, cu_k: int32 device tensors [batch + 1] of row bounds, cu_k None: the same as cu_q."""
-        total_q, total_k = q.shape[0], k.shape[0]
-        batch = cu_q.numel() - 1
+        try:
+            total_q, total_k, batch = q.shape[0], k.shape[0], cu_q.numel() - 1
+        except (AttributeError, IndexError):
+            raise TypeError("q, k, cu_q: expected device tensors") from None
         if batch < 1:
             raise ValueError("cu_q: expected at least two bounds")
         at_q = ints(cu_q, "cu_q", batch + 1, self._device)
