@@ -47,6 +47,7 @@ struct Block {
   int place, row;          // of this lane's token; packed row
   bool real;               // the block holds a new token for this lane
   bool whole;              // all 8 places are new tokens (uniform)
+  bool sound;              // the sequence does not begin before its first place
   char* page;              // the page, or nullptr where the table names none
 };
 
@@ -64,8 +65,9 @@ __device__ __forceinline__ bool block_of(const Places& p, const Pool& pool, int 
   x.row = r0 + (int)(place - from);
   x.whole = first >= from && first + 8 <= from + (r1 - r0);
   x.page = nullptr;
+  x.sound = start >= 0;
   const int entry = (int)first >> pool.page_shift;
-  if (start >= 0 && entry < p.width) {
+  if (x.sound && entry < p.width) {
     const int page = p.table[x.b * p.table_stride + entry];
     if (page >= 0 && page < pool.pages) x.page = pool.head(page, 0);
   }
@@ -218,7 +220,7 @@ __global__ __launch_bounds__(256) void ftcache_put(const Args a) {
   Block x;
   if (!block_of(a.at, a.pool, blockIdx.x, x)) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), t = lane >> 3, c = lane & 7, e0 = c * N;
-  const bool known = x.place < a.positions, kept = x.real && known && x.page;
+  const bool known = x.sound && x.place < a.positions, kept = x.real && known && x.page;
   if (blockIdx.y == 0 && wave == 0) {
     const uint64_t refused = __ballot(x.real && !kept && c == 0);
     if (refused && lane == 0) atomicAdd(a.refused, (unsigned long long)__popcll(refused));
@@ -363,6 +365,7 @@ struct OneArgs {
 
 constexpr int ONE_WAVES = 4, ONE_STEP = 32, ONE_UNIT = ONE_WAVES * ONE_STEP;      // tokens of a step of a wave, of a workgroup
 constexpr int CUS = 256, ONE_GROUPS = 8 * CUS, ROUND = 3 * CUS;      // workgroups that a call is divided among (more where sequences are many), and that fit side by side
+constexpr int SPLIT_TO = 4 * CUS;                    // workgroups of append and read, where heads give as many
 constexpr int MOST_PARTS = 2 * CUS, JOIN = 16, LEVELS = 3;      // of one sequence, where there is one head; put together at a time
 static_assert(JOIN * JOIN * JOIN >= MOST_PARTS, "levels");
 constexpr int LONG = 8, SOME = 6;                    // units of a piece, see piece_of
@@ -411,17 +414,17 @@ __device__ __forceinline__ int max_upto(int x) {      // of values >= 0
 struct Piece { int b, first, count, part, parts, slot; };      // tokens first .. first + count of sequence b, part of parts; place of part 0's state
 
 // Sequences are divided into pieces of one length, the same for all, chosen so that there are about `chunks` pieces in all: the last of a sequence is
-// shorter.  Lengths count in units of ONE_UNIT tokens (all of them together below 2^31, see ftcache_attend).  Lane l looks after sequences l * per ..;
-// with up to 64 of them each length is loaded once.
+// shorter.  Lengths count in units of ONE_UNIT tokens (all of them together below 2^31, see ftcache_attend).  A wave looks at 64 sequences at a time.
 __device__ __forceinline__ bool piece_of(const OneArgs& a, int id, Piece& p, bool& known) {
-  const int lane = threadIdx.x & 63, per = (a.batch + 63) / 64, most = a.most;
+  const int lane = threadIdx.x & 63, most = a.most;
   auto length = [&](int b) { return b < a.batch ? a.lengths[b] : 0; };
   auto sound = [&](int n) { return n < 0 || n > most ? 0 : n; };
   auto units = [&](int n) { return (int)(((uint32_t)sound(n) + ONE_UNIT - 1) / ONE_UNIT); };
-  const int mine = length(lane * per);
+  const int mine = length(lane);
   int total = units(mine), longest = total;
-  for (int i = 1; i < per; ++i) {
-    const int u = units(length(lane * per + i));
+#pragma unroll 4
+  for (int b = lane + 64; b < a.batch; b += 64) {
+    const int u = units(a.lengths[b]);
     total += u;
     longest = u > longest ? u : longest;
   }
@@ -429,36 +432,27 @@ __device__ __forceinline__ bool piece_of(const OneArgs& a, int id, Piece& p, boo
   longest = __builtin_amdgcn_readlane(max_upto(longest), 63);
   // Pieces that leave every CU several are best where there is enough to read (1.25 M tokens of 96 sequences and 8 heads: 297 us in 3 workgroups a CU,
   // 265 in 8), one round of what fits side by side where there is not (35,000 tokens of 32: 15.9 us in 3, 17.4 in 8), and few enough parts to be put together
-  // at once where that makes them no longer than some steps
+  // at once where that makes them no longer than some steps (4 sequences of 8000: 18.0 us with more than 16 parts, 13.7 with 16).
   auto of = [&](int n, int chunks) { return (n + chunks - 1) / chunks; };
   auto larger = [](int x, int y) { return x > y ? x : y; };
   auto smaller = [](int x, int y) { return x < y ? x : y; };
   const int size = larger(larger(larger(of(total, a.chunks), of(longest, a.most_parts)), 1), larger(smaller(of(total, a.one_round), LONG), smaller(of(longest, JOIN), SOME)));
   auto parts_of = [&](int n) { const int u = units(n); return u > size && u > SHORT ? (u + size - 1) / size : 1; };
-  int pieces = 0, slots = 0;          // and those of divided sequences, which leave a state
-  for (int i = 0; i < per; ++i) {
-    const int b = lane * per + i, n = parts_of(i == 0 ? mine : length(b));
-    pieces += b < a.batch ? n : 0;
-    slots += n > 1 ? n : 0;
-  }
-  const int upto = sum_upto(pieces), slots_upto = sum_upto(slots);
-  const uint64_t beyond = __ballot(upto > id);
-  if (!beyond) return false;
-  const int owner = __ffsll((unsigned long long)beyond) - 1;
-  int left = id - __builtin_amdgcn_readlane(upto - pieces, owner), slot = __builtin_amdgcn_readlane(slots_upto - slots, owner);
-  int n = __builtin_amdgcn_readlane(mine, owner), b = owner * per;
-  for (int i = 0; i < per; ++i, ++b) {
-    if (b >= a.batch) return false;
-    if (i) n = __builtin_amdgcn_readfirstlane(length(b));
-    const int parts = parts_of(n);
-    if (left < parts) {
-      known = n == sound(n);
-      const int first = left * size * ONE_UNIT, rest = sound(n) - first;
-      p = Piece{b, first, parts == 1 || rest < size * ONE_UNIT ? rest : size * ONE_UNIT, left, parts, slot};
-      return true;
+  int slot = 0;                       // states of the divided sequences so far
+  for (int b0 = 0; b0 < a.batch; b0 += 64) {
+    const int n = b0 ? length(b0 + lane) : mine, parts = b0 + lane < a.batch ? parts_of(n) : 0, states = parts > 1 ? parts : 0;
+    const int upto = sum_upto(parts), states_upto = sum_upto(states), all = __builtin_amdgcn_readlane(upto, 63);
+    if (id >= all) {
+      id -= all;
+      slot += __builtin_amdgcn_readlane(states_upto, 63);
+      continue;
     }
-    left -= parts;
-    slot += parts > 1 ? parts : 0;
+    const int owner = __ffsll((unsigned long long)__ballot(upto > id)) - 1;
+    auto from_owner = [&](int v) { return __builtin_amdgcn_readlane(v, owner); };
+    const int raw = from_owner(n), part = id - from_owner(upto - parts), count = from_owner(parts), first = part * size * ONE_UNIT, rest = sound(raw) - first;
+    known = raw == sound(raw);
+    p = Piece{b0 + owner, first, count == 1 || rest < size * ONE_UNIT ? rest : size * ONE_UNIT, part, count, slot + from_owner(states_upto - states)};
+    return true;
   }
   return false;
 }
@@ -959,7 +953,7 @@ extern "C" int ftcache_append(ftcache_ctx* c, void* pool, const ftcache_places* 
   a.refused = c->refused;
   const int blocks = a.at.tokens / 8 + 2 * a.at.batch, items = (a.q.data ? e.heads : 0) + e.kv_heads;
   // few blocks: their heads are dealt to more workgroups
-  int split = (4 * CUS + blocks - 1) / blocks;
+  int split = (SPLIT_TO + blocks - 1) / blocks;
   split = split < 1 ? 1 : split > (items + 3) / 4 ? (items + 3) / 4 : split;
   OnDevice here(e.device);
   if (here.status != hipSuccess) return cfail_hip(c, "device", here.status);
@@ -982,7 +976,7 @@ extern "C" int ftcache_read(ftcache_ctx* c, const void* pool, const ftcache_plac
   a.pool = pool_of(c, pool);
   a.refused = c->refused;
   const int blocks = a.at.tokens / 8 + 2 * a.at.batch, items = 2 * e.kv_heads;
-  int split = (4 * CUS + blocks - 1) / blocks;
+  int split = (SPLIT_TO + blocks - 1) / blocks;
   split = split < 1 ? 1 : split > (items + 3) / 4 ? (items + 3) / 4 : split;
   OnDevice here(e.device);
   if (here.status != hipSuccess) return cfail_hip(c, "device", here.status);
@@ -1009,7 +1003,7 @@ extern "C" int ftcache_attend(ftcache_ctx* c, const void* pool, int32_t batch, c
   a.table_stride = table_stride;
   a.batch = batch;
   const int64_t most = (int64_t)table_width << c->shift;
-  a.most = (int32_t)(most > 0x7FFFFF00 ? 0x7FFFFF00 : most);
+  a.most = (int32_t)(most > 0x7FFF0000 ? 0x7FFF0000 : most);      // (places a few steps behind the end still fit 32 bits)
   if (((int64_t)a.most + ONE_UNIT - 1) / ONE_UNIT * batch > 0x7FFFFFFFll) return cfail(c, FTCACHE_EUNSUPPORTED, "the page table has room for too many tokens");
   a.group = e.heads / e.kv_heads;
   a.row_tiles = c->row_tiles;

@@ -26,7 +26,7 @@ constexpr int BM = 128, BN = 64, NW = 4, STAGES = 2;      // rows of a workgroup
 // tiles: pieces have LEAST tiles, or FEW where row tiles leave half of the CUs idle, and a row tile a third longer than a piece stays whole.  Measured (us; whole,
 // divided): 3 x 20 queries over 8000 keys, 32 heads on 8: 135, 38; 6 chunks of up to 509 over 3000, 16 on 4: 70, 55; 1 x 4000, 8 on 2: 79, 58;
 // 2 x 9090, 5 on 1, of 64: 120, 99.  With pieces of 10: 1 x 2000, 32 on 8: 53, 60; 24 of up to 1531, 12, of 64: 29, 36.
-constexpr int SHARES = 512, LEAST = 24, FEW = 12, STATES = 2 * SHARES;
+constexpr int SHARES = 512, LEAST = 24, FEW = 12, STATES = 2 * SHARES, MANY = 64;
 
 struct Rows { char* data; int64_t token, head; };         // strides in bytes
 
@@ -34,7 +34,7 @@ struct Args {
   Rows q, k, v, o;
   const int32_t *cu_q, *cu_k;
   int32_t batch, total_q, total_k, kv_heads, group;
-  int32_t divide;          // 0: no row tile can be long enough to be divided
+  int32_t divide;          // 0: no row tile is divided
   float scale_log2;
   float* ws;               // states of shares, STATES of them
   uint32_t* done;          // shares of a row tile that are there, by its first state; 0 between calls
@@ -117,64 +117,50 @@ struct Share {
   int tile, part, parts, slot;      // slot: number of the row tile's first state
 };
 __device__ __forceinline__ bool share_of(const Args& a, int id, Share& x) {
-  const int lane = threadIdx.x & 63, per = (a.batch + 63) / 64, G = a.group;
-  const Sequence mine = sequence(a, lane * per);
-  auto of_lane = [&](int i) { return i == 0 ? mine : sequence(a, lane * per + i); };
-  // key tiles of all row tiles, not too few: they rise by at most one tile's worth of rows from one to the next
-  float work = 0.f;
-  int row_tiles = 0;
-  for (int i = 0; i < per; ++i) {
-    const Sequence s = of_lane(i);
-    row_tiles += s.tiles;
-    if (a.divide && s.tiles) work += (0.5f * (float)(s.key_tiles(0, G) + s.key_tiles(s.tiles - 1, G)) + 1.f) * (float)s.tiles;
+  const int lane = threadIdx.x & 63, G = a.group;
+  if (!a.divide) {
+    // sequence b owns the numbers from cu_q[b] * G / BM + b on: at least as many as it has row tiles, whatever the others have
+    auto before = [&](int b) { return (int64_t)clamped(a.cu_q[b], a.total_q) * G / BM + b; };
+    const int last = (int)((int64_t)a.total_q * G / BM) + a.batch - 1 - id;
+    if (last < 0) return false;
+    const int b = sequence_of(a.batch, last, before);
+    x.s = sequence(a, b);
+    x.tile = last - (int)before(b);
+    x.part = x.slot = 0;
+    x.parts = 1;
+    return x.tile >= 0 && x.tile < x.s.tiles;
   }
-  const int row_tiles_upto = sum_upto(row_tiles), all_tiles = __builtin_amdgcn_readlane(row_tiles_upto, 63);
-  int piece = 100000000;
-  if (a.divide) {
-    work = as_f((uint32_t)__builtin_amdgcn_readlane(scan<plus_float>((int)as_u(work)), 63));
-    const float fair = work * (float)a.kv_heads * (1.001f / SHARES);
-    const int least = all_tiles < 128 / a.kv_heads ? FEW : LEAST;
-    piece = __builtin_amdgcn_readfirstlane(fair < (float)least ? least : fair > 1e8f ? 100000000 : (int)fair + 1);
-  }
-  auto count = [&](const Sequence& s, int part) { return part == 0 ? s.tiles : s.tiles - s.first_with(part, piece, G); };
+  // lane b looks after sequence b
+  const Sequence mine = sequence(a, lane);
+  // bounds that fall: more rows than there are, and not a workgroup for each; nothing is divided then
+  const bool fall = lane < a.batch && a.cu_q[lane + 1] < a.cu_q[lane];
+  // key tiles of all row tiles, not too few: they rise evenly from one to the next
+  const float work = mine.tiles ? (0.5f * (float)(mine.key_tiles(0, G) + mine.key_tiles(mine.tiles - 1, G)) + 1.f) * (float)mine.tiles : 0.f;
+  const int tiles_upto = sum_upto(mine.tiles), least = __builtin_amdgcn_readlane(tiles_upto, 63) < 128 / a.kv_heads ? FEW : LEAST;
+  const float fair = as_f((uint32_t)__builtin_amdgcn_readlane(scan<plus_float>((int)as_u(work)), 63)) * (float)a.kv_heads * (1.001f / SHARES);
+  const int piece = __builtin_amdgcn_readfirstlane(__any(fall) || fair > 1e8f ? 100000000 : fair < (float)least ? least : (int)fair + 1);
   for (int part = 0;; ++part) {
-    int n = row_tiles;
-    if (part) {
-      n = 0;
-      for (int i = 0; i < per; ++i) n += count(of_lane(i), part);
-    }
-    const int upto = part ? sum_upto(n) : row_tiles_upto, all = __builtin_amdgcn_readlane(upto, 63);
+    const int n = part == 0 ? mine.tiles : mine.tiles - mine.first_with(part, piece, G), upto = part == 0 ? tiles_upto : sum_upto(n);
+    const int all = __builtin_amdgcn_readlane(upto, 63);
     if (all == 0) return false;
     if (id >= all) {
       id -= all;
       continue;
     }
     const int owner = __ffsll((unsigned long long)__ballot(upto > id)) - 1;
-    int left = id - __builtin_amdgcn_readlane(upto - n, owner), b = __builtin_amdgcn_readfirstlane(owner * per);
     auto from_owner = [&](int v) { return __builtin_amdgcn_readlane(v, owner); };
     x.s = Sequence{from_owner(mine.q0), from_owner(mine.k0), from_owner(mine.nq), from_owner(mine.nk), from_owner(mine.rows), from_owner(mine.tiles)};
-    for (;;) {
-      const int c = count(x.s, part);
-      if (left < c || b + 1 >= a.batch) break;
-      left -= c;
-      x.s = sequence(a, ++b);
-    }
-    x.tile = x.s.tiles - 1 - left;
+    x.tile = x.s.tiles - 1 - (id - from_owner(upto - n));
     x.part = part;
     const int length = x.s.key_tiles(x.tile, G);
     x.parts = length > piece + piece / 3 ? (length + piece - 1) / piece : 1;
     x.slot = 0;
     if (x.parts > 1)      // states of the divided row tiles before this one: of each q, the tiles of more than q shares; those of more than 0 are those of more than 1
       for (int q = 1;; ++q) {
-        int m = 0, before = 0;
-        for (int i = 0; i < per; ++i) {
-          const int c = count(of_lane(i), q);
-          m += c;
-          before += lane * per + i < b ? c : 0;
-        }
-        if (__builtin_amdgcn_readlane(sum_upto(m), 63) == 0) break;
+        const int m = mine.tiles - mine.first_with(q, piece, G), m_upto = sum_upto(m);
+        if (__builtin_amdgcn_readlane(m_upto, 63) == 0) break;
         const int first = x.s.first_with(q, piece, G), here = x.tile > first ? x.tile - first : 0;
-        x.slot += (q == 1 ? 2 : 1) * (__builtin_amdgcn_readlane(sum_upto(before), 63) + here);
+        x.slot += (q == 1 ? 2 : 1) * (from_owner(m_upto - m) + here);
       }
     return true;
   }
@@ -580,10 +566,12 @@ extern "C" int ftprompt_forward(ftprompt_ctx* c, const ftprompt_rows* q, const f
   }
   if (total_q == 0) return FTPROMPT_OK;
   const int group = e.heads / e.kv_heads;
+  // (with more sequences there are row tiles enough, and every workgroup would look through all of them)
+  const int32_t divide = total_k > (FEW + FEW / 3) * BN && batch <= MANY;
   // row tiles at most, and as many shares again as they are divided into at most
   const int64_t shares = (int64_t)total_q * group / BM + batch + (SHARES + e.kv_heads - 1) / e.kv_heads;
   if ((int64_t)total_q * group > 0x7FFFFF00ll || shares * e.kv_heads > 0x7FFFFFFFll) return pfail(c, FTPROMPT_EUNSUPPORTED, "too many rows");
-  Args a{r[0], r[1], r[2], r[3], cu_q, cu_k, batch, total_q, total_k, e.kv_heads, group, total_k > (FEW + FEW / 3) * BN, e.softmax_scale * LOG2E,
+  Args a{r[0], r[1], r[2], r[3], cu_q, cu_k, batch, total_q, total_k, e.kv_heads, group, divide, e.softmax_scale * LOG2E,
          reinterpret_cast<float*>(static_cast<char*>(c->scratch) + STATES * sizeof(uint32_t)), static_cast<uint32_t*>(c->scratch)};
   int before = 0;
   hipError_t he = hipGetDevice(&before);
