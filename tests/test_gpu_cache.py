@@ -458,3 +458,78 @@ def test_refusals_on_the_gpu():
     three = s.table_dev[:1].expand(3, -1)
     with pytest.raises((ftcache.FtCacheError, ValueError)):       # more sequences than the context was made for
         s.ctx.attend(s.pool, q[:3], q[:3].clone(), ints([1, 1, 1]), three.contiguous())
+
+
+@pytest.mark.gpu
+def test_sequences_that_begin_before_their_first_place():
+    s = Setup(2, 2, 1, 64, 16, ftcache.F16, [16, 16])
+    rotation = torch.from_numpy(ftcache.rotation_table(16, 64)).cuda()
+    q, k, v = s.normal(10, 2, 64), s.normal(10, 1, 64), s.normal(10, 1, 64)
+    q_out, k_out, seen = torch.empty_like(q), torch.empty_like(k), [torch.empty_like(k) for _ in range(2)]
+    before = s.pool.clone()
+    s.ctx.append(s.pool, q, k, v, rotation, bounds([5, 5]), ints([-2, -2 ** 31]), s.table_dev, q_out, k_out)
+    assert torch.equal(s.pool, before) and torch.isnan(q_out).all() and torch.isnan(k_out).all() and s.ctx.report() == (10, 0)
+    s.ctx.read(s.pool, *seen, bounds([5, 5]), ints([-1, 2 ** 31 - 3]), s.table_dev)
+    # (the second sequence's places pass 2^31: they are no places, and its rows are left as they were)
+    assert all(torch.isnan(x[:5]).all() for x in seen) and s.ctx.report()[0] >= 5
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [ftcache.F16, ftcache.BF16])
+def test_one_head_of_a_very_long_sequence(dtype):
+    """One key head: hundreds of parts, put together in three levels."""
+    lengths = [400001, 900]
+    s = Setup(9, 2, 1, 64, 64, dtype, lengths)
+    q, m = s.normal(2, 2, 64), s.model()
+    o = torch.empty(2, 2, 64, dtype=TYPES[dtype], device="cuda")
+    s.ctx.attend(s.pool, q, o, ints(lengths), s.table_dev)
+    first = o.clone()
+    for _ in range(3):
+        s.ctx.attend(s.pool, q, o.zero_(), ints(lengths), s.table_dev)
+        assert torch.equal(o, first)
+    for b, n in enumerate(lengths):
+        k, v = (x[:, 0].cuda() for x in m_sequence(s, m, b, n))
+        w = torch.softmax(64 ** -0.5 * q[b].double() @ k.T, -1)
+        assert ((first[b].double() - w @ v).abs() <= tolerance(dtype, dtype) * v.abs().max()).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("batch", [64, 65, 700])
+def test_many_sequences(batch):
+    lengths = [(13 * i) % 41 for i in range(batch)]
+    lengths[batch - 2] = 5000
+    s = Setup(batch, 2, 1, 64, 16, ftcache.F16, lengths)
+    q = s.normal(batch, 2, 64)
+    o = torch.empty_like(q)
+    s.ctx.attend(s.pool, q, o, ints(lengths), s.table_dev)
+    m = s.model()
+    for b in list(range(0, batch, 29)) + [batch - 2, batch - 1]:
+        n = lengths[b]
+        if n == 0:
+            assert (o[b] == 0).all()
+            continue
+        k, v = (x[:, 0].cuda() for x in m_sequence(s, m, b, n))
+        w = torch.softmax(64 ** -0.5 * q[b].double() @ k.T, -1)
+        assert ((o[b].double() - w @ v).abs() <= tolerance(ftcache.F16, ftcache.F16) * v.abs().max()).all()
+    s.ctx.attend(s.pool, q, q, ints(lengths), s.table_dev)          # the result in place of the queries
+    assert torch.equal(q, o)
+
+
+@pytest.mark.gpu
+def test_rows_apart_and_shared():
+    """Results and queries as views, a page table that is part of a wider one, and sequences that read the same pages."""
+    lengths = [50, 50, 33]
+    s = Setup(21, 4, 2, 128, 16, ftcache.BF16, lengths)
+    wide = torch.full((3, 9), -1, dtype=torch.int32, device="cuda")
+    wide[:, 2:2 + s.table.shape[1]] = s.table_dev
+    wide[1] = wide[0]
+    table = wide[:, 2:2 + s.table.shape[1]]
+    x = s.normal(3, 12, 128)
+    q, o = x[:, 0:4], torch.full((3, 8, 128), 7.0, dtype=torch.bfloat16, device="cuda")
+    s.ctx.attend(s.pool, q, o[:, 2:6], ints(lengths), table)
+    s.table[1] = s.table[0]
+    s.check_attend(o[:, 2:6], q, lengths)
+    assert (o[:, :2] == 7.0).all() and (o[:, 6:] == 7.0).all()
+    k, v = torch.zeros(2, 3, 128, dtype=torch.bfloat16, device="cuda"), torch.zeros(2, 2, 256, dtype=torch.bfloat16, device="cuda")
+    s.ctx.read(s.pool, k[:, :2], v[:, :, 128:], bounds([1, 1, 0]), ints([7, 7, 0]), table)
+    assert torch.equal(k[0], k[1]) and (k[:, 2] == 0).all() and (v[:, :, :128] == 0).all() and (k[:, :2] != 0).any()

@@ -198,3 +198,103 @@ def test_refusals_on_the_gpu():
         ctx.forward(torch.empty(4 * 64 * 10 + 8, dtype=torch.float16, device="cuda")[1:1 + 2560].view(10, 4, 64), k, v, o, cu)
     ctx.forward(q[:0], k[:0], v[:0], o[:0], bounds([0, 0]))
     ctx.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [ftprompt.F16, ftprompt.BF16])
+@pytest.mark.parametrize("heads,kv_heads,d,nq,nk", [
+    (4, 1, 64, [20, 0, 7], [6000, 50, 2500]), (2, 2, 128, [3, 130], [4500, 1800]), (8, 2, 128, [1500], [1500]), (1, 1, 64, [2, 1], [9000, 8999]),
+])
+def test_long_row_tiles_divided_among_workgroups(heads, kv_heads, d, nq, nk, dtype):
+    """Few rows over many keys: the same result every time, and the formula's."""
+    q, k, v = made(sum(nk), sum(nq), sum(nk), heads, kv_heads, d, dtype)
+    ctx = ftprompt.FtPrompt(heads, kv_heads, d, dtype)
+    o = torch.empty(sum(nq), heads, d, dtype=TYPES[dtype], device="cuda")
+    args = (bounds(nq), bounds(nk))
+    ctx.forward(q, k, v, o, *args)
+    check(o, q, k, v, nq, nk, dtype)
+    first = o.clone()
+    for _ in range(5):
+        ctx.forward(q, k, v, o.zero_(), *args)
+        assert torch.equal(o, first)
+    # captured, between eager calls of the same context
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        ctx.forward(q, k, v, o, *args, stream=torch.cuda.current_stream().cuda_stream)
+    for i in range(3):
+        q.copy_(made(i, sum(nq), 1, heads, kv_heads, d, dtype)[0])
+        ctx.forward(q, k, v, first, *args)
+        o.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(o, first)
+    check(o, q, k, v, nq, nk, dtype)
+    ctx.close()
+
+
+@pytest.mark.gpu
+def test_infinite_values_in_divided_row_tiles():
+    """Values that only later queries see, at the end of a long row tile and inside one of its shares."""
+    nk = 3000
+    q, k, v = made(31, 100, nk, 2, 1, 64, ftprompt.BF16)
+    ctx = ftprompt.FtPrompt(2, 1, 64, ftprompt.BF16)
+    o, clean = (torch.empty(100, 2, 64, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    ctx.forward(q, k, v, clean, bounds([100]), bounds([nk]))
+    v[nk - 40, 0, 9], v[nk - 1], k[nk - 20, 0, 0] = float("inf"), float("nan"), float("nan")
+    ctx.forward(q, k, v, o, bounds([100]), bounds([nk]))
+    assert torch.equal(o[:60], clean[:60])
+    assert (o[60:80, :, 9] == float("inf")).all() and torch.isnan(o[80:]).all()
+    keep = [e for e in range(64) if e != 9]
+    assert torch.equal(o[60:80][..., keep], clean[60:80][..., keep])
+    v[100, 0, 3] = float("-inf")
+    ctx.forward(q, k, v, o, bounds([100]), bounds([nk]))
+    assert (o[:80, :, 3] == float("-inf")).all() and torch.equal(o[:60][..., 4:], clean[:60][..., 4:])
+    ctx.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("batch", [65, 300])
+def test_many_sequences(batch):
+    """More sequences than a wave has lanes, one of them long."""
+    lengths = [(7 * i) % 23 for i in range(batch)]
+    lengths[batch // 2] = 1700
+    total = sum(lengths)
+    q, k, v = made(batch, total, total, 2, 1, 64, ftprompt.F16)
+    o = torch.empty(total, 2, 64, dtype=torch.float16, device="cuda")
+    ctx = ftprompt.FtPrompt(2, 1, 64, ftprompt.F16)
+    ctx.forward(q, k, v, o, bounds(lengths))
+    check(o, q, k, v, lengths, lengths, ftprompt.F16)
+    ctx.close()
+
+
+@pytest.mark.gpu
+def test_the_result_in_place_of_the_queries_and_no_keys_at_all():
+    lengths = [300, 40]
+    q, k, v = made(77, 340, 340, 4, 4, 128, ftprompt.F16)
+    ctx = ftprompt.FtPrompt(4, 4, 128, ftprompt.F16)
+    o = torch.empty_like(q)
+    ctx.forward(q, k, v, o, bounds(lengths))
+    ctx.forward(q, k, v, q, bounds(lengths))
+    assert torch.equal(q, o)
+    o.fill_(7.0)
+    ctx.forward(q, k[:0], v[:0], o, bounds(lengths), bounds([0, 0]))
+    assert (o == 0).all()
+    ctx.close()
+
+
+@pytest.mark.gpu
+def test_bounds_that_fall_leave_the_next_call_right():
+    """Bounds that fall, lie beyond the tensors or below 0 read and write nothing out of range, and the calls behind them are as ever."""
+    nq, nk = [20, 30], [5000, 3000]
+    q, k, v = made(8, 50, 8000, 4, 1, 64, ftprompt.BF16)
+    ctx = ftprompt.FtPrompt(4, 1, 64, ftprompt.BF16)
+    o, want = (torch.empty(50, 4, 64, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    ctx.forward(q, k, v, want, bounds(nq), bounds(nk))
+    ints = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    for bad_q, bad_k in [([0, 40, 10], [0, 5000, 8000]), ([0, 50, 90], [0, 9000, 20000]), ([-5, 20, 50], [-7, 6000, 100]), ([0, 20, 50], [0, 8000, 3000]),
+                         ([50, 20, 0], [8000, 5000, 0]), ([2 ** 31 - 1, 0, 2 ** 31 - 1], [0, 2 ** 31 - 1, 0])]:
+        ctx.forward(q, k, v, o, ints(bad_q), ints(bad_k))
+        for _ in range(2):
+            ctx.forward(q, k, v, o.zero_(), bounds(nq), bounds(nk))
+            assert torch.equal(o, want)
+    ctx.close()
