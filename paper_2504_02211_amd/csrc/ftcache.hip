@@ -1004,7 +1004,10 @@ extern "C" int ftcache_attend(ftcache_ctx* c, const void* pool, int32_t batch, c
   a.batch = batch;
   const int64_t most = (int64_t)table_width << c->shift;
   a.most = (int32_t)(most > 0x7FFF0000 ? 0x7FFF0000 : most);      // (places a few steps behind the end still fit 32 bits)
-  if (((int64_t)a.most + ONE_UNIT - 1) / ONE_UNIT * batch > 0x7FFFFFFFll) return cfail(c, FTCACHE_EUNSUPPORTED, "the page table has room for too many tokens");
+  // pieces at most: what lengths that the table has room for can give
+  const int64_t units = ((int64_t)a.most + ONE_UNIT - 1) / ONE_UNIT, room = units <= SHORT ? batch : units * batch;
+  if (units * batch > 0x7FFFFFFFll) return cfail(c, FTCACHE_EUNSUPPORTED, "the page table has room for too many tokens");
+  const int64_t pieces = room < (int64_t)c->chunks + batch ? room : (int64_t)c->chunks + batch;
   a.group = e.heads / e.kv_heads;
   a.row_tiles = c->row_tiles;
   a.chunks = c->chunks;
@@ -1017,7 +1020,7 @@ extern "C" int ftcache_attend(ftcache_ctx* c, const void* pool, int32_t batch, c
   a.refused = c->refused;
   OnDevice here(e.device);
   if (here.status != hipSuccess) return cfail_hip(c, "device", here.status);
-  hipLaunchKernelGGL(c->one, dim3((uint32_t)((c->chunks + batch) * e.kv_heads * c->row_tiles)), dim3(ONE_WAVES * 64), 0, (hipStream_t)hip_stream, a);
+  hipLaunchKernelGGL(c->one, dim3((uint32_t)(pieces * e.kv_heads * c->row_tiles)), dim3(ONE_WAVES * 64), 0, (hipStream_t)hip_stream, a);
   const hipError_t he = hipGetLastError();
   return he == hipSuccess ? FTCACHE_OK : cfail_hip(c, "launch", he);
 }
