@@ -18,7 +18,7 @@ HEADERS = [os.path.join(PKG, "csrc", "ftattn_device.h"), os.path.join(PKG, "csrc
            os.path.join(PKG, "csrc", "ftgemm_main.h"), os.path.join(ROOT, "include", "ftattn.h"),
            os.path.join(PKG, "csrc", "ftserve_device.h"),
            os.path.join(ROOT, "include", "ftgemm.h"), os.path.join(ROOT, "include", "ftdecoupled.h"),
-           os.path.join(ROOT, "include", "ftprompt.h"), os.path.join(ROOT, "include", "ftcache.h")]
+           os.path.join(PKG, "include", "ftprompt.h"), os.path.join(PKG, "include", "ftcache.h")]
 OBJDIR = os.path.join(PKG, "_build")
 
 
@@ -29,7 +29,7 @@ def build(verbose: bool = True, extra_flags=()) -> str:
     flags = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
              "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
              "-Wno-unused-value", "-Wno-unknown-attributes", "-Wno-inline-asm",
-             "-I", os.path.join(ROOT, "include"), "-I", os.path.join(PKG, "csrc"), *extra_flags]
+             "-I", os.path.join(ROOT, "include"), "-I", os.path.join(PKG, "include"), "-I", os.path.join(PKG, "csrc"), *extra_flags]
     os.makedirs(OBJDIR, exist_ok=True)
     objs, procs = [], []
     for src in SOURCES:

@@ -1,4 +1,4 @@
-// Paged key / value cache in 4 bits: the kernels and the C ABI of include/ftcache.h.
+// Paged key / value cache in 4 bits: the kernels and the C ABI of ../include/ftcache.h.
 //
 //   ftcache_put     rotates the new tokens' queries and keys, writes both, and puts keys and values into their pages
 //   ftcache_get     the reverse of the second half: cached tokens as 16-bit rows

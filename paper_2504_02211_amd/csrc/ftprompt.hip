@@ -1,4 +1,4 @@
-// Attention over packed prompts with grouped heads: the kernel and the C ABI of include/ftprompt.h.
+// Attention over packed prompts with grouped heads: the kernel and the C ABI of ../include/ftprompt.h.
 //
 // One pass over the keys with a running maximum and sum (the weights never leave the registers).  A workgroup owns 128 rows of one
 // (sequence, key / value head); a ROW is one (query, head of the group), numbered query-major, so that the heads of a group share

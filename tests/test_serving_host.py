@@ -77,7 +77,7 @@ def test_a_sound_configuration_without_a_gpu_is_an_error_of_the_device():
 
 @pytest.mark.parametrize("header,module", [("ftprompt.h", ftprompt), ("ftcache.h", ftcache)])
 def test_bindings_name_what_the_headers_declare(header, module):
-    with open(os.path.join(ROOT, "include", header)) as f:
+    with open(os.path.join(ROOT, "paper_2504_02211_amd", "include", header)) as f:
         text = re.sub(r"/\*.*?\*/", "", f.read(), flags=re.S)
     name = header[:-2]
     declared = set(re.findall(r"\b(%s_\w+)\(" % name, text))
