@@ -385,12 +385,8 @@ __device__ __forceinline__ uint4v key_operand(uint32_t w) {
   const uint32_t u = w >> 8;
   return uint4v{w & 0x000F000Fu, w & 0x00F000F0u, u & 0x000F000Fu, u & 0x00F000F0u};
 }
-// (as an instruction: of two constants one has to lie in a vector register, else it is an AND and an OR)
-__device__ __forceinline__ uint32_t value_codes(uint32_t w, uint32_t bits128) {
-  uint32_t x;
-  asm("v_and_or_b32 %0, %1, %2, %3" : "=v"(x) : "v"(w), "s"(0x000F000Fu), "v"(bits128));
-  return x;
-}
+// (bits128: those of 128, twice, in a vector register: with two constants it is an AND and an OR)
+__device__ __forceinline__ uint32_t value_codes(uint32_t w, uint32_t bits128) { return (w & 0x000F000Fu) | bits128; }
 
 // sum over the lanes up to this one: register moves within rows of 16 lanes, then from row to row
 __device__ __forceinline__ int sum_upto(int x) {
@@ -733,6 +729,7 @@ __global__ __launch_bounds__(ONE_WAVES * 64, 3) void ftcache_one(const OneArgs a
   int parts = p.parts, part = p.part, apart = 1;                   // of this level; a part's states lie `apart` pieces from the next one's
   for (uint32_t* level = a.done; parts > 1; level += a.done_level) {
     const int first = part / JOIN * JOIN, members = parts - first < JOIN ? parts - first : JOIN;
+    asm volatile("" ::: "memory");
     __builtin_amdgcn_s_waitcnt(0x0F70);          // (vmcnt(0): the state is where every XCD sees it)
     __syncthreads();
     if (tid == 0) {

@@ -49,11 +49,19 @@ struct Args {
 template <int D> constexpr int tile_bytes() { return BN * D * 2; }
 template <int D> constexpr int lds_bytes() { return STAGES * 2 * tile_bytes<D>(); }
 
-// 16 bytes per lane from (uniform base + per-lane byte offset) straight into LDS at (uniform LDS address + 16 * lane).
-// (Opaque to the compiler, which would wait for the tile in flight before it reads another; ordering against barriers and counted waits is kept
-// because all of them are side-effecting instructions.)
-__device__ __forceinline__ void load_lds16(const void* base, uint32_t byte_off, uint32_t lds_addr) {
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(byte_off), "s"(base), "s"(lds_addr) : "memory");
+// N times 16 bytes per lane from (uniform base + per-lane byte offsets) straight into LDS, 1 KB apart from the uniform LDS address on.
+// (Opaque to the compiler, which would wait for the tile in flight before it reads another; ordering against barriers and counted waits is kept because all of
+// them are side-effecting instructions.  The first wait covers a base that a vector instruction has moved to its scalar registers just before: five states.)
+template <int N> __device__ __forceinline__ void load_lds16(const void* base, const uint32_t (&off)[N], uint32_t lds_addr) {
+  static_assert(N == 2 || N == 4, "loads of a wave for a tile");
+#define FTPROMPT_NEXT(r) "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %" #r ", %[base]\n\t"
+  if constexpr (N == 4)
+    asm volatile("s_mov_b32 m0, %[lds]\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %0, %[base]\n\t" FTPROMPT_NEXT(1) FTPROMPT_NEXT(2) FTPROMPT_NEXT(3)
+                 ::"v"(off[0]), "v"(off[1]), "v"(off[2 % N]), "v"(off[3 % N]), [base] "s"(base), [lds] "s"(lds_addr) : "memory", "scc");
+  else
+    asm volatile("s_mov_b32 m0, %[lds]\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %0, %[base]\n\t" FTPROMPT_NEXT(1)
+                 ::"v"(off[0]), "v"(off[1]), [base] "s"(base), [lds] "s"(lds_addr) : "memory", "scc");
+#undef FTPROMPT_NEXT
 }
 
 template <bool BF> __device__ __forceinline__ float16v mfma32(uint4v a, uint4v b, float16v c) {
@@ -218,15 +226,16 @@ __global__ __launch_bounds__(NW * 64, 2) void ftprompt_main(const Args a) {
   auto issue_one = [&](const char* base, int64_t stride, const uint32_t (&off)[LOADS], auto chunk, int t, uint32_t to) __attribute__((always_inline)) {
     const char* const p = base + (int64_t)t * BN * stride;
     to += (uint32_t)wave * (LOADS * 1024);
-    if ((t + 1) * BN <= nk) {
-#pragma unroll
-      for (int i = 0; i < LOADS; ++i) load_lds16(p, off[i], to + i * 1024);
+    if ((int64_t)(t + 1) * BN <= nk) {
+      load_lds16<LOADS>(p, off, to);
     } else {           // rows behind the last key: the last one again (no row sees them)
+      uint32_t held[LOADS];
 #pragma unroll
       for (int i = 0; i < LOADS; ++i) {
         const int r = (wave * LOADS + i) * RPL + lane / CH, rc = r < nk - 1 - t * BN ? r : nk - 1 - t * BN;
-        load_lds16(p, (uint32_t)rc * (uint32_t)stride + chunk(r), to + i * 1024);
+        held[i] = (uint32_t)rc * (uint32_t)stride + chunk(r);
       }
+      load_lds16<LOADS>(p, held, to);
     }
   };
   auto issue_k = [&](int t, uint32_t to) __attribute__((always_inline)) { issue_one(kbase, a.k.token, koff, chunk_k, t, to); };
@@ -327,6 +336,7 @@ __global__ __launch_bounds__(NW * 64, 2) void ftprompt_main(const Args a) {
   // exponentials of its own (vector instructions in the shadow of the wave's own matrix instructions are nearly free), then its products beside the maxima of the next.
   auto arrive = [&](int t) __attribute__((always_inline)) {
     // what iteration t reads is there, and nobody reads what t - 1 did any more: it makes room for t + 1
+    asm volatile("" ::: "memory");
     __builtin_amdgcn_s_waitcnt(0x0F70);
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
@@ -422,13 +432,15 @@ __global__ __launch_bounds__(NW * 64, 2) void ftprompt_main(const Args a) {
     float* const first = a.ws + ((int64_t)x.slot * a.kv_heads + hk) * STATE;
     float* const mine = first + x.part * next;
     const bool used = row0 < rows;               // (waves without rows have no state)
+    float one = 1.f;                             // (the stores take what a vector instruction has left, for which the compiler waits, not the matrix instructions' results)
+    asm("" : "+v"(one));
     if (used) {
       __hip_atomic_store(reinterpret_cast<uint64_t*>(mine + (wave * 64 + lane) * 2), (uint64_t)as_u(ref) | (uint64_t)as_u(l) << 32, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 #pragma unroll
       for (int f = 0; f < NF; ++f)
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
-          const float4v y = {o[f][4 * g], o[f][4 * g + 1], o[f][4 * g + 2], o[f][4 * g + 3]};
+          const float4v y = {o[f][4 * g] * one, o[f][4 * g + 1] * one, o[f][4 * g + 2] * one, o[f][4 * g + 3] * one};
           asm volatile("global_store_dwordx4 %0, %1, off sc0 sc1" ::"v"(mine + ROWS + ((wave * NF + f) * 4 + g) * 256 + lane * 4), "v"(y) : "memory");
         }
     }

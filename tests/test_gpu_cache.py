@@ -533,3 +533,26 @@ def test_rows_apart_and_shared():
     k, v = torch.zeros(2, 3, 128, dtype=torch.bfloat16, device="cuda"), torch.zeros(2, 2, 256, dtype=torch.bfloat16, device="cuda")
     s.ctx.read(s.pool, k[:, :2], v[:, :, 128:], bounds([1, 1, 0]), ints([7, 7, 0]), table)
     assert torch.equal(k[0], k[1]) and (k[:, 2] == 0).all() and (v[:, :, :128] == 0).all() and (k[:, :2] != 0).any()
+
+
+@pytest.mark.gpu
+def test_tokens_far_apart():
+    """Rows of tokens 40 MB apart: 12 GB between the first and the last."""
+    stride, n = 20 * 2 ** 20 + 8, 300
+    whole = torch.empty(n * stride, dtype=torch.float16, device="cuda")
+    view = lambda at, heads: torch.as_strided(whole, (n, heads, 64), (stride, 128, 1), at)
+    q, k, v, q_out, k_out = view(0, 4), view(4096, 2), view(8192, 2), view(12288, 4), view(16384, 2)
+    s = Setup(17, 4, 2, 64, 16, ftcache.F16, [n])
+    near = [s.normal(n, h, 64) for h in (4, 2, 2)]
+    for x, y in zip((q, k, v), near):
+        x.copy_(y)
+    args = (torch.from_numpy(ftcache.rotation_table(n, 64)).cuda(), bounds([n]), ints([0]), s.table_dev)
+    want = [torch.empty_like(near[0]), torch.empty_like(near[1])]
+    s.ctx.append(s.pool, *near, *args, *want)
+    pool = s.pool.clone()
+    s.ctx.append(s.pool, q, k, v, *args, q_out, k_out)
+    assert torch.equal(s.pool, pool) and torch.equal(q_out, want[0]) and torch.equal(k_out, want[1])
+    seen = [torch.empty_like(near[1]) for _ in range(2)]
+    s.ctx.read(s.pool, *seen, *args[1:])
+    s.ctx.read(s.pool, k, v, *args[1:])
+    assert torch.equal(k, seen[0]) and torch.equal(v, seen[1])

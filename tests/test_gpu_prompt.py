@@ -298,3 +298,21 @@ def test_bounds_that_fall_leave_the_next_call_right():
             ctx.forward(q, k, v, o.zero_(), bounds(nq), bounds(nk))
             assert torch.equal(o, want)
     ctx.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d", [64, 128])
+def test_rows_far_apart(d):
+    """Tokens 2^24 elements apart, the most that is allowed: 10 GB between the first row and the last."""
+    lengths, stride = [170, 130], 2 ** 24
+    whole = torch.empty(300 * stride, dtype=torch.bfloat16, device="cuda")
+    view = lambda at, heads: torch.as_strided(whole, (300, heads, d), (stride, 2 * d, 1), at)
+    q, k, v, o = view(0, 4), view(4096, 2), view(8192, 2), view(12288, 4)
+    for x, y in zip((q, k, v), made(13, 300, 300, 4, 2, d, ftprompt.BF16)):
+        x.copy_(y)
+    ctx = ftprompt.FtPrompt(4, 2, d, ftprompt.BF16)
+    ctx.forward(q, k, v, o, bounds(lengths))
+    check(o, q, k, v, lengths, lengths, ftprompt.BF16)
+    with pytest.raises(ftprompt.FtPromptError):
+        ctx.forward(torch.as_strided(whole, (290, 4, d), (stride + 8, 2 * d, 1), 0), k[:290], v[:290], o[:290], bounds([290]))
+    ctx.close()
