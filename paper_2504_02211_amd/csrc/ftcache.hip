@@ -362,7 +362,7 @@ struct OneArgs {
   int32_t chunks, one_round, most_parts;        // pieces over all sequences: at most about, at a time; at most of one
   float scale_log2;
   float* ws;                                    // states of divided sequences
-  uint32_t* done;                               // [level][state]: parts that are there, 0 between calls
+  uint32_t* done;                               // [level][state]: parts that are there, and behind the last level whether a sequence has been refused; 0 between calls
   int64_t done_level;
   unsigned long long* refused;
 };
@@ -484,7 +484,7 @@ __global__ __launch_bounds__(ONE_WAVES * 64, 3) void ftcache_one(const OneArgs a
   constexpr int PITCH = D + 4;
   __shared__ __attribute__((aligned(16))) float merged[ONE_WAVES * 16 * PITCH];      // the waves' outputs
   __shared__ float refs[ONE_WAVES][16], sums[ONE_WAVES][16];
-  __shared__ int last;
+  __shared__ int last, wrong[ONE_WAVES];
   const int heads = a.pool.kv_heads * a.row_tiles, hr = blockIdx.x % heads, hk = hr / a.row_tiles, tile = hr % a.row_tiles;
   Piece p;
   bool known;
@@ -688,6 +688,7 @@ __global__ __launch_bounds__(ONE_WAVES * 64, 3) void ftcache_one(const OneArgs a
   const float shift = z - 136.f * ones[0];
   if (bad) l = __builtin_nanf("");
   if (g == 0) { refs[wave][n] = ref; sums[wave][n] = l; }
+  if (lane == 0) wrong[wave] = bad;
 #pragma unroll
   for (int i = 0; i < NO; ++i)
 #pragma unroll
@@ -723,7 +724,12 @@ __global__ __launch_bounds__(ONE_WAVES * 64, 3) void ftcache_one(const OneArgs a
       if (e == 0) put_state(ws + 2 * row, most, sum);
     }
   }
-  if (tid == 0 && bad && p.part == 0 && hr == 0) atomicAdd(a.refused + 1, 1ull);
+  // a sequence counts once: of its parts, the first that finds something wrong says so for all
+  uint32_t* const told = a.done + LEVELS * a.done_level + (int64_t)p.slot * heads;      // (of a divided sequence)
+  bool any_bad = false;
+#pragma unroll
+  for (int w = 0; w < ONE_WAVES; ++w) any_bad |= wrong[w] != 0;
+  if (any_bad && tid == 0 && hr == 0 && (p.parts == 1 || atomicExch(told, 1u) == 0)) atomicAdd(a.refused + 1, 1ull);
   // Parts are put together by sixteens: the workgroup that comes last of sixteen leaves their sum where the first of them had its state and goes on as one part of
   // the next sixteen.  (One workgroup for 128 parts took 11 us for them.)
   int parts = p.parts, part = p.part, apart = 1;                   // of this level; a part's states lie `apart` pieces from the next one's
@@ -736,6 +742,7 @@ __global__ __launch_bounds__(ONE_WAVES * 64, 3) void ftcache_one(const OneArgs a
       uint32_t* const done = level + (int64_t)(p.slot + first * apart) * heads + hr;
       last = atomicAdd(done, 1u) + 1 == (uint32_t)members;
       if (last) *done = 0;
+      if (last && parts <= JOIN && hr == 0) *told = 0;
     }
     __syncthreads();
     if (!last) return;
@@ -896,7 +903,7 @@ extern "C" int ftcache_create(const ftcache_config* cfg, ftcache_ctx** out) {
   c->one_round = (int)(ROUND / heads < 1 ? 1 : ROUND / heads);
   c->most_parts = (int)(MOST_PARTS / heads < 1 ? 1 : MOST_PARTS / heads);
   // divided sequences are longer than a piece: together they have fewer than twice `chunks` pieces
-  const size_t states = (size_t)2 * c->chunks * heads, ws = states * (32 + 16 * e.head_dim) * sizeof(float), done = LEVELS * states * sizeof(uint32_t);
+  const size_t states = (size_t)2 * c->chunks * heads, ws = states * (32 + 16 * e.head_dim) * sizeof(float), done = (LEVELS + 1) * states * sizeof(uint32_t);
   c->done_level = (int64_t)states;
   OnDevice here(e.device);
   hipError_t he = here.status;

@@ -74,8 +74,8 @@ typedef struct {
 } ftcache_places;
 
 typedef struct {
-  int64_t refused_tokens;    /* tokens of append and read whose page or position does not exist (counted once per workgroup that met them) */
-  int64_t refused_sequences; /* sequences of attend whose length or pages do not exist (likewise) */
+  int64_t refused_tokens;    /* tokens of append and read whose page or position does not exist */
+  int64_t refused_sequences; /* sequences of attend whose length or pages do not exist */
 } ftcache_report_view;
 
 int ftcache_create(const ftcache_config* cfg, ftcache_ctx** out);

@@ -556,3 +556,25 @@ def test_tokens_far_apart():
     s.ctx.read(s.pool, *seen, *args[1:])
     s.ctx.read(s.pool, k, v, *args[1:])
     assert torch.equal(k, seen[0]) and torch.equal(v, seen[1])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("heads,kv_heads", [(2, 1), (40, 2)])
+def test_a_bad_page_anywhere_in_a_long_sequence_counts_once(heads, kv_heads):
+    """At its beginning, inside, in its last block, in several places; the calls behind it are as ever."""
+    lengths = [20000, 300, 7]
+    s = Setup(15, heads, kv_heads, 64, 16, ftcache.BF16, lengths)
+    q = s.normal(3, heads, 64)
+    o, want = torch.empty_like(q), torch.empty_like(q)
+    s.ctx.attend(s.pool, q, want, ints(lengths), s.table_dev)
+    for bad in [[(0, 0)], [(0, 700)], [(0, 1249)], [(0, 3), (0, 900), (0, 901)], [(1, 18)], [(0, 1200), (1, 9), (2, 0)]]:
+        table = s.table_dev.clone()
+        for b, entry in bad:
+            table[b, entry] = s.pages if entry % 2 else -3
+        s.ctx.attend(s.pool, q, o, ints(lengths), table)
+        hit = sorted({b for b, _ in bad})
+        assert s.ctx.report() == (0, len(hit))
+        for b in range(3):
+            assert torch.isnan(o[b]).all() if b in hit else torch.equal(o[b], want[b])
+        s.ctx.attend(s.pool, q, o, ints(lengths), s.table_dev)
+        assert torch.equal(o, want) and s.ctx.report() == (0, 0)
