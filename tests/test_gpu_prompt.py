@@ -316,3 +316,25 @@ def test_rows_far_apart(d):
     with pytest.raises(ftprompt.FtPromptError):
         ctx.forward(torch.as_strided(whole, (290, 4, d), (stride + 8, 2 * d, 1), 0), k[:290], v[:290], o[:290], bounds([290]))
     ctx.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [ftprompt.F16, ftprompt.BF16])
+@pytest.mark.parametrize("heads,kv_heads,d", [(16, 4, 128), (12, 3, 64)])
+def test_divided_row_tiles_many_times(heads, kv_heads, d, dtype):
+    """Chunks behind prefixes, with the chip full and the states of many shares on their way at once: the same bits in every call and in every context."""
+    nq, nk = [509, 60, 301, 77, 440, 130], [3509, 1060, 2301, 877, 2440, 3130]
+    q, k, v = made(5, sum(nq), sum(nk), heads, kv_heads, d, dtype)
+    o = torch.empty(40, sum(nq), heads, d, dtype=TYPES[dtype], device="cuda")
+    args = (bounds(nq), bounds(nk))
+    first = None
+    for _ in range(8):
+        ctx = ftprompt.FtPrompt(heads, kv_heads, d, dtype)
+        o.zero_()
+        for i in range(40):
+            ctx.forward(q, k, v, o[i], *args, stream=torch.cuda.current_stream().cuda_stream)
+        torch.cuda.synchronize()
+        ctx.close()
+        first = o[0].clone() if first is None else first
+        differ = (o != first).flatten(1).any(1)
+        assert not differ.any(), differ.nonzero().flatten().tolist()
