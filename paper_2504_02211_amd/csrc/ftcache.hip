@@ -43,11 +43,11 @@ struct Args {
 
 // Tokens of 8 consecutive places of a sequence (a block of the page layout), one of them per lane group of 8.
 struct Block {
-  int b, first;            // sequence, its first place in the block
+  int b;                   // sequence
   int place, row;          // of this lane's token; packed row
   bool real;               // the block holds a new token for this lane
   bool whole;              // all 8 places are new tokens (uniform)
-  bool sound;              // the sequence does not begin before its first place
+  bool sound;              // the sequence does not begin before its first place, nor does the block lie behind the last one
   char* page;              // the page, or nullptr where the table names none
 };
 
@@ -57,15 +57,14 @@ __device__ __forceinline__ bool block_of(const Places& p, const Pool& pool, int 
   x.b = sequence_of(p.batch, id, before);
   const int r0 = clamped(p.cu[x.b], p.tokens), r1 = clamped(p.cu[x.b + 1], p.tokens), start = p.starts[x.b];
   const int64_t from = start < 0 ? 0 : start, first = (from / 8 + (id - before(x.b))) * 8;
-  if (r1 <= r0 || id < before(x.b) || first >= from + (r1 - r0) || first > 0x7FFFFFF0) return false;
-  const int lane = threadIdx.x & 63, place = (int)first + (lane >> 3);
-  x.first = (int)first;
-  x.place = place;
+  if (r1 <= r0 || id < before(x.b) || first >= from + (r1 - r0)) return false;
+  const int64_t place = first + ((threadIdx.x & 63) >> 3);
+  x.place = (int)place;
   x.real = place >= from && place < from + (r1 - r0);
   x.row = r0 + (int)(place - from);
   x.whole = first >= from && first + 8 <= from + (r1 - r0);
   x.page = nullptr;
-  x.sound = start >= 0;
+  x.sound = start >= 0 && first < 0x7FFFFFF0;
   const int entry = (int)first >> pool.page_shift;
   if (x.sound && entry < p.width) {
     const int page = p.table[x.b * p.table_stride + entry];

@@ -62,7 +62,7 @@ typedef struct { void* data; int64_t token_stride, head_stride; } ftcache_rows;
 
 /* Which tokens a call is about.  Sequence b has rows cu_seqlens[b] .. cu_seqlens[b + 1] of the packed tokens (cu_seqlens[0] = 0; rows
  * behind the last sequence are left as they are), which stand at the places starts[b], starts[b] + 1, .. of the sequence; place p lies in
- * page page_table[b * table_stride + p / page_size].  Places lie below 2^31 - 16.  Entries of the table that no place needs may hold anything. */
+ * page page_table[b * table_stride + p / page_size].  There are 2^31 - 16 places.  Entries of the table that no place needs may hold anything. */
 typedef struct {
   int32_t batch;             /* sequences, >= 1 */
   int32_t tokens;            /* packed rows */

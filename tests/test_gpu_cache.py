@@ -470,8 +470,8 @@ def test_sequences_that_begin_before_their_first_place():
     s.ctx.append(s.pool, q, k, v, rotation, bounds([5, 5]), ints([-2, -2 ** 31]), s.table_dev, q_out, k_out)
     assert torch.equal(s.pool, before) and torch.isnan(q_out).all() and torch.isnan(k_out).all() and s.ctx.report() == (10, 0)
     s.ctx.read(s.pool, *seen, bounds([5, 5]), ints([-1, 2 ** 31 - 3]), s.table_dev)
-    # (the second sequence's places pass 2^31: they are no places, and its rows are left as they were)
-    assert all(torch.isnan(x[:5]).all() for x in seen) and s.ctx.report()[0] >= 5
+    # (the second sequence's places pass the last one)
+    assert all(torch.isnan(x).all() for x in seen) and s.ctx.report()[0] == 10
 
 
 @pytest.mark.gpu
@@ -578,3 +578,41 @@ def test_a_bad_page_anywhere_in_a_long_sequence_counts_once(heads, kv_heads):
             assert torch.isnan(o[b]).all() if b in hit else torch.equal(o[b], want[b])
         s.ctx.attend(s.pool, q, o, ints(lengths), s.table_dev)
         assert torch.equal(o, want) and s.ctx.report() == (0, 0)
+
+
+@pytest.mark.gpu
+def test_places_behind_the_last_one():
+    """Sequences that pass 2^31 - 16 places: what lies behind them is refused like any place without a page, and counted."""
+    s = Setup(16, 2, 1, 64, 16, ftcache.F16, [16, 16])
+    rotation = torch.from_numpy(ftcache.rotation_table(16, 64)).cuda()
+    q, k, v = s.normal(40, 2, 64), s.normal(40, 1, 64), s.normal(40, 1, 64)
+    q_out, k_out, seen = torch.empty_like(q), torch.empty_like(k), [torch.empty_like(k) for _ in range(2)]
+    before = s.pool.clone()
+    for starts in [[2 ** 31 - 1, 2 ** 31 - 20], [2 ** 31 - 17, 2 ** 31 - 8]]:
+        for x in (q_out, k_out, *seen):
+            x.zero_()
+        s.ctx.append(s.pool, q, k, v, rotation, bounds([17, 23]), ints(starts), s.table_dev, q_out, k_out)
+        assert torch.equal(s.pool, before) and torch.isnan(q_out).all() and torch.isnan(k_out).all() and s.ctx.report() == (40, 0)
+        s.ctx.read(s.pool, *seen, bounds([17, 23]), ints(starts), s.table_dev)
+        assert all(torch.isnan(x).all() for x in seen) and s.ctx.report() == (40, 0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("heads,kv_heads,d,dtype", [(32, 8, 128, ftcache.BF16), (12, 2, 64, ftcache.F16)])
+def test_attention_many_times(heads, kv_heads, d, dtype):
+    """Sequences divided among workgroups, with the chip full: the same bits in every call and in every context."""
+    lengths = [9000, 0, 333, 4100, 17000, 1, 2500, 6400]
+    s = Setup(17, heads, kv_heads, d, 32, dtype, lengths)
+    q = s.normal(8, heads, d)
+    o = torch.empty(60, 8, heads, d, dtype=q.dtype, device="cuda")
+    at, first = ints(lengths), None
+    for _ in range(6):
+        ctx = ftcache.FtCache(heads, kv_heads, d, s.pages, 32, dtype, max_batch=8)
+        o.zero_()
+        for i in range(60):
+            ctx.attend(s.pool, q, o[i], at, s.table_dev, stream=torch.cuda.current_stream().cuda_stream)
+        torch.cuda.synchronize()
+        ctx.close()
+        first = o[0].clone() if first is None else first
+        differ = (o != first).flatten(1).any(1)
+        assert not differ.any(), differ.nonzero().flatten().tolist()
