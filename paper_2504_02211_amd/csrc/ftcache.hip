@@ -640,6 +640,7 @@ __global__ __launch_bounds__(ONE_WAVES * 64, 3) void ftcache_one(const OneArgs a
     weights(std::integral_constant<int, 2>{});
     weights(std::integral_constant<int, 3>{});
     // weights in bf16; for fp16 tokens in two words, the second what the first leaves, so that they are no coarser than the tokens
+    // (for bf16 tokens two would bring the error from 2.3e-3 to that of the rounded result, 1.7e-3, in 1.5 to 9 % more time)
     uint4v ph, pl;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
