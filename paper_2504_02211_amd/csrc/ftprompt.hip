@@ -355,6 +355,7 @@ __global__ __launch_bounds__(NW * 64, 2) void ftprompt_main(const Args a) {
     issue_k(begin, lds0 + other);
     issue_v(begin, lds0 + first + TILE);
     if (tiles > begin + 1) issue_k(begin + 1, lds0 + first);
+    asm volatile("" ::: "memory");
     __builtin_amdgcn_s_waitcnt(0x0F70);
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
@@ -449,7 +450,9 @@ __global__ __launch_bounds__(NW * 64, 2) void ftprompt_main(const Args a) {
           put(to + 2, o[f][4 * g + 2], o[f][4 * g + 3]);
         }
     }
-    __builtin_amdgcn_s_waitcnt(0x0F70);
+    // (the wait itself is nothing to the compiler that stores have to stand before)
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0F70);          // (vmcnt(0): the state is where every XCD sees it)
     __syncthreads();
     uint32_t* const last = reinterpret_cast<uint32_t*>(lds);
     if (threadIdx.x == 0) {
