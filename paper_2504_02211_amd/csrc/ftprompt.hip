@@ -57,10 +57,10 @@ template <int N> __device__ __forceinline__ void load_lds16(const void* base, co
 #define FTPROMPT_NEXT(r) "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %" #r ", %[base]\n\t"
   if constexpr (N == 4)
     asm volatile("s_mov_b32 m0, %[lds]\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %0, %[base]\n\t" FTPROMPT_NEXT(1) FTPROMPT_NEXT(2) FTPROMPT_NEXT(3)
-                 ::"v"(off[0]), "v"(off[1]), "v"(off[2 % N]), "v"(off[3 % N]), [base] "s"(base), [lds] "s"(lds_addr) : "memory", "scc");
+                 ::"v"(off[0]), "v"(off[1]), "v"(off[2 % N]), "v"(off[3 % N]), [base] "s"(base), [lds] "s"(lds_addr) : "memory", "scc", "m0");
   else
     asm volatile("s_mov_b32 m0, %[lds]\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %0, %[base]\n\t" FTPROMPT_NEXT(1)
-                 ::"v"(off[0]), "v"(off[1]), [base] "s"(base), [lds] "s"(lds_addr) : "memory", "scc");
+                 ::"v"(off[0]), "v"(off[1]), [base] "s"(base), [lds] "s"(lds_addr) : "memory", "scc", "m0");
 #undef FTPROMPT_NEXT
 }
 

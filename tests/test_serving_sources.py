@@ -1,4 +1,4 @@
-"""What the serving kernels' sources have to say to the compiler for their hand-written waits to hold.
+"""What the serving kernels' sources have to say to the compiler for their hand-written waits and register writes to hold.
 (Where it is missing, today's compiler may still order things well: no result shows it.)"""
 import os
 import re
@@ -22,3 +22,10 @@ def test_no_memory_operation_moves_behind_a_wait_that_counts_it(name):
     assert waits
     for at in waits:
         assert text[:at].rstrip().endswith('asm volatile("" ::: "memory");'), text[max(0, at - 200):at + 40]
+
+
+@pytest.mark.parametrize("name", ["ftprompt.hip", "ftcache.hip", "ftserve_device.h"])
+def test_assembly_that_writes_m0_says_so(name):
+    for statement in re.findall(r"asm volatile\((?:[^;]|(?<=\\n\\t);)*;", source(name)):
+        if re.search(r"s_\w+ m0,", statement):
+            assert re.search(r':[^:]*"m0"[^:]*\);$', statement), statement
