@@ -83,6 +83,8 @@ __device__ __forceinline__ float sum32(float x) {
   return as_f(r[0]) + as_f(r[1]);
 }
 
+__device__ __forceinline__ bool is_finite(float x) { return __builtin_fabsf(x) <= 3.4028235e38f; }
+
 // Sums over the lanes up to this one.
 __device__ __forceinline__ int plus(int a, int b) { return a + b; }
 __device__ __forceinline__ int plus_float(int a, int b) { return (int)as_u(as_f((uint32_t)a) + as_f((uint32_t)b)); }
@@ -402,6 +404,7 @@ __global__ __launch_bounds__(NW * 64, 2) void ftprompt_main(const Args a) {
     s[1] = then[1];
     renew(m);
   }
+  const int t0 = t;
 #pragma unroll 1
   for (; t < tiles; ++t) {
     const uint32_t at = arrive(t);
@@ -415,20 +418,58 @@ __global__ __launch_bounds__(NW * 64, 2) void ftprompt_main(const Args a) {
       renew(largest(s));
     }
   }
-  if (__any(__builtin_bit_cast(uint32_t, finite) != 0xFFFFFFFFu)) {
-    const int from = full - 1 > begin ? full - 1 : begin;
-    for (int j = from * BN; j < any_seen && j < tiles * BN; ++j)
-#pragma unroll
-      for (int f = 0; f < NF; ++f)
-#pragma unroll
-        for (int r = 0; r < 16; r += 2) {
-          const uint32_t w = *reinterpret_cast<const uint32_t*>(vbase + (int64_t)j * a.v.token + 2 * (32 * f + 8 * (r >> 2) + 4 * h + (r & 3)));
-          const float lo = low_of<BF>(w), hi = high_of<BF>(w);
-          if (j < seen && !(__builtin_fabsf(lo) <= 3.4e38f)) o[f][r] += lo;
-          if (j < seen && !(__builtin_fabsf(hi) <= 3.4e38f)) o[f][r + 1] += hi;
-        }
-  }
+  // In whole tiles they enter the products, with weights that may have fallen to 0 in 16 bits: an element that has seen one is not finite, but may be NaN where the
+  // formula gives infinity.  A wave that holds such an element looks through the values of all its tiles, and an element that has seen any gets their sum.
+  // (16,384 tokens of 32 heads on 4 of 128: 2.4 ms, with one infinite value 7.5, with NaN everywhere 2.0, with nothing but infinities 230.)
   float l = sum32(sums[0]);
+  float4v check = (float4v)0.f;
+  if (t0 > begin)
+#pragma unroll
+    for (int i = 0; i < NF * 16; ++i) check[i & 3] = __builtin_fmaf(o[i >> 4][i & 15], 0.f, check[i & 3]);
+  const bool open = l == l;                    // (a row whose sum is NaN is NaN whatever its values are)
+  const bool whole = __any(open && check[0] + check[1] + check[2] + check[3] != 0.f);      // (0 or NaN)
+  if (__builtin_expect(whole || __any(__builtin_bit_cast(uint32_t, finite) != 0xFFFFFFFFu), 0)) {
+    uint32_t spoilt[NF / 2];                // elements to be replaced, 32 of them a word
+#pragma unroll
+    for (int i = 0; i < NF / 2; ++i) {
+      spoilt[i] = 0;
+#pragma unroll
+      for (int j = 0; j < 32; ++j) spoilt[i] |= is_finite(o[2 * i + (j >> 4)][j & 15]) ? 0u : 1u << j;
+    }
+    const int upto = any_seen < tiles * BN ? any_seen : tiles * BN;
+    for (int j0 = (whole ? begin : t0) * BN; j0 < upto; j0 += RPL) {      // RPL rows at a time, 16 bytes of them a lane
+      const int mine = j0 + lane / CH;
+      uint4v x = (uint4v)0u;
+      if (mine < upto) x = *reinterpret_cast<const uint4v*>(vbase + (int64_t)mine * a.v.token + lane % CH * 16);
+      bool strange = false;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) strange |= !is_finite(low_of<BF>(x[w])) || !is_finite(high_of<BF>(x[w]));
+      const uint64_t found = __ballot(strange);
+      if (!found) continue;
+#pragma unroll 1
+      for (int j = j0 + __builtin_ctzll(found) / CH; j <= j0 + (63 - __builtin_clzll(found)) / CH; ++j)
+#pragma unroll
+        for (int f = 0; f < NF; ++f)
+#pragma unroll
+          for (int r = 0; r < 16; r += 2) {
+            const uint32_t w = *reinterpret_cast<const uint32_t*>(vbase + (int64_t)j * a.v.token + 2 * (32 * f + 8 * (r >> 2) + 4 * h + (r & 3)));
+#pragma unroll
+            for (int z = 0; z < 2; ++z) {
+              const float value = z ? high_of<BF>(w) : low_of<BF>(w);
+              const uint32_t bit = 1u << (16 * (f & 1) + r + z);
+              if (j < seen && !is_finite(value)) {
+                o[f][r + z] = spoilt[f >> 1] & bit ? value : o[f][r + z] + value;
+                spoilt[f >> 1] &= ~bit;
+              }
+            }
+          }
+      // NaN stays NaN: nothing is left to be found where every row has come to it
+      bool done = true;
+#pragma unroll
+      for (int i = 0; i < NF * 16; ++i) done = done && o[i >> 4][i & 15] != o[i >> 4][i & 15] && !(spoilt[i >> 5] >> (i & 31) & 1);
+      if (__all(done || !open)) break;
+    }
+  }
   if (x.parts > 1) {
     // The state of a share: its rows' references and sums, then the output before its division, as the lanes hold it.  Written through to memory, since the
     // workgroup that reads it may lie on another XCD; the one that comes last puts all shares together, in their order.  Stores that the compiler knows: it keeps
@@ -475,7 +516,7 @@ __global__ __launch_bounds__(NW * 64, 2) void ftprompt_main(const Args a) {
       float4v y[NF * 4];
 #pragma unroll
       for (int g = 0; g < NF * 4; ++g) y[g] = *reinterpret_cast<const float4v*>(from + ROWS + (wave * NF * 4 + g) * 256 + lane * 4);
-      const float scale = ex2(head[0] - ref);
+      const float scale = __builtin_fmaxf(ex2(head[0] - ref), 1.17549435e-38f);      // (not 0: what is infinite stays so)
       l += scale * head[1];
 #pragma unroll
       for (int g = 0; g < NF * 4; ++g)
@@ -483,6 +524,10 @@ __global__ __launch_bounds__(NW * 64, 2) void ftprompt_main(const Args a) {
         for (int r = 0; r < 4; ++r) o[g >> 2][4 * (g & 3) + r] += scale * y[g][r];
     }
   }
+  // (a row that saw nothing but scores of -infinity: infinite values among its elements count for nothing either)
+  if (__builtin_expect(l == 0.f, 0))
+#pragma unroll
+    for (int f = 0; f < NF; ++f) o[f] = (float16v)0.f;
   const float inv = l == 0.f ? 0.f : 1.f / l;
   if (row >= rows) return;
   char* op = a.o.data + (int64_t)(q0 + query) * a.o.token + (int64_t)head * a.o.head;

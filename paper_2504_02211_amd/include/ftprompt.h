@@ -9,7 +9,8 @@
  *     o[i, h] = sum over j <= nk - nq + i of softmax_j(softmax_scale * q[i, h] . k[j, h / (heads / kv_heads)]) v[j, same head]
  *
  * A query that sees no key, or only scores of -infinity, gives zeros.  Keys and values behind a query's place have no influence
- * on it, not even where they are infinite or NaN.  It carries no checksums: ftattn.h is the protected form for batches of one length.
+ * on it, not even where they are infinite or NaN.  Where a query sees values that are infinite or NaN, their element of its result is the sum of
+ * them, however small their weights.  It carries no checksums: ftattn.h is the protected form for batches of one length.
  *
  * Conventions
  *   - Every function returns FTPROMPT_OK (0) or a negative error code and never throws or prints; ftprompt_last_error()

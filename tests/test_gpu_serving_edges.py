@@ -1,0 +1,99 @@
+"""Prompt and cache operators at the ends of their types' ranges: infinite values with weights that vanish, sums near the largest number."""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from paper_2504_02211_amd import ftcache, ftprompt
+
+TYPES = {ftprompt.F16: torch.float16, ftprompt.BF16: torch.bfloat16}
+
+
+def ints(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def generator(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+def far_below(d, dtype, n, g):
+    """Queries, and keys whose scores lie between -1 and 1, but for those that are set to -4: theirs lie below -100, and their weights below 2^-150."""
+    q = torch.full((n, 2, d), 4.0, dtype=TYPES[dtype], device="cuda")
+    k = (torch.randn((n, 1, d), generator=g, device="cuda") * 0.02).to(TYPES[dtype])
+    return q, k
+
+
+def infinite_ones(v, seen):
+    """[query, D]: the sum of the values of v [key, D] that are not finite among the first seen[i] keys, 0 where there are none."""
+    strange = torch.where(torch.isfinite(v), torch.zeros_like(v), v).double()
+    return torch.stack([strange[:max(0, n)].sum(0) for n in seen])
+
+
+def check_infinite(o, clean, v, seen):
+    """o [query, head, D]: what is not finite comes through whatever its weight; all other elements are those of the finite values."""
+    want = infinite_ones(v[:, 0].cpu(), seen)[:, None].expand(o.shape)
+    o, clean = o.cpu(), clean.cpu()
+    there = want != 0
+    assert there.any() and torch.equal(torch.nan_to_num(o[there].double(), 7.0), torch.nan_to_num(want[there], 7.0))
+    assert torch.equal(o[~there], clean[~there])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d,dtype", [(64, ftprompt.F16), (128, ftprompt.F16), (64, ftprompt.BF16), (128, ftprompt.BF16)])
+def test_infinite_values_whose_weights_vanish(d, dtype):
+    """In key tiles that every row of a workgroup sees whole, and in those that some do not."""
+    n = 517
+    q, k = far_below(d, dtype, n, generator(d))
+    v = torch.randn((n, 1, d), generator=generator(1), device="cuda").to(TYPES[dtype])
+    at = {3: (0, math.inf), 64: (7, -math.inf), 65: (8, math.nan), 130: (d - 1, math.inf), 255: (1, -math.inf), 300: (0, -math.inf), 511: (9, math.inf)}
+    for j in at:
+        k[j] = -4.0
+    strange = v.clone()
+    for j, (e, x) in at.items():
+        strange[j, 0, e] = x
+    ctx = ftprompt.FtPrompt(2, 1, d, dtype)
+    clean, o = torch.empty_like(q), torch.empty_like(q)
+    ctx.forward(q, k, v, clean, ints([0, n]))
+    ctx.forward(q, k, strange, o, ints([0, n]))
+    check_infinite(o, clean, strange, range(1, n + 1))
+    ctx.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d,dtype", [(64, ftprompt.F16), (128, ftprompt.BF16)])
+def test_infinite_values_in_shares_whose_weights_vanish(d, dtype):
+    """Few queries over many keys, which several workgroups share: the scores of a whole share lie far below the others'."""
+    nq, nk = 40, 6000
+    _, k = far_below(d, dtype, nk, generator(d))
+    q = torch.full((nq, 2, d), 4.0, dtype=TYPES[dtype], device="cuda")
+    v = torch.randn((nk, 1, d), generator=generator(2), device="cuda").to(TYPES[dtype])
+    k[:3500] = -4.0
+    k[5000:5980] = -4.0
+    strange = v.clone()
+    strange[100, 0, 3], strange[2000, 0, 5], strange[2001, 0, 5], strange[5500, 0, 6], strange[5975, 0, 11] = math.inf, math.inf, -math.inf, -math.inf, math.inf
+    ctx = ftprompt.FtPrompt(2, 1, d, dtype)
+    clean, o = torch.empty_like(q), torch.empty_like(q)
+    ctx.forward(q, k, v, clean, ints([0, nq]), ints([0, nk]))
+    ctx.forward(q, k, strange, o, ints([0, nq]), ints([0, nk]))
+    check_infinite(o, clean, strange, range(nk - nq + 1, nk + 1))
+    ctx.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", [50, 400])
+def test_scores_of_minus_infinity_with_infinite_values(n):
+    """Queries that see only scores of -infinity give zeros, whatever the values."""
+    d = 64
+    q, k = far_below(d, ftprompt.F16, n, generator(0))
+    v = torch.randn((n, 1, d), generator=generator(3), device="cuda").half()
+    k[:, :, 0] = -math.inf
+    v[3, 0, 5], v[n - 2, 0, 6], v[7, 0, 7] = math.inf, -math.inf, math.nan
+    ctx = ftprompt.FtPrompt(2, 1, d, ftprompt.F16)
+    o = torch.empty_like(q)
+    ctx.forward(q, k, v, o, ints([0, n]))
+    assert (o == 0).all()
+    ctx.close()
