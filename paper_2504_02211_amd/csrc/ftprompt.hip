@@ -285,8 +285,9 @@ __global__ __launch_bounds__(NW * 64, 2) void ftprompt_main(const Args a) {
     for (int v = 0; v < 32; ++v)
       if (limit <= 8 * (v >> 2) + (v & 3)) x[v >> 4][v & 15] = -__builtin_inff();
   };
-  // fp16 weights reach 2^14 rather than 2^8, so that those far below the largest keep their bits
-  constexpr float ROOM = 8.f, UP = BF ? 0.f : 6.f;
+  // The reference lies UP below the largest score that it was made from, and weights reach 2^(ROOM + UP).  fp16: 2^14, so that those far below the largest keep their
+  // bits.  bf16: 1, so that sums of weights and values stay finite where those of the formula do.
+  constexpr float ROOM = 8.f, UP = BF ? -8.f : 6.f;
   auto largest = [&](const float16v (&x)[2]) __attribute__((always_inline)) {
     float m = __builtin_fmaxf(x[0][0], x[1][0]);
 #pragma unroll

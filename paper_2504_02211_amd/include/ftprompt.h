@@ -41,7 +41,8 @@ typedef struct {
   int32_t heads, kv_heads;  /* heads: a multiple of kv_heads; query head h reads key / value head h / (heads / kv_heads) */
   int32_t head_dim;         /* 64 or 128 */
   int32_t in_dtype;         /* FTPROMPT_F16 | FTPROMPT_BF16: the products run on the MFMA of that type with fp32 accumulation;
-                               weights are rounded to it before they meet the values */
+                               weights are rounded to it before they meet the values.  Sums of keys' weights of at most 1 (bf16; 2^14
+                               in fp16) times values are held in fp32: in bf16 keys * max|v| has to stay below its largest number */
   int32_t out_dtype;        /* FTPROMPT_F32, or in_dtype */
   float softmax_scale;      /* <= 0 selects 1/sqrt(head_dim) */
   int32_t device;           /* HIP device ordinal */

@@ -97,3 +97,22 @@ def test_scores_of_minus_infinity_with_infinite_values(n):
     ctx.forward(q, k, v, o, ints([0, n]))
     assert (o == 0).all()
     ctx.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d", [64, 128])
+def test_prompt_values_near_the_largest_number(d):
+    """Sums of weights of at most 1 times values stay finite: 128 of 2e36.  Scores of the second half of the keys lie 7.2 powers of two above the first's."""
+    n = 128
+    q = torch.ones((n, 2, d), dtype=torch.bfloat16, device="cuda")
+    k = (torch.randn((n, 1, d), generator=generator(d), device="cuda") * 0.02).bfloat16()
+    k[64:] += 5.0 / math.sqrt(d)
+    v = (torch.rand((n, 1, d), generator=generator(4), device="cuda") * 1e36 + 1e36).bfloat16()
+    ctx = ftprompt.FtPrompt(2, 1, d, ftprompt.BF16)
+    o = torch.empty_like(q)
+    ctx.forward(q, k, v, o, ints([0, n]))
+    s = (q[:, 0].double() @ k[:, 0].double().T / math.sqrt(d)).masked_fill(torch.ones(n, n, device="cuda").triu(1) > 0, -math.inf)
+    want = s.softmax(1) @ v[:, 0].double()
+    # weights rounded to bf16, divided by the sum of the rounded ones: u = 2^-8 of each and of their sum; the result's rounding another u; fp32 sums
+    assert ((o.double() - want[:, None]).abs() <= (3 * 2.0 ** -8 + 2.0 ** -14) * 2e36).all()
+    ctx.close()
