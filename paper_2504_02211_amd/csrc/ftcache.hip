@@ -577,6 +577,9 @@ __global__ __launch_bounds__(ONE_WAVES * 64, 3) void ftcache_one(const OneArgs a
     x.par = *reinterpret_cast<const uint32_t*>(ppool + (vpage + vin * 8));
     return x;
   };
+  // The reference lies DOWN above the largest score that it was made from, and weights reach 2^(8 - DOWN).  bf16: a weight times its value's scale meets 128 + c, up to
+  // 143 of 15 steps that span at most twice the largest |v|; at 2^-5 of weight their sums stay finite where those of the formula do.
+  constexpr float DOWN = BF ? 13.f : 0.f;
   auto step = [&](int t0, const Loaded<D>& y) __attribute__((always_inline)) {
     float4v s[2];
 #pragma unroll
@@ -611,10 +614,10 @@ __global__ __launch_bounds__(ONE_WAVES * 64, 3) void ftcache_one(const OneArgs a
 #pragma unroll
     for (int j = 2; j < 8; ++j) m = __builtin_fmaxf(m, x[j]);
     m *= alpha;
-    if (__any(m > ref + 8.f)) {
+    if (__any(m > ref + (8.f - DOWN))) {
       m = __builtin_fmaxf(m, __shfl_xor(m, 16));
       m = __builtin_fmaxf(m, __shfl_xor(m, 32));
-      const float next = __builtin_fmaxf(m, ref), f = ex2(ref - next);
+      const float next = __builtin_fmaxf(m + DOWN, ref), f = ex2(ref - next);
       ref = next;
       l *= f;
       z *= f;

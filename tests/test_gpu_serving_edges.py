@@ -116,3 +116,30 @@ def test_prompt_values_near_the_largest_number(d):
     # weights rounded to bf16, divided by the sum of the rounded ones: u = 2^-8 of each and of their sum; the result's rounding another u; fp32 sums
     assert ((o.double() - want[:, None]).abs() <= (3 * 2.0 ** -8 + 2.0 ** -14) * 2e36).all()
     ctx.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d,n", [(64, 100), (128, 100), (64, 5000)])
+def test_cached_values_near_the_largest_number(d, n):
+    """As many as let sums of weights of at most 1 times values stay finite."""
+    top = 2.5e38 / n
+    k = torch.randn((n, 1, d), generator=generator(d), device="cuda").bfloat16()
+    v = ((torch.rand((n, 1, d), generator=generator(5), device="cuda") * 2 - 1) * top).bfloat16()
+    q = torch.randn((1, 2, d), generator=generator(6), device="cuda").bfloat16()
+    pages = (n + 15) // 16
+    ctx = ftcache.FtCache(2, 1, d, pages, 16, ftcache.BF16)
+    pool = torch.zeros(pages * ctx.page_bytes, dtype=torch.uint8, device="cuda")
+    table = torch.arange(pages, dtype=torch.int32, device="cuda")[None]
+    rotation = torch.from_numpy(ftcache.rotation_table(n, d)).cuda()
+    ctx.append(pool, None, k, v, rotation, ints([0, n]), ints([0]), table, None, None)
+    o = torch.empty_like(q)
+    ctx.attend(pool, q, o, ints([n]), table)
+    seen = [torch.empty_like(k) for _ in range(2)]
+    ctx.read(pool, *seen, ints([0, n]), ints([0]), table)
+    ks, vs = (x[:, 0].double() for x in seen)
+    want = (q[0].double() @ ks.T / math.sqrt(d)).softmax(-1) @ vs
+    # cached keys rounded to bf16 by read: a score is off by at most 2^-8 * sum |q k| / sqrt(d); the weight by twice as much, relatively; the weights'
+    # rounding over codes 2 * 2^-8, read's rounding of values and the result's own 2^-8 each, fp32 sums
+    scores = 2.0 ** -8 * (q[0].double().abs() @ ks.abs().T / math.sqrt(d)).max()
+    assert ((o[0].double() - want).abs() <= (2 * scores + 4 * 2.0 ** -8 + 2.0 ** -14) * vs.abs().max()).all()
+    ctx.close()
