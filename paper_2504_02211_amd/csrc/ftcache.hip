@@ -287,10 +287,8 @@ __global__ __launch_bounds__(256) void ftcache_put(const Args a) {
 }
 
 // the type's finite numbers: a scale that was rounded up can take the largest code of the largest element beyond them (NaN stays)
-template <bool BF> __device__ __forceinline__ float held(float x) {
-  constexpr float top = BF ? 3.38953139e38f : 65504.f;
-  return x > top ? top : x < -top ? -top : x;
-}
+template <bool BF> __device__ __forceinline__ constexpr float largest() { return BF ? 3.38953139e38f : 65504.f; }
+template <bool BF> __device__ __forceinline__ float held(float x) { return x > largest<BF>() ? largest<BF>() : x < -largest<BF>() ? -largest<BF>() : x; }
 
 template <int D, bool BF>
 __global__ __launch_bounds__(256) void ftcache_get(const Args a) {
@@ -702,8 +700,14 @@ __global__ __launch_bounds__(ONE_WAVES * 64, 3) void ftcache_one(const OneArgs a
   auto finish = [&](int row, int e, float4v value, float sum) {
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
     char* op = a.o.data + (int64_t)p.b * a.o.token + (int64_t)(head0 + row) * a.o.head;
-    if constexpr (F32OUT) *reinterpret_cast<float4v*>(op + 4 * e) = value * inv;
-    else *reinterpret_cast<uint2v*>(op + 2 * e) = uint2v{pack2<BF>(value[0] * inv, value[1] * inv), pack2<BF>(value[2] * inv, value[3] * inv)};
+    value *= inv;
+    if constexpr (F32OUT) *reinterpret_cast<float4v*>(op + 4 * e) = value;
+    else {
+      const float most = __builtin_fmaxf(__builtin_fmaxf(__builtin_fabsf(value[0]), __builtin_fabsf(value[1])), __builtin_fmaxf(__builtin_fabsf(value[2]), __builtin_fabsf(value[3])));
+      if (__builtin_expect(__any(most > largest<BF>()), 0))      // (as values read back are held; rare)
+        value = float4v{held<BF>(value[0]), held<BF>(value[1]), held<BF>(value[2]), held<BF>(value[3])};
+      *reinterpret_cast<uint2v*>(op + 2 * e) = uint2v{pack2<BF>(value[0], value[1]), pack2<BF>(value[2], value[3])};
+    }
   };
   constexpr int CD = D / 4;               // columns of four elements of a row
   for (int x = tid; x < rows * CD; x += THREADS) {

@@ -143,3 +143,26 @@ def test_cached_values_near_the_largest_number(d, n):
     scores = 2.0 ** -8 * (q[0].double().abs() @ ks.abs().T / math.sqrt(d)).max()
     assert ((o[0].double() - want).abs() <= (2 * scores + 4 * 2.0 ** -8 + 2.0 ** -14) * vs.abs().max()).all()
     ctx.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [ftcache.F16, ftcache.BF16])
+def test_cached_values_beyond_the_largest_number(dtype):
+    """A scale that was rounded up takes the largest code of the largest number beyond it: the result is held to the type's numbers as a value read back is."""
+    d, top = 64, float(torch.finfo(TYPES[dtype]).max)
+    v = torch.full((3, 1, d), top, device="cuda")
+    v[:, 0, ::2] *= -1
+    v = v.to(TYPES[dtype])
+    k = torch.ones_like(v)
+    q = torch.ones((1, 1, d), dtype=v.dtype, device="cuda")
+    ctx = ftcache.FtCache(1, 1, d, 1, 16, dtype)
+    pool = torch.zeros(ctx.page_bytes, dtype=torch.uint8, device="cuda")
+    table, rotation = ints([[0]]), torch.from_numpy(ftcache.rotation_table(16, d)).cuda()
+    ctx.append(pool, None, k, v, rotation, ints([0, 3]), ints([0]), table, None, None)
+    o, seen = torch.empty_like(q), [torch.empty_like(k) for _ in range(2)]
+    ctx.read(pool, *seen, ints([0, 3]), ints([0]), table)
+    ctx.attend(pool, q, o, ints([1]), table)
+    assert torch.isfinite(seen[1]).all() and torch.isfinite(o).all()
+    # one token, weight 1: the same value, but for the rounding of weight times scale over 15 steps and that of the offset's sums
+    assert ((o[0].double() - seen[1][0].double()).abs() <= (2 * 2.0 ** -8 + 2.0 ** -8) * top).all()
+    ctx.close()
