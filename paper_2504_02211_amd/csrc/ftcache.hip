@@ -885,7 +885,7 @@ extern "C" int ftcache_create(const ftcache_config* cfg, ftcache_ctx** out) {
   if (cfg->out_dtype != FTCACHE_F32 && cfg->out_dtype != cfg->in_dtype) return cfail(nullptr, FTCACHE_EINVAL, "out_dtype must be F32 or the input type");
   if (cfg->rotary_dim < 0 || cfg->rotary_dim > cfg->head_dim || cfg->rotary_dim % 16) return cfail(nullptr, FTCACHE_EUNSUPPORTED, "rotary_dim must be a multiple of 16 up to head_dim");
   if (cfg->interleaved != 0 && cfg->interleaved != 1) return cfail(nullptr, FTCACHE_EINVAL, "interleaved must be 0 or 1");
-  if (!(std::fabs(cfg->softmax_scale) <= 3.0e38f)) return cfail(nullptr, FTCACHE_EINVAL, "softmax_scale is not finite");
+  if (!(std::fabs(cfg->softmax_scale) <= 3.0e38f) || cfg->softmax_scale * LOG2E > 3.4e38f) return cfail(nullptr, FTCACHE_EINVAL, "softmax_scale is not finite, or too large");
   if (cfg->max_batch < 1 || cfg->max_batch > 65536) return cfail(nullptr, FTCACHE_EINVAL, "max_batch must be 1 to 65536");
   ftcache_ctx* c = new (std::nothrow) ftcache_ctx();
   if (!c) return cfail(nullptr, FTCACHE_ENOMEM, "out of host memory");

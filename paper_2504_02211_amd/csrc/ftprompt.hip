@@ -585,7 +585,7 @@ extern "C" int ftprompt_create(const ftprompt_config* cfg, ftprompt_ctx** out) {
   if (cfg->head_dim != 64 && cfg->head_dim != 128) return pfail(nullptr, FTPROMPT_EUNSUPPORTED, "head_dim must be 64 or 128");
   if (cfg->in_dtype != FTPROMPT_F16 && cfg->in_dtype != FTPROMPT_BF16) return pfail(nullptr, FTPROMPT_EINVAL, "in_dtype must be F16 or BF16");
   if (cfg->out_dtype != FTPROMPT_F32 && cfg->out_dtype != cfg->in_dtype) return pfail(nullptr, FTPROMPT_EINVAL, "out_dtype must be F32 or the input type");
-  if (!(std::fabs(cfg->softmax_scale) <= 3.0e38f)) return pfail(nullptr, FTPROMPT_EINVAL, "softmax_scale is not finite");
+  if (!(std::fabs(cfg->softmax_scale) <= 3.0e38f) || cfg->softmax_scale * LOG2E > 3.4e38f) return pfail(nullptr, FTPROMPT_EINVAL, "softmax_scale is not finite, or too large");
   ftprompt_ctx* c = new (std::nothrow) ftprompt_ctx();
   if (!c) return pfail(nullptr, FTPROMPT_ENOMEM, "out of host memory");
   c->cfg = *cfg;

@@ -123,3 +123,11 @@ def test_kernels_spill_no_vector_registers():
     mine = {n: k for n, k in built_kernels(LIB_PATH).items() if "ftprompt_main" in n or "ftcache_" in n}
     assert len(mine) == 8 + 8 + 4 + 8
     assert {n for n, k in mine.items() if k[".vgpr_spill_count"] or k[".private_segment_fixed_size"]} == set()
+
+
+@pytest.mark.parametrize("scale", [2.4e38, 2.9e38])
+def test_softmax_scales_beyond_what_the_kernels_hold(scale):
+    """The kernels multiply by log2(e) first: a scale above 3.4e38 / log2(e) would be infinite there, and a score of 0 NaN."""
+    for module, name, fields in ((ftprompt, "ftprompt", PROMPT), (ftcache, "ftcache", CACHE)):
+        rc, message = create(module, name, {**fields, "softmax_scale": scale})
+        assert rc == -1 and "softmax" in message
