@@ -866,10 +866,12 @@ const char* places_of(const ftcache_places* p, Places& out) {
   if (!p || !p->cu_seqlens || !p->starts || !p->page_table) return "null argument";
   if (p->batch < 1 || p->tokens < 0) return "batch must be >= 1 and tokens >= 0";
   if (p->table_width < 1 || p->table_stride < p->table_width) return "table_width must be >= 1 and at most table_stride";
-  if ((int64_t)p->tokens / 8 + 2ll * p->batch > 0x7FFFFFFFll) return "too many tokens";
   out = Places{p->cu_seqlens, p->starts, p->page_table, p->table_stride, p->batch, p->tokens, p->table_width};
   return nullptr;
 }
+// blocks of 8 places that new tokens can touch: workgroups of append and read
+int64_t blocks_of(const Places& p) { return (int64_t)p.tokens / 8 + 2ll * p.batch; }
+const char* const TOO_MANY = "more tokens and sequences than a launch has workgroups for";
 }  // namespace
 
 extern "C" int ftcache_create(const ftcache_config* cfg, ftcache_ctx** out) {
@@ -966,7 +968,8 @@ extern "C" int ftcache_append(ftcache_ctx* c, void* pool, const ftcache_places* 
   a.heads = e.heads;
   a.rotary = e.rotary_dim;
   a.refused = c->refused;
-  const int blocks = a.at.tokens / 8 + 2 * a.at.batch, items = (a.q.data ? e.heads : 0) + e.kv_heads;
+  if (blocks_of(a.at) > MOST_GROUPS) return cfail(c, FTCACHE_EUNSUPPORTED, TOO_MANY);
+  const int blocks = (int)blocks_of(a.at), items = (a.q.data ? e.heads : 0) + e.kv_heads;
   // few blocks: their heads are dealt to more workgroups
   int split = (SPLIT_TO + blocks - 1) / blocks;
   split = split < 1 ? 1 : split > (items + 3) / 4 ? (items + 3) / 4 : split;
@@ -990,7 +993,8 @@ extern "C" int ftcache_read(ftcache_ctx* c, const void* pool, const ftcache_plac
   if (none) return FTCACHE_OK;
   a.pool = pool_of(c, pool);
   a.refused = c->refused;
-  const int blocks = a.at.tokens / 8 + 2 * a.at.batch, items = 2 * e.kv_heads;
+  if (blocks_of(a.at) > MOST_GROUPS) return cfail(c, FTCACHE_EUNSUPPORTED, TOO_MANY);
+  const int blocks = (int)blocks_of(a.at), items = 2 * e.kv_heads;
   int split = (SPLIT_TO + blocks - 1) / blocks;
   split = split < 1 ? 1 : split > (items + 3) / 4 ? (items + 3) / 4 : split;
   OnDevice here(e.device);
@@ -1023,6 +1027,7 @@ extern "C" int ftcache_attend(ftcache_ctx* c, const void* pool, int32_t batch, c
   const int64_t units = ((int64_t)a.most + ONE_UNIT - 1) / ONE_UNIT, room = units <= SHORT ? batch : units * batch;
   if (units * batch > 0x7FFFFFFFll) return cfail(c, FTCACHE_EUNSUPPORTED, "the page table has room for too many tokens");
   const int64_t pieces = room < (int64_t)c->chunks + batch ? room : (int64_t)c->chunks + batch;
+  if (pieces * e.kv_heads * c->row_tiles > MOST_GROUPS) return cfail(c, FTCACHE_EUNSUPPORTED, TOO_MANY);
   a.group = e.heads / e.kv_heads;
   a.row_tiles = c->row_tiles;
   a.chunks = c->chunks;

@@ -642,7 +642,7 @@ extern "C" int ftprompt_forward(ftprompt_ctx* c, const ftprompt_rows* q, const f
   const int32_t divide = total_k > (FEW + FEW / 3) * BN && batch <= MANY;
   // row tiles at most, and as many shares again as they are divided into at most
   const int64_t shares = (int64_t)total_q * group / BM + batch + (divide ? (SHARES + e.kv_heads - 1) / e.kv_heads : 0);
-  if ((int64_t)total_q * group > 0x7FFFFF00ll || shares * e.kv_heads > 0x7FFFFFFFll) return pfail(c, FTPROMPT_EUNSUPPORTED, "too many rows");
+  if ((int64_t)total_q * group > 0x7FFFFF00ll || shares * e.kv_heads > MOST_GROUPS) return pfail(c, FTPROMPT_EUNSUPPORTED, "too many rows");
   Args a{r[0], r[1], r[2], r[3], cu_q, cu_k, batch, total_q, total_k, e.kv_heads, group, divide, e.softmax_scale * LOG2E,
          reinterpret_cast<float*>(static_cast<char*>(c->scratch) + STATES * sizeof(uint32_t)), static_cast<uint32_t*>(c->scratch)};
   int before = 0;

@@ -20,6 +20,7 @@ typedef short short2v __attribute__((ext_vector_type(2)));
 typedef short short4v __attribute__((ext_vector_type(4)));
 
 constexpr float LOG2E = 1.4426950408889634f;
+constexpr int64_t MOST_GROUPS = (1ll << 24) - 1;      // workgroups of 256 threads: a launch has fewer than 2^32 threads in a dimension
 
 __device__ __forceinline__ float as_f(uint32_t u) { return __builtin_bit_cast(float, u); }
 __device__ __forceinline__ uint32_t as_u(float f) { return __builtin_bit_cast(uint32_t, f); }

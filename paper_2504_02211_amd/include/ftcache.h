@@ -62,7 +62,8 @@ typedef struct { void* data; int64_t token_stride, head_stride; } ftcache_rows;
 
 /* Which tokens a call is about.  Sequence b has rows cu_seqlens[b] .. cu_seqlens[b + 1] of the packed tokens (cu_seqlens[0] = 0; rows
  * behind the last sequence are left as they are), which stand at the places starts[b], starts[b] + 1, .. of the sequence; place p lies in
- * page page_table[b * table_stride + p / page_size].  There are 2^31 - 16 places.  Entries of the table that no place needs may hold anything. */
+ * page page_table[b * table_stride + p / page_size].  There are 2^31 - 16 places.  Entries of the table that no place needs may hold anything.
+ * tokens / 8 + 2 * batch has to be below 2^24 (FTCACHE_EUNSUPPORTED). */
 typedef struct {
   int32_t batch;             /* sequences, >= 1 */
   int32_t tokens;            /* packed rows */
@@ -95,6 +96,7 @@ int ftcache_append(ftcache_ctx* ctx, void* pool, const ftcache_places* places, c
 int ftcache_read(ftcache_ctx* ctx, const void* pool, const ftcache_places* places, const ftcache_rows* k, const ftcache_rows* v,
                  void* hip_stream);
 /* o[b, h] = softmax(softmax_scale * q[b, h] K^T) V over the first lengths[b] cached tokens of sequence b, one row per sequence.
+ * batch * kv_heads * ceil(heads / kv_heads / 16) and some thousands more have to stay below 2^24 (FTCACHE_EUNSUPPORTED).
  * A length of 0 gives zeros; a 16-bit result is held to its type's finite numbers.  Codes enter the matrix products as they are and scales and minima in 32 bits; the weights are rounded
  * to bf16 once (bf16) or to two bf16 words (fp16).  Sums are held in fp32: the elements of keys and of queries, these also times softmax_scale, have to
  * stay below 2^110 and lengths[b] * max|v| below 2^127; in bf16, value scales below 2^-113 (values below about 2^-110) lose bits. */

@@ -55,7 +55,8 @@ typedef struct { void* data; int64_t token_stride, head_stride; } ftprompt_rows;
 int ftprompt_create(const ftprompt_config* cfg, ftprompt_ctx** out);
 /* Copies the configuration in effect (defaults resolved). */
 int ftprompt_get_config(const ftprompt_ctx* ctx, ftprompt_config* effective);
-/* One pass over `batch` sequences.  cu_k may be cu_q: prompts that begin with their first key. */
+/* One pass over `batch` sequences.  cu_k may be cu_q: prompts that begin with their first key.  total_q * heads / 128 + batch * kv_heads and some
+ * hundreds more have to stay below 2^24 (FTPROMPT_EUNSUPPORTED). */
 int ftprompt_forward(ftprompt_ctx* ctx, const ftprompt_rows* q, const ftprompt_rows* k, const ftprompt_rows* v, const ftprompt_rows* o,
                      const int32_t* cu_q, const int32_t* cu_k, int32_t batch, int32_t total_q, int32_t total_k, void* hip_stream);
 int ftprompt_destroy(ftprompt_ctx* ctx);
