@@ -638,7 +638,9 @@ extern "C" int ftprompt_forward(ftprompt_ctx* c, const ftprompt_rows* q, const f
   }
   if (total_q == 0) return FTPROMPT_OK;
   const int group = e.heads / e.kv_heads;
-  // (with more sequences there are row tiles enough, and every workgroup would look through all of them)
+  // A lane of share_of looks after one sequence, so more than MANY are not divided.  With several key heads or rows there are workgroups enough all the same; without, the
+  // step shows: sequences of 1 query over 8000 keys, 8 heads on 1 of 128, bf16: 64 of them 55 us, 65 134, 256 212; of 20 queries: 102, 137, 405; on 8 key heads, 32 heads: 379, 504, 1626;
+  // of 20 queries over 2000 keys, 8 heads on 1: 43, 43, 118.
   const int32_t divide = total_k > (FEW + FEW / 3) * BN && batch <= MANY;
   // row tiles at most, and as many shares again as they are divided into at most
   const int64_t shares = (int64_t)total_q * group / BM + batch + (divide ? (SHARES + e.kv_heads - 1) / e.kv_heads : 0);
