@@ -34,6 +34,9 @@
  *     Without a fault list (and with timing off) the call is kernel launches only: no
  *     allocation, memset or copy, so it may be recorded into a HIP graph by stream capture.
  *   - One context serves one shape; calls on one context must not overlap in time.
+ *
+ * Attention over packed prompts with grouped heads and the paged key / value cache of the same library, which carry no checksums,
+ * are declared in ftprompt.h and ftcache.h, which lie with the Python package: paper_2504_02211_amd/include.
  */
 #ifndef FTATTN_H
 #define FTATTN_H

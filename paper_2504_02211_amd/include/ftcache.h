@@ -23,7 +23,8 @@
  *     them are HOST memory.  The calls leave the current device as it was.
  *   - ftcache_append, _read and _attend allocate nothing and are one kernel launch each on `hip_stream`: they may be recorded into a HIP
  *     graph by stream capture.  What the host cannot see is checked by the kernels: a page number outside the pool or a
- *     position outside the rotation table reads and writes nothing out of bounds, gives NaN in its place and is counted (ftcache_report).
+ *     position outside the rotation table reads and writes nothing out of bounds and is counted (ftcache_report).  append puts nothing into the cache for
+ *     such a token, and NaN into q_out and k_out where its position has no rotation; read and attend give NaN in its place.
  *   - append and read calls on one context may overlap in time; attend calls (which share the context's workspace)
  *     may not, captured graphs of them included.
  */
@@ -79,6 +80,8 @@ typedef struct {
   int64_t refused_sequences; /* sequences of attend whose length or pages do not exist */
 } ftcache_report_view;
 
+/* A context holds device memory for the states of sequences that attend divides, whatever the calls' sizes: 34 MB at head_dim 128, 17 MB at 64 (more
+ * only above 2048 key / value heads).  One serves all layers of a model that run one after the other, each with a pool of its own. */
 int ftcache_create(const ftcache_config* cfg, ftcache_ctx** out);
 /* Copies the configuration in effect (defaults resolved). */
 int ftcache_get_config(const ftcache_ctx* ctx, ftcache_config* effective);

@@ -52,10 +52,13 @@ typedef struct {
  * in elements and multiples of 8 (of 4 for 32-bit elements), at most 2^24. */
 typedef struct { void* data; int64_t token_stride, head_stride; } ftprompt_rows;
 
+/* A context holds device memory for the states of row tiles that are divided by their keys, whatever the calls' sizes: 69 MB at head_dim 128, 36 MB
+ * at 64.  One serves all layers of a model that run one after the other. */
 int ftprompt_create(const ftprompt_config* cfg, ftprompt_ctx** out);
 /* Copies the configuration in effect (defaults resolved). */
 int ftprompt_get_config(const ftprompt_ctx* ctx, ftprompt_config* effective);
-/* One pass over `batch` sequences.  cu_k may be cu_q: prompts that begin with their first key.  total_q * heads / 128 + batch * kv_heads and some
+/* One pass over `batch` sequences.  cu_k may be cu_q: prompts that begin with their first key.  o may be q.  Calls of more than 64 sequences divide no
+ * row tile by its keys: a few queries over long prefixes on one or two key heads are faster in calls of 64.  total_q * heads / 128 + batch * kv_heads and some
  * hundreds more have to stay below 2^24 (FTPROMPT_EUNSUPPORTED). */
 int ftprompt_forward(ftprompt_ctx* ctx, const ftprompt_rows* q, const ftprompt_rows* k, const ftprompt_rows* v, const ftprompt_rows* o,
                      const int32_t* cu_q, const int32_t* cu_k, int32_t batch, int32_t total_q, int32_t total_k, void* hip_stream);
