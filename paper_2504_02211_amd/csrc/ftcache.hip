@@ -210,7 +210,7 @@ template <int N, bool BF> __device__ __forceinline__ Codes<N> coded(const Elemen
 }
 
 // A wave takes 8 places of a sequence, two query heads, or the key and value of a head, at a time: lane 8t + c has elements c * D/8 .. of token t.
-// Bound by memory: 20,278 tokens of 32 + 8 heads of 128 in 101 us, 484 MB at 4.8 TB/s; with one head at a time and its partners' sign by
+// Bound by memory: 20,278 tokens of 32 + 8 heads of 128 in 101 us, 484 MB at 4.8 TB/s (a copy reaches 4.9); with one head at a time and its partners' sign by
 // branches it took 147.
 template <int D, bool BF, bool PAIRS>
 __global__ __launch_bounds__(256) void ftcache_put(const Args a) {
@@ -287,8 +287,11 @@ __global__ __launch_bounds__(256) void ftcache_put(const Args a) {
 }
 
 // the type's finite numbers: a scale that was rounded up can take the largest code of the largest element beyond them (NaN stays)
-template <bool BF> __device__ __forceinline__ constexpr float largest() { return BF ? 3.38953139e38f : 65504.f; }
-template <bool BF> __device__ __forceinline__ float held(float x) { return x > largest<BF>() ? largest<BF>() : x < -largest<BF>() ? -largest<BF>() : x; }
+template <bool BF> constexpr float LARGEST = BF ? 3.38953139e38f : 65504.f;
+template <bool BF> __device__ __forceinline__ float held(float x) {
+  constexpr float top = LARGEST<BF>;
+  return x > top ? top : x < -top ? -top : x;
+}
 
 template <int D, bool BF>
 __global__ __launch_bounds__(256) void ftcache_get(const Args a) {
@@ -346,9 +349,10 @@ __global__ __launch_bounds__(256) void ftcache_get(const Args a) {
 // power of two, which the score loses again.  Value codes lie under the bits of 128 in bf16, 128 + c; the offset leaves through the sum of the weights.
 // Scale and minimum of a token are applied to its scores and to its weights, in 32 bits:
 //     score = ks (q . c) + kz (sum q),   O = sum (p vs) (c' - 8) + sum p (vz + 8 vs)
-// (about the middle of the codes, so that rounding p vs costs half of what it would).  Bound: memory where there is enough to read, 1.25 M tokens of 96 sequences,
-// 32 heads on 8 of 128, 1.36 GB in 266 us (5.1 TB/s, a copy reaches 4.9); below that the start of a piece (3 us) and putting parts together (3 us a level): 131,072
-// tokens of one sequence 23 us, 35,000 of 32 sequences 16.  Three workgroups of four waves to a CU hold the loads under way that memory takes; two, by
+// (about the middle of the codes, so that rounding p vs costs half of what it would).  Bound: loads under way where there is enough to read, 1.25 M tokens of 96 sequences,
+// 32 heads on 8 of 128, 1.36 GB in 266 us: 5.1 TB/s, where a kernel that does nothing but read reaches 7.1 (waves wait for 63 % of their time; vector instructions take
+// half of the cycles, the matrix pipe 13 %).  Below that the start of a piece (3 us) and putting parts together (3 us a level): 131,072
+// tokens of one sequence 23 us, 35,000 of 32 sequences 16.  Three workgroups of four waves to a CU; two, by
 // more registers, took 314 us for the first, four, with registers spilled, 384.
 struct OneArgs {
   Pool pool;
@@ -704,7 +708,7 @@ __global__ __launch_bounds__(ONE_WAVES * 64, 3) void ftcache_one(const OneArgs a
     if constexpr (F32OUT) *reinterpret_cast<float4v*>(op + 4 * e) = value;
     else {
       const float most = __builtin_fmaxf(__builtin_fmaxf(__builtin_fabsf(value[0]), __builtin_fabsf(value[1])), __builtin_fmaxf(__builtin_fabsf(value[2]), __builtin_fabsf(value[3])));
-      if (__builtin_expect(__any(most > largest<BF>()), 0))      // (as values read back are held; rare)
+      if (__builtin_expect(__any(most > LARGEST<BF>), 0))      // (as values read back are held; rare)
         value = float4v{held<BF>(value[0]), held<BF>(value[1]), held<BF>(value[2]), held<BF>(value[3])};
       *reinterpret_cast<uint2v*>(op + 2 * e) = uint2v{pack2<BF>(value[0], value[1]), pack2<BF>(value[2], value[3])};
     }

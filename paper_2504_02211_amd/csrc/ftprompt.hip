@@ -10,9 +10,9 @@
 // The weights then are the right-hand operand of O^T = V^T P^T as they lie, where contraction slot (h, 4s + r) stands for key 16i + 8s + 4h + r;
 // V^T in that order comes from row-major LDS tiles by transposing reads of four keys each.
 //
-// Bound: 16,384 tokens of 32 heads on 4 of 128 (2.2e12 operations) take 2.0 to 2.15 ms by card, 1030 to 1100 TFLOP/s where a large library product reaches 1222;
+// Bound: 16,384 tokens of 32 heads on 4 of 128 (2.2e12 operations) take 1.97 to 2.15 ms by card, 1020 to 1115 TFLOP/s where a large library product reaches 1222;
 // the clock falls to 1.64 GHz under it with the matrix pipe 63 % busy.  With fewer rows it is the time of a key tile in one workgroup, 1.0 us at head_dim 128 and
-// 0.7 at 64, of which a row tile needs one after the other: 24 prompts of up to 1531 tokens, 12 heads of 64, take 25 us.  Four waves of 32 rows, two
+// 0.7 at 64, of which a row tile needs one after the other: 24 prompts of up to 1531 tokens, 12 heads of 64, take 26 to 28 us.  Four waves of 32 rows, two
 // workgroups to a CU: waves of 64 rows would read half as much from LDS, but came out of the compiler with their accumulators copied (3.6 ms); three workgroups to a CU at
 // head_dim 64 have too few registers (one prompt of 16,000 tokens, 4 heads on 1: 205 us, 259 with three).
 #include "ftprompt.h"
