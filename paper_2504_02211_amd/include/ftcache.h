@@ -100,6 +100,7 @@ int ftcache_read(ftcache_ctx* ctx, const void* pool, const ftcache_places* place
                  void* hip_stream);
 /* o[b, h] = softmax(softmax_scale * q[b, h] K^T) V over the first lengths[b] cached tokens of sequence b, one row per sequence.
  * batch * kv_heads * ceil(heads / kv_heads / 16) and some thousands more have to stay below 2^24 (FTCACHE_EUNSUPPORTED).
+ * Every workgroup looks through all lengths: from some hundred sequences on the time grows with the square of the batch.
  * A length of 0 gives zeros; a 16-bit result is held to its type's finite numbers.  Codes enter the matrix products as they are and scales and minima in 32 bits; the weights are rounded
  * to bf16 once (bf16) or to two bf16 words (fp16).  Sums are held in fp32: the elements of keys and of queries, these also times softmax_scale, have to
  * stay below 2^110 and lengths[b] * max|v| below 2^127; in bf16, value scales below 2^-113 (values below about 2^-110) lose bits. */
