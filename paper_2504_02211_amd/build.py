@@ -13,12 +13,14 @@ SOURCES = [os.path.join(PKG, "csrc", "ftattn.hip"), os.path.join(PKG, "csrc", "f
            os.path.join(PKG, "csrc", "ftattn_split.hip"), os.path.join(PKG, "csrc", "ftattn_self.hip"),
            os.path.join(PKG, "csrc", "ftgemm.hip"), os.path.join(PKG, "csrc", "ftgemm_f16.hip"),
            os.path.join(PKG, "csrc", "ftgemm_bf16.hip"), os.path.join(PKG, "csrc", "ftdecoupled.hip"),
-           os.path.join(PKG, "csrc", "ftprompt.hip"), os.path.join(PKG, "csrc", "ftcache.hip")]
+           os.path.join(PKG, "csrc", "ftprompt.hip"), os.path.join(PKG, "csrc", "ftcache.hip"),
+           os.path.join(PKG, "csrc", "ftint8.hip"), os.path.join(PKG, "csrc", "ftdecay.hip"), os.path.join(PKG, "csrc", "ftsample.hip")]
 HEADERS = [os.path.join(PKG, "csrc", "ftattn_device.h"), os.path.join(PKG, "csrc", "ftattn_main.h"),
            os.path.join(PKG, "csrc", "ftgemm_main.h"), os.path.join(ROOT, "include", "ftattn.h"),
            os.path.join(PKG, "csrc", "ftserve_device.h"),
            os.path.join(ROOT, "include", "ftgemm.h"), os.path.join(ROOT, "include", "ftdecoupled.h"),
-           os.path.join(PKG, "include", "ftprompt.h"), os.path.join(PKG, "include", "ftcache.h")]
+           os.path.join(PKG, "include", "ftprompt.h"), os.path.join(PKG, "include", "ftcache.h"),
+           os.path.join(PKG, "include", "ftint8.h"), os.path.join(PKG, "include", "ftdecay.h"), os.path.join(PKG, "include", "ftsample.h")]
 OBJDIR = os.path.join(PKG, "_build")
 
 

@@ -102,6 +102,23 @@ def ints(t, name: str, n: int, device: int) -> int:
     raise ValueError(f"{name}: tensor has {t.numel()} elements, expected {n}")
 
 
+def array(t, name: str, n: int, dtype, device: int) -> int:
+    """Address of a contiguous device tensor of n elements of a torch type."""
+    if isinstance(t, _base._torch_tensor) and t.dtype is dtype and t.get_device() == device and t.is_contiguous() and t.numel() == n:
+        return t.data_ptr()
+    if not hasattr(t, "data_ptr"):
+        raise TypeError(f"{name}: expected a device tensor, got {type(t).__name__}")
+    if t.dtype is not dtype:
+        raise ValueError(f"{name}: tensor is {t.dtype}, expected {dtype}")
+    if not t.is_cuda:
+        raise ValueError(f"{name}: tensor is not on a GPU")
+    if t.get_device() != device:
+        raise ValueError(f"{name}: tensor is on device {t.get_device()}, the context on device {device}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name}: tensor is not contiguous")
+    raise ValueError(f"{name}: tensor has {t.numel()} elements, expected {n}")
+
+
 class FtPrompt:
     """One context of the C library: causal attention of packed sequences for one set of heads on one device."""
 
