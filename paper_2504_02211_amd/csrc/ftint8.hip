@@ -4,6 +4,8 @@
 
 #include <new>
 #include <string>
+#include <type_traits>
+#include <utility>
 
 namespace ftint8 {
 using namespace ftserve;
@@ -21,13 +23,41 @@ template <int DT> __device__ __forceinline__ float element(const void* row, int6
 struct EncodeArgs {
   const char* x;
   int64_t stride;      // bytes
-  int32_t k, k_padded;
+  int32_t k, k_padded, rows;
   int8_t* codes;
   float* scales;
 };
 
-// A row a workgroup: its largest magnitude, then its codes.
-template <int DT> __global__ __launch_bounds__(256) void ftint8_encode_rows(const EncodeArgs a) {
+// How the rows of one call are encoded, from the largest magnitude (as its bits) on: infinity and NaN are above all numbers.  Rows below 2^-100 are taken times
+// 2^100, where the reciprocal stays finite.
+struct Coding {
+  float up, inverse;
+  bool fine;
+  __device__ __forceinline__ explicit Coding(uint32_t most) {
+    fine = most < 0x7F800000u;
+    up = as_f(most) < 0x1p-100f ? 0x1p100f : 1.f;
+    inverse = most == 0 || !fine ? 0.f : 127.f * (1.f / (as_f(most) * up));
+  }
+  // The code in the lowest byte.  (The sum with 1.5 * 2^23 rounds to a whole number, ties to even; the product is rounded before it: no fused instruction.)
+  __device__ __forceinline__ uint32_t code(float x) const {
+    float y = x * up * inverse;
+    asm("" : "+v"(y));
+    return as_u(y + 12582912.f);
+  }
+};
+__device__ __forceinline__ void put_scale(const EncodeArgs& a, int row, uint32_t most, bool fine) { a.scales[row] = fine ? as_f(most) / 127.f : __builtin_nanf(""); }
+
+__device__ __forceinline__ uint32_t largest_of_wave(uint32_t x) {
+#pragma unroll
+  for (int d = 32; d; d >>= 1) {
+    const uint32_t y = __shfl_xor(x, d);
+    x = y > x ? y : x;
+  }
+  return x;
+}
+
+// Rows that begin anywhere, or are longer than the registers of a workgroup: a row a workgroup, element after element, read twice.
+template <int DT> __global__ __launch_bounds__(256) void ftint8_encode_any(const EncodeArgs a) {
   __shared__ uint32_t most_of[4];
   const int row = blockIdx.x, tid = threadIdx.x;
   const char* const x = a.x + (int64_t)row * a.stride;
@@ -36,21 +66,62 @@ template <int DT> __global__ __launch_bounds__(256) void ftint8_encode_rows(cons
     const uint32_t u = as_u(element<DT>(x, i)) & 0x7FFFFFFFu;
     most = u > most ? u : most;
   }
-  for (int d = 32; d; d >>= 1) {
-    const uint32_t y = __shfl_xor(most, d);
-    most = y > most ? y : most;
-  }
+  most = largest_of_wave(most);
   if ((tid & 63) == 0) most_of[tid >> 6] = most;
   __syncthreads();
   for (int w = 0; w < 4; ++w) most = most_of[w] > most ? most_of[w] : most;
-  // infinities and NaN are above all numbers.  Rows below 2^-100 are taken times 2^100, where the quotient stays finite.
-  const bool fine = most < 0x7F800000u;
-  const float up = as_f(most) < 0x1p-100f ? 0x1p100f : 1.f, inverse = most == 0 || !fine ? 0.f : 127.f * (1.f / (as_f(most) * up));
-  if (tid == 0) a.scales[row] = fine ? as_f(most) / 127.f : __builtin_nanf("");
+  const Coding c(most);
+  if (tid == 0) put_scale(a, row, most, c.fine);
   int8_t* const codes = a.codes + (int64_t)row * a.k_padded;
-  for (int i = tid; i < a.k_padded; i += 256) {
-    const float y = i < a.k && fine ? element<DT>(x, i) * up * inverse : 0.f;
-    codes[i] = (int8_t)(int)__builtin_rintf(y);
+  for (int i = tid; i < a.k_padded; i += 256) codes[i] = i < a.k && c.fine ? (int8_t)c.code(element<DT>(x, i)) : (int8_t)0;
+}
+
+// Rows that begin at multiples of 16 bytes: WAVES waves hold a row in their registers, 8 elements in each of VECS words of a lane, from the one read to the write.
+// Bound: memory.
+template <int DT, int WAVES, int VECS> __global__ __launch_bounds__(256) void ftint8_encode_rows(const EncodeArgs a) {
+  __shared__ uint32_t most_of[4];
+  const int wave = threadIdx.x >> 6, t = threadIdx.x % (64 * WAVES), row = blockIdx.x * (4 / WAVES) + wave / WAVES;
+  const bool on = row < a.rows;
+  const char* const x = a.x + (int64_t)(on ? row : a.rows - 1) * a.stride;
+  uint4v v[VECS];
+  uint32_t most16 = 0;      // (of the magnitudes' 16 bits, which are ordered as the numbers are)
+#pragma unroll
+  for (int i = 0; i < VECS; ++i) {
+    const int at = 8 * (t + 64 * WAVES * i);
+    v[i] = (uint4v)0u;
+    if (at + 8 <= a.k) v[i] = *reinterpret_cast<const uint4v*>(x + 2 * at);
+    else if (at < a.k)
+      for (int e = 0; e < a.k - at; ++e) v[i][e >> 1] |= (uint32_t)reinterpret_cast<const uint16_t*>(x)[at + e] << 16 * (e & 1);
+  }
+#pragma unroll
+  for (int i = 0; i < VECS; ++i)
+#pragma unroll
+    for (int w = 0; w < 4; ++w)
+      most16 = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(ushort2v, most16), __builtin_bit_cast(ushort2v, v[i][w] & 0x7FFF7FFFu)));
+  most16 = (most16 & 0xFFFFu) > most16 >> 16 ? most16 & 0xFFFFu : most16 >> 16;
+  most16 = largest_of_wave(most16);
+  if constexpr (WAVES == 4) {
+    if ((threadIdx.x & 63) == 0) most_of[wave] = most16;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < 4; ++w) most16 = most_of[w] > most16 ? most_of[w] : most16;
+  }
+  if (!on) return;
+  const uint32_t most = as_u(low_of<DT == FTINT8_BF16>(most16));
+  const Coding c(most);
+  if (t == 0) put_scale(a, row, most, c.fine);
+  int8_t* const codes = a.codes + (int64_t)row * a.k_padded;
+#pragma unroll
+  for (int i = 0; i < VECS; ++i) {
+    const int at = 8 * (t + 64 * WAVES * i);
+    uint2v out;
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+      const uint32_t lo = v[i][2 * w], hi = v[i][2 * w + 1];
+      const uint32_t c0 = c.code(low_of<DT == FTINT8_BF16>(lo)), c1 = c.code(high_of<DT == FTINT8_BF16>(lo)), c2 = c.code(low_of<DT == FTINT8_BF16>(hi)), c3 = c.code(high_of<DT == FTINT8_BF16>(hi));
+      out[w] = c.fine ? __builtin_amdgcn_perm(c1, c0, 0x0C0C0400u) | __builtin_amdgcn_perm(c3, c2, 0x04000C0Cu) : 0u;
+    }
+    if (at < a.k_padded) *reinterpret_cast<uint2v*>(codes + at) = out;
   }
 }
 
@@ -60,46 +131,252 @@ struct ProductArgs {
   char* y;
   int64_t y_stride;      // bytes
   int32_t m, n, k_padded;
+  int32_t wide;          // rows of y begin at multiples of 16 bytes
 };
 
-// Y^T = W X^T: a wave takes 16 features and 64 tokens of a tile of 64 x 64.
-template <int DT> __global__ __launch_bounds__(256) void ftint8_tile(const ProductArgs a) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, lq = lane & 15, lg = lane >> 4;
-  const int m0 = blockIdx.y * 64, n0 = blockIdx.x * 64 + wave * 16;
-  if (n0 >= a.n) return;
-  int4v acc[4];
-  const int8_t *wp, *xp[4];
-  wp = a.w + (int64_t)(n0 + lq < a.n ? n0 + lq : a.n - 1) * a.k_padded + 16 * lg;
-  for (int t = 0; t < 4; ++t) {
-    const int r = m0 + 16 * t + lq;
-    xp[t] = a.x + (int64_t)(r < a.m ? r : a.m - 1) * a.k_padded + 16 * lg;
-    acc[t] = (int4v)0;
+template <int N> __device__ __forceinline__ void wait_loads() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | ((N >> 4) << 14));
+}
+__device__ __forceinline__ void wait_lds() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0xC07F);
+}
+__device__ __forceinline__ void barrier() {
+  __builtin_amdgcn_sched_barrier(0);
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_sched_barrier(0);
+}
+// 16 bytes per lane from (uniform base + per-lane byte offset) straight into LDS at (uniform LDS address + 16 * lane).  (Opaque to the compiler, which would wait
+// for the stage in flight before it reads another.  The wait covers a base that a vector instruction has moved to its scalar registers just before: five states.)
+__device__ __forceinline__ void load_lds16(const void* base, uint32_t off, uint32_t lds_addr) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(lds_addr) : "m0");
+}
+// f(0), f(1), ... f(N - 1) with the index as a compile-time constant
+template <class F, int... I> __device__ __forceinline__ void for_each_of(F&& f, std::integer_sequence<int, I...>) { (f(std::integral_constant<int, I>{}), ...); }
+template <int N, class F> __device__ __forceinline__ void for_each(F&& f) { for_each_of(f, std::make_integer_sequence<int, N>{}); }
+
+// A result: the sum rounded to 32 bits, times the product of the scales.
+__device__ __forceinline__ float scaled(int sum, float sx, float sw) {
+  float y = (float)sum * (sx * sw);
+  asm("" : "+v"(y));      // (rounded to 32 bits: the compiler would make one instruction of this product and its rounding to 16)
+  return y;
+}
+
+// Tile shape: BM tokens x BF features, a wave takes WT x WF blocks of 16 x 16, a ring of NST stages of 128 columns, PER_CU workgroups to a CU.
+template <int BM_, int BF_, int WT_, int WF_, int NST_, int PER_CU_ = 1> struct Tile {
+  static constexpr int BM = BM_, BF = BF_, WT = WT_, WF = WF_, NST = NST_, PER_CU = PER_CU_;
+  static constexpr int NWT = BM / (16 * WT), NWF = BF / (16 * WF), NW = NWT * NWF;      // waves along the tokens and along the features
+  static constexpr int BK = 128, STAGE = (BM + BF) * BK, LDS = NST * STAGE;
+  static constexpr int XP = BM / 8, WP = BF / 8;                                         // pieces of 8 rows, 1 KB
+  static_assert(XP % NW == 0 && WP % NW == 0 && (NW == 4 || NW == 8), "pieces split evenly");
+  static constexpr int XW = XP / NW, WW = WP / NW, NLOAD = XW + WW;                      // ... of a wave
+  static constexpr int PITCH = 16 * WF * 4 + 16;                                         // of a row of results on its way through LDS
+  static_assert(NW * 16 * PITCH <= LDS && PER_CU * LDS <= 160 * 1024 && (NST - 1) * NLOAD <= 63, "LDS; counted waits");
+};
+
+// Y^T = W X^T on 16x16x64 products: rows of weights are the left operand, tokens the right one, so that a lane holds one token per block of tokens and four features that lie
+// side by side per block of features.  The steps of 128 columns go through a ring of LDS stages that direct loads fill; a row's 16-byte chunk c lies at place c ^ (row / 2 % 8), which keeps
+// the reads of operands free of bank conflicts.  Operands are read ahead of their products, also across the border of two stages: the barrier of a stage sits AHEAD rows of
+// products before its end, where its last operands are in registers, so that no wave waits for LDS behind it.
+template <class T, int DT> __global__ __launch_bounds__(T::NW * 64, T::PER_CU * T::NW / 4) void ftint8_tile(const ProductArgs a) {
+  constexpr int WT = T::WT, WF = T::WF, NST = T::NST, BK = T::BK, STAGE = T::STAGE, NLOAD = T::NLOAD, NKS = 2, AHEAD = 3;
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  const int tid = threadIdx.x, lane = tid & 63, lq = lane & 15, lg = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wt = wave / T::NWF, wf = wave % T::NWF;
+  // Workgroups go round the 8 XCDs; each XCD gets neighbouring tiles, numbered in groups of 8 token tiles x all feature tiles, so that
+  // what it runs at a time shares rows of weights and of tokens in its L2.
+  int tm, tn;
+  {
+    const int tiles_m = (a.m + T::BM - 1) / T::BM, tiles_n = (a.n + T::BF - 1) / T::BF;
+    const int total = tiles_m * tiles_n, xcd = blockIdx.x & 7, slot = blockIdx.x >> 3, per = total >> 3, more = total & 7;
+    const int t = xcd * per + (xcd < more ? xcd : more) + slot;
+    constexpr int GM = 8;
+    const int group = t / (GM * tiles_n), first = group * GM, rows = tiles_m - first < GM ? tiles_m - first : GM, in = t - group * GM * tiles_n;
+    tm = __builtin_amdgcn_readfirstlane(first + in % rows);
+    tn = __builtin_amdgcn_readfirstlane(in / rows);
   }
-  for (int k = 0; k < a.k_padded; k += 64) {
-    const int4v w = *reinterpret_cast<const int4v*>(wp + k);
+  const int m0 = tm * T::BM, n0 = tn * T::BF, steps = a.k_padded / BK;
+  const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
+
+  // Piece p of an operand is its rows 8p .. 8p + 7; wave w takes pieces w, w + NW, ...  Rows behind the last one are the last one again (their results are not used).
+  auto swizzle = [](int row) __attribute__((always_inline)) { return row >> 1 & 7; };
+  const int chunk = (lane & 7) ^ swizzle(8 * wave + (lane >> 3));
+  uint32_t off[NLOAD];
 #pragma unroll
-    for (int t = 0; t < 4; ++t) acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w, *reinterpret_cast<const int4v*>(xp[t] + k), acc[t], 0, 0, 0);
+  for (int i = 0; i < NLOAD; ++i) {
+    const int left = i < T::XW ? a.m - m0 : a.n - n0;
+    int r = 8 * (wave + T::NW * (i < T::XW ? i : i - T::XW)) + (lane >> 3);
+    r = r < left ? r : left - 1;
+    off[i] = (uint32_t)r * (uint32_t)a.k_padded + 16u * chunk;
   }
+  const int8_t *xb = a.x + (int64_t)m0 * a.k_padded, *wb = a.w + (int64_t)n0 * a.k_padded;
+  const uint32_t wave_at = base + (uint32_t)wave * 1024u;
+  auto issue = [&](int i, uint32_t stage) __attribute__((always_inline)) {
+    load_lds16(i < T::XW ? xb : wb, off[i], wave_at + stage + (uint32_t)((i < T::XW ? T::NW * i : T::XP + T::NW * (i - T::XW)) * 1024));
+  };
+  auto next_step = [&]() __attribute__((always_inline)) { xb += BK; wb += BK; };
+
+  int4v acc[WF][WT];
 #pragma unroll
-  for (int t = 0; t < 4; ++t) {
-    const int row = m0 + 16 * t + lq;
-    if (row >= a.m) continue;
-    const float sx = a.sx[row];
+  for (int f = 0; f < WF; ++f)
+#pragma unroll
+    for (int t = 0; t < WT; ++t) acc[f][t] = (int4v)0;
+
+  const uint32_t lane_at = base + (uint32_t)(lq * BK + ((lg ^ swizzle(lq)) << 4));
+  const uint32_t xrow = lane_at + (uint32_t)(16 * WT * wt * BK), wrow = lane_at + (uint32_t)((T::BM + 16 * WF * wf) * BK);
+  auto read = [](uint32_t at) __attribute__((always_inline)) { return *(const __attribute__((address_space(3))) int4v*)(uintptr_t)at; };
+  // Operands in registers: tokens of two half-steps of 64 columns (one in use, one on its way), a ring of four blocks of weights.
+  int4v xr[2][WT], wr[4];
+  static_assert(WF >= AHEAD + 1 && (NKS * WF) % 4 == 0, "operand rings");
+  auto read_x = [&](int ks, int t, uint32_t stage) __attribute__((always_inline)) { xr[ks & 1][t] = read(((xrow + stage) ^ (uint32_t)(ks << 6)) + t * 16 * BK); };
+  auto read_w = [&](int p, uint32_t stage) __attribute__((always_inline)) { wr[p & 3] = read(((wrow + stage) ^ (uint32_t)(p / WF << 6)) + p % WF * 16 * BK); };
+  // keeps `n` LDS reads behind the product they were written after
+  auto pin = [](int n) __attribute__((always_inline)) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    if (n == 1) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    else if (n == 2) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+    else if (n == 3) __builtin_amdgcn_sched_group_barrier(0x100, 3, 0);
+  };
+#pragma unroll
+  for (int st = 0; st < NST; ++st)
+    if (st < steps) {
+#pragma unroll
+      for (int i = 0; i < NLOAD; ++i) issue(i, (uint32_t)(st * STAGE));
+      next_step();
+    }
+  if (steps < NST) wait_loads<0>();
+  else wait_loads<(NST - 1) * NLOAD>();
+  barrier();
+  uint32_t stage = 0;
+  auto row_step = [&](auto row_tag, uint32_t stage, uint32_t next, auto load_tag) __attribute__((always_inline)) {
+    constexpr bool LOAD = decltype(load_tag)::value;
+    constexpr int ks = decltype(row_tag)::value / WF, y = decltype(row_tag)::value % WF;
+    constexpr bool last = ks == NKS - 1, tail = last && y >= WF - AHEAD;
+    constexpr int rows = last ? AHEAD : WF, r = last ? y - (WF - AHEAD) : y;
+    constexpr int x0 = last && !tail ? 0 : WT * r / rows, x1 = last && !tail ? 0 : WT * (r + 1) / rows;      // operands of the next half-step that are read here
+    int reads[WT];
+#pragma unroll
+    for (int m = 0; m < WT; ++m) {
+      acc[y][m] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wr[(ks * WF + y) & 3], xr[ks & 1][m], acc[y][m], 0, 0, 0);
+      int n = 0;
+      constexpr int p = ks * WF + y + AHEAD;
+      if (m == 0) { read_w(p % (NKS * WF), p < NKS * WF ? stage : next); ++n; }
+      if (WT == 1) { if (x0 < x1) { read_x((ks + 1) % NKS, 0, last ? next : stage); ++n; } }
+      else if (m >= 1 && x0 + m - 1 < x1) { read_x((ks + 1) % NKS, x0 + m - 1, last ? next : stage); ++n; }
+      reads[m] = n;
+      if (LOAD && tail) {
+        constexpr int TAIL = AHEAD * WT;
+        const int q = (y - (WF - AHEAD)) * WT + m;
+#pragma unroll
+        for (int i = NLOAD * q / TAIL; i < NLOAD * (q + 1) / TAIL; ++i) issue(i, stage);
+      }
+    }
+#pragma unroll
+    for (int m = 0; m < WT; ++m) pin(reads[m]);
+  };
+  auto stage_step = [&](int kb, auto load_tag) __attribute__((always_inline)) {
+    constexpr bool LOAD = decltype(load_tag)::value;
+    const uint32_t next = stage == (uint32_t)((NST - 1) * STAGE) ? 0u : stage + (uint32_t)STAGE;
+    for_each<NKS * WF - AHEAD>([&](auto row) __attribute__((always_inline)) { row_step(row, stage, next, load_tag); });
+    wait_lds();                            // the operands of the last rows are in registers: this wave is done with the stage
+    if (LOAD || kb + NST - 1 < steps) wait_loads<(NST - 2) * NLOAD>();      // the next stage has landed; younger ones may be in flight
+    else wait_loads<0>();
+    barrier();                             // ... everyone's pieces of it, and everyone is done with this one
+    for_each<AHEAD>([&](auto row) __attribute__((always_inline)) {
+      row_step(std::integral_constant<int, NKS * WF - AHEAD + decltype(row)::value>{}, stage, next, load_tag);
+    });
+    if (LOAD) next_step();
+    stage = next;
+  };
+#pragma unroll
+  for (int t = 0; t < WT; ++t) read_x(0, t, 0u);
+#pragma unroll
+  for (int p = 0; p < AHEAD; ++p) read_w(p, 0u);
+  int kb = 0;
+  for (; kb + NST < steps; ++kb) stage_step(kb, std::true_type{});
+  for (; kb < steps; ++kb) stage_step(kb, std::false_type{});
+  wait_lds();
+  barrier();                               // the ring is free
+
+  // Results go through LDS, a block of 16 tokens at a time, so that a wave stores whole rows.
+  constexpr int ES = DT == FTINT8_F32 ? 4 : 2, PER = 16 / ES, LPR = 16 * WF / PER, RPI = 64 / LPR > 16 ? 16 : 64 / LPR;      // elements of a store; lanes of a row; rows of a store
+  char* const out = smem + wave * 16 * T::PITCH;
+  const int nf0 = n0 + 16 * WF * wf, mt0 = m0 + 16 * WT * wt;
+  float sw[WF][4];
+#pragma unroll
+  for (int f = 0; f < WF; ++f)
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const int col = n0 + 4 * lg + r;
-      if (col >= a.n) continue;
-      float y = (float)acc[t][r] * (sx * a.sw[col]);
-      asm("" : "+v"(y));      // (rounded to 32 bits: the compiler would make one instruction of this product and its rounding to 16)
-      char* const to = a.y + (int64_t)row * a.y_stride;
-      if constexpr (DT == FTINT8_F32) reinterpret_cast<float*>(to)[col] = y;
-      else reinterpret_cast<uint16_t*>(to)[col] = (uint16_t)pack2<DT == FTINT8_BF16>(y, y);
+      const int col = nf0 + 16 * f + 4 * lg + r;
+      sw[f][r] = a.sw[col < a.n ? col : a.n - 1];
     }
+#pragma unroll
+  for (int t = 0; t < WT; ++t) {
+    const int mine = mt0 + 16 * t + lq;
+    const float sx = a.sx[mine < a.m ? mine : a.m - 1];
+#pragma unroll
+    for (int f = 0; f < WF; ++f) {
+      float y[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) y[r] = scaled(acc[f][t][r], sx, sw[f][r]);
+      char* const at = out + lq * T::PITCH + (16 * f + 4 * lg) * ES;
+      if constexpr (ES == 4) *reinterpret_cast<float4v*>(at) = float4v{y[0], y[1], y[2], y[3]};
+      else *reinterpret_cast<uint2v*>(at) = uint2v{pack2<DT == FTINT8_BF16>(y[0], y[1]), pack2<DT == FTINT8_BF16>(y[2], y[3])};
+    }
+    const int r0 = mt0 + 16 * t;
+    if (a.wide) {
+      const int col = nf0 + lane % LPR * PER;
+#pragma unroll
+      for (int i = 0; i < 16 / RPI; ++i) {
+        const int r = i * RPI + lane / LPR;
+        const uint4v v = *reinterpret_cast<const uint4v*>(out + (r & 15) * T::PITCH + lane % LPR * 16);
+        if (lane / LPR >= RPI || r0 + r >= a.m || col >= a.n) continue;
+        char* const to = a.y + (int64_t)(r0 + r) * a.y_stride + col * ES;
+        if (col + PER <= a.n) *reinterpret_cast<uint4v*>(to) = v;
+        else
+          for (int e = 0; e < a.n - col; ++e) {
+            if constexpr (ES == 4) reinterpret_cast<uint32_t*>(to)[e] = v[e];
+            else reinterpret_cast<uint16_t*>(to)[e] = (uint16_t)(v[e >> 1] >> 16 * (e & 1));
+          }
+      }
+    } else {
+      for (int e = lane; e < 16 * 16 * WF; e += 64) {
+        const int r = e / (16 * WF), c = e % (16 * WF);
+        if (r0 + r >= a.m || nf0 + c >= a.n) continue;
+        char* const to = a.y + (int64_t)(r0 + r) * a.y_stride + (nf0 + c) * ES;
+        if constexpr (ES == 4) *reinterpret_cast<float*>(to) = *reinterpret_cast<const float*>(out + r * T::PITCH + c * ES);
+        else *reinterpret_cast<uint16_t*>(to) = *reinterpret_cast<const uint16_t*>(out + r * T::PITCH + c * ES);
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);      // (one block's results at a time out of the accumulators)
   }
 }
 
 typedef void (*encode_fn)(const EncodeArgs);
 typedef void (*product_fn)(const ProductArgs);
+
+// The kernel for rows of k_padded codes; per: rows of a workgroup.  Rows of up to 2048 elements take a wave each, of up to 16384 a workgroup.
+template <int DT> encode_fn encode_of(int k_padded, bool whole, int& per) {
+  if (!whole || k_padded > 16384) return ftint8_encode_any<DT>;
+  if (k_padded <= 2048) {
+    per = 4;
+    return k_padded <= 512 ? ftint8_encode_rows<DT, 1, 1> : k_padded <= 1024 ? ftint8_encode_rows<DT, 1, 2> : ftint8_encode_rows<DT, 1, 4>;
+  }
+  return k_padded <= 4096 ? ftint8_encode_rows<DT, 4, 2> : k_padded <= 8192 ? ftint8_encode_rows<DT, 4, 4> : ftint8_encode_rows<DT, 4, 8>;
+}
+
+enum { WIDE, HALF, QUARTER, SMALL, N_TILES };
+using TileWide = Tile<256, 256, 4, 8, 2>;
+using TileHalf = Tile<128, 256, 4, 4, 3>;
+using TileQuarter = Tile<64, 256, 2, 4, 3>;
+using TileSmall = Tile<64, 128, 2, 4, 3, 2>;
+struct TileInfo { int bm, bf, threads, lds; };
+template <class T> constexpr TileInfo info_of() { return {T::BM, T::BF, T::NW * 64, T::LDS}; }
+constexpr TileInfo TILES[N_TILES] = {info_of<TileWide>(), info_of<TileHalf>(), info_of<TileQuarter>(), info_of<TileSmall>()};
+template <int DT> product_fn tile_of(int tile) {
+  return tile == WIDE ? ftint8_tile<TileWide, DT> : tile == HALF ? ftint8_tile<TileHalf, DT> : tile == QUARTER ? ftint8_tile<TileQuarter, DT> : ftint8_tile<TileSmall, DT>;
+}
 
 }  // namespace ftint8
 
@@ -108,8 +385,7 @@ using namespace ftint8;
 struct ftint8_ctx {
   ftint8_config cfg;
   int k_padded = 0;
-  encode_fn encode = nullptr;
-  product_fn product = nullptr;
+  product_fn product[N_TILES] = {};
   int8_t* codes = nullptr;       // of the tokens of a forward, and their scales behind them
   float* scales = nullptr;
   std::string err;
@@ -146,14 +422,15 @@ extern "C" int ftint8_create(const ftint8_config* cfg, ftint8_ctx** out) {
   if (!c) return ifail(nullptr, FTINT8_ENOMEM, "out of host memory");
   c->cfg = *cfg;
   c->k_padded = (cfg->k + KEXTRA - 1) / KEXTRA * KEXTRA;
-  c->encode = cfg->in_dtype == FTINT8_BF16 ? ftint8_encode_rows<FTINT8_BF16> : ftint8_encode_rows<FTINT8_F16>;
-  c->product = cfg->out_dtype == FTINT8_F32 ? ftint8_tile<FTINT8_F32> : cfg->out_dtype == FTINT8_BF16 ? ftint8_tile<FTINT8_BF16> : ftint8_tile<FTINT8_F16>;
+  for (int t = 0; t < N_TILES; ++t)
+    c->product[t] = cfg->out_dtype == FTINT8_F32 ? tile_of<FTINT8_F32>(t) : cfg->out_dtype == FTINT8_BF16 ? tile_of<FTINT8_BF16>(t) : tile_of<FTINT8_F16>(t);
   const size_t bytes = (size_t)cfg->max_tokens * c->k_padded;
   int before = 0;
   hipError_t he = hipGetDevice(&before);
   if (he == hipSuccess) he = hipSetDevice(cfg->device);
   if (he == hipSuccess) {
-    he = hipMalloc((void**)&c->codes, bytes + (size_t)cfg->max_tokens * sizeof(float));
+    for (int t = 0; t < N_TILES && he == hipSuccess; ++t) he = hipFuncSetAttribute((const void*)c->product[t], hipFuncAttributeMaxDynamicSharedMemorySize, TILES[t].lds);
+    if (he == hipSuccess) he = hipMalloc((void**)&c->codes, bytes + (size_t)cfg->max_tokens * sizeof(float));
     (void)hipSetDevice(before);
   }
   if (he != hipSuccess) {
@@ -202,14 +479,21 @@ struct OnDevice {      // the context's device for the length of a call
 }  // namespace
 
 static hipError_t launch_encode(ftint8_ctx* c, const ftint8_matrix* x, int32_t rows, int8_t* codes, float* scales, hipStream_t st) {
-  const EncodeArgs a{static_cast<const char*>(x->data), x->stride * 2, c->cfg.k, c->k_padded, codes, scales};
-  hipLaunchKernelGGL(c->encode, dim3((uint32_t)rows), dim3(256), 0, st, a);
+  const EncodeArgs a{static_cast<const char*>(x->data), x->stride * 2, c->cfg.k, c->k_padded, rows, codes, scales};
+  const bool bf = c->cfg.in_dtype == FTINT8_BF16, whole = ((uintptr_t)x->data | (uintptr_t)(x->stride * 2)) % 16 == 0;
+  int per = 1;
+  const encode_fn fn = bf ? encode_of<FTINT8_BF16>(c->k_padded, whole, per) : encode_of<FTINT8_F16>(c->k_padded, whole, per);
+  hipLaunchKernelGGL(fn, dim3((uint32_t)((rows + per - 1) / per)), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 static hipError_t launch_product(ftint8_ctx* c, const int8_t* x, const float* sx, int32_t m, const int8_t* w, const float* sw, const ftint8_matrix* y, hipStream_t st) {
   const int size = c->cfg.out_dtype == FTINT8_F32 ? 4 : 2;
-  const ProductArgs a{x, w, sx, sw, static_cast<char*>(y->data), y->stride * size, m, c->cfg.n, c->k_padded};
-  hipLaunchKernelGGL(c->product, dim3((uint32_t)((c->cfg.n + 63) / 64), (uint32_t)((m + 63) / 64)), dim3(256), 0, st, a);
+  const int32_t wide = ((uintptr_t)y->data | (uintptr_t)(y->stride * size)) % 16 == 0;
+  const ProductArgs a{x, w, sx, sw, static_cast<char*>(y->data), y->stride * size, m, c->cfg.n, c->k_padded, wide};
+  auto tiles = [&](int t) { return (int64_t)((m + TILES[t].bm - 1) / TILES[t].bm) * ((c->cfg.n + TILES[t].bf - 1) / TILES[t].bf); };
+  int tile = WIDE;
+  while (tile + 1 < N_TILES && tiles(tile) < 256) ++tile;
+  hipLaunchKernelGGL(c->product[tile], dim3((uint32_t)tiles(tile)), dim3(TILES[tile].threads), TILES[tile].lds, st, a);
   return hipGetLastError();
 }
 
