@@ -18,6 +18,8 @@ struct Args {
   const int32_t *slots, *cu, *starts;      // cu NULL: one token of every sequence
   int32_t n_slots, batch, total, heads, group;
   float scale;
+  int32_t per;             // tokens of a segment, whole chunks
+  float* between;          // states between segments
 };
 
 template <bool BF> __device__ __forceinline__ float element(const char* row, int i) {
@@ -79,6 +81,535 @@ template <int D, bool BF> __global__ __launch_bounds__(256) void ftdecay_recurre
     for (int i = 0; i < R; ++i) state[(g * R + i) * D + e] = s[i];
 }
 
+// ---- Prompts, in chunks of 64 tokens.  With S the state before a chunk (D x D) and i, j places in it,
+//
+//     O[i] = scale (decay^(i+1) q_i S + sum over j <= i of decay^(i-j) (q_i . k_j) v_j),      S' = decay^n S + sum over j of decay^(n-1-j) k_j v_j^T
+//
+// (n tokens), all of them matrix products.  A wave owns 32 columns of values: its slab of S stays in registers (accumulators of k^T v, which are the left operand
+// of O^T = S^T q^T as they lie) and so does its part of O; the weights q . k of a chunk are computed once, a 32 x 32 tile a wave, and shared through LDS.
+//
+// What is rounded to 16 bits before a product is held in more than one word.  bf16: weights and S in two words (2^-16 relative), decayed values in three (S is a state of
+// 32 bits).  fp16: S under one power of two for its slab, and the decayed values, in two words, the lower one times 2^11 (22 bits; what the products of lower words add is kept apart until it is
+// scaled back); weights, which have no bound, in two words of bf16 with the values as two words of bf16, which hold fp16 exactly.
+constexpr int C = 64, STATES = 1024, LEAST = 256;
+
+template <int D> constexpr int tile_bytes() { return C * D * 2; }
+constexpr int P_BYTES = C * C * 2;      // a word of the weights
+template <int D> constexpr int lds_bytes() { return 4 * tile_bytes<D>() + 2 * P_BYTES; }
+template <int D> constexpr int gather_lds_bytes() { return 4 * tile_bytes<D>() + P_BYTES / 2; }
+
+template <bool BF> __device__ __forceinline__ float16v mfma32(uint4v a, uint4v b, float16v c) {
+  if constexpr (BF) return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf8v, a), __builtin_bit_cast(bf8v, b), c, 0, 0, 0);
+  else return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8v, a), __builtin_bit_cast(half8v, b), c, 0, 0, 0);
+}
+
+// N times 16 bytes per lane from (uniform base + per-lane byte offsets) straight into LDS, 1 KB apart from the uniform LDS address on.  (Opaque to the compiler, which
+// would wait for the tile in flight before it reads another.  The first wait covers a base that a vector instruction has moved to its scalar registers just before: five states.)
+__device__ __forceinline__ void load_lds16(const void* base, uint32_t off, uint32_t lds_addr) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(lds_addr) : "memory", "m0");
+}
+__device__ __forceinline__ void everything_landed() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0x0F70);      // vmcnt(0)
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+__device__ __forceinline__ void lds_written() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0xC07F);      // lgkmcnt(0)
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// Row r of a tile has its 16-byte chunk c at place c ^ place_of(r): sixteen lanes that read a chunk of as many rows meet all banks once, and so do
+// 32 that read 32 bytes of four rows, twice.
+template <int D> __device__ __forceinline__ int place_of(int r) { return D == 128 ? (r & 3) << 2 | (r >> 2 & 3) : (r >> 1 & 1) << 2 | (r >> 2 & 3); }
+
+// Loads of a tile: rows t0 .. t0 + 63 of one head, those behind the last one are the last one again.
+template <int D, int NW> struct Loader {
+  static constexpr int CH = D / 8, RPL = 64 / CH, LOADS = tile_bytes<D>() / 1024 / NW;      // chunks of a row; rows of a load; loads of a wave
+  const char* base;
+  int64_t token;
+  int wave, lane;
+  __device__ __forceinline__ Loader(const Rows& r, int64_t row0, int head, int wave, int lane)
+      : base(r.data + row0 * r.token + (int64_t)head * r.head), token(r.token), wave(wave), lane(lane) {}
+  __device__ __forceinline__ void issue(int chunk, int tokens, uint32_t to) const {
+    const char* const p = base + (int64_t)(chunk * C) * token;
+    const int left = tokens - chunk * C, first = wave * LOADS * RPL;
+    to += (uint32_t)(wave * LOADS) * 1024;
+    int l = lane;
+    asm volatile("" : "+v"(l));      // (nothing of this is worth a register outside of here)
+    const int r = l / CH;
+    if (left >= C) {
+      const uint32_t row = (uint32_t)r * (uint32_t)token, place = (uint32_t)((l % CH) ^ place_of<D>(first + r)) * 16;
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) load_lds16(p + (int64_t)(first + i * RPL) * token, row + (place ^ (uint32_t)(place_of<D>(i * RPL) * 16)), to + (uint32_t)i * 1024);
+    } else {
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) {
+        const int x = first + i * RPL + r, rc = x < left ? x : left - 1;
+        load_lds16(p, (uint32_t)rc * (uint32_t)token + (uint32_t)((l % CH) ^ place_of<D>(x)) * 16, to + (uint32_t)i * 1024);
+      }
+    }
+  }
+};
+
+// A segment: tokens of one sequence and head that one workgroup takes, `per` or fewer.
+struct Segment {
+  int b, h, number, tokens, first;      // number in its sequence; tokens of it; its first row
+  bool last;
+  int64_t before;                       // number of the sequence's first state between segments
+};
+__device__ __forceinline__ bool segment_of(const Args& a, int64_t id, Segment& s) {
+  // The heads of a group, which share keys and values, run one after the other on one XCD; groups go round the XCDs, so that all have as many of them.
+  // (Neighbouring groups on one XCD leave another without: 16,384 tokens of 32 heads on 8 took 316 us.)
+  const int xcd = (int)(id & 7), place = (int)(id >> 3), group = __builtin_amdgcn_readfirstlane((place / a.group) * 8 + xcd), kv_heads = a.heads / a.group;
+  // (divisions leave the scalar unit; everything here is the same in all lanes)
+  const int unit = __builtin_amdgcn_readfirstlane(group / kv_heads);
+  s.h = __builtin_amdgcn_readfirstlane(group % kv_heads * a.group + place % a.group);
+  if (unit >= a.total / a.per + a.batch) return false;
+  // sequence b owns the numbers from cu[b] / per + b on: at least as many as it has segments, whatever the others have
+  auto begin = [&](int b) { return (int64_t)(clamped(a.cu[b], a.total) / a.per + b); };
+  s.b = sequence_of(a.batch, unit, begin);
+  const int t0 = clamped(a.cu[s.b], a.total), t1 = clamped(a.cu[s.b + 1], a.total), n = t1 > t0 ? t1 - t0 : 0;
+  s.number = __builtin_amdgcn_readfirstlane(unit - (int)begin(s.b));
+  const int segments = __builtin_amdgcn_readfirstlane(n > a.per ? (n + a.per - 1) / a.per : 1);
+  if (s.number < 0 || s.number >= segments) return false;
+  s.last = s.number == segments - 1;
+  s.first = t0 + s.number * a.per;
+  s.tokens = s.last ? n - s.number * a.per : a.per;
+  s.before = __builtin_amdgcn_readfirstlane(t0 / a.per);
+  return true;
+}
+
+// log2 of the decay in two words: its multiples are exact to 32 bits
+struct Powers {
+  float high, low;
+  double log;
+  __device__ __forceinline__ Powers(const Args& a, int h) {
+    log = (double)__builtin_fmaxf(__builtin_fminf(a.log_decay[h], 0.f), -1e30f);
+    const double x = log * 1.4426950408889634074;
+    high = (float)x;
+    low = (float)(x - (double)high);
+  }
+  __device__ __forceinline__ float to(int n) const { return ex2(__builtin_fmaf((float)n, high, (float)n * low)); }
+  __device__ __forceinline__ Decay whole(int n) const {
+    const double d = exp((double)n * log);
+    const float f = (float)d;
+    return Decay{f, (float)(d - (double)f)};
+  }
+};
+
+// Row m of an accumulator tile of the state stands for row swapped(m) of its 32: register 4g + r of lane (h, n) for 16 (g / 2) + 8h + 4 (g % 2) + r, eight in a row for each
+// pair of g, as operands have them.
+__device__ __forceinline__ int row_of(int v, int h) { return 16 * (v >> 3) + 8 * h + (v & 7); }
+
+template <int D, bool BF> struct Chunk {
+  static constexpr int NW = D / 32, NB = D / 32, KS = C / 16;      // waves; blocks of 32 rows of the state; steps of 16 tokens
+  int lane, wave, h, n;
+  uint32_t rows_at, columns_at[2];      // places of this lane's reads in a tile: of rows (block of 16 elements 0), transposed (the state's rows; values)
+  // This wave's factors, in a place that the weights leave free: 16-byte words of queries 4 wave .. 4 wave + 3 for keys from 32 on, which these do not see.
+  uint32_t falls_at;
+  __device__ __forceinline__ uint32_t fall_word(int x) const {
+    const int r = 4 * wave + (x >> 2);
+    return falls_at + (uint32_t)(r * (2 * C) + (((4 + (x & 3)) ^ (r >> 1 & 7)) * 16));
+  }
+  __device__ __forceinline__ explicit Chunk(uint32_t weights) : lane(threadIdx.x & 63), wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)), h(lane >> 5), n(lane & 31) {
+    // (what the place of a row's chunk depends on is the same for rows 32 apart, and for tokens 16 apart)
+    rows_at = (uint32_t)(n * (2 * D) + ((h ^ place_of<D>(n)) * 16));
+    const int rr = lane >> 2 & 3, r = 8 * h + rr;
+#pragma unroll
+    for (int swap = 0; swap < 2; ++swap) {
+      const int u = swap ? (lane & 1) << 1 | (lane >> 1 & 1) : lane & 3;
+      columns_at[swap] = (uint32_t)(r * (2 * D) + (((2 * (lane >> 4 & 1) + (u >> 1)) ^ place_of<D>(r)) * 16) + (u & 1) * 8);
+    }
+    falls_at = weights;
+  }
+
+  // New values, as far as the compiler knows: what is computed from them in a loop stays there, where it would fill the registers in front of it.
+  __device__ __forceinline__ void renew() { asm volatile("" : "+v"(rows_at), "+v"(columns_at[0]), "+v"(columns_at[1]), "+v"(falls_at)); }
+
+  // The transposed operand of tokens 16s + 8h .. + 7 (two a register): column 32f + m in lane (h, n), m = n (values), or n with bits 2 and 3 exchanged.
+  // Sixteen lanes read four rows of 16 columns, 8 bytes a lane, and get a column of four rows each.  Rows 4 further on have their chunks at places that differ in one bit.
+  template <bool SWAP> __device__ __forceinline__ uint4v transposed(uint32_t tile, int s, int f) const {
+    const uint32_t at = tile + (columns_at[SWAP] ^ (uint32_t)(f << 6));
+    const uint2v x = __builtin_bit_cast(uint2v, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)(uintptr_t)(at + s * 32 * D)));
+    const uint32_t further = tile + (columns_at[SWAP] ^ (uint32_t)(f << 6 | 16));
+    const uint2v y = __builtin_bit_cast(uint2v, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)(uintptr_t)(further + s * 32 * D + 8 * D)));
+    return uint4v{x[0], x[1], y[0], y[1]};
+  }
+  // Elements 16x + 8h .. + 7 of row 32t + n; `at`: rows_at, or that of another row.
+  __device__ __forceinline__ uint4v row(uint32_t tile, uint32_t at, int t, int x) const {
+    return *(const __attribute__((address_space(3))) uint4v*)(uintptr_t)(tile + (at ^ (uint32_t)(x << 5)) + t * 64 * D);
+  }
+
+  // The decays from every token of a chunk of `tokens` to its end, to where this wave reads them.
+  __device__ __forceinline__ void set_falls(const Powers& p, int tokens) const {
+    const int left = tokens - 1 - lane;
+    *(__attribute__((address_space(3))) float*)(uintptr_t)(fall_word(lane >> 2) + 4 * (lane & 3)) = left < 0 ? 0.f : p.to(left);
+  }
+
+  // The values of tokens 16s + 8h .. + 7, decayed to the end of the chunk, in words.
+  template <int WORDS> __device__ __forceinline__ void decayed(uint4v v, int s, uint4v (&w)[WORDS]) const {
+    // (words 4s + 2h and the next one: the same row, places 2h and 1 from each other)
+    const uint32_t first = fall_word(4 * s) ^ (uint32_t)(h << 5);
+    const float4v f[2] = {*(const __attribute__((address_space(3))) float4v*)(uintptr_t)first, *(const __attribute__((address_space(3))) float4v*)(uintptr_t)(first ^ 16u)};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float x = low_of<BF>(v[i]) * f[i >> 1][2 * (i & 1)], y = high_of<BF>(v[i]) * f[i >> 1][2 * (i & 1) + 1];
+      w[0][i] = pack2<BF>(x, y);
+      x -= low_of<BF>(w[0][i]);
+      y -= high_of<BF>(w[0][i]);
+      if constexpr (BF) {
+        w[1][i] = pack2<BF>(x, y);
+        w[2][i] = pack2<BF>(x - low_of<BF>(w[1][i]), y - high_of<BF>(w[1][i]));
+      } else {
+        w[1][i] = pack2<BF>(x * 2048.f, y * 2048.f);
+      }
+    }
+  }
+
+  // The slab of the state moves on by a chunk.  vr: its values, raw.
+  __device__ __forceinline__ void update(float16v (&S)[NB], const uint4v (&vr)[KS], const Decay& whole, uint32_t ktile) const {
+    if constexpr (BF) {
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) S[b][v] = __builtin_fmaf(S[b][v], whole.high, S[b][v] * whole.low);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        uint4v w[3], k[NB];
+#pragma unroll
+        for (int b = 0; b < NB; ++b) k[b] = transposed<true>(ktile, s, b);
+        decayed<3>(vr[s], s, w);
+#pragma unroll
+        for (int x = 2; x >= 0; --x)
+#pragma unroll
+          for (int b = 0; b < NB; ++b) S[b] = mfma32<BF>(k[b], w[x], S[b]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    } else {
+      uint4v w[KS][2];
+#pragma unroll
+      for (int s = 0; s < KS; ++s) decayed<2>(vr[s], s, w[s]);
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        uint4v k[KS];
+        float16v low = (float16v)0.f;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) k[s] = transposed<true>(ktile, s, b);
+#pragma unroll
+        for (int s = 0; s < KS; ++s) low = mfma32<BF>(k[s], w[s][1], low);
+#pragma unroll
+        for (int v = 0; v < 16; ++v) S[b][v] = __builtin_fmaf(low[v], 0x1p-11f, __builtin_fmaf(S[b][v], whole.high, S[b][v] * whole.low));
+#pragma unroll
+        for (int s = 0; s < KS; ++s) S[b] = mfma32<BF>(k[s], w[s][0], S[b]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+  }
+
+  // The slab from and to memory: [row][column] of 32 bits.
+  __device__ __forceinline__ void fetch(float16v (&S)[NB], const float* from) const {
+    if (from) {
+      const float* const at = from + 8 * h * D + 32 * wave + n;
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) S[b][v] = at[(32 * b + row_of(v, 0)) * D];
+    } else {
+#pragma unroll
+      for (int b = 0; b < NB; ++b) S[b] = (float16v)0.f;
+    }
+  }
+  __device__ __forceinline__ void put(const float16v (&S)[NB], float* to) const {
+    float* const at = to + 8 * h * D + 32 * wave + n;
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) at[(32 * b + row_of(v, 0)) * D] = S[b][v];
+  }
+};
+
+typedef __attribute__((address_space(3))) char lds_char;
+
+// What a segment alone adds to the state, for all but the last of a sequence: to the states between segments.
+template <int D, bool BF> __global__ __launch_bounds__(2 * D, 2) void ftdecay_gather(const Args a) {
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  Segment g;
+  if (!segment_of(a, blockIdx.x, g) || g.last) return;
+  constexpr uint32_t TILE = tile_bytes<D>();
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_char*)smem;
+  Chunk<D, BF> c(lds0 + 4 * TILE);
+  const int hk = __builtin_amdgcn_readfirstlane(g.h / a.group), chunks = (g.tokens + C - 1) / C;
+  const Powers powers(a, g.h);
+  const Loader<D, D / 32> lk(a.k, g.first, hk, c.wave, c.lane), lv(a.v, g.first, hk, c.wave, c.lane);
+  lk.issue(0, g.tokens, lds0);
+  lv.issue(0, g.tokens, lds0 + TILE);
+  c.set_falls(powers, C);
+  const Decay whole = powers.whole(C);
+  float16v S[D / 32];
+  c.fetch(S, nullptr);
+  for (int i = 0; i < chunks; ++i) {
+    const uint32_t tile = lds0 + (i & 1) * 2 * TILE;
+    c.renew();
+    everything_landed();
+    if (i + 1 < chunks) {
+      const uint32_t next = lds0 + (~i & 1) * 2 * TILE;
+      lk.issue(i + 1, g.tokens, next);
+      lv.issue(i + 1, g.tokens, next + TILE);
+    }
+    uint4v vr[C / 16];
+#pragma unroll
+    for (int s = 0; s < C / 16; ++s) vr[s] = c.template transposed<false>(tile + TILE, s, c.wave);
+    c.update(S, vr, whole, tile);
+  }
+  c.put(S, a.between + ((g.before + g.number) * a.heads + g.h) * (D * D));
+}
+
+// The states between segments: each the sum of what the segments before it add, decayed, and of the sequence's first state.
+template <int D> __global__ __launch_bounds__(256) void ftdecay_join(const Args a) {
+  constexpr int BLOCKS = D * D / 1024;
+  const int unit = blockIdx.x / BLOCKS, b = unit / a.heads, h = unit % a.heads, e = (blockIdx.x % BLOCKS * 256 + threadIdx.x) * 4;
+  const int t0 = clamped(a.cu[b], a.total), t1 = clamped(a.cu[b + 1], a.total), n = t1 > t0 ? t1 - t0 : 0;
+  const int segments = n > a.per ? (n + a.per - 1) / a.per : 1;
+  if (segments < 2) return;
+  const float* const first = a.starts && a.starts[b] > 0 ? state_of<D>(a, b, h) : nullptr;
+  float4v x = first ? *reinterpret_cast<const float4v*>(first + e) : (float4v)0.f;
+  const Decay whole = Powers(a, h).whole(a.per);
+  for (int s = 0; s + 1 < segments; ++s) {
+    float4v* const at = reinterpret_cast<float4v*>(a.between + ((int64_t)(t0 / a.per + s) * a.heads + h) * (D * D) + e);
+    const float4v y = *at;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = __builtin_fmaf(x[i], whole.high, __builtin_fmaf(x[i], whole.low, y[i]));
+    *at = x;
+  }
+}
+
+template <int D, bool BF> __global__ __launch_bounds__(2 * D, 2) void ftdecay_chunks(const Args a) {
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  constexpr int NW = D / 32, NB = D / 32, KS = C / 16;
+  constexpr uint32_t TILE = tile_bytes<D>();
+  Segment g;
+  if (!segment_of(a, blockIdx.x, g)) return;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_char*)smem, qt = lds0, vt = lds0 + TILE, keys = lds0 + 2 * TILE, pt = lds0 + 4 * TILE;
+  Chunk<D, BF> c(pt);
+  const int lane = c.lane, wave = c.wave, h = c.h, n = c.n;
+  const int hk = __builtin_amdgcn_readfirstlane(g.h / a.group), chunks = (g.tokens + C - 1) / C;
+  float* const state = state_of<D>(a, g.b, g.h);
+  const float* from = nullptr;
+  if (g.number > 0) from = a.between + ((g.before + g.number - 1) * a.heads + g.h) * (D * D);
+  else if (a.starts && a.starts[g.b] > 0) from = state;
+  const Loader<D, NW> lq(a.q, g.first, g.h, wave, lane), lk(a.k, g.first, hk, wave, lane), lv(a.v, g.first, hk, wave, lane);
+  if (chunks > 0) {
+    lq.issue(0, g.tokens, qt);
+    lk.issue(0, g.tokens, keys);
+    lv.issue(0, g.tokens, vt);
+  }
+  float16v S[NB];
+  c.fetch(S, from);
+  const Powers powers(a, g.h);
+  // Weights are computed in tiles of 32 keys x 32 queries: (0, 0), (0, 1) and (1, 1); no query of the other sees its keys.  Waves 0, 1 and 2 take one each, of two
+  // waves the first takes those on the diagonal.  Lane (h, n) has query n and keys row_of(v, h).
+  const int jt0 = wave == 2, it0 = wave > 0;
+  float rise[2], factor[16];
+  c.set_falls(powers, C);
+  const Decay whole = powers.whole(C), rest = powers.whole(g.tokens - (chunks - 1) * C);      // of a chunk, of the last one
+#pragma unroll
+  for (int t = 0; t < 2; ++t) rise[t] = a.scale * powers.to(32 * t + n + 1);
+#pragma unroll
+  for (int v = 0; v < 16; ++v) factor[v] = a.scale * powers.to(32 * (it0 - jt0) + n - row_of(v, h));      // (those of keys behind the query are not used)
+  const int m = (n & 0x13) | (n & 4) << 1 | (n & 8) >> 1;      // (row n of the left operand is key m)
+  uint32_t key_at = (uint32_t)(m * (2 * D) + ((h ^ place_of<D>(m)) * 16));
+  uint32_t weight_at = (uint32_t)(n * (2 * C) + ((h ^ (n >> 1 & 7)) * 16));      // (the same for queries 32 apart)
+  char* const o0 = a.o.data + (int64_t)g.first * a.o.token + (int64_t)g.h * a.o.head + 64 * wave;
+
+  for (int i = 0; i < chunks; ++i) {
+    const int left = g.tokens - i * C, tokens = left < C ? left : C;
+    c.renew();
+    asm volatile("" : "+v"(key_at), "+v"(weight_at));
+    const uint32_t kt = keys + (i & 1) * TILE;
+    everything_landed();
+    if (i + 1 < chunks) lk.issue(i + 1, g.tokens, keys + (~i & 1) * TILE);
+    if (tokens < C) c.set_falls(powers, tokens);
+    auto weights = [&](int jt, int it, bool diagonal) __attribute__((always_inline)) {
+      int limit = diagonal ? n - 8 * h : C;      // the last key of a row that the query sees, counted from 8h on
+      asm volatile("" : "+v"(limit));
+      float16v w = (float16v)0.f;
+#pragma unroll
+      for (int x = 0; x < D / 16; ++x) w = mfma32<BF>(c.row(kt + jt * 64 * D, key_at, 0, x), c.row(qt + it * 64 * D, c.rows_at, 0, x), w);
+      const uint32_t at = pt + it * (64 * C);
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        uint4v words[2];
+#pragma unroll
+        for (int v = 8 * y; v < 8 * y + 8; v += 2) {
+          const float p0 = row_of(v, 0) > limit ? 0.f : w[v] * factor[v], p1 = row_of(v + 1, 0) > limit ? 0.f : w[v + 1] * factor[v + 1];
+          const uint32_t high = pack2<true>(p0, p1);
+          words[0][v >> 1 & 3] = high;
+          words[1][v >> 1 & 3] = pack2<true>(p0 - low_of<true>(high), p1 - high_of<true>(high));
+        }
+#pragma unroll
+        for (int x = 0; x < 2; ++x) *(__attribute__((address_space(3))) uint4v*)(uintptr_t)(at + x * P_BYTES + (weight_at ^ (uint32_t)((4 * jt + 2 * y) << 4))) = words[x];
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    if (NW == 2 || wave < 3) weights(jt0, it0, it0 == jt0);
+    if (NW == 2 && wave == 0) weights(1, 1, true);
+    // What the state has of earlier tokens.
+    float16v O[2];
+    O[0] = O[1] = (float16v)0.f;
+    if constexpr (BF) {
+#pragma unroll
+      for (int x = 0; x < D / 16; ++x) {
+        uint4v high, low;
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          const float y = S[x >> 1][8 * (x & 1) + 2 * v], z = S[x >> 1][8 * (x & 1) + 2 * v + 1];
+          high[v] = pack2<true>(y, z);
+          low[v] = pack2<true>(y - low_of<true>(high[v]), z - high_of<true>(high[v]));
+        }
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          const uint4v q = c.row(qt, c.rows_at, t, x);
+          O[t] = mfma32<true>(low, q, O[t]);
+          O[t] = mfma32<true>(high, q, O[t]);
+        }
+        if (x & 1) __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int t = 0; t < 2; ++t) O[t] *= rise[t];
+    } else {
+      // S times the power of two that brings its largest to 2^13
+      float most = 0.f;
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) most = __builtin_fmaxf(most, __builtin_fabsf(S[b][v]));
+#pragma unroll
+      for (int d = 32; d; d >>= 1) most = __builtin_fmaxf(most, __shfl_xor(most, d));
+      if (__builtin_expect(most > 3.4028235e38f, 0)) {      // (what is infinite is not counted: other columns stay what they are)
+        most = 0.f;
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int v = 0; v < 16; ++v) most = __builtin_fabsf(S[b][v]) <= 3.4028235e38f ? __builtin_fmaxf(most, __builtin_fabsf(S[b][v])) : most;
+#pragma unroll
+        for (int d = 32; d; d >>= 1) most = __builtin_fmaxf(most, __shfl_xor(most, d));
+      }
+      int e = most > 0.f ? 140 - (int)(as_u(most) >> 23) : 0;
+      e = __builtin_amdgcn_readfirstlane(e > 100 ? 100 : e);
+      const float up = as_f((uint32_t)(127 + e) << 23);
+#pragma unroll
+      for (int word = 1; word >= 0; --word) {
+#pragma unroll
+        for (int x = 0; x < D / 16; ++x) {
+          uint4v w;
+#pragma unroll
+          for (int v = 0; v < 4; ++v) {
+            const float y = S[x >> 1][8 * (x & 1) + 2 * v] * up, z = S[x >> 1][8 * (x & 1) + 2 * v + 1] * up;
+            w[v] = pack2<false>(y, z);
+            if (word) w[v] = pack2<false>((y - low_of<false>(w[v])) * 2048.f, (z - high_of<false>(w[v])) * 2048.f);
+          }
+#pragma unroll
+          for (int t = 0; t < 2; ++t) O[t] = mfma32<false>(w, c.row(qt, c.rows_at, t, x), O[t]);
+          if (x & 1) __builtin_amdgcn_sched_barrier(0);
+        }
+        if (word) {
+#pragma unroll
+          for (int t = 0; t < 2; ++t) O[t] *= 0x1p-11f;
+        }
+      }
+      const float down = as_f((uint32_t)(127 - e) << 23);
+#pragma unroll
+      for (int t = 0; t < 2; ++t) O[t] *= rise[t] * down;
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    uint4v vr[KS];
+#pragma unroll
+    for (int s = 0; s < KS; ++s) vr[s] = c.template transposed<false>(vt, s, wave);
+    lds_written();                         // the weights are there, and nobody reads this chunk's queries and values any more
+    if (i + 1 < chunks) {
+      lq.issue(i + 1, g.tokens, qt);
+      lv.issue(i + 1, g.tokens, vt);
+    }
+    // Values that are not finite are left out of the product, which would bring them to tokens before theirs (0 times infinity); the tokens from theirs on get NaN.
+    int strange = C;
+    uint32_t most = 0;
+#pragma unroll
+    for (int s = 0; s < KS; ++s)
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+        most = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(ushort2v, most), __builtin_bit_cast(ushort2v, vr[s][x] & 0x7FFF7FFFu)));
+    constexpr uint32_t INF = BF ? 0x7F80u : 0x7C00u;
+    const bool any = __any((most & 0xFFFFu) >= INF || most >> 16 >= INF);
+    if (__builtin_expect(any, 0)) {
+#pragma unroll
+      for (int s = KS - 1; s >= 0; --s)
+#pragma unroll
+        for (int x = 7; x >= 0; --x) {
+          const uint32_t mask = INF << 16 * (x & 1);
+          if ((vr[s][x >> 1] & mask) == mask) strange = 16 * s + x;
+        }
+      strange = strange < C ? strange + 8 * h : C;
+      const int other = __shfl_xor(strange, 32);
+      strange = other < strange ? other : strange;
+    }
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      uint4v v0 = vr[s], v1;
+      if (__builtin_expect(any, 0))
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const uint32_t low = (v0[x] & INF) == INF ? 0u : 0xFFFFu, high = (v0[x] & INF << 16) == INF << 16 ? 0u : 0xFFFF0000u;
+          v0[x] &= low | high;
+        }
+      if constexpr (!BF) {
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const float y = low_of<false>(v0[x]), z = high_of<false>(v0[x]);
+          v0[x] = pack2<true>(y, z);
+          v1[x] = pack2<true>(y - low_of<true>(v0[x]), z - high_of<true>(v0[x]));
+        }
+      }
+#pragma unroll
+      for (int t = s / 2; t < 2; ++t) {
+        const uint32_t at = pt + t * (64 * C) + (weight_at ^ (uint32_t)(s << 5));
+        const uint4v p0 = *(const __attribute__((address_space(3))) uint4v*)(uintptr_t)at, p1 = *(const __attribute__((address_space(3))) uint4v*)(uintptr_t)(at + P_BYTES);
+        O[t] = mfma32<true>(v0, p1, O[t]);
+        if constexpr (!BF) O[t] = mfma32<true>(v1, p0, O[t]);
+        O[t] = mfma32<true>(v0, p0, O[t]);
+      }
+    }
+    if (__builtin_expect(any, 0)) {
+      int first = 4 * h;
+      asm volatile("" : "+v"(first));
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        const int from_token = __shfl(strange, first + 8 * (v >> 2) + (v & 3));
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+          if (32 * t + n >= from_token) O[t][v] = __builtin_nanf("");
+      }
+    }
+    // lane (h, n): token n of a block, columns 8g + 4h + r of the slab
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int r = 32 * t + n;
+      if (r < tokens) {
+        char* const to = o0 + (int64_t)(i * C + r) * a.o.token;
+#pragma unroll
+        for (int y = 0; y < 4; ++y)
+          *reinterpret_cast<uint2v*>(to + 2 * (8 * y + 4 * h)) = uint2v{pack2<BF>(O[t][4 * y], O[t][4 * y + 1]), pack2<BF>(O[t][4 * y + 2], O[t][4 * y + 3])};
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    c.update(S, vr, tokens < C ? rest : whole, kt);
+  }
+  if (g.last && state) c.put(S, state);
+}
+
 typedef void (*kernel_fn)(const Args);
 
 }  // namespace ftdecay
@@ -87,7 +618,9 @@ using namespace ftdecay;
 
 struct ftdecay_ctx {
   ftdecay_config cfg;
-  kernel_fn recurrent = nullptr;
+  kernel_fn recurrent = nullptr, gather = nullptr, join = nullptr, chunks = nullptr;
+  int lds = 0, gather_lds = 0;
+  float* between = nullptr;
   std::string err;
 };
 
@@ -108,6 +641,15 @@ static int dfail_hip(ftdecay_ctx* c, const char* what, hipError_t e) {
   return e == hipErrorOutOfMemory ? FTDECAY_ENOMEM : FTDECAY_EHIP;
 }
 
+template <int D, bool BF> static void choose_kernels(ftdecay_ctx* c) {
+  c->recurrent = ftdecay_recurrent<D, BF>;
+  c->gather = ftdecay_gather<D, BF>;
+  c->join = ftdecay_join<D>;
+  c->chunks = ftdecay_chunks<D, BF>;
+  c->lds = lds_bytes<D>();
+  c->gather_lds = gather_lds_bytes<D>();
+}
+
 extern "C" int ftdecay_create(const ftdecay_config* cfg, ftdecay_ctx** out) {
   if (!cfg || !out) return dfail(nullptr, FTDECAY_EINVAL, "null argument");
   *out = nullptr;
@@ -121,12 +663,22 @@ extern "C" int ftdecay_create(const ftdecay_config* cfg, ftdecay_ctx** out) {
   if (!c) return dfail(nullptr, FTDECAY_ENOMEM, "out of host memory");
   c->cfg = *cfg;
   if (!(c->cfg.scale > 0.f)) c->cfg.scale = 1.0f / std::sqrt((float)cfg->head_dim);
-  const bool bf = cfg->in_dtype == FTDECAY_BF16;
-  c->recurrent = cfg->head_dim == 128 ? (bf ? ftdecay_recurrent<128, true> : ftdecay_recurrent<128, false>) : (bf ? ftdecay_recurrent<64, true> : ftdecay_recurrent<64, false>);
+  if (cfg->head_dim == 128) {
+    if (cfg->in_dtype == FTDECAY_BF16) choose_kernels<128, true>(c);
+    else choose_kernels<128, false>(c);
+  } else {
+    if (cfg->in_dtype == FTDECAY_BF16) choose_kernels<64, true>(c);
+    else choose_kernels<64, false>(c);
+  }
   int before = 0;
   hipError_t he = hipGetDevice(&before);
   if (he == hipSuccess) he = hipSetDevice(cfg->device);
-  if (he == hipSuccess) (void)hipSetDevice(before);
+  if (he == hipSuccess) {
+    he = hipFuncSetAttribute((const void*)c->chunks, hipFuncAttributeMaxDynamicSharedMemorySize, c->lds);
+    if (he == hipSuccess) he = hipFuncSetAttribute((const void*)c->gather, hipFuncAttributeMaxDynamicSharedMemorySize, c->gather_lds);
+    if (he == hipSuccess) he = hipMalloc((void**)&c->between, (size_t)STATES * cfg->head_dim * cfg->head_dim * sizeof(float));
+    (void)hipSetDevice(before);
+  }
   if (he != hipSuccess) {
     const int rc = dfail_hip(nullptr, "device", he);
     delete c;
@@ -165,12 +717,26 @@ static const char* wrong_states(const float* log_decay, const float* states, int
   return nullptr;
 }
 
+// Groups of heads of an XCD, over all segments.
+static uint32_t groups_of(const Args& a) { return (uint32_t)(((int64_t)(a.total / a.per + a.batch) * (a.heads / a.group) + 7) / 8); }
+
+// One pass over the sequences: prompts in segments, single tokens (no cu) a workgroup each.
 static int launch(ftdecay_ctx* c, const Args& a, hipStream_t st) {
   int before = 0;
   hipError_t he = hipGetDevice(&before);
   if (he == hipSuccess && before != c->cfg.device) he = hipSetDevice(c->cfg.device);
   if (he != hipSuccess) return dfail_hip(c, "device", he);
-  hipLaunchKernelGGL(c->recurrent, dim3((uint32_t)(a.batch * a.heads)), dim3(256), 0, st, a);
+  const int threads = 2 * c->cfg.head_dim;
+  if (!a.cu) {
+    hipLaunchKernelGGL(c->recurrent, dim3((uint32_t)(a.batch * a.heads)), dim3(256), 0, st, a);
+  } else {
+    const dim3 grid(groups_of(a) * 8u * (uint32_t)a.group);
+    if (a.total > a.per) {
+      hipLaunchKernelGGL(c->gather, grid, dim3(threads), c->gather_lds, st, a);
+      hipLaunchKernelGGL(c->join, dim3((uint32_t)(a.batch * a.heads * (c->cfg.head_dim * c->cfg.head_dim / 1024))), dim3(256), 0, st, a);
+    }
+    hipLaunchKernelGGL(c->chunks, grid, dim3(threads), c->lds, st, a);
+  }
   he = hipGetLastError();
   if (before != c->cfg.device) (void)hipSetDevice(before);
   return he == hipSuccess ? FTDECAY_OK : dfail_hip(c, "launch", he);
@@ -189,8 +755,15 @@ extern "C" int ftdecay_forward(ftdecay_ctx* c, const ftdecay_rows* q, const ftde
   bad = wrong_states(log_decay, states, n_slots, slots, batch);
   if (bad) return dfail(c, FTDECAY_EINVAL, bad);
   const ftdecay_config& e = c->cfg;
-  if ((int64_t)batch * e.heads > MOST_GROUPS) return dfail(c, FTDECAY_EUNSUPPORTED, "too many sequences");
-  return launch(c, Args{r[0], r[1], r[2], r[3], log_decay, states, slots, cu, starts, n_slots, batch, total, e.heads, e.heads / e.kv_heads, e.scale}, (hipStream_t)hip_stream);
+  int64_t per = ((int64_t)total * e.heads + 511) / 512;
+  per = per < LEAST ? LEAST : per;
+  const int64_t least = ((int64_t)total * e.heads + STATES - 1) / STATES;      // total / per * heads states between segments, at most STATES
+  per = ((per > least ? per : least) + C - 1) / C * C;
+  // workgroups of the launches: segments, blocks of joined states
+  const int64_t segments = (total / per + batch) * e.heads, blocks = total > per ? (int64_t)batch * e.heads * (e.head_dim * e.head_dim / 1024) : 0;
+  if (segments + 8 * (e.heads / e.kv_heads) > MOST_GROUPS || blocks > MOST_GROUPS) return dfail(c, FTDECAY_EUNSUPPORTED, "too many sequences");
+  return launch(c, Args{r[0], r[1], r[2], r[3], log_decay, states, slots, cu, starts, n_slots, batch, total, e.heads, e.heads / e.kv_heads, e.scale, (int32_t)per, c->between},
+                (hipStream_t)hip_stream);
 }
 
 extern "C" int ftdecay_step(ftdecay_ctx* c, const ftdecay_rows* q, const ftdecay_rows* k, const ftdecay_rows* v, const ftdecay_rows* o, const float* log_decay, float* states,
@@ -207,10 +780,15 @@ extern "C" int ftdecay_step(ftdecay_ctx* c, const ftdecay_rows* q, const ftdecay
   if (bad) return dfail(c, FTDECAY_EINVAL, bad);
   const ftdecay_config& e = c->cfg;
   if ((int64_t)batch * e.heads > MOST_GROUPS) return dfail(c, FTDECAY_EUNSUPPORTED, "too many sequences");
-  return launch(c, Args{r[0], r[1], r[2], r[3], log_decay, states, slots, nullptr, nullptr, n_slots, batch, batch, e.heads, e.heads / e.kv_heads, e.scale}, (hipStream_t)hip_stream);
+  return launch(c, Args{r[0], r[1], r[2], r[3], log_decay, states, slots, nullptr, nullptr, n_slots, batch, batch, e.heads, e.heads / e.kv_heads, e.scale, C, nullptr}, (hipStream_t)hip_stream);
 }
 
 extern "C" int ftdecay_destroy(ftdecay_ctx* c) {
+  if (!c) return FTDECAY_OK;
+  int before = 0;
+  const bool moved = hipGetDevice(&before) == hipSuccess && before != c->cfg.device && hipSetDevice(c->cfg.device) == hipSuccess;
+  (void)hipFree(c->between);
+  if (moved) (void)hipSetDevice(before);
   delete c;
   return FTDECAY_OK;
 }
