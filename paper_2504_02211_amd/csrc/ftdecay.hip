@@ -28,7 +28,11 @@ template <bool BF> __device__ __forceinline__ float element(const char* row, int
 }
 
 // The decay in two words: rounded to one, it is off by up to 2^-25 in the same direction at every token, and a state that remembers thousands of tokens by 2^-13.
-struct Decay { float high, low; };
+struct Decay {
+  float high, low;
+  // Of the i-th in a row: `high`, and every eighth time what `high` alone has left out of eight.
+  __device__ __forceinline__ float of(int i) const { return (i & 7) == 7 ? __builtin_fmaf(8.f, low, high) : high; }
+};
 __device__ __forceinline__ Decay decay_of(const Args& a, int h) {
   const double d = exp((double)__builtin_fminf(a.log_decay[h], 0.f));
   const float high = (float)d;
@@ -37,7 +41,7 @@ __device__ __forceinline__ Decay decay_of(const Args& a, int h) {
 
 // Where sequence b has its state; NULL: nowhere.
 template <int D> __device__ __forceinline__ float* state_of(const Args& a, int b, int h) {
-  const int slot = a.slots ? a.slots[b] : b;
+  const int slot = __builtin_amdgcn_readfirstlane(a.slots ? a.slots[b] : b);
   return a.states && slot >= 0 && slot < a.n_slots ? a.states + ((int64_t)slot * a.heads + h) * (D * D) : nullptr;
 }
 
@@ -182,6 +186,8 @@ __device__ __forceinline__ bool segment_of(const Args& a, int64_t id, Segment& s
   return true;
 }
 
+__device__ __forceinline__ float in_scalar(float x) { return as_f((uint32_t)__builtin_amdgcn_readfirstlane((int)as_u(x))); }      // (the same in all lanes)
+
 // log2 of the decay in two words: its multiples are exact to 32 bits
 struct Powers {
   float high, low;
@@ -189,14 +195,14 @@ struct Powers {
   __device__ __forceinline__ Powers(const Args& a, int h) {
     log = (double)__builtin_fmaxf(__builtin_fminf(a.log_decay[h], 0.f), -1e30f);
     const double x = log * 1.4426950408889634074;
-    high = (float)x;
-    low = (float)(x - (double)high);
+    high = in_scalar((float)x);
+    low = in_scalar((float)(x - (double)(float)x));
   }
   __device__ __forceinline__ float to(int n) const { return ex2(__builtin_fmaf((float)n, high, (float)n * low)); }
   __device__ __forceinline__ Decay whole(int n) const {
     const double d = exp((double)n * log);
     const float f = (float)d;
-    return Decay{f, (float)(d - (double)f)};
+    return Decay{in_scalar(f), in_scalar((float)(d - (double)f))};
   }
 };
 
@@ -227,7 +233,7 @@ template <int D, bool BF> struct Chunk {
   }
 
   // New values, as far as the compiler knows: what is computed from them in a loop stays there, where it would fill the registers in front of it.
-  __device__ __forceinline__ void renew() { asm volatile("" : "+v"(rows_at), "+v"(columns_at[0]), "+v"(columns_at[1]), "+v"(falls_at)); }
+  __device__ __forceinline__ void renew() { asm volatile("" : "+v"(rows_at), "+v"(columns_at[0]), "+v"(columns_at[1]), "+s"(falls_at)); }
 
   // The transposed operand of tokens 16s + 8h .. + 7 (two a register): column 32f + m in lane (h, n), m = n (values), or n with bits 2 and 3 exchanged.
   // Sixteen lanes read four rows of 16 columns, 8 bytes a lane, and get a column of four rows each.  Rows 4 further on have their chunks at places that differ in one bit.
@@ -249,65 +255,78 @@ template <int D, bool BF> struct Chunk {
     *(__attribute__((address_space(3))) float*)(uintptr_t)(fall_word(lane >> 2) + 4 * (lane & 3)) = left < 0 ? 0.f : p.to(left);
   }
 
-  // The values of tokens 16s + 8h .. + 7, decayed to the end of the chunk, in words.
-  template <int WORDS> __device__ __forceinline__ void decayed(uint4v v, int s, uint4v (&w)[WORDS]) const {
+  // The values of tokens 16s + 8h .. + 7, decayed to the end of the chunk, in words: in parts, so that matrix instructions can stand between them.
+  static constexpr int WORDS = BF ? 3 : 2, PARTS = 4 * WORDS;
+  struct Decayed {
+    float4v f[2];
+    float x, y;
+    uint4v w[WORDS];
+  };
+  __device__ __forceinline__ void begin(Decayed& d, int s) const {
     // (words 4s + 2h and the next one: the same row, places 2h and 1 from each other)
     const uint32_t first = fall_word(4 * s) ^ (uint32_t)(h << 5);
-    const float4v f[2] = {*(const __attribute__((address_space(3))) float4v*)(uintptr_t)first, *(const __attribute__((address_space(3))) float4v*)(uintptr_t)(first ^ 16u)};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      float x = low_of<BF>(v[i]) * f[i >> 1][2 * (i & 1)], y = high_of<BF>(v[i]) * f[i >> 1][2 * (i & 1) + 1];
-      w[0][i] = pack2<BF>(x, y);
-      x -= low_of<BF>(w[0][i]);
-      y -= high_of<BF>(w[0][i]);
-      if constexpr (BF) {
-        w[1][i] = pack2<BF>(x, y);
-        w[2][i] = pack2<BF>(x - low_of<BF>(w[1][i]), y - high_of<BF>(w[1][i]));
-      } else {
-        w[1][i] = pack2<BF>(x * 2048.f, y * 2048.f);
-      }
+    d.f[0] = *(const __attribute__((address_space(3))) float4v*)(uintptr_t)first;
+    d.f[1] = *(const __attribute__((address_space(3))) float4v*)(uintptr_t)(first ^ 16u);
+  }
+  __device__ __forceinline__ void part(Decayed& d, const uint4v& v, int x) const {
+    const int i = x / WORDS;
+    if (x % WORDS == 0) {
+      d.x = low_of<BF>(v[i]) * d.f[i >> 1][2 * (i & 1)];
+      d.y = high_of<BF>(v[i]) * d.f[i >> 1][2 * (i & 1) + 1];
+      d.w[0][i] = pack2<BF>(d.x, d.y);
+    } else if (x % WORDS == 1) {
+      d.x -= low_of<BF>(d.w[0][i]);
+      d.y -= high_of<BF>(d.w[0][i]);
+      d.w[1][i] = BF ? pack2<BF>(d.x, d.y) : pack2<BF>(d.x * 2048.f, d.y * 2048.f);
+    } else {
+      d.w[WORDS - 1][i] = pack2<BF>(d.x - low_of<BF>(d.w[1][i]), d.y - high_of<BF>(d.w[1][i]));
     }
   }
+  static __device__ __forceinline__ void here() { __builtin_amdgcn_sched_barrier(0); }
 
-  // The slab of the state moves on by a chunk.  vr: its values, raw.
-  __device__ __forceinline__ void update(float16v (&S)[NB], const uint4v (&vr)[KS], const Decay& whole, uint32_t ktile) const {
-    if constexpr (BF) {
+  // A sixteenth of the slab, decayed by a chunk.
+  __device__ __forceinline__ void fade(float16v (&S)[NB], float by, int x) const {
+#pragma unroll
+    for (int v = x * NB; v < (x + 1) * NB; ++v) S[v >> 4][v & 15] *= by;
+  }
+
+  // The slab, decayed already, moves on by a chunk.  vr: its values, raw; d: those of the first step, ready.  `beside(i)`: what else is done, in 8 parts.
+  template <class F> __device__ __forceinline__ void update(float16v (&S)[NB], const uint4v (&vr)[KS], Decayed& d, uint32_t ktile, F beside) const {
+    uint4v k[2][NB];
+    float16v low[BF ? 1 : NB];
+    if constexpr (!BF)
+#pragma unroll
+      for (int b = 0; b < NB; ++b) low[b] = (float16v)0.f;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) k[0][b] = transposed<true>(ktile, 0, b);
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      uint4v w[WORDS];
+#pragma unroll
+      for (int x = 0; x < WORDS; ++x) w[x] = d.w[x];
+      if (s + 1 < KS) begin(d, s + 1);
+      here();
+#pragma unroll
+      for (int i = 0; i < WORDS * NB; ++i) {
+        const int x = WORDS - 1 - i / NB, b = i % NB;
+        if (!BF && x) low[BF ? 0 : b] = mfma32<BF>(k[s & 1][b], w[x], low[BF ? 0 : b]);
+        else S[b] = mfma32<BF>(k[s & 1][b], w[x], S[b]);
+        if (s + 1 < KS) {
+          if (i < NB) k[(s + 1) & 1][i] = transposed<true>(ktile, s + 1, i);
+#pragma unroll
+          for (int y = PARTS * i / (WORDS * NB); y < PARTS * (i + 1) / (WORDS * NB); ++y) part(d, vr[s + 1 < KS ? s + 1 : 0], y);
+        }
+        if (s == 0)
+#pragma unroll
+          for (int y = 8 * i / (WORDS * NB); y < 8 * (i + 1) / (WORDS * NB); ++y) beside(y);
+        here();
+      }
+    }
+    if constexpr (!BF)
 #pragma unroll
       for (int b = 0; b < NB; ++b)
 #pragma unroll
-        for (int v = 0; v < 16; ++v) S[b][v] = __builtin_fmaf(S[b][v], whole.high, S[b][v] * whole.low);
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int s = 0; s < KS; ++s) {
-        uint4v w[3], k[NB];
-#pragma unroll
-        for (int b = 0; b < NB; ++b) k[b] = transposed<true>(ktile, s, b);
-        decayed<3>(vr[s], s, w);
-#pragma unroll
-        for (int x = 2; x >= 0; --x)
-#pragma unroll
-          for (int b = 0; b < NB; ++b) S[b] = mfma32<BF>(k[b], w[x], S[b]);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-    } else {
-      uint4v w[KS][2];
-#pragma unroll
-      for (int s = 0; s < KS; ++s) decayed<2>(vr[s], s, w[s]);
-#pragma unroll
-      for (int b = 0; b < NB; ++b) {
-        uint4v k[KS];
-        float16v low = (float16v)0.f;
-#pragma unroll
-        for (int s = 0; s < KS; ++s) k[s] = transposed<true>(ktile, s, b);
-#pragma unroll
-        for (int s = 0; s < KS; ++s) low = mfma32<BF>(k[s], w[s][1], low);
-#pragma unroll
-        for (int v = 0; v < 16; ++v) S[b][v] = __builtin_fmaf(low[v], 0x1p-11f, __builtin_fmaf(S[b][v], whole.high, S[b][v] * whole.low));
-#pragma unroll
-        for (int s = 0; s < KS; ++s) S[b] = mfma32<BF>(k[s], w[s][0], S[b]);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-    }
+        for (int v = 0; v < 16; ++v) S[b][v] = __builtin_fmaf(low[b][v], 0x1p-11f, S[b][v]);
   }
 
   // The slab from and to memory: [row][column] of 32 bits.
@@ -363,7 +382,14 @@ template <int D, bool BF> __global__ __launch_bounds__(2 * D, 2) void ftdecay_ga
     uint4v vr[C / 16];
 #pragma unroll
     for (int s = 0; s < C / 16; ++s) vr[s] = c.template transposed<false>(tile + TILE, s, c.wave);
-    c.update(S, vr, whole, tile);
+    const float fading = in_scalar(whole.of(i));
+    typename Chunk<D, BF>::Decayed d;
+    c.begin(d, 0);
+#pragma unroll
+    for (int x = 0; x < c.PARTS; ++x) c.part(d, vr[0], x);
+#pragma unroll
+    for (int x = 0; x < 16; ++x) c.fade(S, fading, x);
+    c.update(S, vr, d, tile, [](int) {});
   }
   c.put(S, a.between + ((g.before + g.number) * a.heads + g.h) * (D * D));
 }
@@ -395,13 +421,13 @@ template <int D, bool BF> __global__ __launch_bounds__(2 * D, 2) void ftdecay_ch
   if (!segment_of(a, blockIdx.x, g)) return;
   const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_char*)smem, qt = lds0, vt = lds0 + TILE, keys = lds0 + 2 * TILE, pt = lds0 + 4 * TILE;
   Chunk<D, BF> c(pt);
-  const int lane = c.lane, wave = c.wave, h = c.h, n = c.n;
+  const int wave = c.wave;
   const int hk = __builtin_amdgcn_readfirstlane(g.h / a.group), chunks = (g.tokens + C - 1) / C;
   float* const state = state_of<D>(a, g.b, g.h);
   const float* from = nullptr;
   if (g.number > 0) from = a.between + ((g.before + g.number - 1) * a.heads + g.h) * (D * D);
   else if (a.starts && a.starts[g.b] > 0) from = state;
-  const Loader<D, NW> lq(a.q, g.first, g.h, wave, lane), lk(a.k, g.first, hk, wave, lane), lv(a.v, g.first, hk, wave, lane);
+  const Loader<D, NW> lq(a.q, g.first, g.h, wave, c.lane), lk(a.k, g.first, hk, wave, c.lane), lv(a.v, g.first, hk, wave, c.lane);
   if (chunks > 0) {
     lq.issue(0, g.tokens, qt);
     lk.issue(0, g.tokens, keys);
@@ -410,78 +436,62 @@ template <int D, bool BF> __global__ __launch_bounds__(2 * D, 2) void ftdecay_ch
   float16v S[NB];
   c.fetch(S, from);
   const Powers powers(a, g.h);
-  // Weights are computed in tiles of 32 keys x 32 queries: (0, 0), (0, 1) and (1, 1); no query of the other sees its keys.  Waves 0, 1 and 2 take one each, of two
-  // waves the first takes those on the diagonal.  Lane (h, n) has query n and keys row_of(v, h).
-  const int jt0 = wave == 2, it0 = wave > 0;
-  float rise[2], factor[16];
+  // Weights are computed in tiles of 32 keys x 32 queries: (0, 0), (0, 1) and (1, 1); no query of the other sees its keys.  Waves 0, 1 and 2 take one each, and
+  // wave 3 does as wave 2 does (a branch would cost all of them more); of two waves the first takes both on the diagonal.  Lane (h, n) has query n and keys row_of(v, h).
+  const int jt0 = wave >= 2, it0 = wave > 0;
+  const int h0 = c.lane >> 5, n0 = c.lane & 31;
+  float factor[16];
   c.set_falls(powers, C);
-  const Decay whole = powers.whole(C), rest = powers.whole(g.tokens - (chunks - 1) * C);      // of a chunk, of the last one
+  const Decay whole = powers.whole(C);
+  const float rest = powers.to(g.tokens - (chunks - 1) * C);      // of the last chunk
+  const float rise = a.scale * powers.to(n0 + 1), rise32 = in_scalar(powers.to(32));
 #pragma unroll
-  for (int t = 0; t < 2; ++t) rise[t] = a.scale * powers.to(32 * t + n + 1);
-#pragma unroll
-  for (int v = 0; v < 16; ++v) factor[v] = a.scale * powers.to(32 * (it0 - jt0) + n - row_of(v, h));      // (those of keys behind the query are not used)
-  const int m = (n & 0x13) | (n & 4) << 1 | (n & 8) >> 1;      // (row n of the left operand is key m)
-  uint32_t key_at = (uint32_t)(m * (2 * D) + ((h ^ place_of<D>(m)) * 16));
-  uint32_t weight_at = (uint32_t)(n * (2 * C) + ((h ^ (n >> 1 & 7)) * 16));      // (the same for queries 32 apart)
+  for (int v = 0; v < 16; ++v) factor[v] = a.scale * powers.to(32 * (it0 - jt0) + n0 - row_of(v, h0));      // (those of keys behind the query are not used)
+  const int m = (n0 & 0x13) | (n0 & 4) << 1 | (n0 & 8) >> 1;      // (row n of the left operand is key m)
+  uint32_t key_at = (uint32_t)(m * (2 * D) + ((h0 ^ place_of<D>(m)) * 16));
+  uint32_t weight_at = (uint32_t)(n0 * (2 * C) + ((h0 ^ (n0 >> 1 & 7)) * 16));      // (the same for queries 32 apart)
   char* const o0 = a.o.data + (int64_t)g.first * a.o.token + (int64_t)g.h * a.o.head + 64 * wave;
 
   for (int i = 0; i < chunks; ++i) {
     const int left = g.tokens - i * C, tokens = left < C ? left : C;
     c.renew();
     asm volatile("" : "+v"(key_at), "+v"(weight_at));
+    int h = h0, n = n0;
+    if constexpr (!BF) {      // (two registers less)
+      int lane = c.lane;
+      asm volatile("" : "+v"(lane));
+      h = lane >> 5;
+      n = lane & 31;
+    }
     const uint32_t kt = keys + (i & 1) * TILE;
     everything_landed();
     if (i + 1 < chunks) lk.issue(i + 1, g.tokens, keys + (~i & 1) * TILE);
     if (tokens < C) c.set_falls(powers, tokens);
-    auto weights = [&](int jt, int it, bool diagonal) __attribute__((always_inline)) {
-      int limit = diagonal ? n - 8 * h : C;      // the last key of a row that the query sees, counted from 8h on
-      asm volatile("" : "+v"(limit));
+    // Every matrix instruction is followed by what fits beside it: vector instructions in the shadow of the wave's own matrix instructions are nearly free.
+    uint2v words[2];
+    auto weight = [&](const float16v& w, int limit, int v) __attribute__((always_inline)) {      // weights v and v + 1
+      const float p0 = row_of(v, 0) > limit ? 0.f : w[v] * factor[v], p1 = row_of(v + 1, 0) > limit ? 0.f : w[v + 1] * factor[v + 1];
+      const uint32_t high = pack2<true>(p0, p1);
+      words[0][v >> 1 & 1] = high;
+      words[1][v >> 1 & 1] = pack2<true>(p0 - low_of<true>(high), p1 - high_of<true>(high));
+    };
+    auto share = [&](int jt, int it, int y) __attribute__((always_inline)) {      // four keys' words to LDS
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+        *(__attribute__((address_space(3))) uint2v*)(uintptr_t)(pt + it * (64 * C) + x * P_BYTES + (weight_at ^ (uint32_t)((4 * jt + (y & 2)) << 4)) + 8 * (y & 1)) = words[x];
+    };
+    auto scores = [&](int jt, int it, auto beside) __attribute__((always_inline)) {
       float16v w = (float16v)0.f;
 #pragma unroll
-      for (int x = 0; x < D / 16; ++x) w = mfma32<BF>(c.row(kt + jt * 64 * D, key_at, 0, x), c.row(qt + it * 64 * D, c.rows_at, 0, x), w);
-      const uint32_t at = pt + it * (64 * C);
-#pragma unroll
-      for (int y = 0; y < 2; ++y) {
-        uint4v words[2];
-#pragma unroll
-        for (int v = 8 * y; v < 8 * y + 8; v += 2) {
-          const float p0 = row_of(v, 0) > limit ? 0.f : w[v] * factor[v], p1 = row_of(v + 1, 0) > limit ? 0.f : w[v + 1] * factor[v + 1];
-          const uint32_t high = pack2<true>(p0, p1);
-          words[0][v >> 1 & 3] = high;
-          words[1][v >> 1 & 3] = pack2<true>(p0 - low_of<true>(high), p1 - high_of<true>(high));
-        }
-#pragma unroll
-        for (int x = 0; x < 2; ++x) *(__attribute__((address_space(3))) uint4v*)(uintptr_t)(at + x * P_BYTES + (weight_at ^ (uint32_t)((4 * jt + 2 * y) << 4))) = words[x];
-      }
-      __builtin_amdgcn_sched_barrier(0);
-    };
-    if (NW == 2 || wave < 3) weights(jt0, it0, it0 == jt0);
-    if (NW == 2 && wave == 0) weights(1, 1, true);
-    // What the state has of earlier tokens.
-    float16v O[2];
-    O[0] = O[1] = (float16v)0.f;
-    if constexpr (BF) {
-#pragma unroll
       for (int x = 0; x < D / 16; ++x) {
-        uint4v high, low;
-#pragma unroll
-        for (int v = 0; v < 4; ++v) {
-          const float y = S[x >> 1][8 * (x & 1) + 2 * v], z = S[x >> 1][8 * (x & 1) + 2 * v + 1];
-          high[v] = pack2<true>(y, z);
-          low[v] = pack2<true>(y - low_of<true>(high[v]), z - high_of<true>(high[v]));
-        }
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          const uint4v q = c.row(qt, c.rows_at, t, x);
-          O[t] = mfma32<true>(low, q, O[t]);
-          O[t] = mfma32<true>(high, q, O[t]);
-        }
-        if (x & 1) __builtin_amdgcn_sched_barrier(0);
+        w = mfma32<BF>(c.row(kt + jt * 64 * D, key_at, 0, x), c.row(qt + it * 64 * D, c.rows_at, 0, x), w);
+        beside(x);
       }
-#pragma unroll
-      for (int t = 0; t < 2; ++t) O[t] *= rise[t];
-    } else {
-      // S times the power of two that brings its largest to 2^13
+      return w;
+    };
+    // the slab of the state in words of 16 bits: `high` and `low` of elements 16x + 8h ..  (fp16: times `up`, its largest just below 2^14)
+    float up = 1.f, down = 1.f;
+    if constexpr (!BF) {
       float most = 0.f;
 #pragma unroll
       for (int b = 0; b < NB; ++b)
@@ -500,42 +510,90 @@ template <int D, bool BF> __global__ __launch_bounds__(2 * D, 2) void ftdecay_ch
       }
       int e = most > 0.f ? 140 - (int)(as_u(most) >> 23) : 0;
       e = __builtin_amdgcn_readfirstlane(e > 100 ? 100 : e);
-      const float up = as_f((uint32_t)(127 + e) << 23);
-#pragma unroll
-      for (int word = 1; word >= 0; --word) {
-#pragma unroll
-        for (int x = 0; x < D / 16; ++x) {
-          uint4v w;
-#pragma unroll
-          for (int v = 0; v < 4; ++v) {
-            const float y = S[x >> 1][8 * (x & 1) + 2 * v] * up, z = S[x >> 1][8 * (x & 1) + 2 * v + 1] * up;
-            w[v] = pack2<false>(y, z);
-            if (word) w[v] = pack2<false>((y - low_of<false>(w[v])) * 2048.f, (z - high_of<false>(w[v])) * 2048.f);
-          }
-#pragma unroll
-          for (int t = 0; t < 2; ++t) O[t] = mfma32<false>(w, c.row(qt, c.rows_at, t, x), O[t]);
-          if (x & 1) __builtin_amdgcn_sched_barrier(0);
-        }
-        if (word) {
-#pragma unroll
-          for (int t = 0; t < 2; ++t) O[t] *= 0x1p-11f;
-        }
-      }
-      const float down = as_f((uint32_t)(127 - e) << 23);
-#pragma unroll
-      for (int t = 0; t < 2; ++t) O[t] *= rise[t] * down;
+      up = as_f((uint32_t)(127 + e) << 23);
+      down = as_f((uint32_t)(127 - e) << 23);
     }
-    __builtin_amdgcn_sched_barrier(0);
+    struct Words { uint4v high, low; };
+    auto split = [&](Words& w, int x, int v) __attribute__((always_inline)) {
+      float y = S[x >> 1][8 * (x & 1) + 2 * v], z = S[x >> 1][8 * (x & 1) + 2 * v + 1];
+      if constexpr (!BF) {
+        y *= up;
+        z *= up;
+      }
+      w.high[v] = pack2<BF>(y, z);
+      y -= low_of<BF>(w.high[v]);
+      z -= high_of<BF>(w.high[v]);
+      w.low[v] = BF ? pack2<BF>(y, z) : pack2<BF>(y * 2048.f, z * 2048.f);
+    };
+    Words sw[2];
+    uint4v q[2][2];
+    const float16v w0 = scores(jt0, it0, [&](int x) __attribute__((always_inline)) {
+      if (x < 4) split(sw[0], 0, x);
+    });
+#pragma unroll
+    for (int t = 0; t < 2; ++t) q[0][t] = c.row(qt, c.rows_at, t, 0);
+    int limit = it0 == jt0 ? n - 8 * h : C;      // the last key of a row that the query sees, counted from 8h on
+    asm volatile("" : "+v"(limit));
+    c.here();
+    // What the state has of earlier tokens.
+    float16v O[2], Olow[2];
+    O[0] = O[1] = Olow[0] = Olow[1] = (float16v)0.f;
+    constexpr bool AHEAD = BF || D == 64;      // (queries are read a step ahead where there are registers for them)
+#pragma unroll
+    for (int x = 0; x < D / 16; ++x) {
+      if (!AHEAD && x)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) q[x & 1][t] = c.row(qt, c.rows_at, t, x);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int t = i & 1;
+        if (i < 2) (BF ? O : Olow)[t] = mfma32<BF>(sw[x & 1].low, q[x & 1][t], (BF ? O : Olow)[t]);
+        else O[t] = mfma32<BF>(sw[x & 1].high, q[x & 1][t], O[t]);
+        if (x + 1 < D / 16) {
+          if (i < 2 && AHEAD) q[(x + 1) & 1][t] = c.row(qt, c.rows_at, t, x + 1);
+          split(sw[(x + 1) & 1], x + 1 < D / 16 ? x + 1 : 0, i);
+        }
+        // 8 pairs of weights beside the instructions from the second step on
+        constexpr int STEP = (4 * (D / 16) - 4) / 8;
+        const int at = 4 * x + i - 4;
+        if (at >= 0 && at % STEP == 0 && at / STEP < 8) {
+          const int y = at / STEP;
+          weight(w0, limit, 2 * y);
+          if (y & 1) share(jt0, it0, y >> 1);
+        }
+        c.here();
+      }
+    }
+    if (NW == 2 && wave == 0) {
+      const float16v w1 = scores(1, 1, [](int) {});
+#pragma unroll
+      for (int y = 0; y < 8; ++y) {
+        weight(w1, limit, 2 * y);
+        if (y & 1) share(1, 1, y >> 1);
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const float up_to = t ? rise * rise32 : rise;
+      if constexpr (BF) O[t] *= up_to;
+      else {
+        const float f = up_to * down;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) O[t][v] = __builtin_fmaf(Olow[t][v], 0x1p-11f, O[t][v]) * f;
+      }
+    }
     uint4v vr[KS];
 #pragma unroll
     for (int s = 0; s < KS; ++s) vr[s] = c.template transposed<false>(vt, s, wave);
+    typename Chunk<D, BF>::Decayed d;
+    c.begin(d, 0);
     lds_written();                         // the weights are there, and nobody reads this chunk's queries and values any more
     if (i + 1 < chunks) {
       lq.issue(i + 1, g.tokens, qt);
       lv.issue(i + 1, g.tokens, vt);
     }
-    // Values that are not finite are left out of the product, which would bring them to tokens before theirs (0 times infinity); the tokens from theirs on get NaN.
-    int strange = C;
+    // Values that are not finite are left out of the products, which would bring them to tokens before theirs (0 times infinity); the tokens from theirs on, and the
+    // state, get NaN in their column.
     uint32_t most = 0;
 #pragma unroll
     for (int s = 0; s < KS; ++s)
@@ -543,69 +601,90 @@ template <int D, bool BF> __global__ __launch_bounds__(2 * D, 2) void ftdecay_ch
       for (int x = 0; x < 4; ++x)
         most = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(ushort2v, most), __builtin_bit_cast(ushort2v, vr[s][x] & 0x7FFF7FFFu)));
     constexpr uint32_t INF = BF ? 0x7F80u : 0x7C00u;
-    const bool any = __any((most & 0xFFFFu) >= INF || most >> 16 >= INF);
-    if (__builtin_expect(any, 0)) {
+    if (__builtin_expect(__any((most & 0xFFFFu) >= INF || most >> 16 >= INF), 0)) {
+      int first = C, from = 4 * h;
+      asm volatile("" : "+v"(from));
 #pragma unroll
       for (int s = KS - 1; s >= 0; --s)
 #pragma unroll
         for (int x = 7; x >= 0; --x) {
           const uint32_t mask = INF << 16 * (x & 1);
-          if ((vr[s][x >> 1] & mask) == mask) strange = 16 * s + x;
+          if ((vr[s][x >> 1] & mask) == mask) {
+            first = 16 * s + x;
+            vr[s][x >> 1] &= x & 1 ? 0xFFFFu : 0xFFFF0000u;
+          }
         }
-      strange = strange < C ? strange + 8 * h : C;
-      const int other = __shfl_xor(strange, 32);
-      strange = other < strange ? other : strange;
+      first = first < C ? first + 8 * h : C;
+      const int other = __shfl_xor(first, 32);
+      first = other < first ? other : first;
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        const int token = __shfl(first, from + 8 * (v >> 2) + (v & 3));
+#pragma unroll
+        for (int t = 0; t < 2; ++t) O[t][v] = 32 * t + n >= token ? __builtin_nanf("") : O[t][v];
+      }
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) S[b][v] = first < C ? __builtin_nanf("") : S[b][v];
     }
+    const float fading = in_scalar(tokens < C ? rest : whole.of(i));
+    c.here();
+    // The chunk's own tokens: for each step of 16 keys the query blocks that see some of them, the lower words first.  Beside them the state fades.
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
       uint4v v0 = vr[s], v1;
-      if (__builtin_expect(any, 0))
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          const uint32_t low = (v0[x] & INF) == INF ? 0u : 0xFFFFu, high = (v0[x] & INF << 16) == INF << 16 ? 0u : 0xFFFF0000u;
-          v0[x] &= low | high;
-        }
       if constexpr (!BF) {
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
-          const float y = low_of<false>(v0[x]), z = high_of<false>(v0[x]);
+          const float y = low_of<false>(vr[s][x]), z = high_of<false>(vr[s][x]);
           v0[x] = pack2<true>(y, z);
           v1[x] = pack2<true>(y - low_of<true>(v0[x]), z - high_of<true>(v0[x]));
         }
       }
+      uint4v p[2][2];
 #pragma unroll
       for (int t = s / 2; t < 2; ++t) {
         const uint32_t at = pt + t * (64 * C) + (weight_at ^ (uint32_t)(s << 5));
-        const uint4v p0 = *(const __attribute__((address_space(3))) uint4v*)(uintptr_t)at, p1 = *(const __attribute__((address_space(3))) uint4v*)(uintptr_t)(at + P_BYTES);
-        O[t] = mfma32<true>(v0, p1, O[t]);
-        if constexpr (!BF) O[t] = mfma32<true>(v1, p0, O[t]);
-        O[t] = mfma32<true>(v0, p0, O[t]);
+#pragma unroll
+        for (int x = 0; x < 2; ++x) p[t][x] = *(const __attribute__((address_space(3))) uint4v*)(uintptr_t)(at + x * P_BYTES);
       }
+#pragma unroll
+      for (int x = BF ? 1 : 2; x >= 0; --x)
+#pragma unroll
+        for (int t = s / 2; t < 2; ++t) {
+          O[t] = mfma32<true>(x == 2 ? v1 : v0, p[t][x == 1], O[t]);
+          const int done = x == 0 ? t : -1;
+          if (s < 2 || t == 1) {
+            // 16 parts of the fading, those of the first decayed values, over the last products of each step
+            if (done >= 0) {
+              constexpr int PLACES = 6;
+              const int at = s < 2 ? 2 * s + t : 2 + s;
+#pragma unroll
+              for (int y = 16 * at / PLACES; y < 16 * (at + 1) / PLACES; ++y) c.fade(S, fading, y);
+#pragma unroll
+              for (int y = c.PARTS * at / PLACES; y < c.PARTS * (at + 1) / PLACES; ++y) c.part(d, vr[0], y);
+            }
+          }
+          c.here();
+        }
     }
-    if (__builtin_expect(any, 0)) {
-      int first = 4 * h;
-      asm volatile("" : "+v"(first));
+    // Lane (h, n): token n of a block, columns 8z + 4h + r of the slab.  (Rows behind the last token: an offset that the buffer does not have.)
+    const auto out = __builtin_amdgcn_make_buffer_rsrc(o0 + (int64_t)(i * C) * a.o.token, 0, 0x7FFFFFFF, 0x00027000);
+    uint32_t o_at[2];
 #pragma unroll
-      for (int v = 0; v < 16; ++v) {
-        const int from_token = __shfl(strange, first + 8 * (v >> 2) + (v & 3));
+    for (int t = 0; t < 2; ++t) o_at[t] = 32 * t + n < tokens ? (uint32_t)n * (uint32_t)a.o.token + 8 * h : 0x80000000u;
+    auto store = [&](int y) __attribute__((always_inline)) {
+      const int t = y >> 2, z = y & 3;
+      __builtin_amdgcn_raw_buffer_store_b64(uint2v{pack2<BF>(O[t][4 * z], O[t][4 * z + 1]), pack2<BF>(O[t][4 * z + 2], O[t][4 * z + 3])}, out, (int)(o_at[t] + 16 * z),
+                                            t * 32 * (int)a.o.token, 0);
+    };
+    if constexpr (!BF)      // (the registers of these results are needed)
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
-          if (32 * t + n >= from_token) O[t][v] = __builtin_nanf("");
-      }
-    }
-    // lane (h, n): token n of a block, columns 8g + 4h + r of the slab
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const int r = 32 * t + n;
-      if (r < tokens) {
-        char* const to = o0 + (int64_t)(i * C + r) * a.o.token;
-#pragma unroll
-        for (int y = 0; y < 4; ++y)
-          *reinterpret_cast<uint2v*>(to + 2 * (8 * y + 4 * h)) = uint2v{pack2<BF>(O[t][4 * y], O[t][4 * y + 1]), pack2<BF>(O[t][4 * y + 2], O[t][4 * y + 3])};
-      }
-    }
-    __builtin_amdgcn_sched_barrier(0);
-    c.update(S, vr, tokens < C ? rest : whole, kt);
+      for (int y = 0; y < 8; ++y) store(y);
+    c.update(S, vr, d, kt, [&](int y) __attribute__((always_inline)) {
+      if constexpr (BF) store(y);
+    });
   }
   if (g.last && state) c.put(S, state);
 }
