@@ -38,35 +38,25 @@ struct Args {
   float* probability;
 };
 
-// Keys are ordered as their logits; both zeros have the same.  -infinity and NaN have 0, which nothing keeps.  (16 bits where the logits have as many.)
-template <int DT> struct Keys {
+// Logits of 16 bytes, and their keys: whole numbers that are ordered as they are (both zeros have the same), of as many bits as it takes.
+template <int DT> struct Type {
   static constexpr bool WIDE = DT == FTSAMPLE_F32;
-  static constexpr int PER = WIDE ? 4 : 8;               // elements of 16 bytes
-  static constexpr uint32_t INF = WIDE ? 0x7F800000u : DT == FTSAMPLE_BF16 ? 0x7F80u : 0x7C00u, SIGN = WIDE ? 0x80000000u : 0x8000u, ALL = WIDE ? 0xFFFFFFFFu : 0xFFFFu;
-  static constexpr uint32_t KEY_INFINITY = INF | SIGN;
-  static __device__ __forceinline__ uint32_t of_bits(uint32_t u) {
-    const uint32_t magnitude = u & (ALL ^ SIGN);
-    if (magnitude > INF || u == (INF | SIGN)) return 0;
-    return u & SIGN ? (magnitude ? ALL ^ u : SIGN) : u | SIGN;
+  static constexpr int SIZE = WIDE ? 4 : 2, PER = 16 / SIZE, DROP = WIDE ? 0 : DT == FTSAMPLE_BF16 ? 16 : 13;
+  static constexpr uint32_t NONE = WIDE ? 0xFF800000u : DT == FTSAMPLE_BF16 ? 0xFF80FF80u : 0xFC00FC00u;      // -infinity
+  static __device__ __forceinline__ float logit(const uint4v& r, int e) {
+    if constexpr (WIDE) return as_f(r[e]);
+    else return e & 1 ? high_of<DT == FTSAMPLE_BF16>(r[e >> 1]) : low_of<DT == FTSAMPLE_BF16>(r[e >> 1]);
   }
-  // A key at or below (above: at or above) those of all logits that are at least (at most) x.
-  static __device__ __forceinline__ uint32_t near(float x, bool above) {
-    if (!(x == x)) return above ? ALL : 1u;
-    const uint32_t u = as_u(x), wide = u & 0x80000000u ? ~u : u | 0x80000000u;
-    if constexpr (WIDE) return above ? (wide > 0xFFFFFFF0u ? ALL : wide + 2) : (wide < 3 ? 1u : wide - 2);
-    else if constexpr (DT == FTSAMPLE_BF16) return above ? ((wide >> 16) + 1 > ALL ? ALL : (wide >> 16) + 1) : ((wide >> 16) < 2 ? 1u : (wide >> 16) - 1);
-    else {
-      const uint32_t h = (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)x), k = h & SIGN ? ALL ^ h : h | SIGN;
-      return above ? (k + 1 > ALL ? ALL : k + 1) : (k < 2 ? 1u : k - 1);
-    }
+  static __device__ __forceinline__ uint32_t key(float x) {
+    const uint32_t u = as_u(x + 0.f);
+    return (u & 0x80000000u ? ~u : u | 0x80000000u) >> DROP;
   }
-  static __device__ __forceinline__ float logit(uint32_t k) {
-    const uint32_t u = k & SIGN ? k ^ SIGN : ALL ^ k;
-    if constexpr (WIDE) return as_f(u);
-    else if constexpr (DT == FTSAMPLE_BF16) return as_f(u << 16);
-    else return (float)__builtin_bit_cast(half2v, u)[0];
+  static __device__ __forceinline__ float of_key(uint32_t k) {
+    const uint32_t u = k << DROP;
+    return as_f(u & 0x80000000u ? u ^ 0x80000000u : ~(u | ((1u << DROP) - 1)));
   }
 };
+constexpr float NOTHING = -__builtin_inff();
 
 // The rules of a row, as they hold.
 struct Rules {
@@ -98,13 +88,8 @@ struct Weights {
   double scale, most;        // STEPS / (temperature * ln 2); the largest logit
   const double* table;       // 2^(i / STEPS)
   int shift;
-  uint32_t infinite;         // the largest key where it stands for +infinity, else 0
-  // w, and the number of the bin (0: the largest weights; STEPS * OCTAVES: nothing)
-  __device__ __forceinline__ unsigned long long of(float x, uint32_t key, int& bin) const {
-    if (__builtin_expect(infinite != 0, 0)) {
-      bin = key == infinite ? 0 : STEPS * OCTAVES;
-      return key == infinite ? 1ull << shift : 0ull;
-    }
+  // w (of -infinity and NaN: 0), and the number of the bin (0: the largest weights; STEPS * OCTAVES: nothing)
+  __device__ __forceinline__ unsigned long long of(float x, int& bin) const {
     constexpr double ROUND = 6755399441055744.0;      // 1.5 * 2^52
     const double t = __builtin_fmax(((double)x - most) * scale, -(double)(STEPS * OCTAVES));
     const double at = t + ROUND, r = t - (at - ROUND);
@@ -122,15 +107,55 @@ struct Weights {
 };
 static_assert(STEPS == 128, "the octave is n >> 7");
 
+// Sums over the lanes up to this one: rows of 16 by shifts, then their last lanes handed on.
+template <int CTRL, int ROWS> __device__ __forceinline__ uint32_t shifted(uint32_t x) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xF, false); }
+template <int CTRL, int ROWS> __device__ __forceinline__ unsigned long long shifted(unsigned long long x) {
+  return (unsigned long long)shifted<CTRL, ROWS>((uint32_t)(x >> 32)) << 32 | shifted<CTRL, ROWS>((uint32_t)x);
+}
+template <class T> __device__ __forceinline__ T sum_upto(T x) {
+  x += shifted<0x111, 0xF>(x);
+  x += shifted<0x112, 0xF>(x);
+  x += shifted<0x114, 0xF>(x);
+  x += shifted<0x118, 0xF>(x);
+  x += shifted<0x142, 0xA>(x);
+  return x + shifted<0x143, 0xC>(x);
+}
+// The value of lane ^ J.
+template <int J> __device__ __forceinline__ uint32_t across(uint32_t x) {
+  if constexpr (J == 1) return (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0xB1, 0xF, 0xF, false);           // quad_perm 1 0 3 2
+  else if constexpr (J == 2) return (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x4E, 0xF, 0xF, false);      // quad_perm 2 3 0 1
+  else if constexpr (J == 4) return (uint32_t)__builtin_amdgcn_ds_swizzle((int)x, 4 << 10 | 0x1F);
+  else if constexpr (J == 8) return (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x128, 0xF, 0xF, false);     // row_ror 8
+  else if constexpr (J == 16) {
+    const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    return threadIdx.x & 16 ? r[0] : r[1];
+  } else {
+    const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    return threadIdx.x & 32 ? r[0] : r[1];
+  }
+}
+template <int J> __device__ __forceinline__ float across(float x) { return as_f(across<J>(as_u(x))); }
+template <int J> __device__ __forceinline__ unsigned long long across(unsigned long long x) {
+  return (unsigned long long)across<J>((uint32_t)(x >> 32)) << 32 | across<J>((uint32_t)x);
+}
+// Steps of a bitonic sort, the largest first, over lanes J, J / 2, .. 1 apart; K: how many are merged in one direction.
+template <int J, class T> __device__ __forceinline__ void merge(T& x, int at, int K) {
+  const T other = across<J>(x);
+  const bool larger = ((at & J) == 0) == ((at & K) == 0);
+  x = larger == (other > x) ? other : x;
+  if constexpr (J > 1) merge<J / 2>(x, at, K);
+}
+template <int K = 2, class T> __device__ __forceinline__ void sort_wave(T& x, int at) {
+  merge<K / 2>(x, at, K);
+  if constexpr (K < 64) sort_wave<2 * K>(x, at);
+}
+__device__ __forceinline__ uint32_t last_lane(uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane((int)x, 63); }
+__device__ __forceinline__ unsigned long long last_lane(unsigned long long x) { return (unsigned long long)last_lane((uint32_t)(x >> 32)) << 32 | last_lane((uint32_t)x); }
+
 // Sums over the workgroup of up to and before this thread's value.
 template <class T> __device__ __forceinline__ T before_me(T x, T* scratch, T& all) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  T upto = x;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const T y = __shfl_up(upto, d);
-    if (lane >= d) upto += y;
-  }
+  const T upto = sum_upto(x);
   __syncthreads();
   if (lane == 63) scratch[wave] = upto;
   __syncthreads();
@@ -143,17 +168,10 @@ template <class T> __device__ __forceinline__ T before_me(T x, T* scratch, T& al
   return mine + upto - x;
 }
 
-template <class T> __device__ __forceinline__ T wave_sum(T x) {
+template <class T> __device__ __forceinline__ T wave_sum(T x) { return last_lane(sum_upto(x)); }
+__device__ __forceinline__ float wave_most(float x) {
 #pragma unroll
-  for (int d = 32; d; d >>= 1) x += __shfl_xor(x, d);
-  return x;
-}
-__device__ __forceinline__ uint32_t wave_most(uint32_t x) {
-#pragma unroll
-  for (int d = 32; d; d >>= 1) {
-    const uint32_t y = __shfl_xor(x, d);
-    x = y > x ? y : x;
-  }
+  for (int d = 32; d; d >>= 1) x = __builtin_fmaxf(x, __shfl_xor(x, d));
   return x;
 }
 
@@ -185,43 +203,42 @@ template <int PER, class F> __device__ __forceinline__ void find_bin(Shared& s, 
   __syncthreads();
 }
 
-// The keys of a row, as the waves have them: wave w has neighbouring tokens, lane l of it those of its words l, l + 64, .. of 16 bytes; up to 32 words a lane in
+// The logits of a row, as the waves have them: wave w has neighbouring tokens, lane l of it those of its words l, l + 64, .. of 16 bytes; up to 32 words a lane in
 // registers (HELD), or read anew every time.
 template <int DT, bool HELD> struct Row {
-  typedef Keys<DT> K;
+  typedef Type<DT> L;
   typedef uint32_t Words __attribute__((ext_vector_type(MOST_WORDS)));
-  static constexpr int PER = K::PER;
+  static constexpr int PER = L::PER;
   const char* x;           // aligned to 16 bytes, `skip` elements before the row
   int skip, vocab, words;  // words of a lane
   int first;               // this lane's first word
+  bool flat;               // the largest logit is +infinity: those that are it count as 0, the others as -infinity
   Words held[HELD ? 4 : 1];      // (a register of each word, by its number: read with an index that is the same in all lanes)
   __device__ __forceinline__ Row(const Args& a, int row) : vocab(a.vocab) {
-    constexpr int SIZE = K::WIDE ? 4 : 2;
-    const char* const at = static_cast<const char*>(a.logits) + (int64_t)row * a.stride * SIZE;
-    skip = (int)((uintptr_t)at & 15) / SIZE;
-    x = at - skip * SIZE;
+    const char* const at = static_cast<const char*>(a.logits) + (int64_t)row * a.stride * L::SIZE;
+    skip = (int)((uintptr_t)at & 15) / L::SIZE;
+    x = at - skip * L::SIZE;
     words = ((vocab + skip + PER - 1) / PER + THREADS - 1) / THREADS;
     first = (int)(threadIdx.x >> 6) * words * 64 + (int)(threadIdx.x & 63);
+    flat = false;
     if constexpr (HELD) {
 #pragma unroll
       for (int v = 0; v < MOST_WORDS; ++v) {
-        uint4v r = nothing();
+        uint4v r = {L::NONE, L::NONE, L::NONE, L::NONE};
         if (v < words && whole(first + 64 * v)) r = load(first + 64 * v);
 #pragma unroll
         for (int w = 0; w < 4; ++w) held[w][v] = r[w];
       }
-      // the row's first and last word may lie in it only in part
+      // the row's first and last word, where they lie in it only in part
+      const int last = (vocab + skip - 1) / PER;
 #pragma unroll 1
-      for (int v = 0; v < words; ++v) {
-        uint4v r = {held[0][v], held[1][v], held[2][v], held[3][v]};
-        const int word = first + 64 * v;
-        if (__any(!whole(word) && some(word))) {
-          const uint4v y = part(word);
-          if (!whole(word) && some(word)) r = y;
-        }
-        r = keys(r);
+      for (int side = 0; side < 2; ++side) {
+        const int word = side ? last : 0, w0 = word / (words * 64), v = word % (words * 64) / 64;
+        if ((int)(threadIdx.x >> 6) != w0 || whole(word)) continue;
+        const uint4v y = part(word);
+        const bool mine = first + 64 * v == word;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) held[w][v] = r[w];
+        for (int w = 0; w < 4; ++w) held[w][v] = mine ? y[w] : held[w][v];
       }
     }
   }
@@ -229,90 +246,112 @@ template <int DT, bool HELD> struct Row {
   __device__ __forceinline__ bool whole(int word) const { return word * PER >= skip && word * PER - skip + PER <= vocab; }
   __device__ __forceinline__ bool some(int word) const { return word * PER - skip + PER > 0 && word * PER - skip < vocab; }
   __device__ __forceinline__ uint4v load(int word) const { return *reinterpret_cast<const uint4v*>(x + (int64_t)word * 16); }
-  static __device__ __forceinline__ uint4v nothing() {
-    constexpr uint32_t none = K::WIDE ? K::INF | K::SIGN : (K::INF | K::SIGN) * 0x10001u;
-    return uint4v{none, none, none, none};
-  }
   __device__ __forceinline__ uint4v part(int word) const {
-    uint4v r = nothing();
+    uint4v r = {L::NONE, L::NONE, L::NONE, L::NONE};
     const int i = word * PER - skip;
 #pragma unroll
     for (int e = 0; e < PER; ++e) {
       if (i + e < 0 || i + e >= vocab) continue;
-      if constexpr (K::WIDE) r[e] = reinterpret_cast<const uint32_t*>(x)[(int64_t)word * PER + e];
+      if constexpr (L::WIDE) r[e] = reinterpret_cast<const uint32_t*>(x)[(int64_t)word * PER + e];
       else r[e >> 1] = (r[e >> 1] & ~(0xFFFFu << 16 * (e & 1))) | (uint32_t)reinterpret_cast<const uint16_t*>(x)[(int64_t)word * PER + e] << 16 * (e & 1);
     }
     return r;
   }
-  static __device__ __forceinline__ uint4v keys(uint4v r) {
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      if constexpr (K::WIDE) r[w] = K::of_bits(r[w]);
-      else r[w] = K::of_bits(r[w] & 0xFFFFu) | K::of_bits(r[w] >> 16) << 16;
-    }
-    return r;
-  }
-  static __device__ __forceinline__ uint32_t key(const uint4v& k, int e) {
-    if constexpr (K::WIDE) return k[e];
-    else return k[e >> 1] >> 16 * (e & 1) & 0xFFFFu;
-  }
-  // f(v, keys) for every word of this lane
+  // f(v, word) for every word of this lane
   template <class F> __device__ __forceinline__ void each_word(F f) const {
 #pragma unroll 1
     for (int v = 0; v < words; ++v) {
-      if constexpr (HELD) f(v, uint4v{held[0][v], held[1][v], held[2][v], held[3][v]});
-      else {
-        const int word = first + 64 * v;
-        f(v, keys(whole(word) ? load(word) : part(word)));
-      }
+      if constexpr (HELD) f(v, flattened(uint4v{held[0][v], held[1][v], held[2][v], held[3][v]}));
+      else f(v, word(first + 64 * v));
     }
   }
-  template <class F> __device__ __forceinline__ void each(F f) const {
-    each_word([&](int, const uint4v& k) __attribute__((always_inline)) {
+  // Any word, from memory.
+  __device__ __forceinline__ uint4v word(int i) const { return flattened(whole(i) ? load(i) : part(i)); }
+  __device__ __forceinline__ uint4v flattened(uint4v r) const {
+    if (__builtin_expect(flat, 0)) {
 #pragma unroll
-      for (int e = 0; e < PER; ++e) f(key(k, e));
+      for (int e = 0; e < PER; ++e) {
+        const bool is = L::logit(r, e) == -NOTHING;
+        if constexpr (L::WIDE) r[e] = is ? 0u : L::NONE;
+        else r[e >> 1] = (r[e >> 1] & ~(0xFFFFu << 16 * (e & 1))) | (is ? 0u : L::NONE & 0xFFFFu << 16 * (e & 1));
+      }
+    }
+    return r;
+  }
+  template <class F> __device__ __forceinline__ void each(F f) const {
+    each_word([&](int, const uint4v& r) __attribute__((always_inline)) {
+#pragma unroll
+      for (int e = 0; e < PER; ++e) f(L::logit(r, e));
     });
   }
   __device__ __forceinline__ int token(int v, int e) const { return (first + 64 * v) * PER + e - skip; }
 };
 
-// What the rules have left: keys above `border`, and the first `equal` of those that are it; of those, weights of at least `floor`.
+// What the rules have left: logits above `border`, and the first `equal` of those that are it; of those, weights of at least `floor`.
 struct Kept {
-  uint32_t border;
+  float border;
   int equal;
   unsigned long long floor;
 };
 
 template <int DT, bool HELD>
 __global__ __launch_bounds__(THREADS) void ftsample_row(const Args a) {
-  typedef Keys<DT> K;
+  typedef Type<DT> L;
   __shared__ Shared s;
   __shared__ unsigned long long list[LIST];      // (under top_k) key and place, then weights by place
   __shared__ int listed[LIST];
   const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const Row<DT, HELD> x(a, row);
-  if (tid < STEPS) s.table[tid] = exp2((double)tid / STEPS);
   const Rules r = rules_of(a, row);
+  Row<DT, HELD> x(a, row);
+  if (tid < STEPS) s.table[tid] = exp2((double)tid / STEPS);
 
-  uint32_t mine = 0;
-  x.each([&](uint32_t k) __attribute__((always_inline)) { mine = k > mine ? k : mine; });
-  uint32_t most = wave_most(mine);
-  if (lane == 0) s.words[wave] = most;
+  float mine = NOTHING;
+  x.each([&](float y) __attribute__((always_inline)) { mine = __builtin_fmaxf(mine, y); });
+  float most = wave_most(mine);
+  if (lane == 0) s.words[wave] = as_u(most);
   __syncthreads();
 #pragma unroll
-  for (int w = 0; w < WAVES; ++w) most = s.words[w] > most ? s.words[w] : most;
+  for (int w = 0; w < WAVES; ++w) most = __builtin_fmaxf(most, as_f(s.words[w]));
   auto answer = [&](int token, double chance) {
     a.tokens[row] = token;
     if (a.probability) a.probability[row] = (float)chance;
   };
-  if (most == 0) {
+  if (!(most > NOTHING)) {
     if (tid == 0) answer(-1, 0.0);
     return;
   }
-  const Weights weights{r.per_t * (STEPS / 0.69314718055994530942), (double)K::logit(most), s.table, a.shift, most == K::KEY_INFINITY ? most : 0u};
-  auto weight = [&](uint32_t k) __attribute__((always_inline)) {
+  if (most == -NOTHING) {
+    x.flat = true;
+    most = 0.f;
+    mine = mine == -NOTHING ? 0.f : NOTHING;
+  }
+  if (r.top_k == 1) {      // the first that is as large
+    int token = 0x7FFFFFFF;
+    x.each_word([&](int v, const uint4v& k) __attribute__((always_inline)) {
+#pragma unroll
+      for (int e = L::PER - 1; e >= 0; --e) {
+        const int t = x.token(v, e);
+        token = L::logit(k, e) == most && t < token ? t : token;
+      }
+    });
+#pragma unroll
+    for (int d = 32; d; d >>= 1) {
+      const int y = __shfl_xor(token, d);
+      token = y < token ? y : token;
+    }
+    __syncthreads();
+    if (lane == 0) s.words[wave] = (uint32_t)token;
+    __syncthreads();
+    if (tid == 0) {
+      for (int w = 1; w < WAVES; ++w) token = (int)s.words[w] < token ? (int)s.words[w] : token;
+      answer(token, 1.0);
+    }
+    return;
+  }
+  const Weights weights{r.per_t * (STEPS / 0.69314718055994530942), (double)most, s.table, a.shift};
+  auto weight = [&](float y) __attribute__((always_inline)) {
     int bin;
-    return weights.of(K::logit(k), k, bin);
+    return weights.of(y, bin);
   };
   const unsigned long long floor = (unsigned long long)__builtin_ceil(__builtin_ldexp(r.floor, a.shift));
   auto limit_of = [&](unsigned long long all) -> unsigned long long {      // the least whole number that is top_p of all, or 1
@@ -321,7 +360,7 @@ __global__ __launch_bounds__(THREADS) void ftsample_row(const Args a) {
   };
 
   // The first place at which the sum of kept weights exceeds u times all: whole numbers exceed it where they reach the next one.  sum: this wave's kept weights without those of the
-  // border; ties: how many keys of it are the border.
+  // border; ties: how many logits of it are the border.
   auto choose = [&](const Kept& kept, unsigned long long sum, uint32_t ties) {
     const unsigned long long each = kept.equal ? weight(kept.border) : 0, worth = each >= kept.floor || kept.border == most ? each : 0;
     __syncthreads();
@@ -330,138 +369,183 @@ __global__ __launch_bounds__(THREADS) void ftsample_row(const Args a) {
       s.words[wave] = ties;
     }
     __syncthreads();
-    unsigned long long before = 0, all = 0, inside = 0;
-    int left = kept.equal, allowed = 0;
+    unsigned long long all = 0;
+    {
+      int left = kept.equal;
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) {
-      const int n = (int)s.words[w] < left ? (int)s.words[w] : left;
-      const unsigned long long here = s.sums[w] + (unsigned long long)n * worth;
-      if (w < wave) before += here;
-      if (w == wave) {
-        allowed = n;
-        inside = here;
+      for (int w = 0; w < WAVES; ++w) {
+        const int n = (int)s.words[w] < left ? (int)s.words[w] : left;
+        all += s.sums[w] + (unsigned long long)n * worth;
+        left -= n;
       }
-      left -= n;
-      all += here;
     }
     const unsigned long long goal = (unsigned long long)__builtin_floor(r.u * (double)all) + 1;
-    if (before >= goal || before + inside < goal) return;      // (another wave)
-    bool done = false;
-    x.each_word([&](int v, const uint4v& k) {
-      if (done) return;
-      uint32_t n = 0;
+    // The wave in whose run of words it lies; all waves look for it in an eighth of that run each, and so on until few words are left.
+    auto add_up = [&](const uint4v& k, unsigned long long (&w)[L::PER], uint32_t& n) __attribute__((always_inline)) -> unsigned long long {
+      unsigned long long sum = 0;
 #pragma unroll
-      for (int e = 0; e < K::PER; ++e) n += kept.equal && Row<DT, HELD>::key(k, e) == kept.border;
-      // ties of lanes before this one
-      uint32_t upto = n;
-#pragma unroll
-      for (int d = 1; d < 64; d <<= 1) {
-        const uint32_t y = __shfl_up(upto, d);
-        if (lane >= d) upto += y;
+      for (int e = 0; e < L::PER; ++e) {
+        const float y = L::logit(k, e);
+        w[e] = weight(y);
+        w[e] = y > kept.border && (w[e] >= kept.floor || y == most) ? w[e] : 0;
+        n += kept.equal && y == kept.border;
+        sum += w[e];
       }
-      int mine = allowed - (int)(upto - n);
-      auto one = [&](int e) __attribute__((always_inline)) -> unsigned long long {
-        const uint32_t key = Row<DT, HELD>::key(k, e);
-        if (key == 0 || key < kept.border) return 0;
-        if (key == kept.border) return mine-- > 0 ? worth : 0;
-        const unsigned long long w = weight(key);
-        return key == most || w >= kept.floor ? w : 0;
-      };
-      const int held = mine;
-      unsigned long long lane_sum = 0;
-#pragma unroll
-      for (int e = 0; e < K::PER; ++e) lane_sum += one(e);
-      unsigned long long lane_upto = lane_sum;
-#pragma unroll
-      for (int d = 1; d < 64; d <<= 1) {
-        const unsigned long long y = __shfl_up(lane_upto, d);
-        if (lane >= d) lane_upto += y;
-      }
-      unsigned long long at = before + lane_upto - lane_sum;
-      if (at < goal && at + lane_sum >= goal) {
-        mine = held;
-#pragma unroll
-        for (int e = 0; e < K::PER; ++e) {
-          const unsigned long long w = one(e);
-          if (at < goal && at + w >= goal) answer(x.token(v, e), (double)w / (double)all);
-          at += w;
+      return sum;
+    };
+    unsigned long long before = 0;
+    int left = kept.equal, run = 0, length = x.words;      // of words of 64 lanes each
+    // After the parts' sums are in s: the part that it lies in.  (The last one that is not empty takes what no other does, so that every round leaves an eighth.)
+    auto part_of = [&](int per) {
+#pragma unroll 1
+      for (int w = 0;; ++w) {
+        const int n = (int)s.words[w] < left ? (int)s.words[w] : left;
+        const unsigned long long here = s.sums[w] + (unsigned long long)n * worth;
+        if (before + here >= goal || (w + 1) * per >= length) {
+          run += w * per;
+          length = length - w * per < per ? length - w * per : per;
+          return;
         }
+        before += here;
+        left -= n;
       }
-      const int n_all = (int)__shfl(upto, 63);
-      allowed -= n_all < allowed ? n_all : allowed;
-      before += __shfl(lane_upto, 63);
+    };
+    length = WAVES * x.words;
+    part_of(x.words);
+    while (length > 4) {
+      const int per = (length + WAVES - 1) / WAVES, end = length < (wave + 1) * per ? length : (wave + 1) * per;
+      unsigned long long mine = 0;
+      uint32_t n = 0;
+#pragma unroll 1
+      for (int v = wave * per; v < end; ++v) {
+        unsigned long long w[L::PER];
+        mine += add_up(x.word(64 * (run + v) + lane), w, n);
+      }
+      mine = wave_sum(mine);
+      n = wave_sum(n);
+      __syncthreads();
+      if (lane == 0) {
+        s.sums[wave] = mine;
+        s.words[wave] = n;
+      }
+      __syncthreads();
+      part_of(per);
+    }
+    if (wave) return;
+    bool done = false;
+#pragma unroll 1
+    for (int v = run; v < run + length && !done; ++v) {
+      const uint4v k = x.word(64 * v + lane);
+      unsigned long long w[L::PER];
+      uint32_t n = 0;
+      unsigned long long sum = add_up(k, w, n);
+      if (kept.equal && __any(n != 0)) {
+        // those of the border that are left, in the order of their tokens
+        const uint32_t upto = sum_upto(n);
+        int mine = left - (int)(upto - n);
+#pragma unroll
+        for (int e = 0; e < L::PER; ++e)
+          if (L::logit(k, e) == kept.border && mine-- > 0) {
+            w[e] = worth;
+            sum += worth;
+          }
+        const int all_n = (int)last_lane(upto);
+        left -= all_n < left ? all_n : left;
+      }
+      const unsigned long long upto = sum_upto(sum);
+      unsigned long long at = before + upto - sum;
+      if (at < goal && at + sum >= goal)
+#pragma unroll
+        for (int e = 0; e < L::PER; ++e) {
+          if (at < goal && at + w[e] >= goal) answer((64 * v + lane) * L::PER + e - x.skip, (double)w[e] / (double)all);
+          at += w[e];
+        }
+      before += last_lane(upto);
       done = before >= goal;
-    });
+    }
   };
   auto sum_up = [&](const Kept& kept) {
     unsigned long long sum = 0;
     uint32_t ties = 0;
-    x.each([&](uint32_t k) __attribute__((always_inline)) {
-      if (k > kept.border) {
-        const unsigned long long w = weight(k);
-        sum += k == most || w >= kept.floor ? w : 0;
+    x.each_word([&](int, const uint4v& k) __attribute__((always_inline)) {
+      bool some = false;
+#pragma unroll
+      for (int e = 0; e < L::PER; ++e) some |= L::logit(k, e) >= kept.border;
+      if (!__any(some)) return;
+#pragma unroll
+      for (int e = 0; e < L::PER; ++e) {
+        const float y = L::logit(k, e);
+        const unsigned long long w = weight(y);
+        sum += y > kept.border && (w >= kept.floor || y == most) ? w : 0;
+        ties += y == kept.border;
       }
-      ties += k == kept.border;
     });
     choose(kept, wave_sum(sum), wave_sum(kept.equal ? ties : 0u));
   };
 
-  // The border moves up to the lowest key above which less than `limit` lies, by counts or by sums of weights; among the keys of lowest .. highest.
-  Kept kept{0, 0, floor};
+  // The border moves up to the lowest logit above which less than `limit` lies, by counts or by sums of weights; among those with keys lowest .. highest.
+  Kept kept{NOTHING, 0, floor};
+  const uint32_t top_key = L::key(most);
+  auto empty_bins = [&]() {
+    __syncthreads();
+    for (int i = tid; i < BINS; i += THREADS) s.bins[i] = 0;
+    __syncthreads();
+  };
+  // after bins of keys highest - k >> drop are filled
+  auto narrow = [&](uint32_t& lowest, uint32_t& highest, int drop, unsigned long long& above, unsigned long long limit) {
+    __syncthreads();
+    find_bin<BINS / THREADS>(s, above, limit, [&](int i) { return s.bins[i]; });
+    above = s.above;
+    const uint32_t top = highest - (s.bin << drop), least = top - ((1u << drop) - 1);
+    lowest = least > lowest && least <= top ? least : lowest;
+    highest = top;
+  };
+  auto drop_of = [](uint32_t range) {
+    const int bits = 32 - __builtin_clz(range);
+    return bits > BITS ? bits - BITS : 0;
+  };
   auto search = [&](unsigned long long limit, bool by_weight, uint32_t lowest, uint32_t highest, unsigned long long above) {
     while (lowest != highest) {
-      const uint32_t range = highest - lowest;
-      const int bits = 32 - __builtin_clz(range), drop = bits > BITS ? bits - BITS : 0;
-      __syncthreads();
-      for (int i = tid; i < BINS; i += THREADS) s.bins[i] = 0;
-      __syncthreads();
-      x.each([&](uint32_t k) __attribute__((always_inline)) {
-        if (k < lowest || k > highest || k <= kept.border) return;
-        atomicAdd(&s.bins[(highest - k) >> drop], by_weight ? weight(k) : 1ull);
+      const int drop = drop_of(highest - lowest);
+      const float from = L::of_key(lowest), to = L::of_key(highest);
+      empty_bins();
+      x.each_word([&](int, const uint4v& k) __attribute__((always_inline)) {
+#pragma unroll
+        for (int e = 0; e < L::PER; ++e) {
+          const float y = L::logit(k, e);
+          if (y >= from && y <= to && y > kept.border) atomicAdd(&s.bins[(highest - L::key(y)) >> drop], by_weight ? weight(y) : 1ull);
+        }
       });
       __syncthreads();
       // (the kept ones of the border that there is)
-      if (tid == 0 && kept.equal && kept.border >= lowest && kept.border <= highest) s.bins[(highest - kept.border) >> drop] += (by_weight ? weight(kept.border) : 1ull) * (unsigned)kept.equal;
-      __syncthreads();
-      find_bin<BINS / THREADS>(s, above, limit, [&](int i) { return s.bins[i]; });
-      above = s.above;
-      const uint32_t top = highest - (s.bin << drop), least = top - ((1u << drop) - 1);
-      lowest = least > lowest && least <= top ? least : lowest;
-      highest = top;
-      __syncthreads();
+      if (tid == 0 && kept.equal && kept.border >= from && kept.border <= to) s.bins[(highest - L::key(kept.border)) >> drop] += (by_weight ? weight(kept.border) : 1ull) * (unsigned)kept.equal;
+      narrow(lowest, highest, drop, above, limit);
     }
-    // of the keys that are the border, as many as fit
-    const unsigned long long each = by_weight ? weight(lowest) : 1;
+    // of the logits that are the border, as many as fit
+    const float border = L::of_key(lowest);
+    const unsigned long long each = by_weight ? weight(border) : 1;
     unsigned long long fit = each ? (limit - above + each - 1) / each : 0x7FFFFFFFull;
-    if (lowest == kept.border && (unsigned long long)kept.equal < fit) fit = kept.equal;
-    kept.border = lowest;
+    if (border == kept.border && (unsigned long long)kept.equal < fit) fit = kept.equal;
+    kept.border = border;
     kept.equal = (int)(fit > 0x7FFFFFFFull ? 0x7FFFFFFFull : fit);
   };
+  const uint32_t least_key = L::key(NOTHING) + 1;
 
   if (r.top_k < x.vocab) {
-    bool sorted = false;
     if (r.top_k <= MOST_LISTED) {
-      // The top_k-th largest of the threads' maxima: at least top_k keys are as large.  Its highest bits are enough for a bound: two levels.
-      uint32_t lowest = 1, highest = most;
-      unsigned long long above = 0;
-      for (int level = 0; level < 2 && lowest != highest; ++level) {
-        const int bits = 32 - __builtin_clz(highest - lowest), drop = bits > BITS ? bits - BITS : 0;
-        __syncthreads();
-        for (int i = tid; i < BINS; i += THREADS) s.bins[i] = 0;
-        __syncthreads();
-        if (mine >= lowest && mine <= highest) atomicAdd(&s.bins[(highest - mine) >> drop], 1ull);
-        __syncthreads();
-        find_bin<BINS / THREADS>(s, above, (unsigned long long)r.top_k, [&](int i) { return s.bins[i]; });
-        above = s.above;
-        const uint32_t top = highest - (s.bin << drop), least = top - ((1u << drop) - 1);
-        lowest = least > lowest && least <= top ? least : lowest;
-        highest = top;
-        __syncthreads();
-      }
-      uint32_t n = 0, maxima;
-      before_me<uint32_t>(mine >= lowest ? 1u : 0u, s.words, maxima);
-      if (maxima < (uint32_t)r.top_k) lowest = 1;      // (fewer of them that can be chosen)
-      x.each([&](uint32_t k) __attribute__((always_inline)) { n += k >= lowest; });
+      // A bound that at least top_k logits reach (or all that can be chosen): of every wave's 64 maxima the (top_k / 8)-th largest, of these the smallest.
+      float sorted = mine;
+      sort_wave(sorted, lane);
+      const float mine_of_wave = as_f((uint32_t)__builtin_amdgcn_readlane((int)as_u(sorted), (r.top_k + WAVES - 1) / WAVES - 1));
+      __syncthreads();
+      if (lane == 0) s.words[wave] = as_u(mine_of_wave);
+      __syncthreads();
+      float from = as_f(s.words[0]);
+#pragma unroll
+      for (int w = 1; w < WAVES; ++w) from = __builtin_fminf(from, as_f(s.words[w]));
+      from = __builtin_fmaxf(from, L::of_key(least_key));      // (where fewer can be chosen)
+      uint32_t n = 0;
+      x.each([&](float y) __attribute__((always_inline)) { n += y >= from; });
       __syncthreads();
       const uint32_t in_wave = wave_sum(n);
       if (lane == 0) s.words[wave] = in_wave;
@@ -473,53 +557,41 @@ __global__ __launch_bounds__(THREADS) void ftsample_row(const Args a) {
         count += s.words[w];
       }
       if (count <= LIST) {
-        sorted = true;
-        // the keys in the order of their tokens: (key, place) in the list, tokens by place
+        // the logits in the order of their tokens: (key, place) in the list, tokens by place
         if (in_wave)
           x.each_word([&](int v, const uint4v& k) {
             uint32_t m = 0;
 #pragma unroll
-            for (int e = 0; e < K::PER; ++e) m += Row<DT, HELD>::key(k, e) >= lowest;
+            for (int e = 0; e < L::PER; ++e) m += L::logit(k, e) >= from;
             if (!__any(m != 0)) return;
-            uint32_t upto = m;
-#pragma unroll
-            for (int d = 1; d < 64; d <<= 1) {
-              const uint32_t y = __shfl_up(upto, d);
-              if (lane >= d) upto += y;
-            }
+            const uint32_t upto = sum_upto(m);
             uint32_t place = at + upto - m;
 #pragma unroll
-            for (int e = 0; e < K::PER; ++e) {
-              const uint32_t key = Row<DT, HELD>::key(k, e);
-              if (key < lowest) continue;
-              list[place] = (unsigned long long)key << 32 | (0xFFFFFFFFu - place);
+            for (int e = 0; e < L::PER; ++e) {
+              const float y = L::logit(k, e);
+              if (!(y >= from)) continue;
+              list[place] = (unsigned long long)L::key(y) << 32 | (0xFFFFFFFFu - place);
               listed[place] = x.token(v, e);
               ++place;
             }
-            at += __shfl(upto, 63);
+            at += last_lane(upto);
           });
         __syncthreads();
-        // sorted, the largest first: thread i has the i-th.  Distances below 64 stay inside a wave.
-        int size = 64;
-        while (size < (int)count) size <<= 1;
+        // sorted, the largest first: thread i has the i-th
         unsigned long long e = tid < (int)count ? list[tid] : 0;
-        for (int k = 2; k <= size; k <<= 1)
-          for (int j = k >> 1; j > 0; j >>= 1) {
-            unsigned long long other;
-            if (j >= 64) {
-              __syncthreads();
-              list[tid] = e;
-              __syncthreads();
-              other = list[tid ^ j];
-            } else {
-              other = __shfl_xor(e, j);
-            }
-            const bool larger_first = (tid & k) == 0, lower = (tid & j) == 0;
-            const bool take = (lower == larger_first) ? other > e : other < e;
-            if (take) e = other;
+        sort_wave(e, tid);
+        for (int k = 128; k < 2 * (int)count && k <= LIST; k <<= 1) {
+          for (int j = k >> 1; j >= 64; j >>= 1) {
+            __syncthreads();
+            list[tid] = e;
+            __syncthreads();
+            const unsigned long long other = list[tid ^ j];
+            const bool larger = ((tid & j) == 0) == ((tid & k) == 0);
+            e = larger == (other > e) ? other : e;
           }
-        const uint32_t key = (uint32_t)(e >> 32);
-        unsigned long long w = tid < (int)count && tid < r.top_k ? weight(key) : 0, all;
+          merge<32>(e, tid, k);
+        }
+        unsigned long long w = tid < (int)count && tid < r.top_k ? weight(L::of_key((uint32_t)(e >> 32))) : 0, all;
         unsigned long long before = before_me<unsigned long long>(w, s.sums, all);
         if (r.cut_p && before >= limit_of(all) && tid > 0) w = 0;
         if (w < floor && tid > 0) w = 0;
@@ -533,49 +605,56 @@ __global__ __launch_bounds__(THREADS) void ftsample_row(const Args a) {
         before = before_me<unsigned long long>(w, s.sums, all);
         const unsigned long long goal = (unsigned long long)__builtin_floor(r.u * (double)all) + 1;
         if (before < goal && before + w >= goal) answer(listed[tid], (double)w / (double)all);
+        return;
       }
     }
-    if (sorted) return;
-    __syncthreads();
-    search((unsigned long long)r.top_k, false, 1, most, 0);
+    search((unsigned long long)r.top_k, false, least_key, top_key, 0);
     if (r.cut_p) {
       unsigned long long sum = 0, all;
       uint32_t there = 0, ties;
-      x.each([&](uint32_t k) __attribute__((always_inline)) {
-        if (k > kept.border) sum += weight(k);
-        there += k == kept.border;
+      x.each([&](float y) __attribute__((always_inline)) {
+        if (y > kept.border) sum += weight(y);
+        there += y == kept.border;
       });
       before_me<unsigned long long>(sum, s.sums, all);
       // (where fewer than top_k can be chosen, fewer are equal than there is room for)
       before_me<uint32_t>(there, s.words, ties);
       if ((uint32_t)kept.equal > ties) kept.equal = (int)ties;
       all += (unsigned long long)kept.equal * weight(kept.border);
-      search(limit_of(all), true, kept.border, most, 0);
+      search(limit_of(all), true, L::key(kept.border), top_key, 0);
     }
     sum_up(kept);
     return;
   }
 
   // No top_k: all weights, those of at least the floor, and (top_p) how they are distributed.
-  if (r.cut_p) {
-    constexpr int N = sizeof(s.bins) / sizeof(s.bins[0]);
-    for (int i = tid; i < N; i += THREADS) s.bins[i] = 0;
-    __syncthreads();
-  }
   unsigned long long sum = 0, high = 0;
-  x.each([&](uint32_t k) __attribute__((always_inline)) {
-    if (k == 0) return;
-    int bin;
-    const unsigned long long w = weights.of(K::logit(k), k, bin);
-    sum += w;
-    high += k == most || w >= floor ? w : 0;
-    if (r.cut_p && w) atomicAdd(&s.bins[bin], w);
-  });
-  high = wave_sum(high);
   if (!r.cut_p) {
-    choose(kept, high, 0);
+    x.each([&](float y) __attribute__((always_inline)) {
+      const unsigned long long w = weight(y);
+      high += w >= floor || y == most ? w : 0;
+    });
+    choose(kept, wave_sum(high), 0);
     return;
   }
+  constexpr int N = sizeof(s.bins) / sizeof(s.bins[0]);
+  for (int i = tid; i < N; i += THREADS) s.bins[i] = 0;
+  __syncthreads();
+  x.each_word([&](int, const uint4v& k) __attribute__((always_inline)) {
+    unsigned long long w[L::PER];
+    int bin[L::PER];
+#pragma unroll
+    for (int e = 0; e < L::PER; ++e) {
+      const float y = L::logit(k, e);
+      w[e] = weights.of(y, bin[e]);
+      sum += w[e];
+      high += w[e] >= floor || y == most ? w[e] : 0;
+    }
+#pragma unroll
+    for (int e = 0; e < L::PER; ++e)
+      if (w[e]) atomicAdd(&s.bins[bin[e]], w[e]);
+  });
+  high = wave_sum(high);
   unsigned long long all, all_high = 0;
   before_me<unsigned long long>(sum, s.sums, all);
   __syncthreads();
@@ -589,48 +668,44 @@ __global__ __launch_bounds__(THREADS) void ftsample_row(const Args a) {
     return;
   }
   __syncthreads();
-  constexpr int PER_THREAD = sizeof(s.bins) / sizeof(s.bins[0]) / THREADS;
-  find_bin<PER_THREAD>(s, 0, limit, [&](int i) { return s.bins[i]; });
+  find_bin<N / THREADS>(s, 0, limit, [&](int i) { return s.bins[i]; });
   const int bin = (int)s.bin;
   const unsigned long long above = s.above;
-  // the keys of that bin, and some more: a bin is as wide as 1 / scale
-  __syncthreads();
-  uint32_t lowest = 0xFFFFFFFFu, highest = 0;
+  // The smallest and the largest logit of that bin, among those that lie near it: a bin is as wide as 1 / scale.  (No scale: all of them.)
+  float lowest = -NOTHING, highest = NOTHING;
   {
-    const double wide = 1.0 / weights.scale, top = weights.most - ((double)bin - 0.5) * wide, margin = wide * 0.01 + __builtin_fabs(weights.most) * 0x1p-40;
-    const float lo = (float)(top - wide - margin), hi = (float)(top + margin);
-    const uint32_t klo = K::near(lo, false), khi = K::near(hi, true);
-    x.each([&](uint32_t k) __attribute__((always_inline)) {
-      if (k < klo || k > khi || k == 0) return;
+    const double wide = 1.0 / weights.scale, top = weights.most - ((double)bin - 0.5) * wide, margin = wide * 0.01 + __builtin_fabs(weights.most) * 0x1p-20;
+    const float from = (float)(top - wide - margin), to = (float)(top + margin);
+    x.each([&](float y) __attribute__((always_inline)) {
+      if (y < from || y > to) return;
       int b;
-      const unsigned long long w = weights.of(K::logit(k), k, b);
-      if (b != bin || !w) return;
-      lowest = k < lowest ? k : lowest;
-      highest = k > highest ? k : highest;
+      if (!weights.of(y, b) || b != bin) return;
+      lowest = __builtin_fminf(lowest, y);
+      highest = __builtin_fmaxf(highest, y);
     });
   }
   highest = wave_most(highest);
-  lowest = ~wave_most(~lowest);
-  if (lane == 0) s.words[wave] = highest;
+  lowest = -wave_most(-lowest);
+  __syncthreads();
+  if (lane == 0) {
+    s.words[wave] = as_u(highest);
+    s.sums[wave] = as_u(lowest);
+  }
   __syncthreads();
 #pragma unroll
-  for (int w = 0; w < WAVES; ++w) highest = s.words[w] > highest ? s.words[w] : highest;
-  __syncthreads();
-  if (lane == 0) s.words[wave] = lowest;
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < WAVES; ++w) lowest = s.words[w] < lowest ? s.words[w] : lowest;
-  search(limit, true, lowest, highest, above);      // (no key between these is in another bin)
+  for (int w = 0; w < WAVES; ++w) {
+    highest = __builtin_fmaxf(highest, as_f(s.words[w]));
+    lowest = __builtin_fminf(lowest, as_f((uint32_t)s.sums[w]));
+  }
+  search(limit, true, L::key(lowest), L::key(highest), above);      // (no logit between these is in another bin)
   sum_up(kept);
 }
 
 typedef void (*kernel_fn)(const Args);
-// The kernel of a vocabulary: rows in registers where they fit, wherever they begin.
-template <int DT> kernel_fn kernel_of(int vocab) {
-  const int words = (vocab + 2 * Keys<DT>::PER - 2) / Keys<DT>::PER;
-  return words <= MOST_WORDS * THREADS ? ftsample_row<DT, true> : ftsample_row<DT, false>;
+// The kernel of a vocabulary: rows in registers where they fit; `skip`: most elements between a word of 16 bytes and the row that begins in it.
+template <int DT> kernel_fn kernel_of(int vocab, int skip) {
+  return (vocab + skip + Type<DT>::PER - 1) / Type<DT>::PER <= MOST_WORDS * THREADS ? ftsample_row<DT, true> : ftsample_row<DT, false>;
 }
-
 
 }  // namespace ftsample
 
@@ -638,7 +713,6 @@ using namespace ftsample;
 
 struct ftsample_ctx {
   ftsample_config cfg;
-  kernel_fn fn = nullptr;
   std::string err;
 };
 
@@ -670,7 +744,6 @@ extern "C" int ftsample_create(const ftsample_config* cfg, ftsample_ctx** out) {
   ftsample_ctx* c = new (std::nothrow) ftsample_ctx();
   if (!c) return sfail(nullptr, FTSAMPLE_ENOMEM, "out of host memory");
   c->cfg = *cfg;
-  c->fn = cfg->in_dtype == FTSAMPLE_F32 ? kernel_of<FTSAMPLE_F32>(cfg->vocab) : cfg->in_dtype == FTSAMPLE_BF16 ? kernel_of<FTSAMPLE_BF16>(cfg->vocab) : kernel_of<FTSAMPLE_F16>(cfg->vocab);
   int before = 0;
   hipError_t he = hipGetDevice(&before);
   if (he == hipSuccess) he = hipSetDevice(cfg->device);
@@ -708,7 +781,9 @@ extern "C" int ftsample_choose(ftsample_ctx* c, const void* logits, int64_t row_
   hipError_t he = hipGetDevice(&before);
   if (he == hipSuccess && before != e.device) he = hipSetDevice(e.device);
   if (he != hipSuccess) return sfail_hip(c, "device", he);
-  hipLaunchKernelGGL(c->fn, dim3((uint32_t)rows), dim3(THREADS), 0, (hipStream_t)hip_stream, a);
+  const int size = e.in_dtype == FTSAMPLE_F32 ? 4 : 2, skip = ((uintptr_t)logits | (uintptr_t)(row_stride * size)) % 16 ? 16 / size - 1 : 0;
+  const kernel_fn fn = e.in_dtype == FTSAMPLE_F32 ? kernel_of<FTSAMPLE_F32>(e.vocab, skip) : e.in_dtype == FTSAMPLE_BF16 ? kernel_of<FTSAMPLE_BF16>(e.vocab, skip) : kernel_of<FTSAMPLE_F16>(e.vocab, skip);
+  hipLaunchKernelGGL(fn, dim3((uint32_t)rows), dim3(THREADS), 0, (hipStream_t)hip_stream, a);
   he = hipGetLastError();
   if (before != e.device) (void)hipSetDevice(before);
   return he == hipSuccess ? FTSAMPLE_OK : sfail_hip(c, "launch", he);
