@@ -20,8 +20,9 @@ using namespace ftserve;
 
 constexpr int THREADS = 512, WAVES = THREADS / 64;
 constexpr int BITS = 11, BINS = 1 << BITS;      // of a level of the search by keys
-constexpr int STEPS = 128;                      // bins of the weights' logarithm to an octave
+constexpr int STEPS = 512;                      // of a weight's logarithm to an octave, for each of which there is a factor in LDS
 constexpr int OCTAVES = 51;                     // what lies further below the largest weight is 0 in all units
+constexpr int TO_BIN = 2, LAST_BIN = STEPS * OCTAVES >> TO_BIN;      // bins of the logarithm: 128 an octave
 constexpr int LIST = THREADS, MOST_LISTED = THREADS / 2;   // tokens that are sorted; largest top_k that is
 constexpr int MOST_WORDS = 32;                  // 16-byte words of a lane in registers
 
@@ -61,7 +62,7 @@ constexpr float NOTHING = -__builtin_inff();
 // The rules of a row, as they hold.
 struct Rules {
   double per_t;        // 1 / temperature
-  double floor;        // least weight that is kept
+  double floor;        // least weight that is kept, 0: any
   double top_p, u;
   int32_t top_k;       // vocab: no limit
   bool cut_p, greedy;
@@ -82,30 +83,37 @@ __device__ __forceinline__ Rules rules_of(const Args& a, int row) {
   return r;
 }
 
-// Weights of keys, given the largest one: w = 2^(n / STEPS) 2^(r / STEPS) with n whole and |r| <= 1/2, the first factor from a table and an exponent, the second
-// from its series (the term left out is below 2^-65), in whole multiples of 2^-shift.
+// Weights of logits, given the largest one: w = 2^(n / STEPS) 2^(r / STEPS) with n whole and |r| <= 1/2, the first factor from a table and an exponent, the second
+// from its series (the term left out is below 2^-46), in whole multiples of 2^-shift.
 struct Weights {
   double scale, most;        // STEPS / (temperature * ln 2); the largest logit
-  const double* table;       // 2^(i / STEPS)
-  int shift;
-  // w (of -infinity and NaN: 0), and the number of the bin (0: the largest weights; STEPS * OCTAVES: nothing)
+  const double* table;       // 2^(i / STEPS + shift)
+  static constexpr double ROUND = 6755399441055744.0;      // 1.5 * 2^52
+  // the logarithm in steps, and the nearest whole number of them; -infinity and NaN: as far below as counts
+  __device__ __forceinline__ double steps(float x, int& n) const {
+    const double t = __builtin_fmax(((double)x - most) * scale, -(double)(STEPS * OCTAVES)), at = t + ROUND;
+    n = (int)(uint32_t)__builtin_bit_cast(uint64_t, at);
+    return t - (at - ROUND);
+  }
+  __device__ __forceinline__ int bin(float x) const {
+    int n;
+    steps(x, n);
+    return -n >> TO_BIN;
+  }
+  // w (of -infinity and NaN: 0), and its bin
   __device__ __forceinline__ unsigned long long of(float x, int& bin) const {
-    constexpr double ROUND = 6755399441055744.0;      // 1.5 * 2^52
-    const double t = __builtin_fmax(((double)x - most) * scale, -(double)(STEPS * OCTAVES));
-    const double at = t + ROUND, r = t - (at - ROUND);
-    const int n = (int)(uint32_t)__builtin_bit_cast(uint64_t, at);
+    int n;
+    const double r = steps(x, n);
     constexpr double L = 0.69314718055994530942 / STEPS;
-    double p = __builtin_fma(r, L * L * L * L * L / 120, L * L * L * L / 24);
-    p = __builtin_fma(r, p, L * L * L / 6);
-    p = __builtin_fma(r, p, L * L / 2);
+    double p = __builtin_fma(r, L * L * L / 6, L * L / 2);
     p = __builtin_fma(r, p, L);
     p = __builtin_fma(r, p, 1.0);
-    bin = -n;
-    const double w = __builtin_ldexp(p * table[n & (STEPS - 1)], (n >> 7) + shift);
+    bin = -n >> TO_BIN;
+    const double w = __builtin_ldexp(p * table[n & (STEPS - 1)], n >> 9);
     return __builtin_bit_cast(uint64_t, w + 0x1p52) & ((1ull << 52) - 1);
   }
 };
-static_assert(STEPS == 128, "the octave is n >> 7");
+static_assert(STEPS == 512, "the octave is n >> 9");
 
 // Sums over the lanes up to this one: rows of 16 by shifts, then their last lanes handed on.
 template <int CTRL, int ROWS> __device__ __forceinline__ uint32_t shifted(uint32_t x) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xF, false); }
@@ -176,7 +184,7 @@ __device__ __forceinline__ float wave_most(float x) {
 }
 
 struct Shared {
-  unsigned long long bins[STEPS * OCTAVES + 1 + (THREADS - (STEPS * OCTAVES + 1) % THREADS) % THREADS];      // whole rounds of all threads
+  unsigned long long bins[(LAST_BIN + THREADS) / THREADS * THREADS];      // whole rounds of all threads
   double table[STEPS];
   unsigned long long sums[WAVES];
   uint32_t words[WAVES];
@@ -287,12 +295,20 @@ template <int DT, bool HELD> struct Row {
   __device__ __forceinline__ int token(int v, int e) const { return (first + 64 * v) * PER + e - skip; }
 };
 
-// What the rules have left: logits above `border`, and the first `equal` of those that are it; of those, weights of at least `floor`.
+// What the rules have left: logits above `border`, and the first `equal` of those that are it.
 struct Kept {
   float border;
   int equal;
-  unsigned long long floor;
 };
+// The number below x, and the least that is not below a number of 64 bits.
+__device__ __forceinline__ float below(float x) {
+  const uint32_t u = as_u(x + 0.f);
+  return as_f(u == 0 ? 0x80000001u : u & 0x80000000u ? u + 1 : u - 1);
+}
+__device__ __forceinline__ float not_below(double x) {
+  const float y = (float)x;
+  return (double)y >= x ? y : -below(-y);
+}
 
 template <int DT, bool HELD>
 __global__ __launch_bounds__(THREADS) void ftsample_row(const Args a) {
@@ -303,7 +319,7 @@ __global__ __launch_bounds__(THREADS) void ftsample_row(const Args a) {
   const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const Rules r = rules_of(a, row);
   Row<DT, HELD> x(a, row);
-  if (tid < STEPS) s.table[tid] = exp2((double)tid / STEPS);
+  for (int i = tid; i < STEPS; i += THREADS) s.table[i] = __builtin_ldexp(exp2((double)i / STEPS), a.shift);
 
   float mine = NOTHING;
   x.each([&](float y) __attribute__((always_inline)) { mine = __builtin_fmaxf(mine, y); });
@@ -348,12 +364,13 @@ __global__ __launch_bounds__(THREADS) void ftsample_row(const Args a) {
     }
     return;
   }
-  const Weights weights{r.per_t * (STEPS / 0.69314718055994530942), (double)most, s.table, a.shift};
+  const Weights weights{r.per_t * (STEPS / 0.69314718055994530942), (double)most, s.table};
   auto weight = [&](float y) __attribute__((always_inline)) {
     int bin;
     return weights.of(y, bin);
   };
-  const unsigned long long floor = (unsigned long long)__builtin_ceil(__builtin_ldexp(r.floor, a.shift));
+  // the least logit that min_p keeps: its weight is at least the floor
+  const float least = r.floor >= 1.0 ? most : r.floor > 0.0 ? not_below((double)most + log(r.floor) / r.per_t) : NOTHING;
   auto limit_of = [&](unsigned long long all) -> unsigned long long {      // the least whole number that is top_p of all, or 1
     const double limit = __builtin_ceil(r.top_p * (double)all);
     return limit >= 1.0 ? (unsigned long long)limit : 1ull;
@@ -362,7 +379,7 @@ __global__ __launch_bounds__(THREADS) void ftsample_row(const Args a) {
   // The first place at which the sum of kept weights exceeds u times all: whole numbers exceed it where they reach the next one.  sum: this wave's kept weights without those of the
   // border; ties: how many logits of it are the border.
   auto choose = [&](const Kept& kept, unsigned long long sum, uint32_t ties) {
-    const unsigned long long each = kept.equal ? weight(kept.border) : 0, worth = each >= kept.floor || kept.border == most ? each : 0;
+    const unsigned long long worth = kept.equal ? weight(kept.border) : 0;
     __syncthreads();
     if (lane == 0) {
       s.sums[wave] = sum;
@@ -387,7 +404,7 @@ __global__ __launch_bounds__(THREADS) void ftsample_row(const Args a) {
       for (int e = 0; e < L::PER; ++e) {
         const float y = L::logit(k, e);
         w[e] = weight(y);
-        w[e] = y > kept.border && (w[e] >= kept.floor || y == most) ? w[e] : 0;
+        w[e] = y > kept.border ? w[e] : 0;
         n += kept.equal && y == kept.border;
         sum += w[e];
       }
@@ -417,9 +434,17 @@ __global__ __launch_bounds__(THREADS) void ftsample_row(const Args a) {
       unsigned long long mine = 0;
       uint32_t n = 0;
 #pragma unroll 1
-      for (int v = wave * per; v < end; ++v) {
-        unsigned long long w[L::PER];
-        mine += add_up(x.word(64 * (run + v) + lane), w, n);
+      for (int v = wave * per; v < end; v += 4) {
+        uint4v k[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (v + i < end) k[i] = x.word(64 * (run + v + i) + lane);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (v + i < end) {
+            unsigned long long w[L::PER];
+            mine += add_up(k[i], w, n);
+          }
       }
       mine = wave_sum(mine);
       n = wave_sum(n);
@@ -433,9 +458,16 @@ __global__ __launch_bounds__(THREADS) void ftsample_row(const Args a) {
     }
     if (wave) return;
     bool done = false;
+    uint4v ahead[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i < length) ahead[i] = x.word(64 * (run + i) + lane);
 #pragma unroll 1
     for (int v = run; v < run + length && !done; ++v) {
-      const uint4v k = x.word(64 * v + lane);
+      const uint4v k = ahead[0];
+      ahead[0] = ahead[1];
+      ahead[1] = ahead[2];
+      ahead[2] = ahead[3];
       unsigned long long w[L::PER];
       uint32_t n = 0;
       unsigned long long sum = add_up(k, w, n);
@@ -464,27 +496,34 @@ __global__ __launch_bounds__(THREADS) void ftsample_row(const Args a) {
       done = before >= goal;
     }
   };
-  auto sum_up = [&](const Kept& kept) {
+  auto sum_up = [&](Kept kept) {
+    if (least > kept.border) kept = Kept{below(least), 0};
     unsigned long long sum = 0;
     uint32_t ties = 0;
-    x.each_word([&](int, const uint4v& k) __attribute__((always_inline)) {
-      bool some = false;
+    if (kept.border == NOTHING) {
+      x.each([&](float y) __attribute__((always_inline)) { sum += weight(y); });
+    } else {
+      x.each_word([&](int, const uint4v& k) __attribute__((always_inline)) {
+        float largest = L::logit(k, 0);
 #pragma unroll
-      for (int e = 0; e < L::PER; ++e) some |= L::logit(k, e) >= kept.border;
-      if (!__any(some)) return;
+        for (int e = 1; e < L::PER; ++e) largest = __builtin_fmaxf(largest, L::logit(k, e));
+        if (!__any(largest >= kept.border)) return;
 #pragma unroll
-      for (int e = 0; e < L::PER; ++e) {
-        const float y = L::logit(k, e);
-        const unsigned long long w = weight(y);
-        sum += y > kept.border && (w >= kept.floor || y == most) ? w : 0;
-        ties += y == kept.border;
-      }
-    });
-    choose(kept, wave_sum(sum), wave_sum(kept.equal ? ties : 0u));
+        for (int e = 0; e < L::PER; ++e) {
+          const float y = L::logit(k, e);
+          const unsigned long long w = weight(y);
+          sum += y > kept.border ? w : 0;
+        }
+        if (kept.equal)
+#pragma unroll
+          for (int e = 0; e < L::PER; ++e) ties += L::logit(k, e) == kept.border;
+      });
+    }
+    choose(kept, wave_sum(sum), wave_sum(ties));
   };
 
-  // The border moves up to the lowest logit above which less than `limit` lies, by counts or by sums of weights; among those with keys lowest .. highest.
-  Kept kept{NOTHING, 0, floor};
+  // The border moves up to the lowest logit above which less than `limit` lies, by counts or by sums of weights; among those with keys lowest .. highest, above which `above` lies.
+  Kept kept{NOTHING, 0};
   const uint32_t top_key = L::key(most);
   auto empty_bins = [&]() {
     __syncthreads();
@@ -530,6 +569,67 @@ __global__ __launch_bounds__(THREADS) void ftsample_row(const Args a) {
     kept.equal = (int)(fit > 0x7FFFFFFFull ? 0x7FFFFFFFull : fit);
   };
   const uint32_t least_key = L::key(NOTHING) + 1;
+  // The same for all that is kept, the bin of the weights' logarithm first; limit: from the sum of all.
+  auto by_bins = [&](bool by_weight, auto limit_from) {
+    constexpr int N = sizeof(s.bins) / sizeof(s.bins[0]);
+    __syncthreads();
+    for (int i = tid; i < N; i += THREADS) s.bins[i] = 0;
+    __syncthreads();
+    uint32_t beyond = 0;
+    x.each_word([&](int, const uint4v& k) __attribute__((always_inline)) {
+      unsigned long long w[L::PER];
+      int bin[L::PER];
+      if (by_weight) {
+#pragma unroll
+        for (int e = 0; e < L::PER; ++e) w[e] = weights.of(L::logit(k, e), bin[e]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < L::PER; ++e) {
+          bin[e] = weights.bin(L::logit(k, e));
+          w[e] = 1;
+          beyond += bin[e] == LAST_BIN && L::logit(k, e) > NOTHING;
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < L::PER; ++e)
+        if (L::logit(k, e) > kept.border && w[e] && bin[e] < LAST_BIN) atomicAdd(&s.bins[bin[e]], w[e]);
+    });
+    __syncthreads();
+    // (what is in the last bin is not counted there: thousands of logits may lie so far below, and would be added up one after the other)
+    if (tid == 0 && kept.equal) s.bins[weights.bin(kept.border)] += (by_weight ? weight(kept.border) : 1ull) * (unsigned)kept.equal;
+    __syncthreads();
+    unsigned long long all, mine = 0;
+    for (int i = 0; i < N / THREADS; ++i) mine += s.bins[tid * (N / THREADS) + i];
+    before_me<unsigned long long>(mine, s.sums, all);
+    const unsigned long long limit = limit_from(all);
+    int bin = LAST_BIN;
+    unsigned long long above = all;
+    if (all < limit && !by_weight) {
+      uint32_t beyond_all;
+      before_me<uint32_t>(beyond, s.words, beyond_all);
+      if (beyond_all == 0) return;      // fewer than that can be chosen: all of them are kept
+    } else {
+      find_bin<N / THREADS>(s, 0, limit, [&](int i) { return s.bins[i]; });
+      bin = (int)s.bin;
+      above = s.above;
+    }
+    // The keys of that bin: those from the first that lies in it or above on, up to before the first that lies above.  64 keys at a time are tried, one a lane.
+    auto first_key = [&](int last) {      // ... whose bin is at most `last`: one of n from `from` on
+      uint32_t from = least_key, n = top_key - least_key + 1;      // (top_key's bin is 0)
+      while (n > 1) {
+        const uint32_t step = (n + 63) >> 6;
+        const uint64_t at = (uint64_t)lane * step;
+        const int low = __popcll(__ballot(at < n && weights.bin(L::of_key(from + (uint32_t)at)) > last));      // the first `low` of the lanes' keys lie below
+        if (low == 0) break;
+        const uint32_t passed = (uint32_t)(low - 1) * step + 1;
+        from += passed;
+        n = n - passed < step ? n - passed : step;
+      }
+      return from;
+    };
+    const uint32_t lowest = bin == LAST_BIN ? least_key : first_key(bin), highest = bin == 0 ? top_key : first_key(bin - 1) - 1;
+    search(limit, by_weight, lowest, highest, above);
+  };
 
   if (r.top_k < x.vocab) {
     if (r.top_k <= MOST_LISTED) {
@@ -594,7 +694,7 @@ __global__ __launch_bounds__(THREADS) void ftsample_row(const Args a) {
         unsigned long long w = tid < (int)count && tid < r.top_k ? weight(L::of_key((uint32_t)(e >> 32))) : 0, all;
         unsigned long long before = before_me<unsigned long long>(w, s.sums, all);
         if (r.cut_p && before >= limit_of(all) && tid > 0) w = 0;
-        if (w < floor && tid > 0) w = 0;
+        if (tid > 0 && L::of_key((uint32_t)(e >> 32)) < least) w = 0;
         __syncthreads();
         list[tid] = 0;
         __syncthreads();
@@ -608,96 +708,16 @@ __global__ __launch_bounds__(THREADS) void ftsample_row(const Args a) {
         return;
       }
     }
-    search((unsigned long long)r.top_k, false, least_key, top_key, 0);
+    by_bins(false, [&](unsigned long long) { return (unsigned long long)r.top_k; });
+    // (where fewer than top_k can be chosen, fewer are equal than there is room for)
     if (r.cut_p) {
-      unsigned long long sum = 0, all;
       uint32_t there = 0, ties;
-      x.each([&](float y) __attribute__((always_inline)) {
-        if (y > kept.border) sum += weight(y);
-        there += y == kept.border;
-      });
-      before_me<unsigned long long>(sum, s.sums, all);
-      // (where fewer than top_k can be chosen, fewer are equal than there is room for)
+      x.each([&](float y) __attribute__((always_inline)) { there += y == kept.border; });
       before_me<uint32_t>(there, s.words, ties);
       if ((uint32_t)kept.equal > ties) kept.equal = (int)ties;
-      all += (unsigned long long)kept.equal * weight(kept.border);
-      search(limit_of(all), true, L::key(kept.border), top_key, 0);
     }
-    sum_up(kept);
-    return;
   }
-
-  // No top_k: all weights, those of at least the floor, and (top_p) how they are distributed.
-  unsigned long long sum = 0, high = 0;
-  if (!r.cut_p) {
-    x.each([&](float y) __attribute__((always_inline)) {
-      const unsigned long long w = weight(y);
-      high += w >= floor || y == most ? w : 0;
-    });
-    choose(kept, wave_sum(high), 0);
-    return;
-  }
-  constexpr int N = sizeof(s.bins) / sizeof(s.bins[0]);
-  for (int i = tid; i < N; i += THREADS) s.bins[i] = 0;
-  __syncthreads();
-  x.each_word([&](int, const uint4v& k) __attribute__((always_inline)) {
-    unsigned long long w[L::PER];
-    int bin[L::PER];
-#pragma unroll
-    for (int e = 0; e < L::PER; ++e) {
-      const float y = L::logit(k, e);
-      w[e] = weights.of(y, bin[e]);
-      sum += w[e];
-      high += w[e] >= floor || y == most ? w[e] : 0;
-    }
-#pragma unroll
-    for (int e = 0; e < L::PER; ++e)
-      if (w[e]) atomicAdd(&s.bins[bin[e]], w[e]);
-  });
-  high = wave_sum(high);
-  unsigned long long all, all_high = 0;
-  before_me<unsigned long long>(sum, s.sums, all);
-  __syncthreads();
-  if (lane == 0) s.sums[wave] = high;
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < WAVES; ++w) all_high += s.sums[w];
-  const unsigned long long limit = limit_of(all);
-  if (all_high <= limit) {      // top_p keeps more than min_p does: what is not below the floor has, before its last, less than the limit
-    choose(kept, high, 0);
-    return;
-  }
-  __syncthreads();
-  find_bin<N / THREADS>(s, 0, limit, [&](int i) { return s.bins[i]; });
-  const int bin = (int)s.bin;
-  const unsigned long long above = s.above;
-  // The smallest and the largest logit of that bin, among those that lie near it: a bin is as wide as 1 / scale.  (No scale: all of them.)
-  float lowest = -NOTHING, highest = NOTHING;
-  {
-    const double wide = 1.0 / weights.scale, top = weights.most - ((double)bin - 0.5) * wide, margin = wide * 0.01 + __builtin_fabs(weights.most) * 0x1p-20;
-    const float from = (float)(top - wide - margin), to = (float)(top + margin);
-    x.each([&](float y) __attribute__((always_inline)) {
-      if (y < from || y > to) return;
-      int b;
-      if (!weights.of(y, b) || b != bin) return;
-      lowest = __builtin_fminf(lowest, y);
-      highest = __builtin_fmaxf(highest, y);
-    });
-  }
-  highest = wave_most(highest);
-  lowest = -wave_most(-lowest);
-  __syncthreads();
-  if (lane == 0) {
-    s.words[wave] = as_u(highest);
-    s.sums[wave] = as_u(lowest);
-  }
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < WAVES; ++w) {
-    highest = __builtin_fmaxf(highest, as_f(s.words[w]));
-    lowest = __builtin_fminf(lowest, as_f((uint32_t)s.sums[w]));
-  }
-  search(limit, true, L::key(lowest), L::key(highest), above);      // (no logit between these is in another bin)
+  if (r.cut_p) by_bins(true, limit_of);
   sum_up(kept);
 }
 
