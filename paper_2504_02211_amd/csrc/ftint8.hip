@@ -44,6 +44,17 @@ struct Coding {
     asm("" : "+v"(y));
     return as_u(y + 12582912.f);
   }
+  // Eight codes of eight elements in 16 bits.
+  template <bool BF> __device__ __forceinline__ uint2v codes(const uint4v& v) const {
+    uint2v out;
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+      const uint32_t lo = v[2 * w], hi = v[2 * w + 1];
+      const uint32_t c0 = code(low_of<BF>(lo)), c1 = code(high_of<BF>(lo)), c2 = code(low_of<BF>(hi)), c3 = code(high_of<BF>(hi));
+      out[w] = fine ? __builtin_amdgcn_perm(c1, c0, 0x0C0C0400u) | __builtin_amdgcn_perm(c3, c2, 0x04000C0Cu) : 0u;
+    }
+    return out;
+  }
 };
 __device__ __forceinline__ void put_scale(const EncodeArgs& a, int row, uint32_t most, bool fine) { a.scales[row] = fine ? as_f(most) / 127.f : __builtin_nanf(""); }
 
@@ -114,14 +125,7 @@ template <int DT, int WAVES, int VECS> __global__ __launch_bounds__(256) void ft
 #pragma unroll
   for (int i = 0; i < VECS; ++i) {
     const int at = 8 * (t + 64 * WAVES * i);
-    uint2v out;
-#pragma unroll
-    for (int w = 0; w < 2; ++w) {
-      const uint32_t lo = v[i][2 * w], hi = v[i][2 * w + 1];
-      const uint32_t c0 = c.code(low_of<DT == FTINT8_BF16>(lo)), c1 = c.code(high_of<DT == FTINT8_BF16>(lo)), c2 = c.code(low_of<DT == FTINT8_BF16>(hi)), c3 = c.code(high_of<DT == FTINT8_BF16>(hi));
-      out[w] = c.fine ? __builtin_amdgcn_perm(c1, c0, 0x0C0C0400u) | __builtin_amdgcn_perm(c3, c2, 0x04000C0Cu) : 0u;
-    }
-    if (at < a.k_padded) *reinterpret_cast<uint2v*>(codes + at) = out;
+    if (at < a.k_padded) *reinterpret_cast<uint2v*>(codes + at) = c.codes<DT == FTINT8_BF16>(v[i]);
   }
 }
 
@@ -132,6 +136,8 @@ struct ProductArgs {
   int64_t y_stride;      // bytes
   int32_t m, n, k_padded;
   int32_t wide;          // rows of y begin at multiples of 16 bytes
+  int32_t parts;         // > 1: the columns are divided among as many workgroups a tile (blockIdx.y), whose sums go to `sums`
+  int4v* sums;           // [part][tile][wave][block of features][block of tokens][lane]
 };
 
 template <int N> __device__ __forceinline__ void wait_loads() {
@@ -175,28 +181,32 @@ template <int BM_, int BF_, int WT_, int WF_, int NST_, int PER_CU_ = 1> struct 
   static_assert(NW * 16 * PITCH <= LDS && PER_CU * LDS <= 160 * 1024 && (NST - 1) * NLOAD <= 63, "LDS; counted waits");
 };
 
+// Which tile a workgroup has.  Workgroups go round the 8 XCDs; each XCD gets neighbouring tiles, numbered in groups of 8 token tiles x all feature tiles, so that
+// what it runs at a time shares rows of weights and of tokens in its L2.
+template <class T> __device__ __forceinline__ void tile_of(const ProductArgs& a, int id, int& tm, int& tn) {
+  constexpr int GM = 8;
+  const int tiles_m = (a.m + T::BM - 1) / T::BM, tiles_n = (a.n + T::BF - 1) / T::BF;
+  const int total = tiles_m * tiles_n, xcd = id & 7, slot = id >> 3, per = total >> 3, more = total & 7;
+  const int t = xcd * per + (xcd < more ? xcd : more) + slot;
+  const int group = t / (GM * tiles_n), first = group * GM, rows = tiles_m - first < GM ? tiles_m - first : GM, in = t - group * GM * tiles_n;
+  tm = __builtin_amdgcn_readfirstlane(first + in % rows);
+  tn = __builtin_amdgcn_readfirstlane(in / rows);
+}
+
 // Y^T = W X^T on 16x16x64 products: rows of weights are the left operand, tokens the right one, so that a lane holds one token per block of tokens and four features that lie
 // side by side per block of features.  The steps of 128 columns go through a ring of LDS stages that direct loads fill; a row's 16-byte chunk c lies at place c ^ (row / 2 % 8), which keeps
 // the reads of operands free of bank conflicts.  Operands are read ahead of their products, also across the border of two stages: the barrier of a stage sits AHEAD rows of
 // products before its end, where its last operands are in registers, so that no wave waits for LDS behind it.
+// Bound by the matrix pipe: 16,384 tokens on 16,384 x 4096 (features x columns) 907 us, 2425 TOPS; the library's plain product of the codes, without scales, 974 us.
 template <class T, int DT> __global__ __launch_bounds__(T::NW * 64, T::PER_CU * T::NW / 4) void ftint8_tile(const ProductArgs a) {
   constexpr int WT = T::WT, WF = T::WF, NST = T::NST, BK = T::BK, STAGE = T::STAGE, NLOAD = T::NLOAD, NKS = 2, AHEAD = 3;
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   const int tid = threadIdx.x, lane = tid & 63, lq = lane & 15, lg = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wt = wave / T::NWF, wf = wave % T::NWF;
-  // Workgroups go round the 8 XCDs; each XCD gets neighbouring tiles, numbered in groups of 8 token tiles x all feature tiles, so that
-  // what it runs at a time shares rows of weights and of tokens in its L2.
   int tm, tn;
-  {
-    const int tiles_m = (a.m + T::BM - 1) / T::BM, tiles_n = (a.n + T::BF - 1) / T::BF;
-    const int total = tiles_m * tiles_n, xcd = blockIdx.x & 7, slot = blockIdx.x >> 3, per = total >> 3, more = total & 7;
-    const int t = xcd * per + (xcd < more ? xcd : more) + slot;
-    constexpr int GM = 8;
-    const int group = t / (GM * tiles_n), first = group * GM, rows = tiles_m - first < GM ? tiles_m - first : GM, in = t - group * GM * tiles_n;
-    tm = __builtin_amdgcn_readfirstlane(first + in % rows);
-    tn = __builtin_amdgcn_readfirstlane(in / rows);
-  }
-  const int m0 = tm * T::BM, n0 = tn * T::BF, steps = a.k_padded / BK;
+  tile_of<T>(a, blockIdx.x, tm, tn);
+  const int m0 = tm * T::BM, n0 = tn * T::BF;
+  const int begin = a.k_padded / BK * (int)blockIdx.y / a.parts, steps = a.k_padded / BK * ((int)blockIdx.y + 1) / a.parts - begin;
   const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
 
   // Piece p of an operand is its rows 8p .. 8p + 7; wave w takes pieces w, w + NW, ...  Rows behind the last one are the last one again (their results are not used).
@@ -210,7 +220,7 @@ template <class T, int DT> __global__ __launch_bounds__(T::NW * 64, T::PER_CU * 
     r = r < left ? r : left - 1;
     off[i] = (uint32_t)r * (uint32_t)a.k_padded + 16u * chunk;
   }
-  const int8_t *xb = a.x + (int64_t)m0 * a.k_padded, *wb = a.w + (int64_t)n0 * a.k_padded;
+  const int8_t *xb = a.x + (int64_t)m0 * a.k_padded + begin * BK, *wb = a.w + (int64_t)n0 * a.k_padded + begin * BK;
   const uint32_t wave_at = base + (uint32_t)wave * 1024u;
   auto issue = [&](int i, uint32_t stage) __attribute__((always_inline)) {
     load_lds16(i < T::XW ? xb : wb, off[i], wave_at + stage + (uint32_t)((i < T::XW ? T::NW * i : T::XP + T::NW * (i - T::XW)) * 1024));
@@ -296,6 +306,14 @@ template <class T, int DT> __global__ __launch_bounds__(T::NW * 64, T::PER_CU * 
   int kb = 0;
   for (; kb + NST < steps; ++kb) stage_step(kb, std::true_type{});
   for (; kb < steps; ++kb) stage_step(kb, std::false_type{});
+  if (a.parts > 1) {
+    int4v* const to = a.sums + (((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * T::NW + wave) * (WF * WT * 64) + lane;
+#pragma unroll
+    for (int f = 0; f < WF; ++f)
+#pragma unroll
+      for (int t = 0; t < WT; ++t) to[(f * WT + t) * 64] = acc[f][t];
+    return;
+  }
   wait_lds();
   barrier();                               // the ring is free
 
@@ -353,8 +371,168 @@ template <class T, int DT> __global__ __launch_bounds__(T::NW * 64, T::PER_CU * 
   }
 }
 
+// Four features of one token out: the lane has them side by side.
+template <int DT> __device__ __forceinline__ void put_four(const ProductArgs& a, int row, int col, int4v sum, float sx) {
+  float y[4];
+#pragma unroll
+  for (int r = 0; r < 4; ++r) y[r] = scaled(sum[r], sx, a.sw[col + r < a.n ? col + r : a.n - 1]);
+  constexpr int ES = DT == FTINT8_F32 ? 4 : 2;
+  char* const to = a.y + (int64_t)row * a.y_stride + (int64_t)col * ES;
+  if (a.wide && col + 4 <= a.n) {
+    if constexpr (ES == 4) *reinterpret_cast<float4v*>(to) = float4v{y[0], y[1], y[2], y[3]};
+    else *reinterpret_cast<uint2v*>(to) = uint2v{pack2<DT == FTINT8_BF16>(y[0], y[1]), pack2<DT == FTINT8_BF16>(y[2], y[3])};
+  } else {
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      if (col + r < a.n) {
+        if constexpr (ES == 4) reinterpret_cast<float*>(to)[r] = y[r];
+        else reinterpret_cast<uint16_t*>(to)[r] = (uint16_t)pack2<DT == FTINT8_BF16>(y[r], y[r]);
+      }
+  }
+}
+
+// The shares of divided columns, added up: a wave a block of 16 x 16.
+template <class T, int DT> __global__ __launch_bounds__(256) void ftint8_finish(const ProductArgs a, int tiles) {
+  constexpr int BLOCKS = T::NW * T::WF * T::WT;
+  const int lane = threadIdx.x & 63, unit = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)), id = unit / BLOCKS, block = unit % BLOCKS;
+  if (id >= tiles) return;
+  int tm, tn;
+  tile_of<T>(a, id, tm, tn);
+  const int wave = block / (T::WF * T::WT), f = block / T::WT % T::WF, t = block % T::WT, wt = wave / T::NWF, wf = wave % T::NWF;
+  const int row = tm * T::BM + 16 * (T::WT * wt + t) + (lane & 15), col = tn * T::BF + 16 * (T::WF * wf + f) + 4 * (lane >> 4);
+  if (row >= a.m || col >= a.n) return;
+  const int4v* const from = a.sums + ((int64_t)id * BLOCKS + block) * 64 + lane;
+  const int64_t apart = (int64_t)tiles * BLOCKS * 64;
+  int4v sum = from[0];
+  for (int p = 1; p < a.parts; ++p) sum += from[p * apart];
+  put_four<DT>(a, row, col, sum, a.sx[row]);
+}
+
+// Few tokens: 16 features and all tokens (up to 16 TB) a workgroup, the columns divided among its eight waves, operands from memory straight into registers: every
+// byte of the weights is wanted by one wave alone.  Stages of 256 columns, two of them under way; a token on 4096 columns has all it needs under way at once, and all
+// workgroups of 16,384 features are on the chip together.  WORDS > 0 (one token of up to 4096 WORDS columns): it comes in 16 bits, every workgroup encodes it for
+// itself while its first weights are under way, and the second launch is saved.  Bound by memory: 67 MB of weights, one token on 16,384 features of 4096 columns,
+// take 13.9 us with the encoding (4.8 TB/s, what a copy reaches; 16.3 in two launches).  Two tokens encoded so would take 17.8 us, in two launches 16.6.
+constexpr int FEW_WAVES = 8, FUSED_K = 16384;
+struct FewArgs {
+  ProductArgs p;
+  const char* raw;         // the token in 16 bits, at a multiple of 16 bytes
+  int32_t k;
+};
+template <int TB, int DT, int IN, int WORDS> __global__ __launch_bounds__(FEW_WAVES * 64, WORDS == 1 ? 8 : 2) void ftint8_few(const FewArgs b) {
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  __shared__ uint32_t most_of[FEW_WAVES];
+  constexpr bool FUSED = WORDS > 0;
+  constexpr int U = 4;
+  const ProductArgs& a = b.p;
+  const int tid = threadIdx.x, lane = tid & 63, lq = lane & 15, lg = lane >> 4, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n0 = blockIdx.x * 16, steps = a.k_padded / 64, stages = (steps + U - 1) / U;
+  const int8_t* const wp = a.w + (int64_t)(n0 + lq < a.n ? n0 + lq : a.n - 1) * a.k_padded + 16 * lg;
+  const int8_t* xp[TB];
+#pragma unroll
+  for (int t = 0; t < TB; ++t) xp[t] = a.x + (int64_t)(16 * t + lq < a.m ? 16 * t + lq : a.m - 1) * a.k_padded + 16 * lg;
+  const uint32_t row_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem + 16u * lg;
+
+  // the token first: what is asked for last is waited for last
+  uint4v raw[FUSED ? WORDS : 1];
+  if constexpr (FUSED) {
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) {
+      const int at = 8 * (tid + 512 * i);
+      raw[i] = (uint4v)0u;
+      if (at + 8 <= b.k) raw[i] = *reinterpret_cast<const uint4v*>(b.raw + 2 * at);
+      else if (at < b.k)
+        for (int e = 0; e < b.k - at; ++e) raw[i][e >> 1] |= (uint32_t)reinterpret_cast<const uint16_t*>(b.raw)[at + e] << 16 * (e & 1);
+    }
+  }
+  int4v acc[TB], wr[2][U], xr[2][FUSED ? 1 : TB][U];
+#pragma unroll
+  for (int t = 0; t < TB; ++t) acc[t] = (int4v)0;
+  auto fetch = [&](int to, int stage) __attribute__((always_inline)) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int s = stage * U + u < steps ? stage * U + u : steps - 1;      // (what is fetched twice is not multiplied twice)
+      wr[to][u] = *reinterpret_cast<const int4v*>(wp + 64 * s);
+      if constexpr (!FUSED)
+#pragma unroll
+        for (int t = 0; t < TB; ++t) xr[to][t][u] = *reinterpret_cast<const int4v*>(xp[t] + 64 * s);
+    }
+  };
+  int stage = wave;
+  if (stage < stages) fetch(0, stage);
+  if (stage + FEW_WAVES < stages) fetch(1, stage + FEW_WAVES);
+  float sx = 0.f;
+  if constexpr (FUSED) {
+    uint32_t most = 0;
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i)
+#pragma unroll
+      for (int w = 0; w < 4; ++w)
+        most = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(ushort2v, most), __builtin_bit_cast(ushort2v, raw[i][w] & 0x7FFF7FFFu)));
+    most = (most & 0xFFFFu) > most >> 16 ? most & 0xFFFFu : most >> 16;
+    most = largest_of_wave(most);
+    if (lane == 0) most_of[wave] = most;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < FEW_WAVES; ++w) most = most_of[w] > most ? most_of[w] : most;
+    most = as_u(low_of<IN == FTINT8_BF16>(most));
+    const Coding c(most);
+    sx = c.fine ? as_f(most) / 127.f : __builtin_nanf("");
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) {
+      const int at = 8 * (tid + 512 * i);
+      if (at < a.k_padded) *reinterpret_cast<uint2v*>(smem + at) = c.codes<IN == FTINT8_BF16>(raw[i]);
+    }
+    __syncthreads();
+  } else if (tid < 64 * TB) {
+    const int r = 16 * (tid >> 6) + lq;
+    sx = a.sx[r < a.m ? r : a.m - 1];
+  }
+  auto multiply = [&](int from, int stage) __attribute__((always_inline)) {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (stage * U + u < steps)
+#pragma unroll
+        for (int t = 0; t < TB; ++t) {
+          int4v x;
+          if constexpr (FUSED) x = *(const __attribute__((address_space(3))) int4v*)(uintptr_t)(row_at + 64u * (stage * U + u));
+          else x = xr[from][t][u];
+          acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wr[from][u], x, acc[t], 0, 0, 0);
+        }
+  };
+  while (stage < stages) {
+    multiply(0, stage);
+    if (stage + 2 * FEW_WAVES < stages) fetch(0, stage + 2 * FEW_WAVES);
+    stage += FEW_WAVES;
+    if (stage >= stages) break;
+    multiply(1, stage);
+    if (stage + 2 * FEW_WAVES < stages) fetch(1, stage + 2 * FEW_WAVES);
+    stage += FEW_WAVES;
+  }
+  // the waves' sums, added up by the first TB of them
+  if constexpr (FUSED) __syncthreads();
+  int4v* const parts = reinterpret_cast<int4v*>(smem);
+#pragma unroll
+  for (int t = 0; t < TB; ++t) parts[(wave * TB + t) * 64 + lane] = acc[t];
+  __syncthreads();
+  if (wave >= TB) return;
+  int4v sum = parts[wave * 64 + lane];
+#pragma unroll
+  for (int w = 1; w < FEW_WAVES; ++w) sum += parts[(w * TB + wave) * 64 + lane];
+  const int row = 16 * wave + lq, col = n0 + 4 * lg;
+  if (row >= a.m) return;
+  if (col < a.n) put_four<DT>(a, row, col, sum, sx);
+}
+
 typedef void (*encode_fn)(const EncodeArgs);
 typedef void (*product_fn)(const ProductArgs);
+typedef void (*few_fn)(const FewArgs);
+template <int DT> few_fn few_of(bool two) { return two ? ftint8_few<2, DT, 0, 0> : ftint8_few<1, DT, 0, 0>; }
+template <int DT> few_fn fused_of(bool bf, bool wide) {
+  if (wide) return bf ? ftint8_few<1, DT, FTINT8_BF16, 4> : ftint8_few<1, DT, FTINT8_F16, 4>;
+  return bf ? ftint8_few<1, DT, FTINT8_BF16, 1> : ftint8_few<1, DT, FTINT8_F16, 1>;
+}
+constexpr int few_lds(int blocks) { return FEW_WAVES * blocks * 64 * 16; }
 
 // The kernel for rows of k_padded codes; per: rows of a workgroup.  Rows of up to 2048 elements take a wave each, of up to 16384 a workgroup.
 template <int DT> encode_fn encode_of(int k_padded, bool whole, int& per) {
@@ -374,9 +552,13 @@ using TileSmall = Tile<64, 128, 2, 4, 3, 2>;
 struct TileInfo { int bm, bf, threads, lds; };
 template <class T> constexpr TileInfo info_of() { return {T::BM, T::BF, T::NW * 64, T::LDS}; }
 constexpr TileInfo TILES[N_TILES] = {info_of<TileWide>(), info_of<TileHalf>(), info_of<TileQuarter>(), info_of<TileSmall>()};
-template <int DT> product_fn tile_of(int tile) {
+typedef void (*finish_fn)(const ProductArgs, int);
+template <int DT> product_fn tile_kernel(int tile) {
   return tile == WIDE ? ftint8_tile<TileWide, DT> : tile == HALF ? ftint8_tile<TileHalf, DT> : tile == QUARTER ? ftint8_tile<TileQuarter, DT> : ftint8_tile<TileSmall, DT>;
 }
+// Shares of divided columns: at most MOST_SHARES of them at a time.
+constexpr int MOST_SHARES = 256;
+constexpr size_t SUMS_BYTES = (size_t)MOST_SHARES * TileSmall::BM * TileSmall::BF * 4;
 
 }  // namespace ftint8
 
@@ -386,6 +568,9 @@ struct ftint8_ctx {
   ftint8_config cfg;
   int k_padded = 0;
   product_fn product[N_TILES] = {};
+  finish_fn finish = nullptr;
+  int4v* sums = nullptr;
+  few_fn few[2] = {}, fused = nullptr;
   int8_t* codes = nullptr;       // of the tokens of a forward, and their scales behind them
   float* scales = nullptr;
   std::string err;
@@ -423,14 +608,19 @@ extern "C" int ftint8_create(const ftint8_config* cfg, ftint8_ctx** out) {
   c->cfg = *cfg;
   c->k_padded = (cfg->k + KEXTRA - 1) / KEXTRA * KEXTRA;
   for (int t = 0; t < N_TILES; ++t)
-    c->product[t] = cfg->out_dtype == FTINT8_F32 ? tile_of<FTINT8_F32>(t) : cfg->out_dtype == FTINT8_BF16 ? tile_of<FTINT8_BF16>(t) : tile_of<FTINT8_F16>(t);
+    c->product[t] = cfg->out_dtype == FTINT8_F32 ? tile_kernel<FTINT8_F32>(t) : cfg->out_dtype == FTINT8_BF16 ? tile_kernel<FTINT8_BF16>(t) : tile_kernel<FTINT8_F16>(t);
+  c->finish = cfg->out_dtype == FTINT8_F32 ? ftint8_finish<TileSmall, FTINT8_F32> : cfg->out_dtype == FTINT8_BF16 ? ftint8_finish<TileSmall, FTINT8_BF16> : ftint8_finish<TileSmall, FTINT8_F16>;
+  const bool bf = cfg->in_dtype == FTINT8_BF16, wide = c->k_padded > 4096;
+  for (int i = 0; i < 2; ++i)
+    c->few[i] = cfg->out_dtype == FTINT8_F32 ? few_of<FTINT8_F32>(i) : cfg->out_dtype == FTINT8_BF16 ? few_of<FTINT8_BF16>(i) : few_of<FTINT8_F16>(i);
+  c->fused = cfg->out_dtype == FTINT8_F32 ? fused_of<FTINT8_F32>(bf, wide) : cfg->out_dtype == FTINT8_BF16 ? fused_of<FTINT8_BF16>(bf, wide) : fused_of<FTINT8_F16>(bf, wide);
   const size_t bytes = (size_t)cfg->max_tokens * c->k_padded;
   int before = 0;
   hipError_t he = hipGetDevice(&before);
   if (he == hipSuccess) he = hipSetDevice(cfg->device);
   if (he == hipSuccess) {
     for (int t = 0; t < N_TILES && he == hipSuccess; ++t) he = hipFuncSetAttribute((const void*)c->product[t], hipFuncAttributeMaxDynamicSharedMemorySize, TILES[t].lds);
-    if (he == hipSuccess) he = hipMalloc((void**)&c->codes, bytes + (size_t)cfg->max_tokens * sizeof(float));
+    if (he == hipSuccess) he = hipMalloc((void**)&c->codes, SUMS_BYTES + bytes + (size_t)cfg->max_tokens * sizeof(float));
     (void)hipSetDevice(before);
   }
   if (he != hipSuccess) {
@@ -438,6 +628,8 @@ extern "C" int ftint8_create(const ftint8_config* cfg, ftint8_ctx** out) {
     delete c;
     return rc;
   }
+  c->sums = reinterpret_cast<int4v*>(c->codes);
+  c->codes += SUMS_BYTES;
   c->scales = reinterpret_cast<float*>(c->codes + bytes);
   *out = c;
   return FTINT8_OK;
@@ -486,17 +678,48 @@ static hipError_t launch_encode(ftint8_ctx* c, const ftint8_matrix* x, int32_t r
   hipLaunchKernelGGL(fn, dim3((uint32_t)((rows + per - 1) / per)), dim3(256), 0, st, a);
   return hipGetLastError();
 }
-static hipError_t launch_product(ftint8_ctx* c, const int8_t* x, const float* sx, int32_t m, const int8_t* w, const float* sw, const ftint8_matrix* y, hipStream_t st) {
+static ProductArgs product_args(ftint8_ctx* c, const int8_t* x, const float* sx, int32_t m, const int8_t* w, const float* sw, const ftint8_matrix* y) {
   const int size = c->cfg.out_dtype == FTINT8_F32 ? 4 : 2;
-  const int32_t wide = ((uintptr_t)y->data | (uintptr_t)(y->stride * size)) % 16 == 0;
-  const ProductArgs a{x, w, sx, sw, static_cast<char*>(y->data), y->stride * size, m, c->cfg.n, c->k_padded, wide};
+  return ProductArgs{x, w, sx, sw, static_cast<char*>(y->data), y->stride * size, m, c->cfg.n, c->k_padded, ((uintptr_t)y->data | (uintptr_t)(y->stride * size)) % 16 == 0, 1, nullptr};
+}
+// Tokens of which a launch cannot have all tiles (it has fewer than 2^32 threads).
+static bool too_many(const ftint8_ctx* c, int32_t m) {
+  const TileInfo& t = TILES[WIDE];
+  return (int64_t)((m + t.bm - 1) / t.bm) * ((c->cfg.n + t.bf - 1) / t.bf) * t.threads >= 1ll << 32;
+}
+static hipError_t launch_product(ftint8_ctx* c, const int8_t* x, const float* sx, int32_t m, const int8_t* w, const float* sw, const ftint8_matrix* y, hipStream_t st) {
+  ProductArgs a = product_args(c, x, sx, m, w, sw, y);
   auto tiles = [&](int t) { return (int64_t)((m + TILES[t].bm - 1) / TILES[t].bm) * ((c->cfg.n + TILES[t].bf - 1) / TILES[t].bf); };
+  // Up to 16 tokens: 9 on 4096 x 16,384 (features x columns) 17.7 us, on tiles 19.6; 16 on 1000 x 500 2.4, 4.0; 16 on 32,000 x 4096 34.5, 32.9.  Up to 32, whose
+  // codes each workgroup reads twice as many of as of weights, where the weights fit a round of workgroups: 32 on 4096 x 4096 8.4 us, 10.2; on 1000 x 1000 3.3, 5.2;
+  // but on 4096 x 8192 15.6, 14.4, on 16,384 x 4096 28.9, 19.9, on 500 x 10,000 15.7, 10.3.  Above that: 64 on 4096 x 4096 11.9, 10.2.
+  if (m <= 16 || (m <= 32 && c->k_padded <= 4096 && c->cfg.n <= 4096)) {
+    const FewArgs f{a, nullptr, 0};
+    const int two = m > 16;
+    hipLaunchKernelGGL(c->few[two], dim3((uint32_t)((c->cfg.n + 15) / 16)), dim3(FEW_WAVES * 64), few_lds(1 + two), st, f);
+    return hipGetLastError();
+  }
+  // The largest tile that gives every CU one.  256 x 256, 128 x 256, 64 x 256, 64 x 128, in us: 4096 tokens on 4096 x 4096 (256 tiles of the first) 55, 64, 87, 88;
+  // 2000 tokens (256 of the second) 49, 36, 47, 50; 1000 (256 of the third) 47, 28, 24, 26; 512 (256 of the last) 46, 27, 21, 16.
   int tile = WIDE;
   while (tile + 1 < N_TILES && tiles(tile) < 256) ++tile;
-  hipLaunchKernelGGL(c->product[tile], dim3((uint32_t)tiles(tile)), dim3(TILES[tile].threads), TILES[tile].lds, st, a);
+  const int64_t count = tiles(tile), stages = c->k_padded / TileSmall::BK;
+  // Too few of the smallest: the columns are divided, in shares of at least eight stages, the fewer in all the less there is to divide, as shares are written and read
+  // once more.  96 tokens on 4096 x 16,384 (64 tiles) 24 us in four, 55 in one; 1000 on 500 x 10,000 15, 27; 64 on 4096 x 4096 (32 tiles, 32 stages) 10.7
+  // in four, 13.9 in one; 256 tokens there (128 tiles) 15.0 in two, 12.5 in one.
+  if (tile == SMALL) {
+    const int64_t shares = (stages < 64 ? 4 * stages : MOST_SHARES) / count;
+    a.parts = (int)(shares < stages / 8 ? shares : stages / 8);
+    if (a.parts < 2) a.parts = 1;
+  }
+  a.sums = c->sums;
+  hipLaunchKernelGGL(c->product[tile], dim3((uint32_t)count, (uint32_t)a.parts), dim3(TILES[tile].threads), TILES[tile].lds, st, a);
+  const hipError_t he = hipGetLastError();
+  if (he != hipSuccess || a.parts == 1) return he;
+  constexpr int BLOCKS = TileSmall::BM * TileSmall::BF / 256;
+  hipLaunchKernelGGL(c->finish, dim3((uint32_t)(count * BLOCKS / 4)), dim3(256), 0, st, a, (int)count);
   return hipGetLastError();
 }
-
 extern "C" int ftint8_encode(ftint8_ctx* c, const ftint8_matrix* x, int32_t rows, int8_t* codes, float* scales, void* hip_stream) {
   if (!c) return FTINT8_EINVAL;
   if (rows < 0) return ifail(c, FTINT8_EINVAL, "rows must be >= 0");
@@ -517,6 +740,7 @@ extern "C" int ftint8_product(ftint8_ctx* c, const int8_t* codes_x, const float*
   if (m < 0) return ifail(c, FTINT8_EINVAL, "m must be >= 0");
   if (m == 0) return FTINT8_OK;
   if (m > 1 << 22) return ifail(c, FTINT8_EUNSUPPORTED, "more than 2^22 tokens");
+  if (too_many(c, m)) return ifail(c, FTINT8_EUNSUPPORTED, "too many tokens for as many features");
   const char* bad = wrong_matrix(y, c->cfg.out_dtype == FTINT8_F32 ? 4 : 2, c->cfg.n);
   if (!bad) bad = wrong_codes(codes_x, scales_x);
   if (!bad) bad = wrong_codes(codes_w, scales_w);
@@ -531,13 +755,21 @@ extern "C" int ftint8_forward(ftint8_ctx* c, const ftint8_matrix* x, int32_t m, 
   if (!c) return FTINT8_EINVAL;
   if (m < 0 || m > c->cfg.max_tokens) return ifail(c, FTINT8_EINVAL, "m must be 0 .. max_tokens");
   if (m == 0) return FTINT8_OK;
+  if (too_many(c, m)) return ifail(c, FTINT8_EUNSUPPORTED, "too many tokens for as many features");
   const char* bad = wrong_matrix(x, 2, c->cfg.k);
   if (!bad) bad = wrong_matrix(y, c->cfg.out_dtype == FTINT8_F32 ? 4 : 2, c->cfg.n);
   if (!bad) bad = wrong_codes(codes_w, scales_w);
   if (bad) return ifail(c, FTINT8_EINVAL, bad);
   OnDevice on(c->cfg.device);
   if (on.error != hipSuccess) return ifail_hip(c, "device", on.error);
-  hipError_t he = launch_encode(c, x, m, c->codes, c->scales, (hipStream_t)hip_stream);
+  hipError_t he;
+  if (m == 1 && c->k_padded <= FUSED_K && (uintptr_t)x->data % 16 == 0) {
+    const FewArgs f{product_args(c, nullptr, nullptr, m, codes_w, scales_w, y), static_cast<const char*>(x->data), c->cfg.k};
+    hipLaunchKernelGGL(c->fused, dim3((uint32_t)((c->cfg.n + 15) / 16)), dim3(FEW_WAVES * 64), c->k_padded > few_lds(1) ? c->k_padded : few_lds(1), (hipStream_t)hip_stream, f);
+    he = hipGetLastError();
+    return he == hipSuccess ? FTINT8_OK : ifail_hip(c, "launch", he);
+  }
+  he = launch_encode(c, x, m, c->codes, c->scales, (hipStream_t)hip_stream);
   if (he == hipSuccess) he = launch_product(c, c->codes, c->scales, m, codes_w, scales_w, y, (hipStream_t)hip_stream);
   return he == hipSuccess ? FTINT8_OK : ifail_hip(c, "launch", he);
 }
@@ -546,7 +778,7 @@ extern "C" int ftint8_destroy(ftint8_ctx* c) {
   if (!c) return FTINT8_OK;
   int before = 0;
   const bool moved = hipGetDevice(&before) == hipSuccess && before != c->cfg.device && hipSetDevice(c->cfg.device) == hipSuccess;
-  (void)hipFree(c->codes);
+  (void)hipFree(c->sums);
   if (moved) (void)hipSetDevice(before);
   delete c;
   return FTINT8_OK;

@@ -37,7 +37,7 @@ typedef struct {
   int32_t n, k;          /* output and input features of the layer: any numbers from 1 on, k at most 130944 (sums of k products of codes stay below 2^31) */
   int32_t in_dtype;      /* FTINT8_F16 | FTINT8_BF16: type of x (and of weights that are encoded here) */
   int32_t out_dtype;     /* FTINT8_F32, or in_dtype */
-  int32_t max_tokens;    /* most tokens of a ftint8_forward: the context holds max_tokens * (k_padded + 4) bytes for their codes and scales */
+  int32_t max_tokens;    /* most tokens of a ftint8_forward: the context holds max_tokens * (k_padded + 4) bytes for their codes and scales, and 8 MB */
   int32_t device;        /* HIP device ordinal */
 } ftint8_config;
 
@@ -52,7 +52,7 @@ int ftint8_get_config(const ftint8_ctx* ctx, ftint8_config* effective);
 int ftint8_k_padded(const ftint8_ctx* ctx);
 /* Codes and scales of the rows of x, [rows, k] of in_dtype: weights once, or tokens that several layers read. */
 int ftint8_encode(ftint8_ctx* ctx, const ftint8_matrix* x, int32_t rows, int8_t* codes, float* scales, void* hip_stream);
-/* y [m, n] from codes and scales of m tokens and of the n channels of weights. */
+/* y [m, n] from codes and scales of m tokens, up to 2^22, and of the n channels of weights.  (More tiles of 256 x 256 than a launch has, 2^23: FTINT8_EUNSUPPORTED.) */
 int ftint8_product(ftint8_ctx* ctx, const int8_t* codes_x, const float* scales_x, int32_t m, const int8_t* codes_w, const float* scales_w, const ftint8_matrix* y,
                    void* hip_stream);
 /* y [m, n] from m tokens x [m, k] in 16 bits: both of the above in one call, m <= max_tokens.  The same results, bit for bit.  y and x may not overlap. */

@@ -105,7 +105,7 @@ def test_rows_of_zeros_of_small_and_of_unbounded_numbers(dtype):
 
 SHAPES = [(1, 1, 1), (1, 16, 64), (1, 515, 4096), (1, 2000, 9000), (2, 33, 65), (5, 4096, 512), (15, 100, 300), (16, 256, 128), (17, 257, 129), (31, 1000, 1000), (33, 48, 4096),
           (64, 64, 64), (65, 700, 260), (96, 512, 2048), (127, 129, 127), (128, 128, 256), (130, 96, 384), (200, 3, 77), (255, 300, 1024), (256, 256, 256), (300, 520, 900), (513, 257, 640),
-          (700, 1030, 200), (1000, 96, 96), (1100, 2100, 512)]
+          (700, 1030, 200), (1000, 96, 96), (1100, 2100, 512), (20, 70, 5001), (50, 200, 5001), (1, 33, 16385), (130, 500, 10000)]
 
 
 @pytest.mark.parametrize("dtype,out", [(ftint8.F16, ftint8.F16), (ftint8.BF16, ftint8.BF16), (ftint8.F16, ftint8.F32), (ftint8.BF16, ftint8.F32)])
@@ -162,7 +162,7 @@ def test_no_tokens():
     torch.cuda.synchronize()
 
 
-@pytest.mark.parametrize("m,n,k", [(1, 600, 512), (40, 300, 700), (300, 260, 384)])
+@pytest.mark.parametrize("m,n,k", [(1, 600, 512), (40, 300, 700), (40, 300, 2100), (300, 260, 384)])
 def test_on_another_stream_and_in_a_graph(m, n, k):
     sizes = inputs(m, n, k, ftint8.F16, 1)
     ctx = ftint8.FtInt8(n, k, ftint8.F16, max_tokens=m)
