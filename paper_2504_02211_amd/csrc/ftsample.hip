@@ -5,15 +5,24 @@
 // numbers depends on the order of its terms.
 //
 // A workgroup takes a row, each of its 8 waves a run of neighbouring tokens, in registers where they fit (131,072 of 16 bits, 65,536 of 32).  Rows with a small top_k keep
-// what lies at or above the top_k-th largest of the threads' maxima (few more than top_k), sort it and sum it up by rank.  Without top_k all weights are formed; for top_p they are added to a histogram over
-// their logarithm, 128 bins an octave, and the bin in which the limit lies is searched by keys.  In all other cases (a large top_k, thousands of equal
-// logits) the border is searched by histograms of the keys' bits.  Last, kept weights are summed wave by wave, and the wave in which the random number falls looks for the token.
+// what lies at or above the top_k-th largest of the threads' maxima (few more than top_k), sort it and sum it up by rank.  In all other cases the border that top_k and
+// top_p draw comes first, then one pass sums up the weights above it, wave by wave and run by run of words, and the lane of the run in which the random number falls finds the
+// token.
+//   - bf16 has few values: each has a number, how often it occurs is counted in LDS, and its weight stands there; no weight is formed per logit.  256 rows of 131,072 with a
+//     temperature of their own take 30 us, with top_p 49 us; with a weight formed for each logit as below they took 46 and 100 us.
+//   - fp16 and fp32: counts or weights are added to a histogram over the weights' logarithm, 128 bins an octave, and the bin in which the limit lies is searched: few logits of
+//     32 bits lie there, which are sorted (48 rows of 50,001 with top_p 44 us; 50 when searched by histograms of the keys' bits); of 16 bits many are equal, and one
+//     histogram of the keys' bits tells (sorted where they fit, 512 rows of 65,536 took 3 us more).  512 rows of 65,536 in fp16 take 48 us, with top_p 100 us.
+// Bound by the row's one CU: reading 67 MB, 131,072 logits a CU, takes 10 of the 49 us (7 TB/s), counting 14, the border 6, the sum 12, where the reads and additions in LDS
+// and the instructions that find their addresses take turns; greedy rows take 21 us.  Rows that do not fit in registers are read anew in each pass: one of 262,144 in
+// fp32 takes 80 us greedy, 235 with top_p.
 #include "ftsample.h"
 #include "ftserve_device.h"
 
 #include <cmath>
 #include <new>
 #include <string>
+#include <type_traits>
 
 namespace ftsample {
 using namespace ftserve;
@@ -72,7 +81,7 @@ __device__ __forceinline__ Rules rules_of(const Args& a, int row) {
   float t = a.temperature ? a.temperature[row] : 1.f;
   if (t != t) t = 1.f;
   r.greedy = t <= 0.f;
-  r.per_t = r.greedy ? 1.0 : 1.0 / (double)t;
+  r.per_t = r.greedy ? 1.0 : __builtin_fmax(1.0 / (double)t, 0x1p-200);      // (never 0: the difference to -infinity is multiplied by it)
   const int32_t k = a.top_k ? a.top_k[row] : 0;
   r.top_k = r.greedy ? 1 : k <= 0 || k > a.vocab ? a.vocab : k;
   const float p = a.top_p ? a.top_p[row] : 1.f, m = a.min_p ? a.min_p[row] : 0.f, u = a.uniform[row];
@@ -86,14 +95,14 @@ __device__ __forceinline__ Rules rules_of(const Args& a, int row) {
 // Weights of logits, given the largest one: w = 2^(n / STEPS) 2^(r / STEPS) with n whole and |r| <= 1/2, the first factor from a table and an exponent, the second
 // from its series (the term left out is below 2^-46), in whole multiples of 2^-shift.
 struct Weights {
-  double scale, most;        // STEPS / (temperature * ln 2); the largest logit
+  double scale, most, least; // STEPS / (temperature * ln 2); the largest logit; the difference to it from which on all weights are 0
   const double* table;       // 2^(i / STEPS + shift)
   static constexpr double ROUND = 6755399441055744.0;      // 1.5 * 2^52
   // the logarithm in steps, and the nearest whole number of them; -infinity and NaN: as far below as counts
   __device__ __forceinline__ double steps(float x, int& n) const {
-    const double t = __builtin_fmax(((double)x - most) * scale, -(double)(STEPS * OCTAVES)), at = t + ROUND;
+    const double d = __builtin_fmax((double)x - most, least), at = __builtin_fma(d, scale, ROUND);
     n = (int)(uint32_t)__builtin_bit_cast(uint64_t, at);
-    return t - (at - ROUND);
+    return __builtin_fma(d, scale, ROUND - at);
   }
   __device__ __forceinline__ int bin(float x) const {
     int n;
@@ -183,8 +192,17 @@ __device__ __forceinline__ float wave_most(float x) {
   return x;
 }
 
-struct Shared {
-  unsigned long long bins[(LAST_BIN + THREADS) / THREADS * THREADS];      // whole rounds of all threads
+// Logits of bf16 by their value: there are few enough of them.  Those of a magnitude from `base` on, 23 octaves of 128, have a number, that of negative ones below 0; what is smaller
+// ("tiny") is taken one by one; what is larger is so far below the largest logit, or NaN, that it has no weight: the numbers at either end.
+constexpr int MAGNITUDES = 23 * 128, VALUES = 2 * MAGNITUDES + 2;
+constexpr int TIE = 57;                  // (its bit: a lane adds up less than 2^56 and 64 ties)
+template <bool KEYED> struct ByValue {};
+template <> struct ByValue<true> {
+  unsigned long long worth[VALUES];      // what a logit adds to the sum, TIE if it is the border
+  uint32_t counts[VALUES];
+};
+template <bool KEYED> struct Shared : ByValue<KEYED> {
+  unsigned long long bins[KEYED ? BINS : (LAST_BIN + THREADS) / THREADS * THREADS];      // whole rounds of all threads
   double table[STEPS];
   unsigned long long sums[WAVES];
   uint32_t words[WAVES];
@@ -192,68 +210,106 @@ struct Shared {
   uint32_t bin, count;
 };
 
-// The first bin, from first_bin on upwards in `order`, before which less than `limit` lies and with which it is reached, or the last that holds anything: s.bin, s.above.
-// value(i): what the i-th bin in falling order of keys holds; PER of them a thread.
-template <int PER, class F> __device__ __forceinline__ void find_bin(Shared& s, unsigned long long above, unsigned long long limit, F value) {
-  unsigned long long mine = 0, all;
+// The first bin in falling order of keys before which less than the limit lies and with which it is reached, or the last that holds anything: s.bin, s.above.
+// value(i): what the i-th bin holds; PER of them a thread; above: what lies before all; limit(all): from what all hold.  Gives what all hold.
+template <int PER, class S, class L, class F> __device__ __forceinline__ unsigned long long find_bin(S& s, unsigned long long above, L limit, F value) {
+  unsigned long long held[PER], mine = 0, all;
   const int first = (int)threadIdx.x * PER;
-  for (int i = 0; i < PER; ++i) mine += value(first + i);
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    held[i] = value(first + i);
+    mine += held[i];
+  }
   unsigned long long at = above + before_me<unsigned long long>(mine, s.sums, all);
+  const unsigned long long reached = limit(all);
   if (mine)
+#pragma unroll
     for (int i = 0; i < PER; ++i) {
-      const unsigned long long n = value(first + i);
-      if (n && at < limit && (at + n >= limit || at + n == above + all)) {
+      const unsigned long long n = held[i];
+      if (n && at < reached && (at + n >= reached || at + n == above + all)) {
         s.bin = (uint32_t)(first + i);
         s.above = at;
       }
       at += n;
     }
   __syncthreads();
+  return all;
 }
 
 // The logits of a row, as the waves have them: wave w has neighbouring tokens, lane l of it those of its words l, l + 64, .. of 16 bytes; up to 32 words a lane in
-// registers (HELD), or read anew every time.
+// registers (HELD), or read anew every time, 8 at once.
 template <int DT, bool HELD> struct Row {
   typedef Type<DT> L;
-  typedef uint32_t Words __attribute__((ext_vector_type(MOST_WORDS)));
+  static constexpr int N = HELD ? MOST_WORDS : 8;
+  typedef uint32_t Words __attribute__((ext_vector_type(N)));
   static constexpr int PER = L::PER;
   const char* x;           // aligned to 16 bytes, `skip` elements before the row
+  __amdgpu_buffer_rsrc_t whole_words;      // from there on: what lies behind them is not read
   int skip, vocab, words;  // words of a lane
   int first;               // this lane's first word
   bool flat;               // the largest logit is +infinity: those that are it count as 0, the others as -infinity
-  Words held[HELD ? 4 : 1];      // (a register of each word, by its number: read with an index that is the same in all lanes)
+  Words held[4];           // (a register of each word, by its number: read with an index that is the same in all lanes)
+  float largest;           // of this lane
   __device__ __forceinline__ Row(const Args& a, int row) : vocab(a.vocab) {
     const char* const at = static_cast<const char*>(a.logits) + (int64_t)row * a.stride * L::SIZE;
     skip = (int)((uintptr_t)at & 15) / L::SIZE;
     x = at - skip * L::SIZE;
+    whole_words = __builtin_amdgcn_make_buffer_rsrc((void*)x, 0, (vocab + skip) / PER * 16, 0x00027000);
     words = ((vocab + skip + PER - 1) / PER + THREADS - 1) / THREADS;
     first = (int)(threadIdx.x >> 6) * words * 64 + (int)(threadIdx.x & 63);
     flat = false;
+    largest = NOTHING;
     if constexpr (HELD) {
+      fill(held, 0, largest);
+    } else {
+      each_word([&](int, const uint4v& k) { larger(largest, k); });
+    }
+  }
+  // This lane's words from v0 on, 8 loads under way at a time.
+  static __device__ __forceinline__ void larger(float& most, const uint4v& r) {
 #pragma unroll
-      for (int v = 0; v < MOST_WORDS; ++v) {
-        uint4v r = {L::NONE, L::NONE, L::NONE, L::NONE};
-        if (v < words && whole(first + 64 * v)) r = load(first + 64 * v);
+    for (int e = 0; e < PER; ++e) most = __builtin_fmaxf(most, L::logit(r, e));
+  }
+  // ...; `most`: the largest of it and them
+  __device__ __forceinline__ void fill(Words (&to)[4], int v0, float& most) const {
 #pragma unroll
-        for (int w = 0; w < 4; ++w) held[w][v] = r[w];
+    for (int g = 0; g < N / 8; ++g) {
+      uint4v r[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) r[i] = (uint4v){L::NONE, L::NONE, L::NONE, L::NONE};
+      if (v0 + 8 * g < words) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) r[i] = load(first + 64 * (v0 + 8 * g + i));
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          r[i] = v0 + 8 * g + i < words && whole(first + 64 * (v0 + 8 * g + i)) ? r[i] : (uint4v){L::NONE, L::NONE, L::NONE, L::NONE};
+          larger(most, r[i]);
+        }
       }
-      // the row's first and last word, where they lie in it only in part
-      const int last = (vocab + skip - 1) / PER;
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) to[w][8 * g + i] = r[i][w];
+    }
+    // the row's first and last word, where they lie in it only in part
+    const int last = (vocab + skip - 1) / PER;
 #pragma unroll 1
-      for (int side = 0; side < 2; ++side) {
-        const int word = side ? last : 0, w0 = word / (words * 64), v = word % (words * 64) / 64;
-        if ((int)(threadIdx.x >> 6) != w0 || whole(word)) continue;
-        const uint4v y = part(word);
-        const bool mine = first + 64 * v == word;
+    for (int side = 0; side < 2; ++side) {
+      const int word = side ? last : 0, w0 = word / (words * 64), v = word % (words * 64) / 64 - v0;
+      if ((int)(threadIdx.x >> 6) != w0 || v < 0 || v >= N || whole(word)) continue;
+      const uint4v y = part(word);
+      const bool mine = first + 64 * (v + v0) == word;
+      if (mine) larger(most, y);
 #pragma unroll
-        for (int w = 0; w < 4; ++w) held[w][v] = mine ? y[w] : held[w][v];
-      }
+      for (int w = 0; w < 4; ++w) to[w][v] = mine ? y[w] : to[w][v];
     }
   }
   // 16 bytes that lie in the row; that do in part (what does not is -infinity); that do not
   __device__ __forceinline__ bool whole(int word) const { return word * PER >= skip && word * PER - skip + PER <= vocab; }
   __device__ __forceinline__ bool some(int word) const { return word * PER - skip + PER > 0 && word * PER - skip < vocab; }
-  __device__ __forceinline__ uint4v load(int word) const { return *reinterpret_cast<const uint4v*>(x + (int64_t)word * 16); }
+  __device__ __forceinline__ uint4v load(int word) const {      // (zeros where it does not lie in the row, or only its end does not)
+    return __builtin_bit_cast(uint4v, __builtin_amdgcn_raw_buffer_load_b128(whole_words, word * PER >= skip ? word * 16 : 1 << 30, 0, 0));
+  }
   __device__ __forceinline__ uint4v part(int word) const {
     uint4v r = {L::NONE, L::NONE, L::NONE, L::NONE};
     const int i = word * PER - skip;
@@ -267,16 +323,35 @@ template <int DT, bool HELD> struct Row {
   }
   // f(v, word) for every word of this lane
   template <class F> __device__ __forceinline__ void each_word(F f) const {
+    if constexpr (HELD) {
 #pragma unroll 1
-    for (int v = 0; v < words; ++v) {
-      if constexpr (HELD) f(v, flattened(uint4v{held[0][v], held[1][v], held[2][v], held[3][v]}));
-      else f(v, word(first + 64 * v));
+      for (int v = 0; v < words; ++v) f(v, at(v));
+    } else {
+#pragma unroll 1
+      for (int v0 = 0; v0 < words; v0 += N) {
+        Words read[4];
+        float unused = NOTHING;
+        fill(read, v0, unused);
+        const int end = words - v0 < N ? words - v0 : N;
+#pragma unroll 1
+        for (int v = 0; v < end; ++v) f(v0 + v, flattened(uint4v{read[0][v], read[1][v], read[2][v], read[3][v]}));
+      }
     }
   }
-  // Any word, from memory.
-  __device__ __forceinline__ uint4v word(int i) const { return flattened(whole(i) ? load(i) : part(i)); }
+  // This lane's v-th word, where they are held.
+  __device__ __forceinline__ uint4v at(int v) const { return flattened(uint4v{held[0][v], held[1][v], held[2][v], held[3][v]}); }
+  // Four words, 64 apart, from memory; those from `end` on are not looked at.
+  __device__ __forceinline__ void four_words(int word, int end, uint4v (&k)[4]) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) k[i] = load(word + 64 * i);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (word + 64 * i < end && !whole(word + 64 * i)) k[i] = part(word + 64 * i);
+      k[i] = flattened(k[i]);
+    }
+  }
   __device__ __forceinline__ uint4v flattened(uint4v r) const {
-    if (__builtin_expect(flat, 0)) {
+    if (__builtin_expect(__builtin_amdgcn_readfirstlane(flat), 0)) {
 #pragma unroll
       for (int e = 0; e < PER; ++e) {
         const bool is = L::logit(r, e) == -NOTHING;
@@ -313,7 +388,8 @@ __device__ __forceinline__ float not_below(double x) {
 template <int DT, bool HELD>
 __global__ __launch_bounds__(THREADS) void ftsample_row(const Args a) {
   typedef Type<DT> L;
-  __shared__ Shared s;
+  constexpr bool KEYED = DT == FTSAMPLE_BF16;
+  __shared__ Shared<KEYED> s;
   __shared__ unsigned long long list[LIST];      // (under top_k) key and place, then weights by place
   __shared__ int listed[LIST];
   const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -321,8 +397,7 @@ __global__ __launch_bounds__(THREADS) void ftsample_row(const Args a) {
   Row<DT, HELD> x(a, row);
   for (int i = tid; i < STEPS; i += THREADS) s.table[i] = __builtin_ldexp(exp2((double)i / STEPS), a.shift);
 
-  float mine = NOTHING;
-  x.each([&](float y) __attribute__((always_inline)) { mine = __builtin_fmaxf(mine, y); });
+  float mine = x.largest;
   float most = wave_most(mine);
   if (lane == 0) s.words[wave] = as_u(most);
   __syncthreads();
@@ -364,7 +439,8 @@ __global__ __launch_bounds__(THREADS) void ftsample_row(const Args a) {
     }
     return;
   }
-  const Weights weights{r.per_t * (STEPS / 0.69314718055994530942), (double)most, s.table};
+  const double scale = r.per_t * (STEPS / 0.69314718055994530942);
+  const Weights weights{scale, (double)most, -(STEPS * OCTAVES + 0.25) / scale, s.table};
   auto weight = [&](float y) __attribute__((always_inline)) {
     int bin;
     return weights.of(y, bin);
@@ -376,105 +452,117 @@ __global__ __launch_bounds__(THREADS) void ftsample_row(const Args a) {
     return limit >= 1.0 ? (unsigned long long)limit : 1ull;
   };
 
-  // The first place at which the sum of kept weights exceeds u times all: whole numbers exceed it where they reach the next one.  sum: this wave's kept weights without those of the
-  // border; ties: how many logits of it are the border.
-  auto choose = [&](const Kept& kept, unsigned long long sum, uint32_t ties) {
-    const unsigned long long worth = kept.equal ? weight(kept.border) : 0;
+  // Logits of bf16 by their value.
+  int base = 0;
+  if constexpr (KEYED) {
+    const float low = most + (float)weights.least, far = __builtin_fmaxf(__builtin_fabsf(most), __builtin_fabsf(low));
+    const int octave = (int)(as_u(far) >> 23) + 2;      // (one more than holds `far`: `low` is rounded)
+    base = (octave < 255 ? octave : 255) * 128 - MAGNITUDES;
+    base = base > 0 ? base : 0;
+  }
+  // The numbers of a word's logits, two in a word and times UNIT; whether one is tiny, and (at_ends) whether one is at either end.
+  auto numbers_of = [&](auto unit, const uint4v& k, uint32_t (&pair)[4], bool& at_ends) __attribute__((always_inline)) {
+    constexpr uint16_t UNIT = decltype(unit)::value;
+    ushort2v furthest = {0, 0};
+    uint32_t signs = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t u = k[i];
+      const ushort2v at = __builtin_bit_cast(ushort2v, u & 0x7FFF7FFFu) - (ushort2v)(uint16_t)base, in = __builtin_elementwise_min(at, (ushort2v)(uint16_t)MAGNITUDES);
+      furthest = __builtin_elementwise_max(furthest, at);
+      signs |= __builtin_bit_cast(uint32_t, at);
+      const ushort2v number = in ^ __builtin_bit_cast(ushort2v, __builtin_bit_cast(short2v, u) >> (short2v)(short)15);
+      pair[i] = __builtin_bit_cast(uint32_t, number * (ushort2v)UNIT + (ushort2v)(uint16_t)((MAGNITUDES + 1) * UNIT));
+    }
+    at_ends = furthest[0] >= MAGNITUDES || furthest[1] >= MAGNITUDES;
+    return (signs & 0x80008000u) != 0;      // (magnitudes and `base` are below 2^15)
+  };
+  auto tiny = [&](float y) { return (int)(as_u(y) >> 16 & 0x7FFF) < base; };
+  auto value_of = [&](int number) {      // (not of those at either end)
+    const int at = number - (MAGNITUDES + 1), magnitude = (at < 0 ? -at - 1 : at) + base;
+    return as_f((uint32_t)magnitude << 16 | (at < 0 ? 0x80000000u : 0u));
+  };
+  bool worth_known = false;
+  auto know_worth = [&]() {
+    if constexpr (KEYED) {
+      if (worth_known) return;
+#pragma unroll 4
+      for (int i = tid; i < VALUES; i += THREADS) s.worth[i] = weight(value_of(i));
+      if (tid == 0) s.worth[0] = 0;
+      if (tid == (VALUES - 1) % THREADS) s.worth[VALUES - 1] = 0;
+      worth_known = true;
+    }
+  };
+  // What the logits of a word that lie above the border add to the sum.
+  auto worths = [&](const uint4v& k, float border, unsigned long long (&w)[L::PER]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int e = 0; e < L::PER; ++e) {
+      const float y = L::logit(k, e);
+      w[e] = weight(y);
+      w[e] = y > border ? w[e] : 0;
+    }
+  };
+
+  // The first place at which the sum of kept weights exceeds u times all: whole numbers exceed it where they reach the next one.  Lane g has of this wave's g-th run of `per` words
+  // the kept weights without those of the border, and how many logits are the border.
+  auto choose = [&](const Kept& kept, int per, unsigned long long sum, uint32_t ties) {
+    const unsigned long long worth = kept.equal ? weight(kept.border) : 0, sums = sum_upto(sum);
+    const uint32_t tied = sum_upto(ties);
     __syncthreads();
-    if (lane == 0) {
-      s.sums[wave] = sum;
-      s.words[wave] = ties;
+    if (lane == 63) {
+      s.sums[wave] = sums;
+      s.words[wave] = tied;
     }
     __syncthreads();
-    unsigned long long all = 0;
-    {
-      int left = kept.equal;
+    unsigned long long all = 0, before = 0;
+    int left = kept.equal, left_here = 0;
 #pragma unroll
-      for (int w = 0; w < WAVES; ++w) {
-        const int n = (int)s.words[w] < left ? (int)s.words[w] : left;
-        all += s.sums[w] + (unsigned long long)n * worth;
-        left -= n;
+    for (int w = 0; w < WAVES; ++w) {
+      if (w == wave) {
+        before = all;
+        left_here = left;
       }
+      const int n = (int)s.words[w] < left ? (int)s.words[w] : left;
+      all += s.sums[w] + (unsigned long long)n * worth;
+      left -= n;
     }
     const unsigned long long goal = (unsigned long long)__builtin_floor(r.u * (double)all) + 1;
-    // The wave in whose run of words it lies; all waves look for it in an eighth of that run each, and so on until few words are left.
-    auto add_up = [&](const uint4v& k, unsigned long long (&w)[L::PER], uint32_t& n) __attribute__((always_inline)) -> unsigned long long {
-      unsigned long long sum = 0;
+    // the run in which it lies, of one lane of one wave
+    left = left_here - (int)(tied - ties);
+    left = left > 0 ? left : 0;
+    before += sums - sum + (unsigned long long)(left_here - left) * worth;
+    const unsigned long long here = sum + (unsigned long long)((int)ties < left ? (int)ties : left) * worth;
+    const uint64_t found = __ballot(before < goal && before + here >= goal);
+    if (!found) return;
+    const int run = __builtin_ctzll(found), end = (run + 1) * per < x.words ? (run + 1) * per : x.words;
+    before = (unsigned long long)(uint32_t)__builtin_amdgcn_readlane((int)(before >> 32), run) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)before, run);
+    left = __builtin_amdgcn_readlane(left, run);
+    uint4v ahead[4];
+#pragma unroll 1
+    for (int v = run * per; v < end; ++v) {
+      uint4v k;
+      if constexpr (HELD) {
+        k = x.at(v);
+      } else {
+        if ((v - run * per) % 4 == 0) x.four_words(x.first + 64 * v, x.first - lane + 64 * end, ahead);
+        k = ahead[0];
+        ahead[0] = ahead[1];
+        ahead[1] = ahead[2];
+        ahead[2] = ahead[3];
+      }
+      unsigned long long w[L::PER];
+      worths(k, kept.border, w);
+      sum = 0;
+      ties = 0;
 #pragma unroll
       for (int e = 0; e < L::PER; ++e) {
-        const float y = L::logit(k, e);
-        w[e] = weight(y);
-        w[e] = y > kept.border ? w[e] : 0;
-        n += kept.equal && y == kept.border;
+        ties += kept.equal && L::logit(k, e) == kept.border;
         sum += w[e];
       }
-      return sum;
-    };
-    unsigned long long before = 0;
-    int left = kept.equal, run = 0, length = x.words;      // of words of 64 lanes each
-    // After the parts' sums are in s: the part that it lies in.  (The last one that is not empty takes what no other does, so that every round leaves an eighth.)
-    auto part_of = [&](int per) {
-#pragma unroll 1
-      for (int w = 0;; ++w) {
-        const int n = (int)s.words[w] < left ? (int)s.words[w] : left;
-        const unsigned long long here = s.sums[w] + (unsigned long long)n * worth;
-        if (before + here >= goal || (w + 1) * per >= length) {
-          run += w * per;
-          length = length - w * per < per ? length - w * per : per;
-          return;
-        }
-        before += here;
-        left -= n;
-      }
-    };
-    length = WAVES * x.words;
-    part_of(x.words);
-    while (length > 4) {
-      const int per = (length + WAVES - 1) / WAVES, end = length < (wave + 1) * per ? length : (wave + 1) * per;
-      unsigned long long mine = 0;
-      uint32_t n = 0;
-#pragma unroll 1
-      for (int v = wave * per; v < end; v += 4) {
-        uint4v k[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (v + i < end) k[i] = x.word(64 * (run + v + i) + lane);
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (v + i < end) {
-            unsigned long long w[L::PER];
-            mine += add_up(k[i], w, n);
-          }
-      }
-      mine = wave_sum(mine);
-      n = wave_sum(n);
-      __syncthreads();
-      if (lane == 0) {
-        s.sums[wave] = mine;
-        s.words[wave] = n;
-      }
-      __syncthreads();
-      part_of(per);
-    }
-    if (wave) return;
-    bool done = false;
-    uint4v ahead[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (i < length) ahead[i] = x.word(64 * (run + i) + lane);
-#pragma unroll 1
-    for (int v = run; v < run + length && !done; ++v) {
-      const uint4v k = ahead[0];
-      ahead[0] = ahead[1];
-      ahead[1] = ahead[2];
-      ahead[2] = ahead[3];
-      unsigned long long w[L::PER];
-      uint32_t n = 0;
-      unsigned long long sum = add_up(k, w, n);
-      if (kept.equal && __any(n != 0)) {
+      if (kept.equal && __any(ties != 0)) {
         // those of the border that are left, in the order of their tokens
-        const uint32_t upto = sum_upto(n);
-        int mine = left - (int)(upto - n);
+        const uint32_t upto = sum_upto(ties);
+        int mine = left - (int)(upto - ties);
 #pragma unroll
         for (int e = 0; e < L::PER; ++e)
           if (L::logit(k, e) == kept.border && mine-- > 0) {
@@ -489,37 +577,74 @@ __global__ __launch_bounds__(THREADS) void ftsample_row(const Args a) {
       if (at < goal && at + sum >= goal)
 #pragma unroll
         for (int e = 0; e < L::PER; ++e) {
-          if (at < goal && at + w[e] >= goal) answer((64 * v + lane) * L::PER + e - x.skip, (double)w[e] / (double)all);
+          if (at < goal && at + w[e] >= goal) answer(x.token(v, e), (double)w[e] / (double)all);
           at += w[e];
         }
       before += last_lane(upto);
-      done = before >= goal;
+      if (before >= goal) return;
     }
   };
   auto sum_up = [&](Kept kept) {
     if (least > kept.border) kept = Kept{below(least), 0};
-    unsigned long long sum = 0;
-    uint32_t ties = 0;
-    if (kept.border == NOTHING) {
-      x.each([&](float y) __attribute__((always_inline)) { sum += weight(y); });
-    } else {
-      x.each_word([&](int, const uint4v& k) __attribute__((always_inline)) {
-        float largest = L::logit(k, 0);
-#pragma unroll
-        for (int e = 1; e < L::PER; ++e) largest = __builtin_fmaxf(largest, L::logit(k, e));
-        if (!__any(largest >= kept.border)) return;
-#pragma unroll
-        for (int e = 0; e < L::PER; ++e) {
-          const float y = L::logit(k, e);
-          const unsigned long long w = weight(y);
-          sum += y > kept.border ? w : 0;
+    if constexpr (KEYED) {
+      know_worth();
+      __syncthreads();
+      if (kept.border > NOTHING) {
+        for (int i = tid; i < VALUES; i += THREADS) {
+          const float y = value_of(i);
+          if (!(y > kept.border)) s.worth[i] = y == kept.border ? 1ull << TIE : 0;
         }
-        if (kept.equal)
-#pragma unroll
-          for (int e = 0; e < L::PER; ++e) ties += L::logit(k, e) == kept.border;
-      });
+        __syncthreads();
+      }
     }
-    choose(kept, wave_sum(sum), wave_sum(ties));
+    const int per = x.words <= 4 * 64 ? 4 : (x.words + 63) / 64;      // of a run
+    unsigned long long sum = 0, sum_of_run = 0;
+    uint32_t ties = 0, ties_of_run = 0;
+    int run = 0, in_run = 0;
+    x.each_word([&](int v, const uint4v& k) __attribute__((always_inline)) {
+      if constexpr (KEYED) {
+        uint32_t pair[4];
+        bool at_ends;
+        const bool some = numbers_of(std::integral_constant<uint16_t, 8>{}, k, pair, at_ends);
+#pragma unroll
+        for (int e = 0; e < L::PER; ++e)
+          sum += *reinterpret_cast<const unsigned long long*>(reinterpret_cast<const char*>(s.worth) + (e & 1 ? pair[e >> 1] >> 16 : pair[e >> 1] & 0xFFFFu));
+        if (__any(some))
+#pragma unroll
+          for (int e = 0; e < L::PER; ++e) {
+            const float y = L::logit(k, e);
+            if (tiny(y) && y >= kept.border) sum += y == kept.border ? 1ull << TIE : weight(y);
+          }
+      } else {
+        float largest = NOTHING;
+        x.larger(largest, k);
+        if (kept.border == NOTHING || __any(largest >= kept.border)) {
+          unsigned long long w[L::PER];
+          worths(k, kept.border, w);
+#pragma unroll
+          for (int e = 0; e < L::PER; ++e) sum += w[e];
+          if (kept.equal)
+#pragma unroll
+            for (int e = 0; e < L::PER; ++e) ties += L::logit(k, e) == kept.border;
+        }
+      }
+      if (++in_run == per || v + 1 == x.words) {
+        if constexpr (KEYED) {
+          ties = (uint32_t)(sum >> TIE);
+          sum &= (1ull << TIE) - 1;
+        }
+        sum = wave_sum(sum);
+        sum_of_run = lane == run ? sum : sum_of_run;
+        if (kept.equal) {
+          ties = wave_sum(ties);
+          ties_of_run = lane == run ? ties : ties_of_run;
+        }
+        ++run;
+        sum = 0;
+        ties = in_run = 0;
+      }
+    });
+    choose(kept, per, sum_of_run, ties_of_run);
   };
 
   // The border moves up to the lowest logit above which less than `limit` lies, by counts or by sums of weights; among those with keys lowest .. highest, above which `above` lies.
@@ -533,7 +658,7 @@ __global__ __launch_bounds__(THREADS) void ftsample_row(const Args a) {
   // after bins of keys highest - k >> drop are filled
   auto narrow = [&](uint32_t& lowest, uint32_t& highest, int drop, unsigned long long& above, unsigned long long limit) {
     __syncthreads();
-    find_bin<BINS / THREADS>(s, above, limit, [&](int i) { return s.bins[i]; });
+    find_bin<BINS / THREADS>(s, above, [&](unsigned long long) { return limit; }, [&](int i) { return s.bins[i]; });
     above = s.above;
     const uint32_t top = highest - (s.bin << drop), least = top - ((1u << drop) - 1);
     lowest = least > lowest && least <= top ? least : lowest;
@@ -569,6 +694,23 @@ __global__ __launch_bounds__(THREADS) void ftsample_row(const Args a) {
     kept.equal = (int)(fit > 0x7FFFFFFFull ? 0x7FFFFFFFull : fit);
   };
   const uint32_t least_key = L::key(NOTHING) + 1;
+  // The i-th largest of `count` in the list, for thread i.
+  auto sorted_list = [&](int count) {
+    unsigned long long e = tid < count ? list[tid] : 0;
+    sort_wave(e, tid);
+    for (int k = 128; k < 2 * count && k <= LIST; k <<= 1) {
+      for (int j = k >> 1; j >= 64; j >>= 1) {
+        __syncthreads();
+        list[tid] = e;
+        __syncthreads();
+        const unsigned long long other = list[tid ^ j];
+        const bool larger = ((tid & j) == 0) == ((tid & k) == 0);
+        e = larger == (other > e) ? other : e;
+      }
+      merge<32>(e, tid, k);
+    }
+    return e;
+  };
   // The same for all that is kept, the bin of the weights' logarithm first; limit: from the sum of all.
   auto by_bins = [&](bool by_weight, auto limit_from) {
     constexpr int N = sizeof(s.bins) / sizeof(s.bins[0]);
@@ -598,10 +740,8 @@ __global__ __launch_bounds__(THREADS) void ftsample_row(const Args a) {
     // (what is in the last bin is not counted there: thousands of logits may lie so far below, and would be added up one after the other)
     if (tid == 0 && kept.equal) s.bins[weights.bin(kept.border)] += (by_weight ? weight(kept.border) : 1ull) * (unsigned)kept.equal;
     __syncthreads();
-    unsigned long long all, mine = 0;
-    for (int i = 0; i < N / THREADS; ++i) mine += s.bins[tid * (N / THREADS) + i];
-    before_me<unsigned long long>(mine, s.sums, all);
-    const unsigned long long limit = limit_from(all);
+    unsigned long long limit = 0;
+    const unsigned long long all = find_bin<N / THREADS>(s, 0, [&](unsigned long long all) { return limit = limit_from(all); }, [&](int i) { return s.bins[i]; });
     int bin = LAST_BIN;
     unsigned long long above = all;
     if (all < limit && !by_weight) {
@@ -609,7 +749,6 @@ __global__ __launch_bounds__(THREADS) void ftsample_row(const Args a) {
       before_me<uint32_t>(beyond, s.words, beyond_all);
       if (beyond_all == 0) return;      // fewer than that can be chosen: all of them are kept
     } else {
-      find_bin<N / THREADS>(s, 0, limit, [&](int i) { return s.bins[i]; });
       bin = (int)s.bin;
       above = s.above;
     }
@@ -628,7 +767,104 @@ __global__ __launch_bounds__(THREADS) void ftsample_row(const Args a) {
       return from;
     };
     const uint32_t lowest = bin == LAST_BIN ? least_key : first_key(bin), highest = bin == 0 ? top_key : first_key(bin - 1) - 1;
+    // Few logits of 32 bits lie there, as a rule: they are sorted.  (Of 16 bits many are equal.)
+    const float from = L::of_key(lowest), to = L::of_key(highest);
+    if (L::WIDE && !(kept.equal && kept.border >= from && kept.border <= to)) {
+      if (tid == 0) s.count = 0;
+      __syncthreads();
+      x.each([&](float y) __attribute__((always_inline)) {
+        if (y >= from && y <= to && y > kept.border) {
+          const uint32_t at = atomicAdd(&s.count, 1u);
+          if (at < LIST) list[at] = (unsigned long long)L::key(y) << 32;
+        }
+      });
+      __syncthreads();
+      const int count = (int)s.count;
+      if (count > 0 && count <= LIST) {
+        const uint32_t key = (uint32_t)(sorted_list(count) >> 32);
+        const unsigned long long each = tid >= count ? 0 : by_weight ? weight(L::of_key(key)) : 1;
+        unsigned long long all_here;
+        const unsigned long long at = above + before_me<unsigned long long>(each, s.sums, all_here);
+        if (at < limit && at + each >= limit) {
+          s.bin = (uint32_t)tid;
+          s.words[0] = key;
+        }
+        __syncthreads();
+        const uint32_t border = s.words[0], last = s.bin;
+        uint32_t equal;
+        before_me<uint32_t>(key == border && tid <= (int)last, s.words, equal);
+        kept.border = L::of_key(border);
+        kept.equal = (int)equal;
+        return;
+      }
+    }
     search(limit, by_weight, lowest, highest, above);
+  };
+
+  // The same for bf16: how many there are of each value tells the border of all limits.
+  constexpr int IN_ORDER = ((2 * MAGNITUDES + THREADS) / THREADS | 1) * THREADS;      // (of a thread an odd number: they lie in different banks)
+  bool counted = false;
+  uint32_t tiny_count = 0;
+  unsigned long long tiny_sum = 0;      // of this thread
+  auto by_values = [&](bool by_weight, auto limit_from) {
+    if constexpr (KEYED) {
+      const bool anew = kept.border > NOTHING && tiny(kept.border);
+      if (!counted) {
+        __syncthreads();
+        for (int i = tid; i < VALUES; i += THREADS) s.counts[i] = 0;
+        __syncthreads();
+      }
+      if (!counted || anew) {
+        tiny_count = 0;
+        tiny_sum = 0;
+        x.each_word([&](int, const uint4v& k) __attribute__((always_inline)) {
+          uint32_t pair[4];
+          bool at_ends;
+          const bool some = numbers_of(std::integral_constant<uint16_t, 4>{}, k, pair, at_ends), checked = __any(at_ends);
+          if (!counted)
+#pragma unroll
+            for (int e = 0; e < L::PER; ++e) {
+              const uint32_t at = e & 1 ? pair[e >> 1] >> 16 : pair[e >> 1] & 0xFFFFu;
+              if (!checked || at - 4 < 4 * (VALUES - 2)) atomicAdd(reinterpret_cast<uint32_t*>(reinterpret_cast<char*>(s.counts) + at), 1u);
+            }
+          if (__any(some))
+#pragma unroll
+            for (int e = 0; e < L::PER; ++e) {
+              const float y = L::logit(k, e);
+              if (tiny(y) && y > kept.border) {
+                ++tiny_count;
+                tiny_sum += weight(y);
+              }
+            }
+        });
+        __syncthreads();
+        counted = true;
+      }
+      // In falling order: positive ones, tiny ones, negative ones.
+      auto number_at = [&](int i) { return i < MAGNITUDES ? VALUES - 2 - i : VALUES - 1 - i; };
+      unsigned long long all_tiny = 0;
+      if (!(kept.border > 0.f && !tiny(kept.border))) before_me<unsigned long long>(by_weight ? tiny_sum : tiny_count, s.sums, all_tiny);
+      if (anew) all_tiny += (by_weight ? weight(kept.border) : 1ull) * (unsigned)kept.equal;
+      auto at = [&](int i) -> unsigned long long {
+        const int number = i > 2 * MAGNITUDES ? 0 : number_at(i);      // (number 0 has no weight, and is not counted)
+        const float y = value_of(number);
+        uint32_t n = s.counts[number];
+        if (base == 0 && number == MAGNITUDES + 1) n += s.counts[MAGNITUDES];      // (both zeros are one)
+        n = base == 0 && number == MAGNITUDES ? 0 : y > kept.border ? n : y == kept.border && n ? (uint32_t)kept.equal : 0;
+        const unsigned long long all_of_it = by_weight ? s.worth[number] * n : n;
+        return i == MAGNITUDES ? all_tiny : all_of_it;
+      };
+      if (by_weight) know_worth();
+      __syncthreads();
+      unsigned long long limit = 0;
+      const unsigned long long all = find_bin<IN_ORDER / THREADS>(s, 0, [&](unsigned long long all) { return limit = limit_from(all); }, at);
+      if (all < limit) return;      // fewer than that have a weight: all of them are kept
+      const int bin = (int)s.bin;
+      const uint32_t one = bin == MAGNITUDES ? 0 : L::key(value_of(number_at(bin))), far = (uint32_t)(base - 1) << 16;
+      search(limit, by_weight, bin == MAGNITUDES ? L::key(as_f(far | 0x80000000u)) : one, bin == MAGNITUDES ? L::key(as_f(far)) : one, s.above);
+    } else {
+      by_bins(by_weight, limit_from);
+    }
   };
 
   if (r.top_k < x.vocab) {
@@ -678,19 +914,7 @@ __global__ __launch_bounds__(THREADS) void ftsample_row(const Args a) {
           });
         __syncthreads();
         // sorted, the largest first: thread i has the i-th
-        unsigned long long e = tid < (int)count ? list[tid] : 0;
-        sort_wave(e, tid);
-        for (int k = 128; k < 2 * (int)count && k <= LIST; k <<= 1) {
-          for (int j = k >> 1; j >= 64; j >>= 1) {
-            __syncthreads();
-            list[tid] = e;
-            __syncthreads();
-            const unsigned long long other = list[tid ^ j];
-            const bool larger = ((tid & j) == 0) == ((tid & k) == 0);
-            e = larger == (other > e) ? other : e;
-          }
-          merge<32>(e, tid, k);
-        }
+        const unsigned long long e = sorted_list((int)count);
         unsigned long long w = tid < (int)count && tid < r.top_k ? weight(L::of_key((uint32_t)(e >> 32))) : 0, all;
         unsigned long long before = before_me<unsigned long long>(w, s.sums, all);
         if (r.cut_p && before >= limit_of(all) && tid > 0) w = 0;
@@ -708,16 +932,16 @@ __global__ __launch_bounds__(THREADS) void ftsample_row(const Args a) {
         return;
       }
     }
-    by_bins(false, [&](unsigned long long) { return (unsigned long long)r.top_k; });
+    by_values(false, [&](unsigned long long) { return (unsigned long long)r.top_k; });
     // (where fewer than top_k can be chosen, fewer are equal than there is room for)
-    if (r.cut_p) {
+    if (!KEYED && r.cut_p) {
       uint32_t there = 0, ties;
       x.each([&](float y) __attribute__((always_inline)) { there += y == kept.border; });
       before_me<uint32_t>(there, s.words, ties);
       if ((uint32_t)kept.equal > ties) kept.equal = (int)ties;
     }
   }
-  if (r.cut_p) by_bins(true, limit_of);
+  if (r.cut_p) by_values(true, limit_of);
   sum_up(kept);
 }
 

@@ -113,6 +113,35 @@ def test_equal_logits(dtype, vocab):
     check(x, u, top_k=k, top_p=p, min_p=torch.full((12,), 0.3))
 
 
+@pytest.mark.parametrize("use", ["", "p", "k", "kp", "pm", "kpm"])
+@pytest.mark.parametrize("dtype", [ftsample.BF16, ftsample.F16, ftsample.F32])
+def test_logits_of_all_magnitudes(dtype, use):
+    """Near zero, zero among others, all of one sign, so small that only a small temperature tells them apart, so large that few have a weight."""
+    g = torch.Generator().manual_seed(41 + len(use))
+    rows, vocab = 10, 9001
+    x = torch.randn((rows, vocab), generator=g) * 3
+    x[0] *= 1e-7
+    x[1, torch.rand(vocab, generator=g) < 0.4] = 0.0
+    x[1, torch.rand(vocab, generator=g) < 0.4] = -0.0
+    x[2] = x[2].abs() * 1e-3
+    x[3] = -x[3].abs() * torch.exp(-20 * torch.rand(vocab, generator=g))
+    x[4] = torch.where(torch.rand(vocab, generator=g) < 0.5, x[4], x[4] * 1e-6)
+    x[5] *= 1e-34 if dtype != ftsample.F16 else 1e-6
+    x[6] *= 2000
+    x[7] = torch.where(torch.rand(vocab, generator=g) < 0.5, -x[7].abs() * 1e-8, -60000.0)
+    x[8] = -1000 - x[8].abs()
+    x[9, torch.rand(vocab, generator=g) < 0.3] = -np.inf
+    t = torch.ones(rows)
+    t[5] = 1e-34 if dtype != ftsample.F16 else 1e-6
+    t[6] = 300.0
+    k = torch.tensor([700, 5000, 6000, 8000, 4500, 3000, 2000, 4000, 900, 6290], dtype=torch.int32)
+    p = torch.tensor([0.9, 0.6, 0.3, 0.99, 0.51, 0.8, 0.95, 0.7, 0.5, 0.9])
+    m = torch.tensor([0.999999, 0.05, 0.999, 0.9, 0.02, 0.1, 0.01, 0.99, 0.1, 0.0])
+    named = dict(k=("top_k", k), p=("top_p", p), m=("min_p", m))
+    for _ in range(2):
+        check(x.to(TYPES[dtype]), torch.rand(rows, generator=g), temperature=t, **{named[c][0]: named[c][1] for c in use})
+
+
 def test_signed_zeros_are_equal():
     x = torch.zeros((2, 500))
     x[:, ::2] = -0.0
