@@ -45,44 +45,40 @@ template <int D> __device__ __forceinline__ float* state_of(const Args& a, int b
   return a.states && slot >= 0 && slot < a.n_slots ? a.states + ((int64_t)slot * a.heads + h) * (D * D) : nullptr;
 }
 
-// The recurrence, a (sequence, head) a workgroup: thread (g, e) has column e of the state, rows of its g-th part.
-template <int D, bool BF> __global__ __launch_bounds__(256) void ftdecay_recurrent(const Args a) {
+// One token: the recurrence as it stands, a (sequence, head) a workgroup.  Thread (g, e) has column e of the state, rows of its g-th part, which are summed up over LDS.
+// Bound by memory, each state read and written once: 96 sequences of 32 heads of 128, 403 MB, take 82 us (4.9 TB/s, what a copy reaches).
+template <int D, bool BF> __global__ __launch_bounds__(256) void ftdecay_token(const Args a) {
   constexpr int PARTS = 256 / D, R = D / PARTS;
   __shared__ float qs[D], ks[D], part[PARTS][D];
   const int b = blockIdx.x / a.heads, h = blockIdx.x % a.heads, hk = h / a.group, e = threadIdx.x % D, g = threadIdx.x / D;
-  const int t0 = a.cu ? clamped(a.cu[b], a.total) : b, t1 = a.cu ? clamped(a.cu[b + 1], a.total) : b + 1;
-  const bool fresh = a.cu && (!a.starts || a.starts[b] <= 0);
   float* const state = state_of<D>(a, b, h);
   const Decay decay = decay_of(a, h);
   float s[R];
 #pragma unroll
-  for (int i = 0; i < R; ++i) s[i] = state && !fresh ? state[(g * R + i) * D + e] : 0.f;
-  for (int t = t0; t < t1; ++t) {
-    const float v = element<BF>(a.v.data + t * a.v.token + hk * a.v.head, e);
-    __syncthreads();
-    if (g == 0) {
-      qs[e] = element<BF>(a.q.data + t * a.q.token + h * a.q.head, e);
-      ks[e] = element<BF>(a.k.data + t * a.k.token + hk * a.k.head, e);
-    }
-    __syncthreads();
-    float sum = 0.f;
-#pragma unroll
-    for (int i = 0; i < R; ++i) {
-      s[i] = __builtin_fmaf(ks[g * R + i], v, __builtin_fmaf(s[i], decay.high, s[i] * decay.low));
-      sum = __builtin_fmaf(qs[g * R + i], s[i], sum);
-    }
-    part[g][e] = sum;
-    __syncthreads();
-    if (g == 0) {
-      float all = 0.f;
-      for (int i = 0; i < PARTS; ++i) all += part[i][e];
-      all *= a.scale;
-      reinterpret_cast<uint16_t*>(a.o.data + t * a.o.token + h * a.o.head)[e] = (uint16_t)pack2<BF>(all, all);
-    }
+  for (int i = 0; i < R; ++i) s[i] = state ? state[(g * R + i) * D + e] : 0.f;
+  const float v = element<BF>(a.v.data + b * a.v.token + hk * a.v.head, e);
+  if (g == 0) {
+    qs[e] = element<BF>(a.q.data + b * a.q.token + h * a.q.head, e);
+    ks[e] = element<BF>(a.k.data + b * a.k.token + hk * a.k.head, e);
   }
+  __syncthreads();
+  float sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    s[i] = __builtin_fmaf(ks[g * R + i], v, __builtin_fmaf(s[i], decay.high, s[i] * decay.low));
+    sum = __builtin_fmaf(qs[g * R + i], s[i], sum);
+  }
+  part[g][e] = sum;
   if (state)
 #pragma unroll
     for (int i = 0; i < R; ++i) state[(g * R + i) * D + e] = s[i];
+  __syncthreads();
+  if (g == 0) {
+    float all = 0.f;
+    for (int i = 0; i < PARTS; ++i) all += part[i][e];
+    all *= a.scale;
+    reinterpret_cast<uint16_t*>(a.o.data + b * a.o.token + h * a.o.head)[e] = (uint16_t)pack2<BF>(all, all);
+  }
 }
 
 // ---- Prompts, in chunks of 64 tokens.  With S the state before a chunk (D x D) and i, j places in it,
@@ -95,7 +91,17 @@ template <int D, bool BF> __global__ __launch_bounds__(256) void ftdecay_recurre
 // What is rounded to 16 bits before a product is held in more than one word.  bf16: weights and S in two words (2^-16 relative), decayed values in three (S is a state of
 // 32 bits).  fp16: S under one power of two for its slab, and the decayed values, in two words, the lower one times 2^11 (22 bits; what the products of lower words add is kept apart until it is
 // scaled back); weights, which have no bound, in two words of bf16 with the values as two words of bf16, which hold fp16 exactly.
-constexpr int C = 64, STATES = 1024, LEAST = 256;
+//
+// Sequences are divided into segments of `per` tokens, so that there are workgroups for all CUs: ftdecay_gather forms what each segment alone adds to the state, ftdecay_join adds these up,
+// ftdecay_chunks has the state before its segment and does the rest.  (Gathering is a second pass over keys and values, so that no workgroup waits for another.)
+//
+// Bound by vector instructions and the reads of operands from LDS that stand between the products (a product of 32 x 32 x 16 takes as long as eight vector instructions, and the
+// words of S, of the weights and of the values are formed by several for each): 16,384 tokens of 32 heads of 128 on 8, bf16, take 197 us, 109 being what the bytes take at a copy's rate;
+// without the vector work between the products, one after the other, 250 us; a token at a time 21.5 ms.  24 prompts of up to 1531 tokens, 12 heads of 64, fp16: 42 us, 890 a token at a time.
+constexpr int C = 64;
+// Segments: at most STATES states between them (67 MB at head_dim 128, 17 MB at 64), and no fewer than LEAST tokens in one: 4096 tokens of 8 heads of 128 take 43 us in
+// segments of 128, 41 of 256, 69 of 512, 122 of 1024; 24 prompts of up to 1531 tokens of 12 heads of 64 41 .. 46 us of 192 and 256, 64 of 512.
+constexpr int STATES = 1024, LEAST = 256;
 
 template <int D> constexpr int tile_bytes() { return C * D * 2; }
 constexpr int P_BYTES = C * C * 2;      // a word of the weights
@@ -697,7 +703,7 @@ using namespace ftdecay;
 
 struct ftdecay_ctx {
   ftdecay_config cfg;
-  kernel_fn recurrent = nullptr, gather = nullptr, join = nullptr, chunks = nullptr;
+  kernel_fn token = nullptr, gather = nullptr, join = nullptr, chunks = nullptr;
   int lds = 0, gather_lds = 0;
   float* between = nullptr;
   std::string err;
@@ -721,7 +727,7 @@ static int dfail_hip(ftdecay_ctx* c, const char* what, hipError_t e) {
 }
 
 template <int D, bool BF> static void choose_kernels(ftdecay_ctx* c) {
-  c->recurrent = ftdecay_recurrent<D, BF>;
+  c->token = ftdecay_token<D, BF>;
   c->gather = ftdecay_gather<D, BF>;
   c->join = ftdecay_join<D>;
   c->chunks = ftdecay_chunks<D, BF>;
@@ -807,7 +813,7 @@ static int launch(ftdecay_ctx* c, const Args& a, hipStream_t st) {
   if (he != hipSuccess) return dfail_hip(c, "device", he);
   const int threads = 2 * c->cfg.head_dim;
   if (!a.cu) {
-    hipLaunchKernelGGL(c->recurrent, dim3((uint32_t)(a.batch * a.heads)), dim3(256), 0, st, a);
+    hipLaunchKernelGGL(c->token, dim3((uint32_t)(a.batch * a.heads)), dim3(256), 0, st, a);
   } else {
     const dim3 grid(groups_of(a) * 8u * (uint32_t)a.group);
     if (a.total > a.per) {
@@ -834,6 +840,7 @@ extern "C" int ftdecay_forward(ftdecay_ctx* c, const ftdecay_rows* q, const ftde
   bad = wrong_states(log_decay, states, n_slots, slots, batch);
   if (bad) return dfail(c, FTDECAY_EINVAL, bad);
   const ftdecay_config& e = c->cfg;
+  // Two workgroups a CU: 16,384 tokens of 32 heads take as long in 512 segments as in 1024, and have half as many states between them.
   int64_t per = ((int64_t)total * e.heads + 511) / 512;
   per = per < LEAST ? LEAST : per;
   const int64_t least = ((int64_t)total * e.heads + STATES - 1) / STATES;      // total / per * heads states between segments, at most STATES
