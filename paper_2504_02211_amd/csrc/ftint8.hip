@@ -197,7 +197,7 @@ template <class T> __device__ __forceinline__ void tile_of(const ProductArgs& a,
 // side by side per block of features.  The steps of 128 columns go through a ring of LDS stages that direct loads fill; a row's 16-byte chunk c lies at place c ^ (row / 2 % 8), which keeps
 // the reads of operands free of bank conflicts.  Operands are read ahead of their products, also across the border of two stages: the barrier of a stage sits AHEAD rows of
 // products before its end, where its last operands are in registers, so that no wave waits for LDS behind it.
-// Bound by the matrix pipe: 16,384 tokens on 16,384 x 4096 (features x columns) 907 us, 2425 TOPS; the library's plain product of the codes, without scales, 974 us.
+// Bound by power (the clock falls to some 1.8 GHz, the matrix pipe is 60 % busy): 16,384 tokens on 16,384 x 4096 (features x columns) 907 us, 2425 TOPS; the library's plain product of the codes, without scales, 974 us.
 template <class T, int DT> __global__ __launch_bounds__(T::NW * 64, T::PER_CU * T::NW / 4) void ftint8_tile(const ProductArgs a) {
   constexpr int WT = T::WT, WF = T::WF, NST = T::NST, BK = T::BK, STAGE = T::STAGE, NLOAD = T::NLOAD, NKS = 2, AHEAD = 3;
   extern __shared__ __attribute__((aligned(1024))) char smem[];
