@@ -139,7 +139,8 @@ def test_longest_sums_of_the_largest_codes(m):
     same(y, product(cx, sx, cw, sw, ftint8.F32))
 
 
-@pytest.mark.parametrize("m,n,k,x_pad,y_pad,offset", [(5, 33, 100, 3, 5, 1), (70, 130, 129, 7, 0, 0), (3, 64, 64, 8, 8, 8), (300, 257, 64, 0, 9, 3), (130, 256, 256, 8, 8, 0), (1, 100, 90, 0, 0, 5)])
+@pytest.mark.parametrize("m,n,k,x_pad,y_pad,offset", [(5, 33, 100, 3, 5, 1), (70, 130, 129, 7, 0, 0), (3, 64, 64, 8, 8, 8), (300, 257, 64, 0, 9, 3), (130, 256, 256, 8, 8, 0), (1, 100, 90, 0, 0, 5), (1, 100, 90, 0, 3, 8), (1, 50, 5000, 8, 1, 0),
+                                                          (20, 100, 300, 8, 1, 0), (40, 130, 2100, 4, 3, 1)])
 def test_views_of_larger_tensors(m, n, k, x_pad, y_pad, offset):
     """Rows apart and beginning anywhere; what lies between the rows of the result stays as it was."""
     x, cw, sw = inputs(m, n, k, ftint8.BF16, 3)

@@ -194,7 +194,7 @@ def test_numbers_of_rows(rows):
     check(rows_of(rows, 9001, ftsample.BF16, g), torch.rand(rows, generator=g), temperature=0.1 + torch.rand(rows, generator=g))
 
 
-@pytest.mark.parametrize("dtype", [ftsample.F16, ftsample.F32])
+@pytest.mark.parametrize("dtype", [ftsample.F16, ftsample.BF16, ftsample.F32])
 @pytest.mark.parametrize("offset,pad", [(1, 0), (3, 5), (0, 8), (7, 1)])
 def test_rows_that_begin_anywhere(dtype, offset, pad):
     """Behind and between the rows lie larger logits, which nothing may choose."""
@@ -206,6 +206,22 @@ def test_rows_that_begin_anywhere(dtype, offset, pad):
     check(x, torch.rand(5, generator=g), view=view, **rules(5, g))
     check(x, torch.rand(5, generator=g), view=view)
     check(x[:1].expand(5, -1), torch.rand(5, generator=g), view=view[:1].expand(5, -1))          # one row for several random numbers
+
+
+@pytest.mark.parametrize("dtype", [ftsample.F16, ftsample.BF16, ftsample.F32])
+@pytest.mark.parametrize("vocab,offset", [(65536, 0), (65537, 1), (131072, 0), (131072, 1), (200003, 5)])
+def test_large_vocabularies(dtype, vocab, offset):
+    """Rows that just fit in registers, and that do not; masked by a tenth."""
+    g = torch.Generator().manual_seed(vocab + offset)
+    x = rows_of(5, vocab, dtype, g, 0.1)
+    flat = torch.full((5 * vocab + offset,), 50.0, dtype=TYPES[dtype], device="cuda")
+    view = flat[offset:].view(5, vocab)
+    view.copy_(x)
+    t, u = torch.tensor([1.0, 0.3, 2.0, 0.7, 1.5]), torch.rand(5, generator=g)
+    k, p = torch.tensor([0, 5000, 20000, 257, 40], dtype=torch.int32), torch.tensor([0.9, 0.6, 0.97, 0.8, 0.5])
+    check(x, u, t, view=view)
+    check(x, u, t, top_p=p, view=view)
+    check(x, u, t, k, p, torch.tensor([0.0, 0.01, 0.0, 0.001, 0.0]), view=view)
 
 
 def test_frequencies():
