@@ -36,7 +36,8 @@
  *   - One context serves one shape; calls on one context must not overlap in time.
  *
  * Attention over packed prompts with grouped heads and the paged key / value cache of the same library, which carry no checksums,
- * are declared in ftprompt.h and ftcache.h, which lie with the Python package: paper_2504_02211_amd/include.
+ * are declared in ftprompt.h and ftcache.h, layers on 8-bit integers, linear attention and the choice of tokens in ftint8.h, ftdecay.h and
+ * ftsample.h; all of these lie with the Python package: paper_2504_02211_amd/include.
  */
 #ifndef FTATTN_H
 #define FTATTN_H

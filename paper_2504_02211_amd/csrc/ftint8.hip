@@ -135,7 +135,6 @@ struct ProductArgs {
   char* y;
   int64_t y_stride;      // bytes
   int32_t m, n, k_padded;
-  int32_t wide;          // rows of y begin at multiples of 16 bytes
   int32_t parts;         // > 1: the columns are divided among as many workgroups a tile (blockIdx.y), whose sums go to `sums`
   int4v* sums;           // [part][tile][wave][block of features][block of tokens][lane]
 };
@@ -162,6 +161,12 @@ __device__ __forceinline__ void load_lds16(const void* base, uint32_t off, uint3
 template <class F, int... I> __device__ __forceinline__ void for_each_of(F&& f, std::integer_sequence<int, I...>) { (f(std::integral_constant<int, I>{}), ...); }
 template <int N, class F> __device__ __forceinline__ void for_each(F&& f) { for_each_of(f, std::make_integer_sequence<int, N>{}); }
 
+// A wide store to an address that is aligned to an element only.  (The device's vector stores take any.  Rows of 4001 results, stored an element at a time, took 4000 tokens on
+// 4001 x 4096 from 51 us to 65.)
+template <int ES, class V> __device__ __forceinline__ void put_anywhere(char* to, V v) {
+  struct __attribute__((packed, aligned(ES))) Loose { V v; };
+  reinterpret_cast<Loose*>(to)->v = v;
+}
 // A result: the sum rounded to 32 bits, times the product of the scales.
 __device__ __forceinline__ float scaled(int sum, float sx, float sw) {
   float y = (float)sum * (sx * sw);
@@ -343,29 +348,19 @@ template <class T, int DT> __global__ __launch_bounds__(T::NW * 64, T::PER_CU * 
       else *reinterpret_cast<uint2v*>(at) = uint2v{pack2<DT == FTINT8_BF16>(y[0], y[1]), pack2<DT == FTINT8_BF16>(y[2], y[3])};
     }
     const int r0 = mt0 + 16 * t;
-    if (a.wide) {
-      const int col = nf0 + lane % LPR * PER;
+    const int col = nf0 + lane % LPR * PER;
 #pragma unroll
-      for (int i = 0; i < 16 / RPI; ++i) {
-        const int r = i * RPI + lane / LPR;
-        const uint4v v = *reinterpret_cast<const uint4v*>(out + (r & 15) * T::PITCH + lane % LPR * 16);
-        if (lane / LPR >= RPI || r0 + r >= a.m || col >= a.n) continue;
-        char* const to = a.y + (int64_t)(r0 + r) * a.y_stride + col * ES;
-        if (col + PER <= a.n) *reinterpret_cast<uint4v*>(to) = v;
-        else
-          for (int e = 0; e < a.n - col; ++e) {
-            if constexpr (ES == 4) reinterpret_cast<uint32_t*>(to)[e] = v[e];
-            else reinterpret_cast<uint16_t*>(to)[e] = (uint16_t)(v[e >> 1] >> 16 * (e & 1));
-          }
-      }
-    } else {
-      for (int e = lane; e < 16 * 16 * WF; e += 64) {
-        const int r = e / (16 * WF), c = e % (16 * WF);
-        if (r0 + r >= a.m || nf0 + c >= a.n) continue;
-        char* const to = a.y + (int64_t)(r0 + r) * a.y_stride + (nf0 + c) * ES;
-        if constexpr (ES == 4) *reinterpret_cast<float*>(to) = *reinterpret_cast<const float*>(out + r * T::PITCH + c * ES);
-        else *reinterpret_cast<uint16_t*>(to) = *reinterpret_cast<const uint16_t*>(out + r * T::PITCH + c * ES);
-      }
+    for (int i = 0; i < 16 / RPI; ++i) {
+      const int r = i * RPI + lane / LPR;
+      const uint4v v = *reinterpret_cast<const uint4v*>(out + (r & 15) * T::PITCH + lane % LPR * 16);
+      if (lane / LPR >= RPI || r0 + r >= a.m || col >= a.n) continue;
+      char* const to = a.y + (int64_t)(r0 + r) * a.y_stride + col * ES;
+      if (col + PER <= a.n) put_anywhere<ES>(to, v);
+      else
+        for (int e = 0; e < a.n - col; ++e) {
+          if constexpr (ES == 4) reinterpret_cast<uint32_t*>(to)[e] = v[e];
+          else reinterpret_cast<uint16_t*>(to)[e] = (uint16_t)(v[e >> 1] >> 16 * (e & 1));
+        }
     }
     __builtin_amdgcn_sched_barrier(0);      // (one block's results at a time out of the accumulators)
   }
@@ -378,9 +373,9 @@ template <int DT> __device__ __forceinline__ void put_four(const ProductArgs& a,
   for (int r = 0; r < 4; ++r) y[r] = scaled(sum[r], sx, a.sw[col + r < a.n ? col + r : a.n - 1]);
   constexpr int ES = DT == FTINT8_F32 ? 4 : 2;
   char* const to = a.y + (int64_t)row * a.y_stride + (int64_t)col * ES;
-  if (a.wide && col + 4 <= a.n) {
-    if constexpr (ES == 4) *reinterpret_cast<float4v*>(to) = float4v{y[0], y[1], y[2], y[3]};
-    else *reinterpret_cast<uint2v*>(to) = uint2v{pack2<DT == FTINT8_BF16>(y[0], y[1]), pack2<DT == FTINT8_BF16>(y[2], y[3])};
+  if (col + 4 <= a.n) {
+    if constexpr (ES == 4) put_anywhere<ES>(to, float4v{y[0], y[1], y[2], y[3]});
+    else put_anywhere<ES>(to, uint2v{pack2<DT == FTINT8_BF16>(y[0], y[1]), pack2<DT == FTINT8_BF16>(y[2], y[3])});
   } else {
 #pragma unroll
     for (int r = 0; r < 4; ++r)
@@ -680,7 +675,7 @@ static hipError_t launch_encode(ftint8_ctx* c, const ftint8_matrix* x, int32_t r
 }
 static ProductArgs product_args(ftint8_ctx* c, const int8_t* x, const float* sx, int32_t m, const int8_t* w, const float* sw, const ftint8_matrix* y) {
   const int size = c->cfg.out_dtype == FTINT8_F32 ? 4 : 2;
-  return ProductArgs{x, w, sx, sw, static_cast<char*>(y->data), y->stride * size, m, c->cfg.n, c->k_padded, ((uintptr_t)y->data | (uintptr_t)(y->stride * size)) % 16 == 0, 1, nullptr};
+  return ProductArgs{x, w, sx, sw, static_cast<char*>(y->data), y->stride * size, m, c->cfg.n, c->k_padded, 1, nullptr};
 }
 // Tokens of which a launch cannot have all tiles (it has fewer than 2^32 threads).
 static bool too_many(const ftint8_ctx* c, int32_t m) {
