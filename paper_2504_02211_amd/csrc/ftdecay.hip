@@ -97,11 +97,11 @@ template <int D, bool BF> __global__ __launch_bounds__(256) void ftdecay_token(c
 //
 // Bound by vector instructions and the reads of operands from LDS that stand between the products (a product of 32 x 32 x 16 takes as long as eight vector instructions, and the
 // words of S, of the weights and of the values are formed by several for each): 16,384 tokens of 32 heads of 128 on 8, bf16, take 197 us, 109 being what the bytes take at a copy's rate;
-// without the vector work between the products, one after the other, 250 us; a token at a time 21.5 ms.  24 prompts of up to 1531 tokens, 12 heads of 64, fp16: 42 us, 890 a token at a time.
+// without the vector work between the products, one after the other, 250 us; a token at a time 21.5 ms.  24 prompts of up to 1531 tokens, 12 heads of 64, fp16: 39 us, 890 a token at a time.
 constexpr int C = 64;
-// Segments: at most STATES states between them (67 MB at head_dim 128, 17 MB at 64), and no fewer than LEAST tokens in one: 4096 tokens of 8 heads of 128 take 43 us in
-// segments of 128, 41 of 256, 69 of 512, 122 of 1024; 24 prompts of up to 1531 tokens of 12 heads of 64 41 .. 46 us of 192 and 256, 64 of 512.
-constexpr int STATES = 1024, LEAST = 256;
+// Segments: at most STATES states between them (67 MB at head_dim 128, 17 MB at 64), and no fewer than LEAST tokens in one: 24 prompts of up to 1531 tokens of 12 heads of 64
+// take 45 us in segments of 128, 39 of 192, 43 of 256, 64 of 512; 4096 tokens of 8 heads of 128 38, 37, 39 and 55 us.
+constexpr int STATES = 1024, LEAST = 192;
 
 template <int D> constexpr int tile_bytes() { return C * D * 2; }
 constexpr int P_BYTES = C * C * 2;      // a word of the weights
@@ -410,12 +410,20 @@ template <int D> __global__ __launch_bounds__(256) void ftdecay_join(const Args 
   const float* const first = a.starts && a.starts[b] > 0 ? state_of<D>(a, b, h) : nullptr;
   float4v x = first ? *reinterpret_cast<const float4v*>(first + e) : (float4v)0.f;
   const Decay whole = Powers(a, h).whole(a.per);
-  for (int s = 0; s + 1 < segments; ++s) {
-    float4v* const at = reinterpret_cast<float4v*>(a.between + ((int64_t)(t0 / a.per + s) * a.heads + h) * (D * D) + e);
-    const float4v y = *at;
+  float4v* const at = reinterpret_cast<float4v*>(a.between + ((int64_t)(t0 / a.per) * a.heads + h) * (D * D) + e);
+  const int64_t apart = (int64_t)a.heads * (D * D / 4);
+  for (int s = 0; s + 1 < segments; s += 8) {      // (eight loads under way at a time)
+    float4v y[8];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = __builtin_fmaf(x[i], whole.high, __builtin_fmaf(x[i], whole.low, y[i]));
-    *at = x;
+    for (int i = 0; i < 8; ++i)
+      if (s + i + 1 < segments) y[i] = at[(s + i) * apart];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (s + i + 1 < segments) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) x[c] = __builtin_fmaf(x[c], whole.high, __builtin_fmaf(x[c], whole.low, y[i][c]));
+        at[(s + i) * apart] = x;
+      }
   }
 }
 
@@ -840,7 +848,7 @@ extern "C" int ftdecay_forward(ftdecay_ctx* c, const ftdecay_rows* q, const ftde
   bad = wrong_states(log_decay, states, n_slots, slots, batch);
   if (bad) return dfail(c, FTDECAY_EINVAL, bad);
   const ftdecay_config& e = c->cfg;
-  // Two workgroups a CU: 16,384 tokens of 32 heads take as long in 512 segments as in 1024, and have half as many states between them.
+  // Two workgroups a CU: 16,384 tokens of 32 heads of 128 take 194 us in 512 segments, 209 in 1024, which have twice as many states between them.
   int64_t per = ((int64_t)total * e.heads + 511) / 512;
   per = per < LEAST ? LEAST : per;
   const int64_t least = ((int64_t)total * e.heads + STATES - 1) / STATES;      // total / per * heads states between segments, at most STATES
