@@ -112,7 +112,7 @@ def test_packed_prompts(lengths, heads, kv_heads, d, dtype):
 
 
 @pytest.mark.parametrize("dtype", [ftdecay.F16, ftdecay.BF16])
-@pytest.mark.parametrize("d,lengths,heads", [(64, [2100, 900], 2), (128, [1700], 1), (128, [1025, 0, 511, 513], 2)])
+@pytest.mark.parametrize("d,lengths,heads", [(64, [2100, 900], 2), (128, [1700], 1), (128, [1025, 0, 511, 513], 2), (64, [193, 385, 384, 191, 1537], 3)])
 def test_long_prompts(d, lengths, heads, dtype):
     c = Case(lengths, heads, heads, d, dtype, starts=[1] * len(lengths))
     _, states = c.check()
