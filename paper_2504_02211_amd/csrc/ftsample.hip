@@ -32,7 +32,7 @@ constexpr int BITS = 11, BINS = 1 << BITS;      // of a level of the search by k
 constexpr int STEPS = 512;                      // of a weight's logarithm to an octave, for each of which there is a factor in LDS
 constexpr int OCTAVES = 51;                     // what lies further below the largest weight is 0 in all units
 constexpr int TO_BIN = 2, LAST_BIN = STEPS * OCTAVES >> TO_BIN;      // bins of the logarithm: 128 an octave
-constexpr int LIST = THREADS, MOST_LISTED = THREADS / 2;   // tokens that are sorted; largest top_k that is
+constexpr int MOST_BOUNDED = 256;               // largest top_k whose border the threads' maxima bound
 constexpr int MOST_WORDS = 32;                  // 16-byte words of a lane in registers
 
 struct Args {
@@ -390,6 +390,7 @@ __global__ __launch_bounds__(THREADS) void ftsample_row(const Args a) {
   typedef Type<DT> L;
   constexpr bool KEYED = DT == FTSAMPLE_BF16;
   __shared__ Shared<KEYED> s;
+  constexpr int LIST = KEYED ? THREADS : 2 * THREADS;      // logits that are sorted
   __shared__ unsigned long long list[LIST];      // (under top_k) key and place, then weights by place
   __shared__ int listed[LIST];
   const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -694,22 +695,36 @@ __global__ __launch_bounds__(THREADS) void ftsample_row(const Args a) {
     kept.equal = (int)(fit > 0x7FFFFFFFull ? 0x7FFFFFFFull : fit);
   };
   const uint32_t least_key = L::key(NOTHING) + 1;
-  // The i-th largest of `count` in the list, for thread i.
-  auto sorted_list = [&](int count) {
-    unsigned long long e = tid < count ? list[tid] : 0;
-    sort_wave(e, tid);
-    for (int k = 128; k < 2 * count && k <= LIST; k <<= 1) {
-      for (int j = k >> 1; j >= 64; j >>= 1) {
-        __syncthreads();
-        list[tid] = e;
-        __syncthreads();
-        const unsigned long long other = list[tid ^ j];
-        const bool larger = ((tid & j) == 0) == ((tid & k) == 0);
-        e = larger == (other > e) ? other : e;
+  // The list's `count` entries in falling order: e[0] the tid-th, e[1] (`large`: there may be more than 512) the (tid + 512)-th.
+  auto sort_list = [&](auto large, int count, unsigned long long (&e)[2]) {
+    const bool two = decltype(large)::value && count > THREADS;
+    e[0] = tid < count ? list[tid] : 0;
+    e[1] = two && tid + THREADS < count ? list[tid + THREADS] : 0;
+    auto exchange = [&](int j, int k) {
+      __syncthreads();
+      list[tid] = e[0];
+      if (two) list[tid + THREADS] = e[1];
+      __syncthreads();
+      const bool first = (tid & j) == 0;
+      const unsigned long long other = list[tid ^ j];
+      e[0] = (first == ((tid & k) == 0)) == (other > e[0]) ? other : e[0];
+      if (two) {
+        const unsigned long long above = list[(tid ^ j) + THREADS];
+        e[1] = (first == ((tid + THREADS & k) == 0)) == (above > e[1]) ? above : e[1];
       }
-      merge<32>(e, tid, k);
+    };
+    sort_wave(e[0], tid);
+    if (two) sort_wave(e[1], tid + THREADS);
+    for (int k = 128; k < 2 * count && k <= LIST; k <<= 1) {
+      if (two && k == LIST) {
+        const unsigned long long larger = e[0] > e[1] ? e[0] : e[1];
+        e[1] = e[0] > e[1] ? e[1] : e[0];
+        e[0] = larger;
+      }
+      for (int j = two && k == LIST ? THREADS / 2 : k >> 1; j >= 64; j >>= 1) exchange(j, k);
+      merge<32>(e[0], tid, k);
+      if (two) merge<32>(e[1], tid + THREADS, k);
     }
-    return e;
   };
   // The same for all that is kept, the bin of the weights' logarithm first; limit: from the sum of all.
   auto by_bins = [&](bool by_weight, auto limit_from) {
@@ -775,13 +790,15 @@ __global__ __launch_bounds__(THREADS) void ftsample_row(const Args a) {
       x.each([&](float y) __attribute__((always_inline)) {
         if (y >= from && y <= to && y > kept.border) {
           const uint32_t at = atomicAdd(&s.count, 1u);
-          if (at < LIST) list[at] = (unsigned long long)L::key(y) << 32;
+          if (at < THREADS) list[at] = (unsigned long long)L::key(y) << 32;
         }
       });
       __syncthreads();
       const int count = (int)s.count;
-      if (count > 0 && count <= LIST) {
-        const uint32_t key = (uint32_t)(sorted_list(count) >> 32);
+      if (count > 0 && count <= THREADS) {
+        unsigned long long e[2];
+        sort_list(std::false_type{}, count, e);
+        const uint32_t key = (uint32_t)(e[0] >> 32);
         const unsigned long long each = tid >= count ? 0 : by_weight ? weight(L::of_key(key)) : 1;
         unsigned long long all_here;
         const unsigned long long at = above + before_me<unsigned long long>(each, s.sums, all_here);
@@ -867,8 +884,82 @@ __global__ __launch_bounds__(THREADS) void ftsample_row(const Args a) {
     }
   };
 
+  // With top_k all that is left may be few: logits from `from` on, top_k or more of them, are sorted.  False: they are too many.
+  auto by_list = [&](auto large, float from) {
+    constexpr int ROOM = decltype(large)::value ? 2 * THREADS : THREADS;
+    uint32_t n = 0;
+    x.each([&](float y) __attribute__((always_inline)) { n += y >= from; });
+    __syncthreads();
+    const uint32_t in_wave = wave_sum(n);
+    if (lane == 0) s.words[wave] = in_wave;
+    __syncthreads();
+    uint32_t at = 0, count = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+      if (w < wave) at += s.words[w];
+      count += s.words[w];
+    }
+    if (count > ROOM) return false;
+    // the logits in the order of their tokens: (key, place) in the list, tokens by place
+    if (in_wave)
+      x.each_word([&](int v, const uint4v& k) {
+        uint32_t m = 0;
+#pragma unroll
+        for (int e = 0; e < L::PER; ++e) m += L::logit(k, e) >= from;
+        if (!__any(m != 0)) return;
+        const uint32_t upto = sum_upto(m);
+        uint32_t place = at + upto - m;
+#pragma unroll
+        for (int e = 0; e < L::PER; ++e) {
+          const float y = L::logit(k, e);
+          if (!(y >= from)) continue;
+          list[place] = (unsigned long long)L::key(y) << 32 | (0xFFFFFFFFu - place);
+          listed[place] = x.token(v, e);
+          ++place;
+        }
+        at += last_lane(upto);
+      });
+    __syncthreads();
+    unsigned long long e[2], w[2], before[2], all, more = 0;
+    sort_list(large, (int)count, e);
+    const bool two = decltype(large)::value && count > THREADS;
+    // Sums in the order of w; both halves' sums of up to before this thread's.
+    auto sum_all = [&]() {
+      before[0] = before_me<unsigned long long>(w[0], s.sums, all);
+      if (two) {
+        before[1] = all + before_me<unsigned long long>(w[1], s.sums, more);
+        all += more;
+      }
+    };
+#pragma unroll
+    for (int i = 0; i < 2; ++i) w[i] = tid + i * THREADS < (int)count && tid + i * THREADS < r.top_k ? weight(L::of_key((uint32_t)(e[i] >> 32))) : 0;
+    sum_all();
+    const unsigned long long limit = limit_of(all);
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      if (tid + i * THREADS > 0 && (L::of_key((uint32_t)(e[i] >> 32)) < least || (r.cut_p && w[i] && before[i] >= limit))) w[i] = 0;
+    __syncthreads();
+    list[tid] = 0;
+    if (two) list[tid + THREADS] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      if (w[i]) list[0xFFFFFFFFu - (uint32_t)e[i]] = w[i];
+    __syncthreads();
+    // and summed up in the order of their tokens
+    w[0] = list[tid];
+    w[1] = two ? list[tid + THREADS] : 0;
+    sum_all();
+    const unsigned long long goal = (unsigned long long)__builtin_floor(r.u * (double)all) + 1;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      if (w[i] && before[i] < goal && before[i] + w[i] >= goal) answer(listed[tid + i * THREADS], (double)w[i] / (double)all);
+    return true;
+  };
+
   if (r.top_k < x.vocab) {
-    if (r.top_k <= MOST_LISTED) {
+    float from = NOTHING;
+    if (r.top_k <= MOST_BOUNDED) {
       // A bound that at least top_k logits reach (or all that can be chosen): of every wave's 64 maxima the (top_k / 8)-th largest, of these the smallest.
       float sorted = mine;
       sort_wave(sorted, lane);
@@ -876,63 +967,18 @@ __global__ __launch_bounds__(THREADS) void ftsample_row(const Args a) {
       __syncthreads();
       if (lane == 0) s.words[wave] = as_u(mine_of_wave);
       __syncthreads();
-      float from = as_f(s.words[0]);
+      from = as_f(s.words[0]);
 #pragma unroll
       for (int w = 1; w < WAVES; ++w) from = __builtin_fminf(from, as_f(s.words[w]));
       from = __builtin_fmaxf(from, L::of_key(least_key));      // (where fewer can be chosen)
-      uint32_t n = 0;
-      x.each([&](float y) __attribute__((always_inline)) { n += y >= from; });
-      __syncthreads();
-      const uint32_t in_wave = wave_sum(n);
-      if (lane == 0) s.words[wave] = in_wave;
-      __syncthreads();
-      uint32_t at = 0, count = 0;
-#pragma unroll
-      for (int w = 0; w < WAVES; ++w) {
-        if (w < wave) at += s.words[w];
-        count += s.words[w];
-      }
-      if (count <= LIST) {
-        // the logits in the order of their tokens: (key, place) in the list, tokens by place
-        if (in_wave)
-          x.each_word([&](int v, const uint4v& k) {
-            uint32_t m = 0;
-#pragma unroll
-            for (int e = 0; e < L::PER; ++e) m += L::logit(k, e) >= from;
-            if (!__any(m != 0)) return;
-            const uint32_t upto = sum_upto(m);
-            uint32_t place = at + upto - m;
-#pragma unroll
-            for (int e = 0; e < L::PER; ++e) {
-              const float y = L::logit(k, e);
-              if (!(y >= from)) continue;
-              list[place] = (unsigned long long)L::key(y) << 32 | (0xFFFFFFFFu - place);
-              listed[place] = x.token(v, e);
-              ++place;
-            }
-            at += last_lane(upto);
-          });
-        __syncthreads();
-        // sorted, the largest first: thread i has the i-th
-        const unsigned long long e = sorted_list((int)count);
-        unsigned long long w = tid < (int)count && tid < r.top_k ? weight(L::of_key((uint32_t)(e >> 32))) : 0, all;
-        unsigned long long before = before_me<unsigned long long>(w, s.sums, all);
-        if (r.cut_p && before >= limit_of(all) && tid > 0) w = 0;
-        if (tid > 0 && L::of_key((uint32_t)(e >> 32)) < least) w = 0;
-        __syncthreads();
-        list[tid] = 0;
-        __syncthreads();
-        if (w) list[0xFFFFFFFFu - (uint32_t)e] = w;
-        __syncthreads();
-        // and summed up in the order of their tokens
-        w = list[tid];
-        before = before_me<unsigned long long>(w, s.sums, all);
-        const unsigned long long goal = (unsigned long long)__builtin_floor(r.u * (double)all) + 1;
-        if (before < goal && before + w >= goal) answer(listed[tid], (double)w / (double)all);
-        return;
-      }
     }
+    if (from > NOTHING && by_list(std::false_type{}, from)) return;
+    // With a larger top_k, or where too many reach the bound, the border itself comes first.
     by_values(false, [&](unsigned long long) { return (unsigned long long)r.top_k; });
+    // (sorted where they are few, not weighed a second time: 48 rows of 50,001 in fp32 with all rules 42 us, else 55; 512 of 65,536 in fp16 77, 98.  In bf16 values are
+    // counted already, and the sort takes 10 us more.)
+    if constexpr (!KEYED)
+      if (r.cut_p && r.top_k <= LIST && kept.border > NOTHING && by_list(std::true_type{}, kept.border)) return;
     // (where fewer than top_k can be chosen, fewer are equal than there is room for)
     if (!KEYED && r.cut_p) {
       uint32_t there = 0, ties;

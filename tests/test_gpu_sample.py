@@ -209,6 +209,21 @@ def test_rows_that_begin_anywhere(dtype, offset, pad):
 
 
 @pytest.mark.parametrize("dtype", [ftsample.F16, ftsample.BF16, ftsample.F32])
+@pytest.mark.parametrize("vocab", [1024, 1100, 40000])
+def test_top_k_of_some_hundreds(dtype, vocab):
+    """About the sizes up to which what top_k leaves is sorted; rows without and with many equal logits."""
+    g = torch.Generator().manual_seed(vocab + dtype)
+    k = torch.tensor([255, 256, 257, 511, 512, 513, 767, 1000, 1023, 1024, 1025, 900], dtype=torch.int32)
+    x = rows_of(12, vocab, dtype, g, 0.05)
+    x[3], x[7], x[9] = (x[i].float().mul(scale).round().div(scale).to(TYPES[dtype]) for i, scale in ((3, 20), (7, 4), (9, 50)))
+    u, p = torch.rand(12, generator=g), torch.tensor([0.999, 0.5, 0.9, 0.97, 0.3, 0.99, 0.7, 0.95, 0.9999, 0.8, 0.6, 0.0])
+    check(x, u, top_k=k)
+    check(x, u, top_k=k, top_p=p)
+    check(x, u, torch.full((12,), 3.0), k, p, torch.full((12,), 1e-3))
+    check(x, u, torch.full((12,), 3.0), k, p)
+
+
+@pytest.mark.parametrize("dtype", [ftsample.F16, ftsample.BF16, ftsample.F32])
 @pytest.mark.parametrize("vocab,offset", [(65536, 0), (65537, 1), (131072, 0), (131072, 1), (200003, 5)])
 def test_large_vocabularies(dtype, vocab, offset):
     """Rows that just fit in registers, and that do not; masked by a tenth."""
