@@ -551,9 +551,12 @@ typedef void (*finish_fn)(const ProductArgs, int);
 template <int DT> product_fn tile_kernel(int tile) {
   return tile == WIDE ? ftint8_tile<TileWide, DT> : tile == HALF ? ftint8_tile<TileHalf, DT> : tile == QUARTER ? ftint8_tile<TileQuarter, DT> : ftint8_tile<TileSmall, DT>;
 }
-// Shares of divided columns: at most MOST_SHARES of them at a time.
-constexpr int MOST_SHARES = 256;
-constexpr size_t SUMS_BYTES = (size_t)MOST_SHARES * TileSmall::BM * TileSmall::BF * 4;
+// Shares of divided columns (stages of TileSmall::BK): at most as many at a time, tiles times parts.
+constexpr int most_shares(int stages) { return stages < 64 ? 4 * stages : 256; }
+// Their room in a context: none where there are too few columns to divide, or tiles enough for any number of tokens.
+constexpr size_t sums_bytes(int n, int stages) {
+  return stages < 16 || 2 * ((n + TileSmall::BF - 1) / TileSmall::BF) > most_shares(stages) ? 0 : (size_t)most_shares(stages) * TileSmall::BM * TileSmall::BF * 4;
+}
 
 }  // namespace ftint8
 
@@ -609,13 +612,13 @@ extern "C" int ftint8_create(const ftint8_config* cfg, ftint8_ctx** out) {
   for (int i = 0; i < 2; ++i)
     c->few[i] = cfg->out_dtype == FTINT8_F32 ? few_of<FTINT8_F32>(i) : cfg->out_dtype == FTINT8_BF16 ? few_of<FTINT8_BF16>(i) : few_of<FTINT8_F16>(i);
   c->fused = cfg->out_dtype == FTINT8_F32 ? fused_of<FTINT8_F32>(bf, wide) : cfg->out_dtype == FTINT8_BF16 ? fused_of<FTINT8_BF16>(bf, wide) : fused_of<FTINT8_F16>(bf, wide);
-  const size_t bytes = (size_t)cfg->max_tokens * c->k_padded;
+  const size_t bytes = (size_t)cfg->max_tokens * c->k_padded, sums = sums_bytes(cfg->n, c->k_padded / TileSmall::BK);
   int before = 0;
   hipError_t he = hipGetDevice(&before);
   if (he == hipSuccess) he = hipSetDevice(cfg->device);
   if (he == hipSuccess) {
     for (int t = 0; t < N_TILES && he == hipSuccess; ++t) he = hipFuncSetAttribute((const void*)c->product[t], hipFuncAttributeMaxDynamicSharedMemorySize, TILES[t].lds);
-    if (he == hipSuccess) he = hipMalloc((void**)&c->codes, SUMS_BYTES + bytes + (size_t)cfg->max_tokens * sizeof(float));
+    if (he == hipSuccess) he = hipMalloc((void**)&c->codes, sums + bytes + (size_t)cfg->max_tokens * sizeof(float));
     (void)hipSetDevice(before);
   }
   if (he != hipSuccess) {
@@ -624,7 +627,7 @@ extern "C" int ftint8_create(const ftint8_config* cfg, ftint8_ctx** out) {
     return rc;
   }
   c->sums = reinterpret_cast<int4v*>(c->codes);
-  c->codes += SUMS_BYTES;
+  c->codes += sums;
   c->scales = reinterpret_cast<float*>(c->codes + bytes);
   *out = c;
   return FTINT8_OK;
@@ -703,7 +706,7 @@ static hipError_t launch_product(ftint8_ctx* c, const int8_t* x, const float* sx
   // once more.  96 tokens on 4096 x 16,384 (64 tiles) 24 us in four, 55 in one; 1000 on 500 x 10,000 15, 27; 64 on 4096 x 4096 (32 tiles, 32 stages) 10.7
   // in four, 13.9 in one; 256 tokens there (128 tiles) 15.0 in two, 12.5 in one.
   if (tile == SMALL) {
-    const int64_t shares = (stages < 64 ? 4 * stages : MOST_SHARES) / count;
+    const int64_t shares = most_shares((int)stages) / count;
     a.parts = (int)(shares < stages / 8 ? shares : stages / 8);
     if (a.parts < 2) a.parts = 1;
   }

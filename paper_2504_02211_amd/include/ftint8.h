@@ -37,12 +37,12 @@ typedef struct {
   int32_t n, k;          /* output and input features of the layer: any numbers from 1 on, k at most 130944 (sums of k products of codes stay below 2^31) */
   int32_t in_dtype;      /* FTINT8_F16 | FTINT8_BF16: type of x (and of weights that are encoded here) */
   int32_t out_dtype;     /* FTINT8_F32, or in_dtype */
-  int32_t max_tokens;    /* most tokens of a ftint8_forward: the context holds max_tokens * (k_padded + 4) bytes for their codes and scales, and 8 MB */
+  int32_t max_tokens;    /* most tokens of a ftint8_forward: the context holds max_tokens * (k_padded + 4) bytes for their codes and scales, and up to 8 MB */
   int32_t device;        /* HIP device ordinal */
 } ftint8_config;
 
 /* A matrix of rows: element e of row r is data[r * stride + e].  data aligned to its elements, stride in elements (any from the row's length on; rows that begin
- * at multiples of 16 bytes are read and written faster). */
+ * at multiples of 16 bytes are read faster). */
 typedef struct { void* data; int64_t stride; } ftint8_matrix;
 
 int ftint8_create(const ftint8_config* cfg, ftint8_ctx** out);

@@ -21,7 +21,7 @@ struct dim { uint32_t x, y, z; };
 static dim grid, block;
 int hipGetDevice(int* d) { *d = 0; return 0; }
 int hipSetDevice(int) { return 0; }
-int hipMalloc(void** p, size_t) { *p = std::aligned_alloc(256, 4096); return 0; }
+int hipMalloc(void** p, size_t n) { std::printf("memory %zu\n", n); *p = std::aligned_alloc(256, 4096); return 0; }
 int hipFree(void* p) { std::free(p); return 0; }
 int hipFuncSetAttribute(const void*, int, int) { return 0; }
 int hipGetLastError() { return 0; }
@@ -70,23 +70,52 @@ DOES_NOT = ["int8,16777216x8,product,32513", "int8,16777216x8,forward,32513", "i
             "decay,128,prompt,0,4194304", "decay,128,prompt,257,262144", "decay,128,prompt,2147483647,2147483647", "decay,128,step,4194304", "decay,64,step,1073741824"]
 
 
+# tokens x (features, columns): columns are divided among workgroups, whose shares lie in the context
+DIVIDED = ["int8,%dx%d,product,%d" % (n, k, m) for n in (1, 128, 500, 2000, 4096, 8192, 16384, 16385, 100000) for k in (100, 2000, 2048, 4096, 8191, 10000, 20000, 130944)
+           for m in (1, 17, 33, 64, 65, 200, 1000, 5000)]
+
+
 @pytest.fixture(scope="module")
 def calls(tmp_path_factory):
+    """What each call gave, its launches and the memory of its context."""
     folder = tmp_path_factory.mktemp("stand_in")
     (folder / "hip.cpp").write_text(STAND_IN)
     (folder / "calls.py").write_text(CALLS)
     subprocess.run(["g++", "-shared", "-fPIC", "-o", str(folder / "hip.so"), str(folder / "hip.cpp")], check=True)
     env = dict(os.environ, PYTHONPATH=ROOT, LD_PRELOAD=" ".join([str(folder / "hip.so"), os.environ.get("LD_PRELOAD", "")]).strip())
-    run = subprocess.run([sys.executable, str(folder / "calls.py"), *FITS, *DOES_NOT], env=env, cwd=ROOT, capture_output=True, text=True, timeout=300)
+    run = subprocess.run([sys.executable, str(folder / "calls.py"), *FITS, *DOES_NOT, *DIVIDED], env=env, cwd=ROOT, capture_output=True, text=True, timeout=300)
     assert run.returncode == 0, run.stderr[-2000:]
-    said, launches = {}, []
+    said, memory, launches, held = {}, {}, [], 0
     for line in run.stdout.splitlines():
         words = line.split()
         if words[:1] == ["launch"]:
             launches.append(tuple(int(x) for x in words[1:]))
+        elif words[:1] == ["memory"]:
+            held = int(words[1])
         elif len(words) == 3 and words[1] == "gives":
+            context = words[0].rsplit(",", 2 if words[0].startswith("int8") else 3)[0]
+            memory.setdefault(context, held)
             said[words[0]], launches = (int(words[2]), launches), []
+    said["memory"] = memory
     return said
+
+
+def test_shares_of_divided_columns_fit_into_the_context(calls):
+    divided = 0
+    for call in DIVIDED:
+        context = call.rsplit(",", 2)[0]
+        k = int(context.split("x")[1])
+        codes = (1 << 22) * ((k + 127) // 128 * 128 + 4)
+        code, launches = calls[call]
+        assert code == 0
+        x, y, _ = launches[0]
+        assert len(launches) == (2 if y > 1 else 1)
+        if y > 1:
+            divided += 1
+            assert x * y * 64 * 128 * 4 + codes <= calls["memory"][context], call
+            assert y <= (k + 127) // 128 // 8
+        assert calls["memory"][context] <= codes + (8 << 20)
+    assert 20 < divided < len(DIVIDED)
 
 
 @pytest.mark.parametrize("call", FITS)
