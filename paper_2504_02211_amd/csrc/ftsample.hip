@@ -656,9 +656,14 @@ __global__ __launch_bounds__(THREADS) void ftsample_row(const Args a) {
     for (int i = tid; i < BINS; i += THREADS) s.bins[i] = 0;
     __syncthreads();
   };
-  // after bins of keys highest - k >> drop are filled
-  auto narrow = [&](uint32_t& lowest, uint32_t& highest, int drop, unsigned long long& above, unsigned long long limit) {
+  // after bins of keys highest - k >> drop are filled; counted: with numbers of logits of one key each, which have a weight
+  auto narrow = [&](uint32_t& lowest, uint32_t& highest, int drop, bool counted, unsigned long long& above, unsigned long long limit) {
     __syncthreads();
+    if (counted) {
+      for (int i = tid; i < BINS; i += THREADS)
+        if (s.bins[i]) s.bins[i] *= weight(L::of_key(highest - i));
+      __syncthreads();
+    }
     find_bin<BINS / THREADS>(s, above, [&](unsigned long long) { return limit; }, [&](int i) { return s.bins[i]; });
     above = s.above;
     const uint32_t top = highest - (s.bin << drop), least = top - ((1u << drop) - 1);
@@ -674,17 +679,22 @@ __global__ __launch_bounds__(THREADS) void ftsample_row(const Args a) {
       const int drop = drop_of(highest - lowest);
       const float from = L::of_key(lowest), to = L::of_key(highest);
       empty_bins();
-      x.each_word([&](int, const uint4v& k) __attribute__((always_inline)) {
+      const bool counted = by_weight && drop == 0;
+      auto fill = [&](auto value) __attribute__((always_inline)) {
+        x.each_word([&](int, const uint4v& k) __attribute__((always_inline)) {
 #pragma unroll
-        for (int e = 0; e < L::PER; ++e) {
-          const float y = L::logit(k, e);
-          if (y >= from && y <= to && y > kept.border) atomicAdd(&s.bins[(highest - L::key(y)) >> drop], by_weight ? weight(y) : 1ull);
-        }
-      });
-      __syncthreads();
-      // (the kept ones of the border that there is)
-      if (tid == 0 && kept.equal && kept.border >= from && kept.border <= to) s.bins[(highest - L::key(kept.border)) >> drop] += (by_weight ? weight(kept.border) : 1ull) * (unsigned)kept.equal;
-      narrow(lowest, highest, drop, above, limit);
+          for (int e = 0; e < L::PER; ++e) {
+            const float y = L::logit(k, e);
+            if (y >= from && y <= to && y > kept.border) atomicAdd(&s.bins[(highest - L::key(y)) >> drop], value(y));
+          }
+        });
+        __syncthreads();
+        // (the kept ones of the border that there is)
+        if (tid == 0 && kept.equal && kept.border >= from && kept.border <= to) s.bins[(highest - L::key(kept.border)) >> drop] += value(kept.border) * (unsigned)kept.equal;
+      };
+      if (by_weight && !counted) fill(weight);
+      else fill([](float) { return 1ull; });
+      narrow(lowest, highest, drop, counted, above, limit);
     }
     // of the logits that are the border, as many as fit
     const float border = L::of_key(lowest);
