@@ -985,7 +985,7 @@ __global__ __launch_bounds__(THREADS) void ftsample_row(const Args a) {
     if (from > NOTHING && by_list(std::false_type{}, from)) return;
     // With a larger top_k, or where too many reach the bound, the border itself comes first.
     by_values(false, [&](unsigned long long) { return (unsigned long long)r.top_k; });
-    // (sorted where they are few, not weighed a second time: 48 rows of 50,001 in fp32 with all rules 42 us, else 55; 512 of 65,536 in fp16 77, 98.  In bf16 values are
+    // (sorted where they are few, not weighed a second time: 48 rows of 50,001 in fp32 with all rules 41 us, else 61; 512 of 65,536 in fp16 68 to 76, 86.  In bf16 values are
     // counted already, and the sort takes 10 us more.)
     if constexpr (!KEYED)
       if (r.cut_p && r.top_k <= LIST && kept.border > NOTHING && by_list(std::true_type{}, kept.border)) return;
