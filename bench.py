@@ -34,7 +34,7 @@ def kernel_sources_sha() -> str:
     h = hashlib.sha1()
     d = os.path.join(ROOT, "paper_2504_02211_amd", "csrc")
     for name in sorted(os.listdir(d)):
-        if name.startswith(("ftprompt", "ftcache", "ftserve")):      # the serving operators, which no workload of this program runs
+        if name.startswith(("ftprompt", "ftcache", "ftserve", "ftint8", "ftdecay", "ftsample")):      # the serving operators, which no workload of this program runs
             continue
         h.update(name.encode())
         h.update(open(os.path.join(d, name), "rb").read())

@@ -150,6 +150,7 @@ __device__ __forceinline__ void wait_lds() {
 __device__ __forceinline__ void barrier() {
   __builtin_amdgcn_sched_barrier(0);
   __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");      // (nor does anything behind it move before it)
   __builtin_amdgcn_sched_barrier(0);
 }
 // 16 bytes per lane from (uniform base + per-lane byte offset) straight into LDS at (uniform LDS address + 16 * lane).  (Opaque to the compiler, which would wait
