@@ -406,18 +406,19 @@ template <class T, int DT> __global__ __launch_bounds__(256) void ftint8_finish(
 
 // Few tokens: 16 features and all tokens (up to 16 TB) a workgroup, the columns divided among its eight waves, operands from memory straight into registers: every
 // byte of the weights is wanted by one wave alone.  Stages of 256 columns, two of them under way; a token on 4096 columns has all it needs under way at once, and all
-// workgroups of 16,384 features are on the chip together.  WORDS > 0 (one token of up to 4096 WORDS columns): it comes in 16 bits, every workgroup encodes it for
+// workgroups of 16,384 features are on the chip together.  WORDS > 0 (up to TOKENS tokens of up to 4096 WORDS columns): they come in 16 bits, every workgroup encodes them for
 // itself while its first weights are under way, and the second launch is saved.  Bound by memory: 67 MB of weights, one token on 16,384 features of 4096 columns,
-// take 13.9 us with the encoding (4.8 TB/s, what a copy reaches; 16.3 in two launches).  Two tokens encoded so would take 17.8 us, in two launches 16.6.
-constexpr int FEW_WAVES = 8, FUSED_K = 16384;
+// take 13.9 us with the encoding (4.8 TB/s, what a copy reaches; 16.3 in two launches).
+constexpr int FEW_WAVES = 8, FUSED_K = 16384, FUSED_TOKENS = 4;
 struct FewArgs {
   ProductArgs p;
-  const char* raw;         // the token in 16 bits, at a multiple of 16 bytes
+  const char* raw;         // tokens in 16 bits, at multiples of 16 bytes
+  int64_t raw_stride;      // bytes
   int32_t k;
 };
-template <int TB, int DT, int IN, int WORDS> __global__ __launch_bounds__(FEW_WAVES * 64, WORDS == 1 ? 8 : 2) void ftint8_few(const FewArgs b) {
+template <int TB, int DT, int IN, int TOKENS, int WORDS> __global__ __launch_bounds__(FEW_WAVES * 64, WORDS == 1 ? TOKENS == 1 ? 8 : 6 : 2) void ftint8_few(const FewArgs b) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
-  __shared__ uint32_t most_of[FEW_WAVES];
+  __shared__ uint32_t most_of[TOKENS][FEW_WAVES];
   constexpr bool FUSED = WORDS > 0;
   constexpr int U = 4;
   const ProductArgs& a = b.p;
@@ -427,19 +428,24 @@ template <int TB, int DT, int IN, int WORDS> __global__ __launch_bounds__(FEW_WA
   const int8_t* xp[TB];
 #pragma unroll
   for (int t = 0; t < TB; ++t) xp[t] = a.x + (int64_t)(16 * t + lq < a.m ? 16 * t + lq : a.m - 1) * a.k_padded + 16 * lg;
-  const uint32_t row_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem + 16u * lg;
+  const int pitch = a.k_padded + 64;      // (four rows' words lie in different banks)
+  const uint32_t row_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem + 16u * lg + (TOKENS > 1 ? (uint32_t)((lq < a.m ? lq : a.m - 1) * pitch) : 0u);
 
-  // the token first: what is asked for last is waited for last
-  uint4v raw[FUSED ? WORDS : 1];
+  // the tokens first: what is asked for last is waited for last
+  uint4v raw[TOKENS][FUSED ? WORDS : 1];
   if constexpr (FUSED) {
 #pragma unroll
-    for (int i = 0; i < WORDS; ++i) {
-      const int at = 8 * (tid + 512 * i);
-      raw[i] = (uint4v)0u;
-      if (at + 8 <= b.k) raw[i] = *reinterpret_cast<const uint4v*>(b.raw + 2 * at);
-      else if (at < b.k)
-        for (int e = 0; e < b.k - at; ++e) raw[i][e >> 1] |= (uint32_t)reinterpret_cast<const uint16_t*>(b.raw)[at + e] << 16 * (e & 1);
-    }
+    for (int t = 0; t < TOKENS; ++t)
+#pragma unroll
+      for (int i = 0; i < WORDS; ++i) {
+        const int at = 8 * (tid + 512 * i);
+        const char* const from = b.raw + t * b.raw_stride;
+        raw[t][i] = (uint4v)0u;
+        if (t > 0 && t >= a.m) continue;
+        if (at + 8 <= b.k) raw[t][i] = *reinterpret_cast<const uint4v*>(from + 2 * at);
+        else if (at < b.k)
+          for (int e = 0; e < b.k - at; ++e) raw[t][i][e >> 1] |= (uint32_t)reinterpret_cast<const uint16_t*>(from)[at + e] << 16 * (e & 1);
+      }
   }
   int4v acc[TB], wr[2][U], xr[2][FUSED ? 1 : TB][U];
 #pragma unroll
@@ -459,25 +465,33 @@ template <int TB, int DT, int IN, int WORDS> __global__ __launch_bounds__(FEW_WA
   if (stage + FEW_WAVES < stages) fetch(1, stage + FEW_WAVES);
   float sx = 0.f;
   if constexpr (FUSED) {
-    uint32_t most = 0;
 #pragma unroll
-    for (int i = 0; i < WORDS; ++i)
+    for (int t = 0; t < TOKENS; ++t) {
+      uint32_t most = 0;
 #pragma unroll
-      for (int w = 0; w < 4; ++w)
-        most = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(ushort2v, most), __builtin_bit_cast(ushort2v, raw[i][w] & 0x7FFF7FFFu)));
-    most = (most & 0xFFFFu) > most >> 16 ? most & 0xFFFFu : most >> 16;
-    most = largest_of_wave(most);
-    if (lane == 0) most_of[wave] = most;
+      for (int i = 0; i < WORDS; ++i)
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+          most = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(ushort2v, most), __builtin_bit_cast(ushort2v, raw[t][i][w] & 0x7FFF7FFFu)));
+      most = (most & 0xFFFFu) > most >> 16 ? most & 0xFFFFu : most >> 16;
+      most = largest_of_wave(most);
+      if (lane == 0) most_of[t][wave] = most;
+    }
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < FEW_WAVES; ++w) most = most_of[w] > most ? most_of[w] : most;
-    most = as_u(low_of<IN == FTINT8_BF16>(most));
-    const Coding c(most);
-    sx = c.fine ? as_f(most) / 127.f : __builtin_nanf("");
+    for (int t = 0; t < TOKENS; ++t) {
+      if (t > 0 && t >= a.m) break;
+      uint32_t most = 0;
 #pragma unroll
-    for (int i = 0; i < WORDS; ++i) {
-      const int at = 8 * (tid + 512 * i);
-      if (at < a.k_padded) *reinterpret_cast<uint2v*>(smem + at) = c.codes<IN == FTINT8_BF16>(raw[i]);
+      for (int w = 0; w < FEW_WAVES; ++w) most = most_of[t][w] > most ? most_of[t][w] : most;
+      most = as_u(low_of<IN == FTINT8_BF16>(most));
+      const Coding c(most);
+      if (TOKENS == 1 || lq == t) sx = c.fine ? as_f(most) / 127.f : __builtin_nanf("");
+#pragma unroll
+      for (int i = 0; i < WORDS; ++i) {
+        const int at = 8 * (tid + 512 * i);
+        if (at < a.k_padded) *reinterpret_cast<uint2v*>(smem + t * pitch + at) = c.codes<IN == FTINT8_BF16>(raw[t][i]);
+      }
     }
     __syncthreads();
   } else if (tid < 64 * TB) {
@@ -523,11 +537,11 @@ template <int TB, int DT, int IN, int WORDS> __global__ __launch_bounds__(FEW_WA
 typedef void (*encode_fn)(const EncodeArgs);
 typedef void (*product_fn)(const ProductArgs);
 typedef void (*few_fn)(const FewArgs);
-template <int DT> few_fn few_of(bool two) { return two ? ftint8_few<2, DT, 0, 0> : ftint8_few<1, DT, 0, 0>; }
-template <int DT> few_fn fused_of(bool bf, bool wide) {
-  if (wide) return bf ? ftint8_few<1, DT, FTINT8_BF16, 4> : ftint8_few<1, DT, FTINT8_F16, 4>;
-  return bf ? ftint8_few<1, DT, FTINT8_BF16, 1> : ftint8_few<1, DT, FTINT8_F16, 1>;
+template <int DT> few_fn few_of(bool two) { return two ? ftint8_few<2, DT, 0, 1, 0> : ftint8_few<1, DT, 0, 1, 0>; }
+template <int DT, int IN> few_fn fused_of(bool several, bool wide) {
+  return several ? ftint8_few<1, DT, IN, FUSED_TOKENS, 1> : wide ? ftint8_few<1, DT, IN, 1, 4> : ftint8_few<1, DT, IN, 1, 1>;
 }
+template <int DT> few_fn fused_of(bool bf, bool several, bool wide) { return bf ? fused_of<DT, FTINT8_BF16>(several, wide) : fused_of<DT, FTINT8_F16>(several, wide); }
 constexpr int few_lds(int blocks) { return FEW_WAVES * blocks * 64 * 16; }
 
 // The kernel for rows of k_padded codes; per: rows of a workgroup.  Rows of up to 2048 elements take a wave each, of up to 16384 a workgroup.
@@ -569,7 +583,7 @@ struct ftint8_ctx {
   product_fn product[N_TILES] = {};
   finish_fn finish = nullptr;
   int4v* sums = nullptr;
-  few_fn few[2] = {}, fused = nullptr;
+  few_fn few[2] = {}, fused[2] = {};
   int8_t* codes = nullptr;       // of the tokens of a forward, and their scales behind them
   float* scales = nullptr;
   std::string err;
@@ -612,7 +626,8 @@ extern "C" int ftint8_create(const ftint8_config* cfg, ftint8_ctx** out) {
   const bool bf = cfg->in_dtype == FTINT8_BF16, wide = c->k_padded > 4096;
   for (int i = 0; i < 2; ++i)
     c->few[i] = cfg->out_dtype == FTINT8_F32 ? few_of<FTINT8_F32>(i) : cfg->out_dtype == FTINT8_BF16 ? few_of<FTINT8_BF16>(i) : few_of<FTINT8_F16>(i);
-  c->fused = cfg->out_dtype == FTINT8_F32 ? fused_of<FTINT8_F32>(bf, wide) : cfg->out_dtype == FTINT8_BF16 ? fused_of<FTINT8_BF16>(bf, wide) : fused_of<FTINT8_F16>(bf, wide);
+  for (int i = 0; i < 2; ++i)
+    c->fused[i] = cfg->out_dtype == FTINT8_F32 ? fused_of<FTINT8_F32>(bf, i, wide) : cfg->out_dtype == FTINT8_BF16 ? fused_of<FTINT8_BF16>(bf, i, wide) : fused_of<FTINT8_F16>(bf, i, wide);
   const size_t bytes = (size_t)cfg->max_tokens * c->k_padded, sums = sums_bytes(cfg->n, c->k_padded / TileSmall::BK);
   int before = 0;
   hipError_t he = hipGetDevice(&before);
@@ -693,7 +708,7 @@ static hipError_t launch_product(ftint8_ctx* c, const int8_t* x, const float* sx
   // codes each workgroup reads twice as many of as of weights, where the weights fit a round of workgroups: 32 on 4096 x 4096 8.4 us, 10.2; on 1000 x 1000 3.3, 5.2;
   // but on 4096 x 8192 15.6, 14.4, on 16,384 x 4096 28.9, 19.9, on 500 x 10,000 15.7, 10.3.  Above that: 64 on 4096 x 4096 11.9, 10.2.
   if (m <= 16 || (m <= 32 && c->k_padded <= 4096 && c->cfg.n <= 4096)) {
-    const FewArgs f{a, nullptr, 0};
+    const FewArgs f{a, nullptr, 0, 0};
     const int two = m > 16;
     hipLaunchKernelGGL(c->few[two], dim3((uint32_t)((c->cfg.n + 15) / 16)), dim3(FEW_WAVES * 64), few_lds(1 + two), st, f);
     return hipGetLastError();
@@ -762,9 +777,14 @@ extern "C" int ftint8_forward(ftint8_ctx* c, const ftint8_matrix* x, int32_t m, 
   OnDevice on(c->cfg.device);
   if (on.error != hipSuccess) return ifail_hip(c, "device", on.error);
   hipError_t he;
-  if (m == 1 && c->k_padded <= FUSED_K && (uintptr_t)x->data % 16 == 0) {
-    const FewArgs f{product_args(c, nullptr, nullptr, m, codes_w, scales_w, y), static_cast<const char*>(x->data), c->cfg.k};
-    hipLaunchKernelGGL(c->fused, dim3((uint32_t)((c->cfg.n + 15) / 16)), dim3(FEW_WAVES * 64), c->k_padded > few_lds(1) ? c->k_padded : few_lds(1), (hipStream_t)hip_stream, f);
+  // One token; up to four on small layers, where an eager call's second launch weighs most (4 on 1024 x 1024 take
+  // 5.9 us in an eager call, 5 of them 8.4 in two launches; in a graph 4 on 4096 x 4096 8.0, in two launches 8.5; on 16,384 x 4096 17.9 and 17.1).
+  const bool several = m > 1;
+  if (several ? m <= FUSED_TOKENS && c->k_padded <= 4096 && c->cfg.n <= 4096 && ((uintptr_t)x->data | (uintptr_t)(x->stride * 2)) % 16 == 0
+              : c->k_padded <= FUSED_K && (uintptr_t)x->data % 16 == 0) {
+    const FewArgs f{product_args(c, nullptr, nullptr, m, codes_w, scales_w, y), static_cast<const char*>(x->data), x->stride * 2, c->cfg.k};
+    const int codes = m * (c->k_padded + 64);
+    hipLaunchKernelGGL(c->fused[several], dim3((uint32_t)((c->cfg.n + 15) / 16)), dim3(FEW_WAVES * 64), codes > few_lds(1) ? codes : few_lds(1), (hipStream_t)hip_stream, f);
     he = hipGetLastError();
     return he == hipSuccess ? FTINT8_OK : ifail_hip(c, "launch", he);
   }

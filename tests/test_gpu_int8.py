@@ -103,7 +103,7 @@ def test_rows_of_zeros_of_small_and_of_unbounded_numbers(dtype):
     assert y[2:5].isnan().all() and not y[5:].isnan().any() and (y[:2] == 0).all()
 
 
-SHAPES = [(1, 1, 1), (1, 16, 64), (1, 515, 4096), (1, 2000, 9000), (2, 33, 65), (5, 4096, 512), (15, 100, 300), (16, 256, 128), (17, 257, 129), (31, 1000, 1000), (33, 48, 4096),
+SHAPES = [(1, 1, 1), (1, 16, 64), (1, 515, 4096), (1, 2000, 9000), (2, 33, 65), (5, 4096, 512), (2, 4096, 4096), (3, 20, 4095), (4, 300, 200), (15, 100, 300), (16, 256, 128), (17, 257, 129), (31, 1000, 1000), (33, 48, 4096),
           (64, 64, 64), (65, 700, 260), (96, 512, 2048), (127, 129, 127), (128, 128, 256), (130, 96, 384), (200, 3, 77), (255, 300, 1024), (256, 256, 256), (300, 520, 900), (513, 257, 640),
           (700, 1030, 200), (1000, 96, 96), (1100, 2100, 512), (20, 70, 5001), (50, 200, 5001), (1, 33, 16385), (130, 500, 10000)]
 
@@ -140,7 +140,7 @@ def test_longest_sums_of_the_largest_codes(m):
 
 
 @pytest.mark.parametrize("m,n,k,x_pad,y_pad,offset", [(5, 33, 100, 3, 5, 1), (70, 130, 129, 7, 0, 0), (3, 64, 64, 8, 8, 8), (300, 257, 64, 0, 9, 3), (130, 256, 256, 8, 8, 0), (1, 100, 90, 0, 0, 5), (1, 100, 90, 0, 3, 8), (1, 50, 5000, 8, 1, 0),
-                                                          (20, 100, 300, 8, 1, 0), (40, 130, 2100, 4, 3, 1)])
+                                                          (20, 100, 300, 8, 1, 0), (3, 100, 300, 4, 1, 0), (4, 4000, 4096, 8, 0, 0), (40, 130, 2100, 4, 3, 1)])
 def test_views_of_larger_tensors(m, n, k, x_pad, y_pad, offset):
     """Rows apart and beginning anywhere; what lies between the rows of the result stays as it was."""
     x, cw, sw = inputs(m, n, k, ftint8.BF16, 3)
