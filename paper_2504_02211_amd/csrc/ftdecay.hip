@@ -19,7 +19,7 @@ struct Args {
   int32_t n_slots, batch, total, heads, group;
   float scale;
   int32_t per;             // tokens of a segment, whole chunks
-  float* between;          // states between segments
+  float* between;          // states between segments, and behind these (STATES of them) the first states of divided sequences
 };
 
 template <bool BF> __device__ __forceinline__ float element(const char* row, int i) {
@@ -94,12 +94,14 @@ template <int D, bool BF> __global__ __launch_bounds__(256) void ftdecay_token(c
 //
 // Sequences are divided into segments of `per` tokens, so that there are workgroups for all CUs: ftdecay_gather forms what each segment alone adds to the state, ftdecay_join adds these up,
 // ftdecay_chunks has the state before its segment and does the rest.  (Gathering is a second pass over keys and values, so that no workgroup waits for another.)
+// The last segment of a sequence stores its state to the pool, which the first one, a workgroup of the same launch, therefore never reads: ftdecay_join keeps
+// the state that a divided sequence begins with.
 //
 // Bound by vector instructions and the reads of operands from LDS that stand between the products (a product of 32 x 32 x 16 takes as long as eight vector instructions, and the
 // words of S, of the weights and of the values are formed by several for each): 16,384 tokens of 32 heads of 128 on 8, bf16, take 197 us, 109 being what the bytes take at a copy's rate;
 // without the vector work between the products, one after the other, 250 us; a token at a time 21.5 ms.  24 prompts of up to 1531 tokens, 12 heads of 64, fp16: 39 us, 890 a token at a time.
 constexpr int C = 64;
-// Segments: at most STATES states between them (67 MB at head_dim 128, 17 MB at 64), and no fewer than LEAST tokens in one: 24 prompts of up to 1531 tokens of 12 heads of 64
+// Segments: at most STATES states between them (67 MB at head_dim 128, 17 MB at 64; and as much room for first states), and no fewer than LEAST tokens in one: 24 prompts of up to 1531 tokens of 12 heads of 64
 // take 45 us in segments of 128, 39 of 192, 43 of 256, 64 of 512; 4096 tokens of 8 heads of 128 38, 37, 39 and 55 us.
 constexpr int STATES = 1024, LEAST = 192;
 
@@ -410,7 +412,9 @@ template <int D> __global__ __launch_bounds__(256) void ftdecay_join(const Args 
   const float* const first = a.starts && a.starts[b] > 0 ? state_of<D>(a, b, h) : nullptr;
   float4v x = first ? *reinterpret_cast<const float4v*>(first + e) : (float4v)0.f;
   const Decay whole = Powers(a, h).whole(a.per);
-  float4v* const at = reinterpret_cast<float4v*>(a.between + ((int64_t)(t0 / a.per) * a.heads + h) * (D * D) + e);
+  const int64_t place = (int64_t)(t0 / a.per) * a.heads + h;      // (divided sequences are longer than `per`: no two begin in the same one)
+  float4v* const at = reinterpret_cast<float4v*>(a.between + place * (D * D) + e);
+  if (first) *reinterpret_cast<float4v*>(a.between + (STATES + place) * (D * D) + e) = x;
   const int64_t apart = (int64_t)a.heads * (D * D / 4);
   for (int s = 0; s + 1 < segments; s += 8) {      // (eight loads under way at a time)
     float4v y[8];
@@ -440,7 +444,7 @@ template <int D, bool BF> __global__ __launch_bounds__(2 * D, 2) void ftdecay_ch
   float* const state = state_of<D>(a, g.b, g.h);
   const float* from = nullptr;
   if (g.number > 0) from = a.between + ((g.before + g.number - 1) * a.heads + g.h) * (D * D);
-  else if (a.starts && a.starts[g.b] > 0) from = state;
+  else if (state && a.starts && a.starts[g.b] > 0) from = g.last ? state : a.between + (STATES + g.before * a.heads + g.h) * (D * D);
   const Loader<D, NW> lq(a.q, g.first, g.h, wave, c.lane), lk(a.k, g.first, hk, wave, c.lane), lv(a.v, g.first, hk, wave, c.lane);
   if (chunks > 0) {
     lq.issue(0, g.tokens, qt);
@@ -769,7 +773,7 @@ extern "C" int ftdecay_create(const ftdecay_config* cfg, ftdecay_ctx** out) {
   if (he == hipSuccess) {
     he = hipFuncSetAttribute((const void*)c->chunks, hipFuncAttributeMaxDynamicSharedMemorySize, c->lds);
     if (he == hipSuccess) he = hipFuncSetAttribute((const void*)c->gather, hipFuncAttributeMaxDynamicSharedMemorySize, c->gather_lds);
-    if (he == hipSuccess) he = hipMalloc((void**)&c->between, (size_t)STATES * cfg->head_dim * cfg->head_dim * sizeof(float));
+    if (he == hipSuccess) he = hipMalloc((void**)&c->between, (size_t)2 * STATES * cfg->head_dim * cfg->head_dim * sizeof(float));
     (void)hipSetDevice(before);
   }
   if (he != hipSuccess) {

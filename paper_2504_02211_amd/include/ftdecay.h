@@ -51,7 +51,7 @@ typedef struct {
  * in elements and multiples of 8, those of tokens at most 2^24. */
 typedef struct { void* data; int64_t token_stride, head_stride; } ftdecay_rows;
 
-/* A context holds device memory for the states between parts of long prompts, whatever the calls' sizes: 1024 * head_dim * head_dim * 4 bytes (67 MB at 128, 17 MB at 64). */
+/* A context holds device memory for the states before and between parts of long prompts, whatever the calls' sizes: 2048 * head_dim * head_dim * 4 bytes (134 MB at 128, 34 MB at 64). */
 int ftdecay_create(const ftdecay_config* cfg, ftdecay_ctx** out);
 /* Copies the configuration in effect (defaults resolved). */
 int ftdecay_get_config(const ftdecay_ctx* ctx, ftdecay_config* effective);
