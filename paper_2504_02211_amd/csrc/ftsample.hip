@@ -664,11 +664,12 @@ __global__ __launch_bounds__(THREADS) void ftsample_row(const Args a) {
         if (s.bins[i]) s.bins[i] *= weight(L::of_key(highest - i));
       __syncthreads();
     }
-    find_bin<BINS / THREADS>(s, above, [&](unsigned long long) { return limit; }, [&](int i) { return s.bins[i]; });
+    if (find_bin<BINS / THREADS>(s, above, [&](unsigned long long) { return limit; }, [&](int i) { return s.bins[i]; }) == 0) return false;
     above = s.above;
     const uint32_t top = highest - (s.bin << drop), least = top - ((1u << drop) - 1);
     lowest = least > lowest && least <= top ? least : lowest;
     highest = top;
+    return true;
   };
   auto drop_of = [](uint32_t range) {
     const int bits = 32 - __builtin_clz(range);
@@ -694,7 +695,7 @@ __global__ __launch_bounds__(THREADS) void ftsample_row(const Args a) {
       };
       if (by_weight && !counted) fill(weight);
       else fill([](float) { return 1ull; });
-      narrow(lowest, highest, drop, counted, above, limit);
+      if (!narrow(lowest, highest, drop, counted, above, limit)) return;      // (none lies there)
     }
     // of the logits that are the border, as many as fit
     const float border = L::of_key(lowest);
@@ -772,7 +773,7 @@ __global__ __launch_bounds__(THREADS) void ftsample_row(const Args a) {
     if (all < limit && !by_weight) {
       uint32_t beyond_all;
       before_me<uint32_t>(beyond, s.words, beyond_all);
-      if (beyond_all == 0) return;      // fewer than that can be chosen: all of them are kept
+      if (all + beyond_all <= limit) return;      // no more than that can be chosen: all of them are kept
     } else {
       bin = (int)s.bin;
       above = s.above;
@@ -812,7 +813,7 @@ __global__ __launch_bounds__(THREADS) void ftsample_row(const Args a) {
         const unsigned long long each = tid >= count ? 0 : by_weight ? weight(L::of_key(key)) : 1;
         unsigned long long all_here;
         const unsigned long long at = above + before_me<unsigned long long>(each, s.sums, all_here);
-        if (at < limit && at + each >= limit) {
+        if (at < limit && (at + each >= limit || tid == count - 1)) {
           s.bin = (uint32_t)tid;
           s.words[0] = key;
         }
@@ -989,13 +990,6 @@ __global__ __launch_bounds__(THREADS) void ftsample_row(const Args a) {
     // counted already, and the sort takes 10 us more.)
     if constexpr (!KEYED)
       if (r.cut_p && r.top_k <= LIST && kept.border > NOTHING && by_list(std::true_type{}, kept.border)) return;
-    // (where fewer than top_k can be chosen, fewer are equal than there is room for)
-    if (!KEYED && r.cut_p) {
-      uint32_t there = 0, ties;
-      x.each([&](float y) __attribute__((always_inline)) { there += y == kept.border; });
-      before_me<uint32_t>(there, s.words, ties);
-      if ((uint32_t)kept.equal > ties) kept.equal = (int)ties;
-    }
   }
   if (r.cut_p) by_values(true, limit_of);
   sum_up(kept);
