@@ -65,6 +65,11 @@ template <int DT> struct Type {
     const uint32_t u = k << DROP;
     return as_f(u & 0x80000000u ? u ^ 0x80000000u : ~(u | ((1u << DROP) - 1)));
   }
+  // The largest number whose key is at most k.  (The key below that of the zeros would be that of -0, which compares as they do.)
+  static __device__ __forceinline__ float upto_key(uint32_t k) {
+    const float x = of_key(k);
+    return as_u(x) == 0x80000000u ? as_f(0x80000001u) : x;
+  }
 };
 constexpr float NOTHING = -__builtin_inff();
 
@@ -678,7 +683,7 @@ __global__ __launch_bounds__(THREADS) void ftsample_row(const Args a) {
   auto search = [&](unsigned long long limit, bool by_weight, uint32_t lowest, uint32_t highest, unsigned long long above) {
     while (lowest != highest) {
       const int drop = drop_of(highest - lowest);
-      const float from = L::of_key(lowest), to = L::of_key(highest);
+      const float from = L::of_key(lowest), to = L::upto_key(highest);
       empty_bins();
       const bool counted = by_weight && drop == 0;
       auto fill = [&](auto value) __attribute__((always_inline)) {
@@ -794,7 +799,7 @@ __global__ __launch_bounds__(THREADS) void ftsample_row(const Args a) {
     };
     const uint32_t lowest = bin == LAST_BIN ? least_key : first_key(bin), highest = bin == 0 ? top_key : first_key(bin - 1) - 1;
     // Few logits of 32 bits lie there, as a rule: they are sorted.  (Of 16 bits many are equal.)
-    const float from = L::of_key(lowest), to = L::of_key(highest);
+    const float from = L::of_key(lowest), to = L::upto_key(highest);
     if (L::WIDE && !(kept.equal && kept.border >= from && kept.border <= to)) {
       if (tid == 0) s.count = 0;
       __syncthreads();

@@ -47,3 +47,25 @@ def test_top_k_at_the_number_of_logits_that_can_be_chosen(k, far, dtype):
     x, u, ks = x.to(TYPES[dtype]), torch.rand(len(counts), generator=g), torch.full((len(counts),), k, dtype=torch.int32)
     check(x, u, top_k=ks)
     check(x, u, top_k=ks, top_p=torch.full((len(counts),), 0.9))
+
+
+@pytest.mark.parametrize("dtype", ALL)
+def test_borders_just_below_zero(dtype):
+    """Zeros of both signs and the smallest negative numbers beside larger ones: the border lies among the latter, whose keys end where those of zeros begin."""
+    g = torch.Generator().manual_seed(9)
+    vocab, zeros, small = 2000, 500, 700
+    unit = {ftsample.F16: 2.0 ** -24, ftsample.BF16: 2.0 ** -133, ftsample.F32: 2.0 ** -149}[dtype]
+    tops = [1.0, 0.8, 0.93, 1.1, 1.3, 2.0, 0.51, 0.7, 0.61, 1.7]
+    rows = len(tops)
+    x = np.full((rows, vocab), -np.inf)
+    for r in range(rows):
+        at = torch.randperm(vocab, generator=g).numpy()
+        x[r, at[:zeros:2]], x[r, at[1:zeros:2]] = 0.0, -0.0
+        x[r, at[zeros:zeros + small]] = -unit * torch.randint(1, 8, (small,), generator=g).numpy()
+        x[r, at[zeros + small:zeros + small + 100]] = -0.6 + 0.5 * torch.rand(100, generator=g).numpy()
+        x[r, at[-1]] = tops[r]
+    x, u = torch.from_numpy(x.astype(np.float32)).to(TYPES[dtype]), torch.rand(rows, generator=g)
+    ks = torch.tensor([zeros + 1 + n for n in (1, 300, 500, 699, 650, 2, 400, 600, 100, 50)], dtype=torch.int32)
+    check(x, u, top_k=ks)
+    check(x, u, top_k=ks, top_p=torch.full((rows,), 0.95))
+    check(x, u, top_p=0.5 + 0.4 * torch.rand(rows, generator=g))

@@ -122,3 +122,26 @@ def test_top_k_at_the_number_of_logits_that_can_be_chosen(library, tmp_path, dty
     for top_p in (None, 0.9):
         rules = {} if top_p is None else {"top_p": [top_p] * len(counts)}
         check(library, tmp_path, x, dtype, g.random(len(counts)), top_k=[k] * len(counts), **rules)
+
+
+@pytest.mark.parametrize("dtype", ALL)
+def test_borders_just_below_zero(library, tmp_path, dtype):
+    """Zeros of both signs and the smallest negative numbers beside larger ones: the border lies among the latter, whose keys end where those of zeros begin."""
+    g = np.random.default_rng(9)
+    vocab, zeros, small = 2000, 500, 700
+    unit = {ftsample.F16: 2.0 ** -24, ftsample.BF16: 2.0 ** -133, ftsample.F32: 2.0 ** -149}[dtype]
+    tops = [1.0, 0.8, 0.93, 1.1, 1.3, 2.0, 0.51, 0.7, 0.61, 1.7]
+    rows = len(tops)
+    x = np.full((rows, vocab), -np.inf)
+    for r in range(rows):
+        at = g.permutation(vocab)
+        x[r, at[:zeros]] = np.where(g.random(zeros) < 0.5, 0.0, -0.0)
+        x[r, at[zeros:zeros + small]] = -unit * g.integers(1, 8, small)
+        x[r, at[zeros + small:zeros + small + 100]] = -0.5 * g.random(100) - 0.1
+        x[r, at[-1]] = tops[r]
+    with np.errstate(under="ignore"):
+        x = x.astype(np.float32)
+    ks = [zeros + 1 + n for n in (1, 300, 500, 699, 650, 2, 400, 600, 100, 50)]
+    check(library, tmp_path, x, dtype, g.random(rows), top_k=ks)
+    check(library, tmp_path, x, dtype, g.random(rows), top_k=ks, top_p=[0.95] * rows)
+    check(library, tmp_path, x, dtype, g.random(rows), top_p=list(0.5 + 0.4 * g.random(rows)))
