@@ -90,7 +90,9 @@ template <int D, bool BF> __global__ __launch_bounds__(256) void ftdecay_token(c
 //
 // What is rounded to 16 bits before a product is held in more than one word.  bf16: weights and S in two words (2^-16 relative), decayed values in three (S is a state of
 // 32 bits).  fp16: S under one power of two for its slab, and the decayed values, in two words, the lower one times 2^11 (22 bits; what the products of lower words add is kept apart until it is
-// scaled back); weights, which have no bound, in two words of bf16 with the values as two words of bf16, which hold fp16 exactly.
+// scaled back); weights, which have no bound, in two words of bf16 with the values as two words of bf16, which hold fp16 exactly.  As fp16 ends at 2^-24, values are lifted by a power of two, up
+// to 2^15, as far as the slab's largest allows, and the state is held times as much until the next chunk: a decayed value is off by 2^-24 of itself, or by 2^-51 of a slab's values below 2 where
+// that is more (2^-36 without it, which left values of 2^-24 with 12 bits; 16,384 tokens of 32 heads on 8, fp16, take 127 us with it and 121 without at head_dim 64, 201 and 200 at 128).
 //
 // Sequences are divided into segments of `per` tokens, so that there are workgroups for all CUs: ftdecay_gather forms what each segment alone adds to the state, ftdecay_join adds these up,
 // ftdecay_chunks has the state before its segment and does the rest.  (Gathering is a second pass over keys and values, so that no workgroup waits for another.)
@@ -263,7 +265,31 @@ template <int D, bool BF> struct Chunk {
     *(__attribute__((address_space(3))) float*)(uintptr_t)(fall_word(lane >> 2) + 4 * (lane & 3)) = left < 0 ? 0.f : p.to(left);
   }
 
-  // The values of tokens 16s + 8h .. + 7, decayed to the end of the chunk, in words: in parts, so that matrix instructions can stand between them.
+  // The largest magnitudes of this lane's values, a pair's, as their 16 bits, which are ordered as the numbers are.
+  static constexpr uint32_t INF = BF ? 0x7F80u : 0x7C00u;
+  static __device__ __forceinline__ uint32_t largest(const uint4v (&vr)[KS]) {
+    uint32_t most = 0;
+#pragma unroll
+    for (int s = 0; s < KS; ++s)
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+        most = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(ushort2v, most), __builtin_bit_cast(ushort2v, vr[s][x] & 0x7FFF7FFFu)));
+    return most;
+  }
+  static __device__ __forceinline__ bool unbounded(uint32_t most) { return __any((most & 0xFFFFu) >= INF || most >> 16 >= INF); }
+  // fp16, whose least number lies 2^-24 below 1: the power of two, up to 2^15, by which the slab's values may be lifted, and the state with them, so that what is left
+  // of a word and of decayed values has room below.  (Exact: the largest stays a number.)
+  static __device__ __forceinline__ int room(uint32_t most) {
+    most = (most & 0xFFFFu) > most >> 16 ? most & 0xFFFFu : most >> 16;
+    int t = 15;
+#pragma unroll
+    for (int b = 8; b; b >>= 1) t += __any(most >= (uint32_t)(t + b) << 10) ? b : 0;
+    return 30 - t;
+  }
+  static __device__ __forceinline__ uint32_t lift_of(int e) { return (uint32_t)(15 + e) * 0x04000400u; }
+  static __device__ __forceinline__ float power(int e) { return as_f((uint32_t)(127 + e) << 23); }
+
+  // The values of tokens 16s + 8h .. + 7, lifted (fp16) and decayed to the end of the chunk, in words: in parts, so that matrix instructions can stand between them.
   static constexpr int WORDS = BF ? 3 : 2, PARTS = 4 * WORDS;
   struct Decayed {
     float4v f[2];
@@ -276,11 +302,12 @@ template <int D, bool BF> struct Chunk {
     d.f[0] = *(const __attribute__((address_space(3))) float4v*)(uintptr_t)first;
     d.f[1] = *(const __attribute__((address_space(3))) float4v*)(uintptr_t)(first ^ 16u);
   }
-  __device__ __forceinline__ void part(Decayed& d, const uint4v& v, int x) const {
+  __device__ __forceinline__ void part(Decayed& d, const uint4v& v, uint32_t lift, int x) const {
     const int i = x / WORDS;
     if (x % WORDS == 0) {
-      d.x = low_of<BF>(v[i]) * d.f[i >> 1][2 * (i & 1)];
-      d.y = high_of<BF>(v[i]) * d.f[i >> 1][2 * (i & 1) + 1];
+      const uint32_t raw = v[i], y = BF ? raw : __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2v, raw) * __builtin_bit_cast(half2v, lift));
+      d.x = low_of<BF>(y) * d.f[i >> 1][2 * (i & 1)];
+      d.y = high_of<BF>(y) * d.f[i >> 1][2 * (i & 1) + 1];
       d.w[0][i] = pack2<BF>(d.x, d.y);
     } else if (x % WORDS == 1) {
       d.x -= low_of<BF>(d.w[0][i]);
@@ -298,8 +325,8 @@ template <int D, bool BF> struct Chunk {
     for (int v = x * NB; v < (x + 1) * NB; ++v) S[v >> 4][v & 15] *= by;
   }
 
-  // The slab, decayed already, moves on by a chunk.  vr: its values, raw; d: those of the first step, ready.  `beside(i)`: what else is done, in 8 parts.
-  template <class F> __device__ __forceinline__ void update(float16v (&S)[NB], const uint4v (&vr)[KS], Decayed& d, uint32_t ktile, F beside) const {
+  // The slab, decayed and lifted already, moves on by a chunk.  vr: its values, raw; d: those of the first step, ready.  `beside(i)`: what else is done, in 8 parts.
+  template <class F> __device__ __forceinline__ void update(float16v (&S)[NB], const uint4v (&vr)[KS], uint32_t lift, Decayed& d, uint32_t ktile, F beside) const {
     uint4v k[2][NB];
     float16v low[BF ? 1 : NB];
     if constexpr (!BF)
@@ -322,7 +349,7 @@ template <int D, bool BF> struct Chunk {
         if (s + 1 < KS) {
           if (i < NB) k[(s + 1) & 1][i] = transposed<true>(ktile, s + 1, i);
 #pragma unroll
-          for (int y = PARTS * i / (WORDS * NB); y < PARTS * (i + 1) / (WORDS * NB); ++y) part(d, vr[s + 1 < KS ? s + 1 : 0], y);
+          for (int y = PARTS * i / (WORDS * NB); y < PARTS * (i + 1) / (WORDS * NB); ++y) part(d, vr[s + 1 < KS ? s + 1 : 0], lift, y);
         }
         if (s == 0)
 #pragma unroll
@@ -350,12 +377,12 @@ template <int D, bool BF> struct Chunk {
       for (int b = 0; b < NB; ++b) S[b] = (float16v)0.f;
     }
   }
-  __device__ __forceinline__ void put(const float16v (&S)[NB], float* to) const {
+  __device__ __forceinline__ void put(const float16v (&S)[NB], float* to, float by) const {      // (times `by` in fp16)
     float* const at = to + 8 * h * D + 32 * wave + n;
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
-      for (int v = 0; v < 16; ++v) at[(32 * b + row_of(v, 0)) * D] = S[b][v];
+      for (int v = 0; v < 16; ++v) at[(32 * b + row_of(v, 0)) * D] = BF ? S[b][v] : S[b][v] * by;
   }
 };
 
@@ -378,6 +405,7 @@ template <int D, bool BF> __global__ __launch_bounds__(2 * D, 2) void ftdecay_ga
   const Decay whole = powers.whole(C);
   float16v S[D / 32];
   c.fetch(S, nullptr);
+  int lifted = 0;      // the slab is 2^lifted times the state
   for (int i = 0; i < chunks; ++i) {
     const uint32_t tile = lds0 + (i & 1) * 2 * TILE;
     c.renew();
@@ -390,16 +418,34 @@ template <int D, bool BF> __global__ __launch_bounds__(2 * D, 2) void ftdecay_ga
     uint4v vr[C / 16];
 #pragma unroll
     for (int s = 0; s < C / 16; ++s) vr[s] = c.template transposed<false>(tile + TILE, s, c.wave);
-    const float fading = in_scalar(whole.of(i));
+    float fading = whole.of(i);
+    uint32_t lift = 0;
     typename Chunk<D, BF>::Decayed d;
     c.begin(d, 0);
+    if constexpr (!BF) {
+      uint32_t most = c.largest(vr);
+      if (__builtin_expect(c.unbounded(most), 0)) {      // (what is not finite counts in its own column alone)
+        uint4v finite[C / 16];
 #pragma unroll
-    for (int x = 0; x < c.PARTS; ++x) c.part(d, vr[0], x);
+        for (int s = 0; s < C / 16; ++s)
+#pragma unroll
+          for (int x = 0; x < 4; ++x)
+            finite[s][x] = vr[s][x] & ((vr[s][x] & c.INF) == c.INF ? 0u : 0xFFFFu) | vr[s][x] & ((vr[s][x] >> 16 & c.INF) == c.INF ? 0u : 0xFFFF0000u);
+        most = c.largest(finite);
+      }
+      const int e = c.room(most);
+      fading *= c.power(e - lifted);
+      lift = c.lift_of(e);
+      lifted = e;
+    }
+    fading = in_scalar(fading);
+#pragma unroll
+    for (int x = 0; x < c.PARTS; ++x) c.part(d, vr[0], lift, x);
 #pragma unroll
     for (int x = 0; x < 16; ++x) c.fade(S, fading, x);
-    c.update(S, vr, d, tile, [](int) {});
+    c.update(S, vr, lift, d, tile, [](int) {});
   }
-  c.put(S, a.between + ((g.before + g.number) * a.heads + g.h) * (D * D));
+  c.put(S, a.between + ((g.before + g.number) * a.heads + g.h) * (D * D), c.power(-lifted));
 }
 
 // The states between segments: each the sum of what the segments before it add, decayed, and of the sequence's first state.
@@ -470,6 +516,8 @@ template <int D, bool BF> __global__ __launch_bounds__(2 * D, 2) void ftdecay_ch
   uint32_t weight_at = (uint32_t)(n0 * (2 * C) + ((h0 ^ (n0 >> 1 & 7)) * 16));      // (the same for queries 32 apart)
   char* const o0 = a.o.data + (int64_t)g.first * a.o.token + (int64_t)g.h * a.o.head + 64 * wave;
 
+  int lifted = 0;      // the slab is 2^lifted times the state
+
   for (int i = 0; i < chunks; ++i) {
     const int left = g.tokens - i * C, tokens = left < C ? left : C;
     c.renew();
@@ -509,6 +557,7 @@ template <int D, bool BF> __global__ __launch_bounds__(2 * D, 2) void ftdecay_ch
     };
     // the slab of the state in words of 16 bits: `high` and `low` of elements 16x + 8h ..  (fp16: times `up`, its largest just below 2^14)
     float up = 1.f, down = 1.f;
+    bool huge = false;      // (a state that has no room to be lifted)
     if constexpr (!BF) {
       float most = 0.f;
 #pragma unroll
@@ -528,8 +577,9 @@ template <int D, bool BF> __global__ __launch_bounds__(2 * D, 2) void ftdecay_ch
       }
       int e = most > 0.f ? 140 - (int)(as_u(most) >> 23) : 0;
       e = __builtin_amdgcn_readfirstlane(e > 100 ? 100 : e);
-      up = as_f((uint32_t)(127 + e) << 23);
-      down = as_f((uint32_t)(127 - e) << 23);
+      up = c.power(e);
+      down = c.power(-e - lifted);
+      huge = e < -90;
     }
     struct Words { uint4v high, low; };
     auto split = [&](Words& w, int x, int v) __attribute__((always_inline)) {
@@ -612,21 +662,15 @@ template <int D, bool BF> __global__ __launch_bounds__(2 * D, 2) void ftdecay_ch
     }
     // Values that are not finite are left out of the products, which would bring them to tokens before theirs (0 times infinity); the tokens from theirs on, and the
     // state, get NaN in their column.
-    uint32_t most = 0;
-#pragma unroll
-    for (int s = 0; s < KS; ++s)
-#pragma unroll
-      for (int x = 0; x < 4; ++x)
-        most = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(ushort2v, most), __builtin_bit_cast(ushort2v, vr[s][x] & 0x7FFF7FFFu)));
-    constexpr uint32_t INF = BF ? 0x7F80u : 0x7C00u;
-    if (__builtin_expect(__any((most & 0xFFFFu) >= INF || most >> 16 >= INF), 0)) {
+    uint32_t most = c.largest(vr);
+    if (__builtin_expect(c.unbounded(most), 0)) {
       int first = C, from = 4 * h;
       asm volatile("" : "+v"(from));
 #pragma unroll
       for (int s = KS - 1; s >= 0; --s)
 #pragma unroll
         for (int x = 7; x >= 0; --x) {
-          const uint32_t mask = INF << 16 * (x & 1);
+          const uint32_t mask = c.INF << 16 * (x & 1);
           if ((vr[s][x >> 1] & mask) == mask) {
             first = 16 * s + x;
             vr[s][x >> 1] &= x & 1 ? 0xFFFFu : 0xFFFF0000u;
@@ -645,8 +689,17 @@ template <int D, bool BF> __global__ __launch_bounds__(2 * D, 2) void ftdecay_ch
       for (int b = 0; b < NB; ++b)
 #pragma unroll
         for (int v = 0; v < 16; ++v) S[b][v] = first < C ? __builtin_nanf("") : S[b][v];
+      if constexpr (!BF) most = c.largest(vr);
     }
-    const float fading = in_scalar(tokens < C ? rest : whole.of(i));
+    float fading = tokens < C ? rest : whole.of(i);
+    uint32_t lift = 0;
+    if constexpr (!BF) {
+      const int e = huge ? 0 : c.room(most);
+      fading *= c.power(e - lifted);
+      lift = c.lift_of(e);
+      lifted = e;
+    }
+    fading = in_scalar(fading);
     c.here();
     // The chunk's own tokens: for each step of 16 keys the query blocks that see some of them, the lower words first.  Beside them the state fades.
 #pragma unroll
@@ -681,7 +734,7 @@ template <int D, bool BF> __global__ __launch_bounds__(2 * D, 2) void ftdecay_ch
 #pragma unroll
               for (int y = 16 * at / PLACES; y < 16 * (at + 1) / PLACES; ++y) c.fade(S, fading, y);
 #pragma unroll
-              for (int y = c.PARTS * at / PLACES; y < c.PARTS * (at + 1) / PLACES; ++y) c.part(d, vr[0], y);
+              for (int y = c.PARTS * at / PLACES; y < c.PARTS * (at + 1) / PLACES; ++y) c.part(d, vr[0], lift, y);
             }
           }
           c.here();
@@ -700,11 +753,11 @@ template <int D, bool BF> __global__ __launch_bounds__(2 * D, 2) void ftdecay_ch
     if constexpr (!BF)      // (the registers of these results are needed)
 #pragma unroll
       for (int y = 0; y < 8; ++y) store(y);
-    c.update(S, vr, d, kt, [&](int y) __attribute__((always_inline)) {
+    c.update(S, vr, lift, d, kt, [&](int y) __attribute__((always_inline)) {
       if constexpr (BF) store(y);
     });
   }
-  if (g.last && state) c.put(S, state);
+  if (g.last && state) c.put(S, state, c.power(-lifted));
 }
 
 typedef void (*kernel_fn)(const Args);

@@ -12,6 +12,10 @@
  * What a query sees ends with its own token: later keys and values have no influence on it, not even where they are infinite or NaN.  From the token on
  * whose key or value is not finite, elements of results and states that it enters are not finite either.
  *
+ * Prompts are computed in chunks of 64 tokens.  Before a product, weights q k decay^n and states are rounded to two words of 16 bits (2^-16 relative), values decayed to the end of
+ * a chunk, which make the states, to three of bf16, or two of fp16: off by 2^-24 relative, or in fp16 by 2^-51 where that is more (chunks with values from 2 on in 32
+ * neighbouring columns: 2^-50, and so on by octaves).  Single tokens are computed in 32 bits.
+ *
  * Conventions
  *   - Every function returns FTDECAY_OK (0) or a negative error code and never throws or prints; ftdecay_last_error() returns the message of the last failure.
  *   - All tensors are DEVICE pointers owned by the caller; the structures that carry them are HOST memory.  The call leaves the current device as it was.

@@ -34,8 +34,8 @@ int main() {
           const Segment g{0, 1, number, 10, 0, number == segments - 1, 3};
           float* const state = there ? pool : nullptr;
           float* to = nullptr;
-          struct { void put(int, float* x) { *at = x; } float** at; } c{&to};
-          const int S = 0;
+          struct { void put(int, float* x, float = 1.f) { *at = x; } float power(int) { return 1.f; } float** at; } c{&to};
+          const int S = 0, lifted = 0;
           %(from)s
           %(to)s
           auto place = [&](const float* x) { return x == nullptr ? -1L : x == pool ? -2L : (long)(x - workspace); };
