@@ -10,7 +10,7 @@ import pytest
 torch = pytest.importorskip("torch")
 
 from paper_2504_02211_amd import ftdecay
-from test_gpu_decay import TYPES, bound, ints, stream
+from test_gpu_decay import TYPES, Case, bound, ints, stream
 from test_gpu_decay_many import recurrence
 
 pytestmark = pytest.mark.gpu
@@ -81,3 +81,19 @@ def test_states_with_no_room_above(d, dtype):
     first = (torch.rand((2, 2, d, d), generator=g) - 0.5) * 2.0 ** torch.tensor([127.0, 104.0])[:, None, None, None]
     states = check(values, [-0.01, -0.3], dtype, first=first, lengths=[70, 60], outputs=False)
     assert states.isfinite().all()
+
+
+@pytest.mark.parametrize("dtype", [ftdecay.F16, ftdecay.BF16])
+@pytest.mark.parametrize("d", [64, 128])
+def test_what_counts_as_no_decay(d, dtype):
+    """A log_decay above 0, or NaN, gives the results and states of 0, bit for bit: prompts, divided ones among them, and single tokens."""
+    lengths, odd = [200, 1, 66, 300], [3.0, float("nan"), float("inf"), 1e-30, -0.1]
+    runs = []
+    for log_decay in (odd, [0.0, 0.0, 0.0, 0.0, -0.1]):
+        c = Case(lengths, 5, 5, d, dtype, starts=[1, 1, 0, 1], log_decay=torch.tensor(log_decay, dtype=torch.float64))
+        o, states = c.run()
+        q, k, v = c.split(c.qkv[:4].cuda())
+        one = torch.empty((4, 5, d), dtype=TYPES[dtype], device="cuda")
+        c.ctx.step(q, k, v, one, c.log_decay.cuda(), states, stream=stream())
+        runs.append((o, states, one))
+    assert all(torch.equal(x, y) and not x.isnan().any() for x, y in zip(*runs))
