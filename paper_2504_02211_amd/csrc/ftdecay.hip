@@ -100,11 +100,12 @@ template <int D, bool BF> __global__ __launch_bounds__(256) void ftdecay_token(c
 // the state that a divided sequence begins with.
 //
 // Bound by vector instructions and the reads of operands from LDS that stand between the products (a product of 32 x 32 x 16 takes as long as eight vector instructions, and the
-// words of S, of the weights and of the values are formed by several for each): 16,384 tokens of 32 heads of 128 on 8, bf16, take 197 us, 109 being what the bytes take at a copy's rate;
-// without the vector work between the products, one after the other, 250 us; a token at a time 21.5 ms.  24 prompts of up to 1531 tokens, 12 heads of 64, fp16: 39 us, 890 a token at a time.
+// words of S, of the weights and of the values are formed by several for each): 16,384 tokens of 32 heads of 128 on 8, bf16, take 194 us.  What goes in and out takes 69 at a
+// copy's rate, with the second pass over keys and values and the states between segments, written twice and read twice, 109.  Without the vector work between the products, one after the
+// other, 250 us; a token at a time 21.5 ms.  24 prompts of up to 1531 tokens, 12 heads of 64, fp16: 38 us, 890 a token at a time.
 constexpr int C = 64;
-// Segments: at most STATES states between them (67 MB at head_dim 128, 17 MB at 64; and as much room for first states), and no fewer than LEAST tokens in one: 24 prompts of up to 1531 tokens of 12 heads of 64
-// take 45 us in segments of 128, 39 of 192, 43 of 256, 64 of 512; 4096 tokens of 8 heads of 128 38, 37, 39 and 55 us.
+// Segments: at most STATES states between them (67 MB at head_dim 128, 17 MB at 64; and as much room for first states), and no fewer than LEAST tokens in one: 24 prompts of up to 1531 tokens of 12 heads of 64, fp16, take
+// 39.2 us in segments of 128, 39.0 of 192, 43.5 of 256, 67.6 of 512; 4096 tokens of 8 heads of 128, bf16, 36.6, 35.4, 38.4 and 55 us.
 constexpr int STATES = 1024, LEAST = 192;
 
 template <int D> constexpr int tile_bytes() { return C * D * 2; }

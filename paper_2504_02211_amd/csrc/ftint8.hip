@@ -67,7 +67,8 @@ __device__ __forceinline__ uint32_t largest_of_wave(uint32_t x) {
   return x;
 }
 
-// Rows that begin anywhere, or are longer than the registers of a workgroup: a row a workgroup, element after element, read twice.
+// Rows that begin anywhere, or are longer than the registers of a workgroup: a row a workgroup, element after element, read twice.  4096 rows of 4001 elements take
+// 25 us (of 4000, as below, 8.7), of 28,672 196 us (of 16,384 31).
 template <int DT> __global__ __launch_bounds__(256) void ftint8_encode_any(const EncodeArgs a) {
   __shared__ uint32_t most_of[4];
   const int row = blockIdx.x, tid = threadIdx.x;
@@ -164,8 +165,8 @@ __device__ __forceinline__ void load_lds16(const void* base, uint32_t off, uint3
 template <class F, int... I> __device__ __forceinline__ void for_each_of(F&& f, std::integer_sequence<int, I...>) { (f(std::integral_constant<int, I>{}), ...); }
 template <int N, class F> __device__ __forceinline__ void for_each(F&& f) { for_each_of(f, std::make_integer_sequence<int, N>{}); }
 
-// A wide store to an address that is aligned to an element only.  (The device's vector stores take any.  Rows of 4001 results, stored an element at a time, took 4000 tokens on
-// 4001 x 4096 from 51 us to 65.)
+// A wide store to an address that is aligned to an element only.  (The device's vector stores take any.  Rows of 4001 results, stored an element at a time, take the product of
+// 4000 tokens on 4001 x 4096 from 54 us to 72.)
 template <int ES, class V> __device__ __forceinline__ void put_anywhere(char* to, V v) {
   struct __attribute__((packed, aligned(ES))) Loose { V v; };
   reinterpret_cast<Loose*>(to)->v = v;
@@ -205,7 +206,8 @@ template <class T> __device__ __forceinline__ void tile_of(const ProductArgs& a,
 // side by side per block of features.  The steps of 128 columns go through a ring of LDS stages that direct loads fill; a row's 16-byte chunk c lies at place c ^ (row / 2 % 8), which keeps
 // the reads of operands free of bank conflicts.  Operands are read ahead of their products, also across the border of two stages: the barrier of a stage sits AHEAD rows of
 // products before its end, where its last operands are in registers, so that no wave waits for LDS behind it.
-// Bound by power (the clock falls to some 1.8 GHz, the matrix pipe is 60 % busy): 16,384 tokens on 16,384 x 4096 (features x columns) 907 us, 2425 TOPS; the library's plain product of the codes, without scales, 974 us.
+// Bound by power (the clock falls to some 1.8 GHz, the matrix pipe is 60 % busy): 16,384 tokens on 16,384 x 4096 (features x columns) 908 us, 2420 TOPS, one behind another (the first ones of a cold card 967 to 1050); the library's
+// plain product of the codes, without scales, 974 us.
 template <class T, int DT> __global__ __launch_bounds__(T::NW * 64, T::PER_CU * T::NW / 4) void ftint8_tile(const ProductArgs a) {
   constexpr int WT = T::WT, WF = T::WF, NST = T::NST, BK = T::BK, STAGE = T::STAGE, NLOAD = T::NLOAD, NKS = 2, AHEAD = 3;
   extern __shared__ __attribute__((aligned(1024))) char smem[];
@@ -410,7 +412,7 @@ template <class T, int DT> __global__ __launch_bounds__(256) void ftint8_finish(
 // byte of the weights is wanted by one wave alone.  Stages of 256 columns, two of them under way; a token on 4096 columns has all it needs under way at once, and all
 // workgroups of 16,384 features are on the chip together.  WORDS > 0 (up to TOKENS tokens of up to 4096 WORDS columns): they come in 16 bits, every workgroup encodes them for
 // itself while its first weights are under way, and the second launch is saved.  Bound by memory: 67 MB of weights, one token on 16,384 features of 4096 columns,
-// take 13.9 us with the encoding (4.8 TB/s, what a copy reaches; 16.3 in two launches).
+// take 12.7 us with the encoding (5.3 TB/s; 15.0 in two launches).
 constexpr int FEW_WAVES = 8, FUSED_K = 16384, FUSED_TOKENS = 4;
 struct FewArgs {
   ProductArgs p;
@@ -706,9 +708,9 @@ static bool too_many(const ftint8_ctx* c, int32_t m) {
 static hipError_t launch_product(ftint8_ctx* c, const int8_t* x, const float* sx, int32_t m, const int8_t* w, const float* sw, const ftint8_matrix* y, hipStream_t st) {
   ProductArgs a = product_args(c, x, sx, m, w, sw, y);
   auto tiles = [&](int t) { return (int64_t)((m + TILES[t].bm - 1) / TILES[t].bm) * ((c->cfg.n + TILES[t].bf - 1) / TILES[t].bf); };
-  // Up to 16 tokens: 9 on 4096 x 16,384 (features x columns) 17.7 us, on tiles 19.6; 16 on 1000 x 500 2.4, 4.0; 16 on 32,000 x 4096 34.5, 32.9.  Up to 32, whose
-  // codes each workgroup reads twice as many of as of weights, where the weights fit a round of workgroups: 32 on 4096 x 4096 8.4 us, 10.2; on 1000 x 1000 3.3, 5.2;
-  // but on 4096 x 8192 15.6, 14.4, on 16,384 x 4096 28.9, 19.9, on 500 x 10,000 15.7, 10.3.  Above that: 64 on 4096 x 4096 11.9, 10.2.
+  // Up to 16 tokens: 9 on 4096 x 16,384 (features x columns) 15.2 us, on tiles 16.8; 16 on 1000 x 500 2.5, 4.1; but 16 on 32,000 x 4096 30.9, 20.8, as each workgroup
+  // reads as many codes of tokens as of weights.  Up to 32, where it reads twice as many, where the weights fit a round of workgroups: 32 on 4096 x 4096 7.7 us, 9.1; on 1000 x 1000 3.4, 5.3;
+  // but on 4096 x 8192 13.1, 12.6, on 16,384 x 4096 23.7, 13.2, on 500 x 10,000 15.2, 9.4.
   if (m <= 16 || (m <= 32 && c->k_padded <= 4096 && c->cfg.n <= 4096)) {
     const FewArgs f{a, nullptr, 0, 0};
     const int two = m > 16;

@@ -14,7 +14,8 @@
  *
  * Prompts are computed in chunks of 64 tokens.  Before a product, weights q k decay^n and states are rounded to two words of 16 bits (2^-16 relative), values decayed to the end of
  * a chunk, which make the states, to three of bf16, or two of fp16: off by 2^-24 relative, or in fp16 by 2^-51 where that is more (chunks with values from 2 on in 32
- * neighbouring columns: 2^-50, and so on by octaves).  Single tokens are computed in 32 bits.
+ * neighbouring columns: 2^-50, and so on by octaves).  The products themselves keep 2^-24 of their largest term; elements of fp16 below 2^-14 count as 2^-14 there.  Single
+ * tokens are computed in 32 bits.
  *
  * Conventions
  *   - Every function returns FTDECAY_OK (0) or a negative error code and never throws or prints; ftdecay_last_error() returns the message of the last failure.

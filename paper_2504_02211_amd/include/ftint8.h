@@ -8,7 +8,8 @@
  *     y[t, n] = (sum over k of code_x[t, k] * code_w[n, k]) * (scale_x[t] * scale_w[n])
  *
  * The sum is exact (32-bit integers).  A row of zeros has scale 0; a row that holds an infinity or NaN has scale NaN and codes 0, which makes its
- * results NaN and no others.  It carries no checksums: ftgemm.h is the protected form in 16 bits.
+ * results NaN and no others.  Scales whose product leaves the numbers of 32 bits do so in the results: infinite, or NaN where the sum is 0.  It carries no checksums:
+ * ftgemm.h is the protected form in 16 bits.
  *
  * Conventions
  *   - Every function returns FTINT8_OK (0) or a negative error code and never throws or prints; ftint8_last_error() returns the message of the last failure.
@@ -42,7 +43,7 @@ typedef struct {
 } ftint8_config;
 
 /* A matrix of rows: element e of row r is data[r * stride + e].  data aligned to its elements, stride in elements (any from the row's length on; rows that begin
- * at multiples of 16 bytes are read faster). */
+ * at multiples of 16 bytes, and have up to 16,384 elements, are encoded two to four times as fast as others). */
 typedef struct { void* data; int64_t stride; } ftint8_matrix;
 
 int ftint8_create(const ftint8_config* cfg, ftint8_ctx** out);
